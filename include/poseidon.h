@@ -408,6 +408,147 @@ typedef struct pos_search_stats {
  */
 pos_status poseidon_search(const pos_problem *problem, pos_plan *out, pos_search_stats *stats);
 
+/* ------------------------------------------------------------------------
+ * Layer operators: what a pipeline stage keeps of a micro-batch in 8 bits
+ * between its forward and its backward pass.  A stage holds the activations
+ * of W_s micro-batches at once and fits when mem_w + W_s * mem_a <= cap, so
+ * the bytes that poseidon_ckpt_bytes returns for the tensors a layer keeps
+ * are what goes into mem_a.
+ *
+ * Every pointer below is a device pointer on the current device unless a
+ * line says otherwise; every call is asynchronous on `stream`.  Strides are
+ * in elements and may be any number >= 0 on tensors that are read (0
+ * repeats a row); rows that are written must not overlap.
+ */
+#define POS_BF16 0
+#define POS_F16 1
+#define POS_F32 2
+
+/*
+ * Checkpoint of a matrix [rows][cols], one buffer: rows of
+ * pitch = 32 * ceil(cols / 32) code bytes (zeros past the last column), then,
+ * from byte rows * pitch, rows of 4 * ceil(groups / 4) scale bytes, one per
+ * group of 32 columns (groups = pitch / 32; the bytes past the last group are
+ * not defined).  A value is code * 2^e with scale byte e + 127:
+ *   POS_CKPT_INT8   code = int8 in [-127, 127], e the smallest with
+ *                   max|x| <= 127 * 2^e, at most 121;
+ *   POS_CKPT_E4M3   code = float8 e4m3, e the smallest with
+ *                   max|x| <= 448 * 2^e, at most 119;
+ * e is at least -110 (a group of smaller magnitudes keeps what is left at
+ * that e).  x / 2^e is exact and is rounded once, to the nearest code, ties
+ * to even; only a group at the largest e saturates.  A group that holds an
+ * infinity or a NaN has scale byte 255 and stands for NaNs.
+ */
+#define POS_CKPT_INT8 0
+#define POS_CKPT_E4M3 1
+
+/* Bytes of a checkpoint: *bytes (host) = rows * (pitch + scale bytes per
+ * row).  POS_EINVAL: rows or cols < 0, cols above 2^31 - 33, a size of 2^62
+ * or more, NULL. */
+pos_status poseidon_ckpt_bytes(int64_t rows, int64_t cols, int64_t *bytes);
+
+/*
+ * Pack x [rows][cols] (rows ldx elements apart) of POS_BF16, POS_F16 or
+ * POS_F32 into the checkpoint d_ckpt (16-byte aligned).
+ * Errors: POS_EINVAL (NULL, negative sizes or stride, dtype or format,
+ * alignment), POS_ECUDA.
+ */
+pos_status poseidon_ckpt_pack(const void *d_x, int32_t dtype, int64_t rows, int64_t cols,
+                              int64_t ldx, int32_t format, void *d_ckpt, void *stream);
+
+/*
+ * The values of a checkpoint as y [rows][cols] (ldy >= cols elements apart).
+ * They are exact in POS_BF16 and POS_F32; POS_F16 rounds to nearest even and
+ * saturates at +-65504.
+ */
+pos_status poseidon_ckpt_unpack(const void *d_ckpt, int32_t format, int64_t rows, int64_t cols,
+                                void *d_y, int32_t dtype, int64_t ldy, void *stream);
+
+/*
+ * Weight gradient of a linear layer y = x W^T, W [n][cols], from the
+ * checkpoint of its input x [rows][cols] and the gradient dy [rows][n] of
+ * its output:
+ *   dw_out[i][j] = dw_in[i][j] + sum_r dy[r][i] * x[r][j]
+ * d_dw_in is NULL (zeros) or has dw_out's layout; it may be dw_out itself,
+ * which adds a micro-batch to the gradients of earlier ones, and must not
+ * overlap it otherwise.  dtype is dy's: POS_BF16 or POS_F16; x is taken as
+ * poseidon_ckpt_unpack gives it in that type.  Products are exact, sums are
+ * kept in 32 bits, in an order that depends on the sizes and the GPU alone.
+ * Scratch from the library's pool (stream-ordered): partial sums where the
+ * rows are split, at most 64 MB; a copy of dy of rows * (n + 7) elements when
+ * it is not 16-byte aligned (base and ld_dy) or ld_dy < n.
+ * A bounded wait that ran out inside the kernel makes the gradients NaN.
+ * Errors: POS_EINVAL (NULL, negative sizes or strides, ld_dw < cols, dtype,
+ * format, rows, n or cols of 2^31 or more, alignment), POS_ENOMEM, POS_ECUDA.
+ */
+pos_status poseidon_ckpt_wgrad(const void *d_ckpt, int32_t format, const void *d_dy,
+                               int32_t dtype, int64_t ld_dy, int64_t rows, int64_t n,
+                               int64_t cols, const float *d_dw_in, float *d_dw_out,
+                               int64_t ld_dw, void *stream);
+
+/* How the first `rot` elements of a head are paired for the rotation. */
+#define POS_ROT_HALF 0      /* (i, i + rot / 2) */
+#define POS_ROT_ADJACENT 1  /* (2 i, 2 i + 1) */
+
+/*
+ * RMS norm of every query and key head with the position rotation in the
+ * same pass.  For a head x [dim] of a token at position p:
+ *   r = 1 / sqrt(mean(x^2) + eps),  u = x * r * w,
+ *   (y_a, y_b) = (u_a c - u_b s, u_b c + u_a s) for the i-th pair (a, b),
+ *   c = cos[p][i], s = sin[p][i]; elements from rot on keep u.
+ * A token at a negative position is padding: its outputs and gradients are
+ * zeros, whatever its inputs hold, and it adds nothing to the weights'
+ * gradients.  A position >= n_pos makes the token's outputs and gradients
+ * NaN.  Norms, rotation and sums are in 32 bits, rounded once on output.
+ */
+typedef struct pos_qk {
+    int64_t tokens;
+    int32_t heads_q, heads_k;   /* >= 0 */
+    int32_t dim;                /* 1..256 */
+    int32_t rot;                /* even, 0..dim */
+    int32_t pairing;            /* POS_ROT_HALF or POS_ROT_ADJACENT */
+    int32_t dtype;              /* of q, k, outputs and their gradients */
+    int32_t format;             /* of the checkpoints */
+    float eps;                  /* >= 0 */
+    const float *w_q, *w_k;     /* [dim]; NULL = ones */
+    const float *cos, *sin;     /* [n_pos][rot / 2] */
+    int64_t n_pos;
+    const int32_t *positions;   /* [tokens]; NULL = 0, 1, 2, ... */
+} pos_qk;
+
+/* A tensor [tokens][heads][dim] with contiguous heads. */
+typedef struct pos_heads {
+    void *data;
+    int64_t token_stride, head_stride;
+} pos_heads;
+
+/*
+ * Forward pass.  x, y: host arrays of two (queries, keys); y may be x itself
+ * (the same pointers and strides).  rstd_q, rstd_k ([tokens][heads], float)
+ * and ckpt_q, ckpt_k (16-byte aligned checkpoints of x as a matrix
+ * [tokens * heads][dim]) are what the backward pass reads; each may be NULL.
+ * Errors: POS_EINVAL, POS_ECUDA.
+ */
+pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_heads *y,
+                               float *rstd_q, float *rstd_k, void *ckpt_q, void *ckpt_k,
+                               void *stream);
+
+/*
+ * Backward pass.  With g the gradient of y turned back, n = x * r, h = g * w:
+ *   dx = r * (h - n * mean(h * n)),  dw = dw_in + sum over tokens, heads of g * n.
+ * x (host array of two) or, where it is NULL, the checkpoints give x; rstd is
+ * the forward pass's.  dy, dx: host arrays of two; dx may be dy itself.
+ * d_dw ([2][dim], queries' then keys') may be NULL, d_dw_in (the same layout)
+ * is NULL for zeros or may be d_dw itself.  The sums' order depends on the
+ * sizes and the GPU alone.  Scratch from the library's pool: 8 * dim bytes for
+ * each block of the grid (at most 8 per SM) when d_dw is not NULL.
+ * Errors: POS_EINVAL, POS_ENOMEM, POS_ECUDA.
+ */
+pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void *ckpt_q,
+                                const void *ckpt_k, const float *rstd_q, const float *rstd_k,
+                                const pos_heads *dy, const pos_heads *dx, const float *d_dw_in,
+                                float *d_dw, void *stream);
+
 /* Message describing the last error of the calling thread ("" if none). */
 const char *poseidon_last_error(void);
 

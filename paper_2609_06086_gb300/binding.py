@@ -28,7 +28,9 @@ MAX_STAGES = 16
 # the exported entry points, as declared in include/poseidon.h
 EXPORTS = ["poseidon_tables_create", "poseidon_tables_destroy", "poseidon_eval_batch",
            "poseidon_eval_batch_ex", "poseidon_eval_batch_host", "poseidon_argmin",
-           "poseidon_argmin_noalloc", "poseidon_search", "poseidon_last_error"]
+           "poseidon_argmin_noalloc", "poseidon_search", "poseidon_ckpt_bytes",
+           "poseidon_ckpt_pack", "poseidon_ckpt_unpack", "poseidon_ckpt_wgrad",
+           "poseidon_qk_forward", "poseidon_qk_backward", "poseidon_last_error"]
 
 
 class pos_tables(C.Structure):
@@ -72,6 +74,23 @@ class pos_search_stats(C.Structure):
                 ("pruned_ridge", C.c_uint64)]
 
 
+POS_BF16, POS_F16, POS_F32 = 0, 1, 2
+POS_CKPT_INT8, POS_CKPT_E4M3 = 0, 1
+POS_ROT_HALF, POS_ROT_ADJACENT = 0, 1
+
+
+class pos_qk(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("heads_q", C.c_int32), ("heads_k", C.c_int32),
+                ("dim", C.c_int32), ("rot", C.c_int32), ("pairing", C.c_int32),
+                ("dtype", C.c_int32), ("format", C.c_int32), ("eps", C.c_float),
+                ("w_q", C.c_void_p), ("w_k", C.c_void_p), ("cos", C.c_void_p),
+                ("sin", C.c_void_p), ("n_pos", C.c_int64), ("positions", C.c_void_p)]
+
+
+class pos_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 class PoseidonError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -98,6 +117,15 @@ def lib():
         L.poseidon_argmin_noalloc.argtypes = [vp, vp, i64, vp, vp]
         L.poseidon_search.argtypes = [C.POINTER(pos_problem), C.POINTER(pos_plan),
                                       C.POINTER(pos_search_stats)]
+        L.poseidon_ckpt_bytes.argtypes = [i64, i64, C.POINTER(i64)]
+        L.poseidon_ckpt_pack.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp]
+        L.poseidon_ckpt_unpack.argtypes = [vp, i32, i64, i64, vp, i32, i64, vp]
+        L.poseidon_ckpt_wgrad.argtypes = [vp, i32, vp, i32, i64, i64, i64, i64, vp, vp, i64, vp]
+        L.poseidon_qk_forward.argtypes = [C.POINTER(pos_qk), C.POINTER(pos_heads),
+                                          C.POINTER(pos_heads), vp, vp, vp, vp, vp]
+        L.poseidon_qk_backward.argtypes = [C.POINTER(pos_qk), C.POINTER(pos_heads), vp, vp, vp,
+                                           vp, C.POINTER(pos_heads), C.POINTER(pos_heads), vp,
+                                           vp, vp]
         L.poseidon_last_error.restype = C.c_char_p
         L.poseidon_last_error.argtypes = []
         for name in EXPORTS[:-1]:
@@ -267,3 +295,48 @@ def poseidon_search(problem: pos_problem):
     plan, st = pos_plan(), pos_search_stats()
     _check(lib().poseidon_search(C.byref(problem), C.byref(plan), C.byref(st)))
     return plan_dict(problem, plan), stats_dict(st)
+
+
+def poseidon_ckpt_bytes(rows: int, cols: int) -> int:
+    """Bytes of the 8-bit checkpoint of a [rows][cols] matrix."""
+    out = C.c_int64()
+    _check(lib().poseidon_ckpt_bytes(rows, cols, C.byref(out)))
+    return out.value
+
+
+def poseidon_ckpt_pack(d_x: int, dtype: int, rows: int, cols: int, ldx: int, format: int,
+                       d_ckpt: int, stream: int = 0):
+    """Device pointers in and out (asynchronous on `stream`)."""
+    _check(lib().poseidon_ckpt_pack(d_x, dtype, rows, cols, ldx, format, d_ckpt, stream))
+
+
+def poseidon_ckpt_unpack(d_ckpt: int, format: int, rows: int, cols: int, d_y: int, dtype: int,
+                         ldy: int, stream: int = 0):
+    _check(lib().poseidon_ckpt_unpack(d_ckpt, format, rows, cols, d_y, dtype, ldy, stream))
+
+
+def poseidon_ckpt_wgrad(d_ckpt: int, format: int, d_dy: int, dtype: int, ld_dy: int, rows: int,
+                        n: int, cols: int, d_dw_in: int, d_dw_out: int, ld_dw: int,
+                        stream: int = 0):
+    """dw_out = dw_in (0: zeros) + dy^T x, x from its checkpoint."""
+    _check(lib().poseidon_ckpt_wgrad(d_ckpt, format, d_dy, dtype, ld_dy, rows, n, cols, d_dw_in,
+                                     d_dw_out, ld_dw, stream))
+
+
+def qk_heads(q: int, q_token: int, q_head: int, k: int, k_token: int, k_head: int):
+    """The (queries, keys) pair of pos_heads that the q/k calls take: pointer,
+    token stride and head stride of each."""
+    return (pos_heads * 2)((q, q_token, q_head), (k, k_token, k_head))
+
+
+def poseidon_qk_forward(qk: pos_qk, x, y, rstd=(0, 0), ckpt=(0, 0), stream: int = 0):
+    """x, y: qk_heads(); rstd, ckpt: (queries, keys) device pointers, 0 = not kept."""
+    _check(lib().poseidon_qk_forward(C.byref(qk), x, y, rstd[0], rstd[1], ckpt[0], ckpt[1],
+                                     stream))
+
+
+def poseidon_qk_backward(qk: pos_qk, dy, dx, rstd, ckpt=(0, 0), x=None, dw_in: int = 0,
+                         dw: int = 0, stream: int = 0):
+    """dy, dx: qk_heads(); x: qk_heads() or None (the checkpoints are read)."""
+    _check(lib().poseidon_qk_backward(C.byref(qk), x, ckpt[0], ckpt[1], rstd[0], rstd[1], dy, dx,
+                                      dw_in, dw, stream))

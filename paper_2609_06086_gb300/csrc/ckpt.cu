@@ -1,0 +1,164 @@
+// poseidon_ckpt_bytes, poseidon_ckpt_pack, poseidon_ckpt_unpack: 8-bit
+// checkpoints of activations (format: poseidon.h).
+#include "layer_ops.cuh"
+
+namespace pos {
+
+constexpr int kPackThreads = 256;
+constexpr int kPackUnroll = 4;  // vectors of 8 elements in flight per thread
+constexpr int kPackBlock = kPackThreads * kPackUnroll;
+
+// n / d for n < 2^31 by a multiplication (round-up method).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    explicit FastDiv(uint32_t v) : d(v), mul(0), shift(0) {
+        while ((1ull << shift) < v) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - v)) / v + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const {
+        return (__umulhi(n, mul) + n) >> shift;
+    }
+};
+
+struct PackParams {
+    const void *x;     // pack: input; unpack: output
+    uint8_t *codes, *scales;
+    int64_t ld, pitch, spitch;
+    uint32_t n_vec;    // rows * pitch / 8
+    int32_t cols;
+    FastDiv per_row;   // pitch / 8
+};
+
+// A thread takes vectors of 8 elements (a warp: 256 consecutive ones), four
+// lanes share a group's largest magnitude by two shuffles.  Bound by HBM:
+// every value is read once and every code written once.
+template <typename T, int F, bool ALIGNED>
+__global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackParams p) {
+    const T *x = static_cast<const T *>(p.x);
+    Raw8<T> raw[kPackUnroll];
+    uint32_t row[kPackUnroll], j[kPackUnroll];
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        const uint32_t r = p.per_row.div(v);
+        row[i] = r;
+        j[i] = v - r * p.per_row.d;
+        const int left = v < p.n_vec ? p.cols - (int)(8 * j[i]) : 0;
+        raw[i] = load8<ALIGNED>(x + (int64_t)r * p.ld + 8 * j[i], left);
+    }
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        uint32_t m = amax_bits(raw[i]);
+        m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const int byte = scale_byte<F>(f32_bits<T>(m));
+        if (v >= p.n_vec) continue;
+        *reinterpret_cast<uint2 *>(p.codes + row[i] * p.pitch + 8 * j[i]) =
+            encode8<F>(to_float(raw[i]), byte);
+        if (j[i] % 4 == 0) p.scales[row[i] * p.spitch + j[i] / 4] = (uint8_t)byte;
+    }
+}
+
+template <typename T, int F, bool ALIGNED>
+__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackParams p) {
+    T *y = static_cast<T *>(const_cast<void *>(p.x));
+    uint2 code[kPackUnroll];
+    int byte[kPackUnroll];
+    uint32_t row[kPackUnroll], j[kPackUnroll];
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        row[i] = p.per_row.div(v);
+        j[i] = v - row[i] * p.per_row.d;
+        if (v >= p.n_vec) continue;
+        code[i] = *reinterpret_cast<const uint2 *>(p.codes + row[i] * p.pitch + 8 * j[i]);
+        byte[i] = p.scales[row[i] * p.spitch + j[i] / 4];
+    }
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        if (v >= p.n_vec) continue;
+        store8<ALIGNED>(y + (int64_t)row[i] * p.ld + 8 * j[i],
+                        from_float<T, true>(decode8<F>(code[i], scale_value(byte[i]))),
+                        p.cols - (int)(8 * j[i]));
+    }
+}
+
+// Both kernels over all rows, at most 2^31 vectors a launch.
+template <typename T, int F>
+static pos_status launch_pack(bool pack, const void *x, int64_t rows, int64_t cols, int64_t ld,
+                              void *ckpt, cudaStream_t stream) {
+    const CkptShape s = ckpt_shape(cols);
+    const int64_t per_row = s.pitch / 8;
+    const int64_t most = std::max<int64_t>(1, (0x7fffffffll - kPackBlock) / per_row);
+    const bool aligned = aligned16(x) && ld * (int64_t)sizeof(T) % 16 == 0;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = std::min(most, rows - r);
+        PackParams p{static_cast<const T *>(x) + r * ld,
+                     static_cast<uint8_t *>(ckpt) + r * s.pitch,
+                     static_cast<uint8_t *>(ckpt) + rows * s.pitch + r * s.spitch,
+                     ld, s.pitch, s.spitch, (uint32_t)(n * per_row), (int32_t)cols,
+                     FastDiv((uint32_t)per_row)};
+        const int grid = (int)((n * per_row + kPackBlock - 1) / kPackBlock);
+        if (pack) {
+            if (aligned) pack_kernel<T, F, true><<<grid, kPackThreads, 0, stream>>>(p);
+            else pack_kernel<T, F, false><<<grid, kPackThreads, 0, stream>>>(p);
+        } else {
+            if (aligned) unpack_kernel<T, F, true><<<grid, kPackThreads, 0, stream>>>(p);
+            else unpack_kernel<T, F, false><<<grid, kPackThreads, 0, stream>>>(p);
+        }
+        POS_CUDA(cudaGetLastError());
+    }
+    return POS_OK;
+}
+
+static pos_status pack_or_unpack(bool pack, const void *x, int32_t dtype, int64_t rows,
+                                 int64_t cols, int64_t ld, int32_t format, void *ckpt,
+                                 void *stream) {
+    if (!ckpt_size_ok(rows, cols)) return fail(POS_EINVAL, "checkpoint: bad rows or cols");
+    if (!dtype_ok(dtype)) return fail(POS_EINVAL, "checkpoint: unknown dtype");
+    if (!format_ok(format)) return fail(POS_EINVAL, "checkpoint: unknown format");
+    if (ld < 0 || ld >= (1ll << 40) || (!pack && ld < cols && rows > 1))
+        return fail(POS_EINVAL, "checkpoint: bad row stride");
+    if (rows == 0 || cols == 0) return POS_OK;
+    if (!x || !ckpt) return fail(POS_EINVAL, "checkpoint: NULL pointer");
+    if (!aligned16(ckpt)) return fail(POS_EINVAL, "checkpoint: buffer not 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(x) % dtype_size(dtype))
+        return fail(POS_EINVAL, "checkpoint: matrix not aligned to its elements");
+    const auto s = static_cast<cudaStream_t>(stream);
+    const bool i8 = format == POS_CKPT_INT8;
+    if (dtype == POS_BF16)
+        return i8 ? launch_pack<__nv_bfloat16, POS_CKPT_INT8>(pack, x, rows, cols, ld, ckpt, s)
+                  : launch_pack<__nv_bfloat16, POS_CKPT_E4M3>(pack, x, rows, cols, ld, ckpt, s);
+    if (dtype == POS_F16)
+        return i8 ? launch_pack<__half, POS_CKPT_INT8>(pack, x, rows, cols, ld, ckpt, s)
+                  : launch_pack<__half, POS_CKPT_E4M3>(pack, x, rows, cols, ld, ckpt, s);
+    return i8 ? launch_pack<float, POS_CKPT_INT8>(pack, x, rows, cols, ld, ckpt, s)
+              : launch_pack<float, POS_CKPT_E4M3>(pack, x, rows, cols, ld, ckpt, s);
+}
+
+}  // namespace pos
+
+extern "C" {
+
+pos_status poseidon_ckpt_bytes(int64_t rows, int64_t cols, int64_t *bytes) {
+    if (!bytes) return pos::fail(POS_EINVAL, "checkpoint: NULL pointer");
+    if (!pos::ckpt_size_ok(rows, cols)) return pos::fail(POS_EINVAL, "checkpoint: bad rows or cols");
+    const pos::CkptShape s = pos::ckpt_shape(cols);
+    *bytes = rows * (s.pitch + s.spitch);
+    return POS_OK;
+}
+
+pos_status poseidon_ckpt_pack(const void *d_x, int32_t dtype, int64_t rows, int64_t cols,
+                              int64_t ldx, int32_t format, void *d_ckpt, void *stream) {
+    return pos::pack_or_unpack(true, d_x, dtype, rows, cols, ldx, format, d_ckpt, stream);
+}
+
+pos_status poseidon_ckpt_unpack(const void *d_ckpt, int32_t format, int64_t rows, int64_t cols,
+                                void *d_y, int32_t dtype, int64_t ldy, void *stream) {
+    return pos::pack_or_unpack(false, d_y, dtype, rows, cols, ldy, format,
+                               const_cast<void *>(d_ckpt), stream);
+}
+
+}  // extern "C"

@@ -438,12 +438,13 @@ pos_status launch_decode(const EvalParams &p, cudaStream_t stream) {
 // Stream-ordered scratch comes from a library-owned pool per device that
 // keeps its memory between calls (release threshold: unlimited), so what is
 // taken from it is bounded: 39 bytes per candidate of a chunk of 2^24, an
-// argmin's partial results, and host batches up to kHostPoolBytes.
+// argmin's partial results, host batches up to kHostPoolBytes, and the layer
+// operators' scratch (poseidon.h).
 constexpr size_t kHostPoolBytes = 64ull << 20;
 static std::mutex g_pool_mutex;
 static cudaMemPool_t g_pool[64];
 
-static pos_status scratch_pool(cudaMemPool_t *out) {
+pos_status scratch_pool(cudaMemPool_t *out) {
     int dev = 0;
     POS_CUDA(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return fail(POS_EINVAL, "device index above 63");

@@ -1,0 +1,302 @@
+// Shared by the layer operators (ckpt.cu, qk.cu, wgrad.cu): element types,
+// 8-element vectors, and the arithmetic of an 8-bit checkpoint (poseidon.h).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <cstring>
+
+#include "common.cuh"
+
+namespace pos {
+
+// The library's scratch pool of the current device (eval.cu).
+pos_status scratch_pool(cudaMemPool_t *out);
+
+constexpr int kGroup = 32;             // columns that share a scale
+constexpr int kScaleLo = 17;           // scale byte of e = -110
+constexpr int kScaleNan = 255;
+template <int F>                       // POS_CKPT_*
+struct Fmt;
+template <>
+struct Fmt<POS_CKPT_INT8> {
+    static constexpr int kScaleHi = 248;  // e = 121: 127 * 2^121 is finite in f32 and bf16
+    // 127 = 1.984375 * 2^6: a larger mantissa carries into the exponent
+    static constexpr uint32_t kCarry = 0x7fffffu - 0x7e0000u;
+    static constexpr int kLead = 6;
+    static constexpr float kTop = 127.f;
+};
+template <>
+struct Fmt<POS_CKPT_E4M3> {
+    static constexpr int kScaleHi = 246;  // e = 119: 448 * 2^119 is finite
+    static constexpr uint32_t kCarry = 0x7fffffu - 0x600000u;  // 448 = 1.75 * 2^8
+    static constexpr int kLead = 8;
+    static constexpr float kTop = 448.f;
+};
+
+// Scale byte of a group from the bits of its largest |x| as f32 (whose order
+// as whole numbers is that of the magnitudes, infinities and NaNs on top).
+template <int F>
+__device__ __forceinline__ int scale_byte(uint32_t amax_bits) {
+    if (amax_bits >= 0x7f800000u) return kScaleNan;
+    const int b = (int)((amax_bits + Fmt<F>::kCarry) >> 23) - Fmt<F>::kLead;
+    return min(max(b, kScaleLo), Fmt<F>::kScaleHi);
+}
+
+// 2^e of a scale byte as f32, a NaN for kScaleNan.
+__device__ __forceinline__ float scale_value(int byte) {
+    return __uint_as_float(byte == kScaleNan ? 0x7fffffffu : (uint32_t)byte << 23);
+}
+
+struct Vec8 {
+    float v[8];
+};
+
+// Codes of 8 values under one scale byte.  x * 2^-e is exact (or an underflow
+// far below half a code), so each code is rounded once: int8 by adding
+// 1.5 * 2^23, whose last bit is a whole number, e4m3 by the conversion.  Only
+// the largest scale can leave values past the top code, which saturate.
+template <int F>
+__device__ __forceinline__ uint2 encode8(const Vec8 &x, int byte) {
+    if (byte == kScaleNan) return make_uint2(0u, 0u);
+    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+    if constexpr (F == POS_CKPT_INT8) {
+        uint32_t b[8];
+        if (byte == Fmt<F>::kScaleHi) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                b[i] = __float_as_uint(fminf(fmaxf(x.v[i] * inv, -127.f), 127.f) + 12582912.f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(x.v[i], inv, 12582912.f));
+        }
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            w[h] = __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040),
+                               __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
+        return make_uint2(w[0], w[1]);
+    } else {
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(
+                make_float2(x.v[4 * h] * inv, x.v[4 * h + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(
+                make_float2(x.v[4 * h + 2] * inv, x.v[4 * h + 3] * inv), __NV_SATFINITE,
+                __NV_E4M3);
+            w[h] = lo | hi << 16;
+        }
+        return make_uint2(w[0], w[1]);
+    }
+}
+
+// The values of 8 codes: exact in f32.
+template <int F>
+__device__ __forceinline__ Vec8 decode8(uint2 c, float scale) {
+    Vec8 x;
+    const uint32_t w[2] = {c.x, c.y};
+    if constexpr (F == POS_CKPT_INT8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // the code + 128 in the last byte of 2^23
+            const uint32_t u = __byte_perm(w[i / 4] ^ 0x80808080u, 0x4b000000u, 0x7440u | i % 4);
+            x.v[i] = (__uint_as_float(u) - 8388736.f) * scale;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
+                (__nv_fp8x2_storage_t)(w[i / 2] >> (16 * (i % 2))), __NV_E4M3);
+            const float2 f = __half22float2(__half2(h));
+            x.v[2 * i] = f.x * scale;
+            x.v[2 * i + 1] = f.y * scale;
+        }
+    }
+    return x;
+}
+
+// ---------------------------------------------------------------------------
+// Element types: 8 consecutive elements as raw words
+// ---------------------------------------------------------------------------
+template <typename T>
+struct Raw8;  // 16 or 32 bytes
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint4 a;
+};
+template <>
+struct Raw8<__half> {
+    uint4 a;
+};
+template <>
+struct Raw8<float> {
+    uint4 a, b;
+};
+
+__device__ __forceinline__ void zero_raw(uint4 &a) { a = make_uint4(0, 0, 0, 0); }
+
+// ALIGNED: p is 16-byte aligned and all 8 elements exist; otherwise `n` of
+// them (any number, <= 0: none) are read one by one, the others are zeros.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ Raw8<T> load8(const T *p, int n) {
+    Raw8<T> r;
+    if constexpr (ALIGNED) {
+        if (n >= 8) {
+            r.a = *reinterpret_cast<const uint4 *>(p);
+            if constexpr (sizeof(T) == 4) r.b = *(reinterpret_cast<const uint4 *>(p) + 1);
+            return r;
+        }
+    }
+    zero_raw(r.a);
+    if constexpr (sizeof(T) == 4) zero_raw(r.b);
+    if constexpr (sizeof(T) == 4) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = i < n ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
+        r.a = make_uint4(w[0], w[1], w[2], w[3]);
+        r.b = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = i < n ? (uint32_t) reinterpret_cast<const uint16_t *>(p)[i] : 0u;
+        r.a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16,
+                         w[6] | w[7] << 16);
+    }
+    return r;
+}
+
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void store8(T *p, const Raw8<T> &r, int n) {
+    if constexpr (ALIGNED) {
+        if (n >= 8) {
+            *reinterpret_cast<uint4 *>(p) = r.a;
+            if constexpr (sizeof(T) == 4) *(reinterpret_cast<uint4 *>(p) + 1) = r.b;
+            return;
+        }
+    }
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) reinterpret_cast<uint32_t *>(p)[i] = w[i];
+    } else {
+        const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ Vec8 to_float(const Raw8<T> &r) {
+    Vec8 x;
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+    if constexpr (std::is_same<T, float>::value) {
+        const uint32_t u[4] = {r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x.v[i] = __uint_as_float(w[i]);
+            x.v[4 + i] = __uint_as_float(u[i]);
+        }
+    } else if constexpr (std::is_same<T, __half>::value) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 h;
+            memcpy(&h, &w[i], 4);
+            const float2 f = __half22float2(h);
+            x.v[2 * i] = f.x;
+            x.v[2 * i + 1] = f.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x.v[2 * i] = __uint_as_float(w[i] << 16);
+            x.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    return x;
+}
+
+// Rounded to nearest even.  SAT: f16 saturates at its largest finite value
+// (NaNs stay).
+template <typename T, bool SAT = false>
+__device__ __forceinline__ Raw8<T> from_float(const Vec8 &x) {
+    Raw8<T> r;
+    if constexpr (std::is_same<T, float>::value) {
+        r.a = make_uint4(__float_as_uint(x.v[0]), __float_as_uint(x.v[1]), __float_as_uint(x.v[2]),
+                         __float_as_uint(x.v[3]));
+        r.b = make_uint4(__float_as_uint(x.v[4]), __float_as_uint(x.v[5]), __float_as_uint(x.v[6]),
+                         __float_as_uint(x.v[7]));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (std::is_same<T, __half>::value) {
+                __half2 h = __floats2half2_rn(x.v[2 * i], x.v[2 * i + 1]);
+                if constexpr (SAT) {
+                    const __half2 top = __half2half2(__ushort_as_half(0x7bff));
+                    h = __hmin2_nan(__hmax2_nan(h, __hneg2(top)), top);
+                }
+                memcpy(&w[i], &h, 4);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x.v[2 * i], x.v[2 * i + 1]);
+                memcpy(&w[i], &h, 4);
+            }
+        }
+        r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return r;
+}
+
+// Bits of the largest |x| of 8 elements, in a form that max_bits() and
+// shuffles combine and f32_bits() turns into the bits of an f32: two 16-bit
+// magnitudes for the 16-bit types, whose bits order them too.
+template <typename T>
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) {
+    if constexpr (sizeof(T) == 4) return max(a, b);
+    else return __vmaxu2(a, b);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t amax_bits(const Raw8<T> &r) {
+    constexpr uint32_t kAbs = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    uint32_t m = max_bits<T>(max_bits<T>(r.a.x & kAbs, r.a.y & kAbs),
+                             max_bits<T>(r.a.z & kAbs, r.a.w & kAbs));
+    if constexpr (sizeof(T) == 4)
+        m = max(m, max(max(r.b.x & kAbs, r.b.y & kAbs), max(r.b.z & kAbs, r.b.w & kAbs)));
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t f32_bits(uint32_t m) {
+    if constexpr (std::is_same<T, float>::value) return m;
+    const uint32_t h = max(m & 0xffffu, m >> 16);
+    if constexpr (std::is_same<T, __half>::value)
+        return __float_as_uint(__half2float(__ushort_as_half((unsigned short)h)));
+    return h << 16;
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct CkptShape {
+    int64_t groups, pitch, spitch;  // per row: groups, code bytes, scale bytes
+};
+inline CkptShape ckpt_shape(int64_t cols) {
+    const int64_t g = (cols + kGroup - 1) / kGroup;
+    return {g, g * kGroup, (g + 3) / 4 * 4};
+}
+// Sizes that a checkpoint can have (its byte count below 2^62).
+inline bool ckpt_size_ok(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || cols > 0x7fffffffll - kGroup) return false;
+    const CkptShape s = ckpt_shape(cols);
+    return s.pitch == 0 || rows < (1ll << 62) / (s.pitch + s.spitch);
+}
+inline bool dtype_ok(int32_t d) { return d == POS_BF16 || d == POS_F16 || d == POS_F32; }
+inline bool format_ok(int32_t f) { return f == POS_CKPT_INT8 || f == POS_CKPT_E4M3; }
+inline int dtype_size(int32_t d) { return d == POS_F32 ? 4 : 2; }
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace pos
