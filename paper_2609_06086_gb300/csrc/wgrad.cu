@@ -20,27 +20,37 @@ namespace pos {
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr int kHalf = 128;              // columns of x, and of dy, of one SM
 constexpr int kStages = 5;              // operands in 16 bits
-constexpr int kCodeStages = 6;          // codes as they come
+constexpr int kCodeStages = 6;          // codes and scales as they come
 constexpr int kABytes = kHalf * kTileK * 2, kBBytes = kHalf * kTileK * 2;
-constexpr int kCodeBytes = kHalf * kTileK;
-constexpr int kDecodeWarps = 8, kEpilogueWarps = 4;
-constexpr int kWgradThreads = 32 * (2 + kDecodeWarps + kEpilogueWarps);
-constexpr int kBars = 3 * kStages + 2 * kCodeStages + 4;
-constexpr int kWgradSmem = 1024 + kStages * (kABytes + kBBytes) + kCodeStages * kCodeBytes +
-                           8 * kBars + 16;
+constexpr int kCodeBytes = kHalf * kTileK, kScaleBytes = kTileK * 4;
+// Warpgroups: one of loads and products, two that decode every other stage
+// each (the latency of a stage is then two stages long), two of sums.
+constexpr int kDecodeGroups = 2, kDecodeWarps = 4, kSumWarps = 8;
+constexpr int kWgradThreads = 128 * (1 + kDecodeGroups) + 32 * kSumWarps;
+// Registers of a thread after the split: 32 + 2 * 56 + 2 * 168 = 480 = 5 * 96,
+// what the block is launched with.
+constexpr int kLoadRegs = 32, kDecodeRegs = 56, kSumRegs = 168;
+constexpr int kBars = 2 * kStages + 2 * kCodeStages + 4;
+constexpr int kWgradSmem = 1024 + kStages * (kABytes + kBBytes) +
+                           kCodeStages * (kCodeBytes + kScaleBytes) + 8 * kBars + 16;
 constexpr int kAccCols = 256;           // TMEM columns of one accumulator; two alternate
+// The tensor cores cut what they add to a sum instead of rounding it, so a
+// long sum drifts towards zero by about 1e-9 of its size per row (measured:
+// 2.6e-6 over 4096 rows).  An accumulator therefore takes 512 rows, and the
+// sums of those are added in registers, with rounding.
+constexpr int kChunkRows = 512;
 
 struct WgradParams {
     const uint8_t *scales;
     const float *in;
-    float *out;
+    float *out, *part;     // part: tiles [256][256] of the split tiles' partial sums
     int64_t rows, ld, spitch;
-    int64_t part_stride;   // elements between the splits' partial sums (0: one split)
     int32_t n, cols;
-    int32_t tiles_m, tiles_n, units;  // units = tiles * splits
+    int32_t tiles_m, tiles_n;
+    int32_t whole;         // tiles with all rows in one unit: the first ones
+    int32_t units;         // whole + splits * (tiles - whole)
     int32_t splits;
-    int64_t split_rows;    // rows of a split, a multiple of chunk_rows
-    int64_t chunk_rows;    // rows summed in one accumulator, a multiple of kTileK
+    int64_t split_rows;    // a multiple of kTileK
 };
 
 // ---------------------------------------------------------------------------
@@ -96,7 +106,7 @@ __device__ __forceinline__ uint64_t now_ns() {
 // Waits for a phase, two seconds at most; false: it did not come, or another
 // wait of the block has already given up.
 constexpr uint64_t kWaitNs = 2000000000ull;
-__device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *gave_up) {
     const uint64_t t0 = now_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
@@ -152,18 +162,31 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "h"((uint16_t)3)
         : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t (&r)[8]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[7])
         : "r"(addr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// Four bytes by an asynchronous copy, or zeros.
+__device__ __forceinline__ void copy_word(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src),
+                 "r"(there ? 4 : 0)
+                 : "memory");
+}
+// Arrives once the thread's asynchronous copies so far have landed.
+__device__ __forceinline__ void bar_arrive_copies(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int R>
+__device__ __forceinline__ void give_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R));
+}
+template <int R>
+__device__ __forceinline__ void take_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
 }
 
 // ---------------------------------------------------------------------------
@@ -224,22 +247,28 @@ __device__ __forceinline__ void decode16(uint4 c, int byte, uint4 (&v)[2]) {
 // ---------------------------------------------------------------------------
 struct Unit {
     int m0, n0;      // first column of x, of dy
-    int64_t r0, r1;  // rows
-    int split;
+    int r0, r1;      // rows
+    int part;        // partial sum that it writes, or -1
 };
 // Units of the pairs that run at once share columns: bands of 8 tiles of dy,
 // through which the tiles of x pass.
+__device__ __forceinline__ void tile_of(const WgradParams &p, int tile, int &m0, int &n0) {
+    const int band = tile / (8 * p.tiles_m), n_band = min(8, p.tiles_n - 8 * band);
+    tile -= band * 8 * p.tiles_m;
+    m0 = tile / n_band * kTileM;
+    n0 = (8 * band + tile % n_band) * kTileN;
+}
 __device__ __forceinline__ Unit unit_of(const WgradParams &p, int u) {
     Unit t;
-    const int tiles = p.tiles_m * p.tiles_n;
-    t.split = u / tiles;
-    u -= t.split * tiles;
-    const int band = u / (8 * p.tiles_m), n_band = min(8, p.tiles_n - 8 * band);
-    u -= band * 8 * p.tiles_m;
-    t.m0 = u / n_band * kTileM;
-    t.n0 = (8 * band + u % n_band) * kTileN;
-    t.r0 = t.split * p.split_rows;
-    t.r1 = min(p.rows, t.r0 + p.split_rows);
+    t.r0 = 0, t.r1 = (int)p.rows, t.part = -1;
+    int tile = u;
+    if (u >= p.whole) {
+        t.part = u - p.whole;
+        tile = p.whole + t.part / p.splits;
+        t.r0 = (int)(t.part % p.splits * p.split_rows);
+        t.r1 = (int)min(p.rows, t.r0 + p.split_rows);
+    }
+    tile_of(p, tile, t.m0, t.n0);
     return t;
 }
 
@@ -251,14 +280,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char *aligned = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t a_at = base, b_at = a_at + kStages * kABytes, c_at = b_at + kStages * kBBytes;
-    const uint32_t bars = c_at + kCodeStages * kCodeBytes;
+    const uint32_t s_at = c_at + kCodeStages * kCodeBytes;
+    const uint32_t bars = s_at + kCodeStages * kScaleBytes;
     const uint32_t full = bars, empty = full + 8 * kStages;
     const uint32_t code_full = empty + 8 * kStages, code_empty = code_full + 8 * kCodeStages;
     const uint32_t acc_full = code_empty + 8 * kCodeStages, acc_empty = acc_full + 16;
     const uint32_t slot = acc_empty + 16;
     unsigned char *tail = aligned + (slot - base);
     volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
 
@@ -270,12 +300,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
             bar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < kCodeStages; ++i) {
-            bar_init(code_full + 8 * i, 1);
+            bar_init(code_full + 8 * i, 1 + 32);  // codes, a warp's copies of scales
             bar_init(code_empty + 8 * i, kDecodeWarps);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(acc_full + 8 * i, 1);
-            bar_init(acc_empty + 8 * i, 2 * kEpilogueWarps);
+            bar_init(acc_empty + 8 * i, 2 * kSumWarps);
         }
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -292,15 +322,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
 
-    if (warp == 0) {
-        if (lane == 0) {
+    if (group == 0) {
+        give_registers<kLoadRegs>();
+        if (warp == 0 && lane == 0) {
             int s = 0, cs = 0;
             uint32_t ph = 1, cph = 1;  // an empty buffer's first wait passes
             const uint32_t leader_full = in_cta(full, 0);
             bool ok = true;
             for (int u = pair; u < p.units && ok; u += pairs) {
                 const Unit t = unit_of(p, u);
-                for (int64_t r = t.r0; r < t.r1 && ok; r += kTileK) {
+                for (int r = t.r0; r < t.r1; r += kTileK) {
                     ok = bar_wait(code_empty + 8 * cs, cph, gave_up);
                     if (!ok) break;
                     bar_expect(code_full + 8 * cs, kCodeBytes);
@@ -317,10 +348,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                     if (++s == kStages) s = 0, ph ^= 1;
                 }
             }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
+        } else if (warp == 1 && rank == 0 && lane == 0) {
             constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             // f32 sums, both operands with M / N contiguous
             constexpr uint32_t kIdesc = 1u << 4 | kType << 7 | kType << 10 | 1u << 15 | 1u << 16 |
@@ -331,11 +359,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
             bool ok = true;
             for (int u = pair; u < p.units && ok; u += pairs) {
                 const Unit t = unit_of(p, u);
-                for (int64_t c = t.r0; c < t.r1 && ok; c += p.chunk_rows) {
-                    const int64_t c1 = min(t.r1, c + p.chunk_rows);
+                for (int c = t.r0; c < t.r1 && ok; c += kChunkRows) {
+                    const int c1 = min(t.r1, c + kChunkRows);
                     ok = bar_wait(acc_empty + 8 * acc, aph, gave_up);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    for (int64_t r = c; r < c1 && ok; r += kTileK) {
+                    for (int r = c; r < c1 && ok; r += kTileK) {
                         ok = bar_wait(full + 8 * s, ph, gave_up);
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -354,56 +382,78 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                     if (acc == 0) aph ^= 1;
                 }
             }
+        } else if (warp == 2) {
+            // The scales of a stage's rows, four groups (a word) each: plain
+            // asynchronous copies, since their rows may start at any word.
+            int cs = 0;
+            uint32_t cph = 1;
+            bool ok = true;
+            for (int u = pair; u < p.units && ok; u += pairs) {
+                const Unit t = unit_of(p, u);
+                const int m0 = t.m0 + (int)rank * kHalf;
+                const uint8_t *sc = p.scales + (m0 < p.cols ? m0 / kGroup : 0);
+                for (int r = t.r0; r < t.r1; r += kTileK) {
+                    ok = bar_wait(code_empty + 8 * cs, cph, gave_up);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int at = r + lane + 32 * h;
+                        // rows and columns past the end: scale 0 (codes are zeros)
+                        const bool there = m0 < p.cols && at < t.r1;
+                        copy_word(s_at + cs * kScaleBytes + 4 * (lane + 32 * h),
+                                  sc + (there ? at * p.spitch : 0), there);
+                    }
+                    bar_arrive_copies(code_full + 8 * cs);
+                    if (++cs == kCodeStages) cs = 0, cph ^= 1;
+                }
+            }
         }
         __syncwarp();
-    } else if (warp < 2 + kDecodeWarps) {
-        // A thread decodes 16 columns of two rows of a stage.
-        const int i = threadIdx.x - 64, piece = i % 8, row = i / 8;
+    } else if (group <= kDecodeGroups) {
+        give_registers<kDecodeRegs>();
+        // A thread decodes 16 columns of four rows of its group's stages.
+        const int mine = group - 1;
+        const int i = threadIdx.x % 128, piece = i % 8, row = i / 8;
         const int block = piece / 4, chunk = piece % 4 * 2;
         const uint32_t leader_full = in_cta(full, 0);
-        int s = 0, cs = 0;
+        int s = mine, cs = mine;
         uint32_t ph = 1, cph = 0;
+        int turn = 0;  // of the groups, over all stages
         bool ok = true;
         for (int u = pair; u < p.units && ok; u += pairs) {
             const Unit t = unit_of(p, u);
-            const int m0 = t.m0 + (int)rank * kHalf;
-            const uint8_t *sc = p.scales + m0 / kGroup;
-            uint32_t next[2];
-            auto scales_at = [&](int64_t r) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t at = r + row + 32 * h;
-                    // rows and columns past the end: 1 (their codes are zeros)
-                    next[h] = 0x7f7f7f7fu;
-                    if (m0 < p.cols && at < t.r1)
-                        next[h] = __ldg(reinterpret_cast<const uint32_t *>(sc + at * p.spitch));
-                }
-            };
-            scales_at(t.r0);
-            for (int64_t r = t.r0; r < t.r1 && ok; r += kTileK) {
-                const uint32_t word[2] = {next[0], next[1]};
+            for (int r = t.r0; r < t.r1; r += kTileK) {
+                const bool skip = turn != mine;
+                if (++turn == kDecodeGroups) turn = 0;
+                if (skip) continue;
                 ok = bar_wait(code_full + 8 * cs, cph, gave_up);
                 if (!ok) break;
-                uint4 c[2];
+                uint4 c[4];
+                uint32_t byte[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t at = c_at + cs * kCodeBytes + (row + 32 * h) * kHalf + piece * 16;
+                for (int h = 0; h < 4; ++h) {
+                    const int tr = row + 16 * h;
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(c[h].x), "=r"(c[h].y), "=r"(c[h].z), "=r"(c[h].w)
-                                 : "r"(at)
+                                 : "r"(c_at + cs * kCodeBytes + tr * kHalf + piece * 16)
+                                 : "memory");
+                    asm volatile("ld.shared.u8 %0, [%1];"
+                                 : "=r"(byte[h])
+                                 : "r"(s_at + cs * kScaleBytes + tr * 4 + piece / 2)
                                  : "memory");
                 }
                 __syncwarp();
                 if (lane == 0) bar_arrive(code_empty + 8 * cs);
-                if (++cs == kCodeStages) cs = 0, cph ^= 1;
-                if (r + kTileK < t.r1) scales_at(r + kTileK);
+                cs += kDecodeGroups;
+                if (cs >= kCodeStages) cs -= kCodeStages, cph ^= 1;
                 ok = bar_wait(empty + 8 * s, ph, gave_up);
                 if (!ok) break;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 4; ++h) {
                     uint4 v[2];
-                    const int tr = row + 32 * h;
-                    decode16<T, F>(c[h], (int)(word[h] >> (piece / 2 * 8) & 0xffu), v);
+                    const int tr = row + 16 * h;
+                    decode16<T, F>(c[h], (int)byte[h], v);
                     const uint32_t to = a_at + s * kABytes + block * (kTileK * 128) + tr * 128;
                     // the upper block's lanes store their second half first:
                     // eight lanes then cover all banks
@@ -420,56 +470,73 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) bar_arrive_cluster(leader_full + 8 * s);
-                if (++s == kStages) s = 0, ph ^= 1;
+                s += kDecodeGroups;
+                if (s >= kStages) s -= kStages, ph ^= 1;
             }
         }
+        __syncwarp();
     } else {
-        // The accumulator's lanes are columns of x, its columns those of dy.
-        const int quarter = warp % 4;
+        take_registers<kSumRegs>();
+        // The accumulator's lanes are columns of x, its columns those of dy: a
+        // warp holds 32 x 128 sums.
+        const int quarter = warp % 4, side = (warp - 4 * (1 + kDecodeGroups)) / 4;
         const uint32_t leader_acc_empty = in_cta(acc_empty, 0);
+        const uint32_t from = tmem + side * 128 + ((uint32_t)(32 * quarter) << 16);
         int acc = 0;
         uint32_t aph = 0;
         bool ok = true;
         for (int u = pair; u < p.units; u += pairs) {
             const Unit t = unit_of(p, u);
-            const int col = t.m0 + (int)rank * kHalf + 32 * quarter + lane;
-            float *out = p.out + t.split * p.part_stride + t.n0 * p.ld + col;
-            const float *in = p.in ? p.in + t.n0 * p.ld + col : nullptr;
-            for (int64_t c = t.r0; c < t.r1; c += p.chunk_rows) {
+            float sum[128];
+#pragma unroll
+            for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+            for (int c = t.r0; c < t.r1; c += kChunkRows) {
                 if (ok) ok = bar_wait(acc_full + 8 * acc, aph, gave_up);
                 ok = __all_sync(0xffffffffu, ok);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int j0 = 0; j0 < kTileN; j0 += 32) {
-                    uint32_t v[32];
-                    if (ok) {
-                        tmem_load32(tmem + acc * kAccCols + j0 + ((uint32_t)(32 * quarter) << 16),
-                                    v);
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0x7fffffffu;
-                    }
-                    if (j0 + 32 == kTileN) {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) bar_arrive_cluster(leader_acc_empty + 8 * acc);
-                    }
-                    const int left = col < p.cols ? min(32, p.n - t.n0 - j0) : 0;
-                    float add[32];
-                    const float *from = c > t.r0 ? out : in;
+                for (int j0 = 0; j0 < 128; j0 += 8) {
+                    uint32_t v[8];
+                    tmem_load8(from + acc * kAccCols + j0, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        add[j] = from && j < left ? from[(j0 + j) * p.ld] : 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < left) out[(j0 + j) * p.ld] = __uint_as_float(v[j]) + add[j];
+                    for (int j = 0; j < 8; ++j) sum[j0 + j] += __uint_as_float(v[j]);
                 }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(leader_acc_empty + 8 * acc);
                 acc ^= 1;
                 if (acc == 0) aph ^= 1;
             }
+            // a wait that gave up: no sums
+            const float lost = ok ? 0.f : __uint_as_float(0x7fffffffu);
+            const int m = (int)rank * kHalf + 32 * quarter + lane, j1 = side * 128;
+            if (t.part >= 0) {
+                float *out = p.part + (int64_t)t.part * (kTileM * kTileN) + j1 * kTileM + m;
+#pragma unroll
+                for (int j = 0; j < 128; ++j) out[j * kTileM] = sum[j] + lost;
+                continue;
+            }
+            if (t.m0 + m >= p.cols) continue;
+            float *out = p.out + (t.n0 + j1) * p.ld + t.m0 + m;
+            const int64_t to_in = p.in ? p.in - p.out : 0;
+            const int left = p.n - t.n0 - j1;
+#pragma unroll
+            for (int j0 = 0; j0 < 128; j0 += 8) {
+                float add[8];
+                float *row = out;
+#pragma unroll
+                for (int j = 0; j < 8; ++j, row += p.ld)
+                    add[j] = (p.in && j0 + j < left ? row[to_in] : 0.f) + lost;
+#pragma unroll
+                for (int j = 0; j < 8; ++j, out += p.ld)
+                    if (j0 + j < left) *out = sum[j0 + j] + add[j];
+            }
         }
+        __syncwarp();
     }
     // Where a wait gave up, copies and products may still be on their way:
     // they end by themselves within microseconds.
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
     if (*gave_up) {
         const uint64_t t0 = now_ns();
@@ -482,6 +549,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                      "r"(2 * kAccCols));
+    }
+}
+
+// The split tiles: dw = in + the parts of each in order.  A block takes 4 rows
+// of a tile, a thread a column of them.
+constexpr int kJoinRows = 4;
+__global__ void __launch_bounds__(kTileM) wgrad_join_kernel(const WgradParams p) {
+    grid_dep_wait();
+    const int tile = blockIdx.x / (kTileN / kJoinRows);
+    const int j0 = blockIdx.x % (kTileN / kJoinRows) * kJoinRows;
+    int m0, n0;
+    tile_of(p, p.whole + tile, m0, n0);
+    const float *part = p.part + (int64_t)tile * p.splits * (kTileM * kTileN) + j0 * kTileM +
+                        threadIdx.x;
+    float sum[kJoinRows] = {};
+    for (int s = 0; s < p.splits; ++s) {
+#pragma unroll
+        for (int j = 0; j < kJoinRows; ++j)
+            sum[j] += part[(int64_t)s * (kTileM * kTileN) + j * kTileM];
+    }
+    const int m = m0 + threadIdx.x;
+    if (m >= p.cols) return;
+#pragma unroll
+    for (int j = 0; j < kJoinRows; ++j) {
+        const int n = n0 + j0 + j;
+        const int64_t at = n * p.ld + m;
+        if (n < p.n) p.out[at] = p.in ? p.in[at] + sum[j] : sum[j];
     }
 }
 
@@ -552,10 +646,35 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
                      dy, p.rows, p.n, ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B));
     auto kern = wgrad_kernel<T, F>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), kWgradSmem));
-    const int pairs = std::max(1, std::min(p.units, sm_count() / 2));
-    kern<<<2 * pairs, kWgradThreads, kWgradSmem, s>>>(codes, grads, p);
+    kern<<<2 * std::min(p.units, sm_count() / 2), kWgradThreads, kWgradSmem, s>>>(codes, grads, p);
     POS_CUDA(cudaGetLastError());
+    const int tiles = p.tiles_m * p.tiles_n - p.whole;
+    if (p.splits > 1)
+        POS_CUDA(launch_dependent(wgrad_join_kernel, tiles * (kTileN / kJoinRows), kTileM, 0, s, p));
     return POS_OK;
+}
+
+// Full rounds of tiles take all rows each; the tiles of the last round are cut
+// along the rows where that ends sooner.  In units of a stage (64 rows of a
+// tile, 0.28 us): a round of `splits` parts takes its share of the rows and
+// about 6 stages to fill and drain, joining takes a launch (10 stages) and
+// reads every part.
+static void cut_rows(WgradParams &p, int pairs) {
+    const int tiles = p.tiles_m * p.tiles_n;
+    p.whole = tiles / pairs * pairs;
+    const int rest = tiles - p.whole;
+    const int64_t stages = (p.rows + kTileK - 1) / kTileK;
+    p.splits = 1, p.split_rows = stages * kTileK;
+    double best = stages + 6.;
+    for (int s = 2; rest > 0 && s <= stages && rest * s <= 3 * pairs; ++s) {
+        const int64_t each = (stages + s - 1) / s;
+        if ((s - 1) * each >= stages) continue;  // the last part would be empty
+        const double t = (double)((rest * s + pairs - 1) / pairs) * (each + 6.) + 10. +
+                         0.2 * rest * s * 4. / pairs;
+        if (t < best) best = t, p.splits = s, p.split_rows = each * kTileK;
+    }
+    if (p.splits == 1) p.whole = tiles;
+    p.units = p.whole + (tiles - p.whole) * p.splits;
 }
 
 static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int32_t dtype,
@@ -575,19 +694,24 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
     p.tiles_n = (int32_t)((n + kTileN - 1) / kTileN);
     if ((int64_t)p.tiles_m * p.tiles_n > 0x7fffffffll)
         return fail(POS_EINVAL, "wgrad: n * cols too large");
-    p.splits = 1;
-    p.units = p.tiles_m * p.tiles_n;
-    p.chunk_rows = 1024;
-    p.split_rows = (rows + p.chunk_rows - 1) / p.chunk_rows * p.chunk_rows;
-    void *copy = nullptr;
-    if (!aligned16(dy) || ld_dy % 8 || ld_dy < n) {
+    cut_rows(p, std::max(1, sm_count() / 2));
+    // scratch: the split tiles' parts, then dy's copy
+    const int64_t part_bytes =
+        p.splits > 1 ? (int64_t)(p.units - p.whole) * (kTileM * kTileN) * 4 : 0;
+    const bool copy = !aligned16(dy) || ld_dy % 8 || ld_dy < n;
+    const int64_t ld2 = (n + 7) / 8 * 8, bytes = part_bytes + (copy ? rows * ld2 * 2 : 0);
+    void *scratch = nullptr;
+    if (bytes) {
         cudaMemPool_t pool;
         POS_TRY(scratch_pool(&pool));
-        const int64_t ld2 = (n + 7) / 8 * 8;
-        POS_CUDA(cudaMallocFromPoolAsync(&copy, (size_t)(rows * ld2) * 2, pool, s));
+        POS_CUDA(cudaMallocFromPoolAsync(&scratch, (size_t)bytes, pool, s));
+        p.part = static_cast<float *>(scratch);
+    }
+    if (copy) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(static_cast<char *>(scratch) + part_bytes);
         wgrad_copy_kernel<<<(int)std::min<int64_t>(rows, 65535), 256, 0, s>>>(
-            static_cast<const uint16_t *>(dy), ld_dy, static_cast<uint16_t *>(copy), ld2, rows, n);
-        dy = copy, ld_dy = ld2;
+            static_cast<const uint16_t *>(dy), ld_dy, to, ld2, rows, n);
+        dy = to, ld_dy = ld2;
     }
     pos_status st;
     if (dtype == POS_BF16)
@@ -598,7 +722,7 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
         st = format == POS_CKPT_INT8
                  ? launch_wgrad<__half, POS_CKPT_INT8>(ckpt, dy, ld_dy, p, s)
                  : launch_wgrad<__half, POS_CKPT_E4M3>(ckpt, dy, ld_dy, p, s);
-    const cudaError_t e = copy ? cudaFreeAsync(copy, s) : cudaSuccess;
+    const cudaError_t e = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
     if (st != POS_OK) return st;
     return e == cudaSuccess ? POS_OK : cuda_fail(e, "wgrad scratch");
 }
