@@ -79,8 +79,13 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {  // own CTA
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {  // any CTA of the pair
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+// A barrier in either CTA of the pair.  The default scope (the CTA) is enough:
+// what the arrival orders is this SM's own shared memory or TMEM, which this
+// SM's tensor core reads or writes; a release to the whole cluster waits for
+// the SM's global accesses too (1884 us instead of 1008 us for 8192 rows, n =
+// 10240, cols = 8192, together with the same change of the waits).
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
@@ -91,7 +96,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
@@ -487,9 +492,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         bool ok = true;
         for (int u = pair; u < p.units; u += pairs) {
             const Unit t = unit_of(p, u);
+            const int m = (int)rank * kHalf + 32 * quarter + lane, j1 = side * 128;
+            const int left = t.m0 + m < p.cols ? p.n - t.n0 - j1 : 0;  // rows of dW to write
+            // dw_in is read while the first products run: all loads at once
             float sum[128];
+            const float *in = p.in + (t.n0 + j1) * p.ld + t.m0 + m;
 #pragma unroll
-            for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+            for (int j = 0; j < 128; ++j, in += p.ld)
+                sum[j] = p.in && t.part < 0 && j < left ? *in : 0.f;
             for (int c = t.r0; c < t.r1; c += kChunkRows) {
                 if (ok) ok = bar_wait(acc_full + 8 * acc, aph, gave_up);
                 ok = __all_sync(0xffffffffu, ok);
@@ -509,27 +519,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
             }
             // a wait that gave up: no sums
             const float lost = ok ? 0.f : __uint_as_float(0x7fffffffu);
-            const int m = (int)rank * kHalf + 32 * quarter + lane, j1 = side * 128;
             if (t.part >= 0) {
                 float *out = p.part + (int64_t)t.part * (kTileM * kTileN) + j1 * kTileM + m;
 #pragma unroll
                 for (int j = 0; j < 128; ++j) out[j * kTileM] = sum[j] + lost;
-                continue;
-            }
-            if (t.m0 + m >= p.cols) continue;
-            float *out = p.out + (t.n0 + j1) * p.ld + t.m0 + m;
-            const int64_t to_in = p.in ? p.in - p.out : 0;
-            const int left = p.n - t.n0 - j1;
+            } else {
+                float *out = p.out + (t.n0 + j1) * p.ld + t.m0 + m;
 #pragma unroll
-            for (int j0 = 0; j0 < 128; j0 += 8) {
-                float add[8];
-                float *row = out;
-#pragma unroll
-                for (int j = 0; j < 8; ++j, row += p.ld)
-                    add[j] = (p.in && j0 + j < left ? row[to_in] : 0.f) + lost;
-#pragma unroll
-                for (int j = 0; j < 8; ++j, out += p.ld)
-                    if (j0 + j < left) *out = sum[j0 + j] + add[j];
+                for (int j = 0; j < 128; ++j, out += p.ld)
+                    if (j < left) *out = sum[j] + lost;
             }
         }
         __syncwarp();
