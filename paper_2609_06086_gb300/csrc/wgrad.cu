@@ -96,10 +96,10 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok)
-        : "r"(bar), "r"(parity)
+        : "r"(bar), "r"(parity), "r"(1000000)  // sleeps for up to 1 ms
         : "memory");
     return ok;
 }
@@ -114,8 +114,7 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 __device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *gave_up) {
     const uint64_t t0 = now_ns();
     for (;;) {
-        for (int i = 0; i < 64; ++i)
-            if (bar_try(bar, parity)) return true;
+        if (bar_try(bar, parity)) return true;
         if (*gave_up) return false;
         if (now_ns() - t0 > kWaitNs) {
             *gave_up = 1;
@@ -195,56 +194,104 @@ __device__ __forceinline__ void take_registers() {
 }
 
 // ---------------------------------------------------------------------------
-// Decoding 16 codes under one scale into 16-bit values
+// Decoding codes into 16-bit values
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t h2_bits(__nv_bfloat162 v) {
-    uint32_t u;
-    memcpy(&u, &v, 4);
-    return u;
-}
-__device__ __forceinline__ __nv_bfloat162 bf2(uint32_t u) {
+__device__ __forceinline__ __nv_bfloat162 as_bf2(uint32_t u) {
     __nv_bfloat162 v;
     memcpy(&v, &u, 4);
     return v;
 }
-// Four codes of a word as two words of bf16 pairs: every step is exact.
-// int8: byte b of bits s m (s: 128) gives 128 + m and 128 + s as bf16, whose
-// difference is the code.  e4m3: sign, exponent and mantissa moved to bf16's
-// places give the value times 2^-120 (subnormals too).
-template <int F>
-__device__ __forceinline__ uint2 decode4_bf16(uint32_t w, __nv_bfloat162 scale) {
-    uint32_t r[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if constexpr (F == POS_CKPT_INT8) {
-            const uint32_t b = __byte_perm(w, 0x43434343u, i ? 0x4342 : 0x4140);
-            const __nv_bfloat162 q = __hsub2(bf2(b & 0xff7fff7fu), bf2(b & 0xff80ff80u));
-            r[i] = h2_bits(__hmul2(q, scale));
-        } else {
-            const uint32_t b = __byte_perm(w, 0u, i ? 0x3424 : 0x1404);
-            const uint32_t q = (b & 0x80008000u) | (b >> 4 & 0x07f007f0u);
-            r[i] = h2_bits(__hmul2(__hmul2(bf2(q), bf2(0x7b807b80u)), scale));
-        }
-    }
-    return make_uint2(r[0], r[1]);
+__device__ __forceinline__ __half2 as_h2(uint32_t u) {
+    __half2 v;
+    memcpy(&v, &u, 4);
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ uint32_t bits_of(V v) {
+    uint32_t u;
+    memcpy(&u, &v, 4);
+    return u;
 }
 
-// 16 codes as two 16-byte words of consecutive values.
+// The order of the columns of x among the rows of a tile: the four of a word
+// of codes give the words (0, 2) and (1, 3), which masks alone separate.
+__device__ __forceinline__ int column_at(int row) {
+    return (row & ~3) | (row & 1) << 1 | (row >> 1 & 1);
+}
+
+// Scales under which the short ways below are exact, or round once as
+// poseidon_ckpt_unpack does, and cannot saturate.
 template <typename T, int F>
-__device__ __forceinline__ void decode16(uint4 c, int byte, uint4 (&v)[2]) {
+__device__ __forceinline__ bool short_way(int byte) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        return F == POS_CKPT_INT8 || byte <= 127 + 7;  // the factor 2^(120 + e) is finite
+    else if constexpr (F == POS_CKPT_INT8)
+        return byte >= 127 - 24 && byte <= 127 + 9;    // 2^e is an f16, 127 * 2^9 < 65504
+    else
+        return byte >= 127 - 32 && byte <= 127 + 7;    // 2^(8 + e) is an f16, 448 * 2^7 < 65504
+}
+// The factor of a short way, in both halves of a word.
+template <typename T, int F>
+__device__ __forceinline__ uint32_t short_factor(int byte) {
+    uint32_t f;
     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        // 2^e as bf16 bits, in both halves
-        const uint32_t s = byte == kScaleNan ? 0x7fffu : (uint32_t)byte << 7;
-        const __nv_bfloat162 s2 = bf2(s | s << 16);
-        const uint2 a = decode4_bf16<F>(c.x, s2), b = decode4_bf16<F>(c.y, s2);
-        const uint2 d = decode4_bf16<F>(c.z, s2), e = decode4_bf16<F>(c.w, s2);
-        v[0] = make_uint4(a.x, a.y, b.x, b.y);
-        v[1] = make_uint4(d.x, d.y, e.x, e.y);
+        f = F == POS_CKPT_INT8 ? (byte == kScaleNan ? 0x7fffu : (uint32_t)byte << 7)
+                               : (uint32_t)(byte + 120) << 7;
     } else {
-        const float s = scale_value(byte);
-        v[0] = from_float<T, true>(decode8<F>(make_uint2(c.x, c.y), s)).a;
-        v[1] = from_float<T, true>(decode8<F>(make_uint2(c.z, c.w), s)).a;
+        const int e = byte - 127 + (F == POS_CKPT_INT8 ? 0 : 8);
+        f = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
     }
+    return f | f << 16;
+}
+// Four codes as two words.
+//   int8 -> bf16: byte s m (s = 128, m < 128) gives 128 + m and 128 + s, whose
+//     difference is the code; all steps are exact.
+//   int8 -> f16: the code + 128 as the last byte of 1024 + it, minus 1152.
+//   e4m3 -> bf16, f16: sign, exponent and mantissa in their places are the
+//     value times 2^-120 or 2^-8, subnormals too.
+template <typename T, int F>
+__device__ __forceinline__ uint2 decode4(uint32_t w, uint32_t factor) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        uint32_t even, odd;
+        if constexpr (F == POS_CKPT_INT8) {
+            const uint32_t h = w >> 8;
+            even = bits_of(__hsub2(as_bf2((w & 0x007f007fu) | 0x43004300u),
+                                   as_bf2((w & 0x00800080u) | 0x43004300u)));
+            odd = bits_of(__hsub2(as_bf2((h & 0x007f007fu) | 0x43004300u),
+                                  as_bf2((h & 0x00800080u) | 0x43004300u)));
+        } else {
+            even = (w << 8 & 0x80008000u) | (w << 4 & 0x07f007f0u);
+            odd = (w & 0x80008000u) | (w >> 4 & 0x07f007f0u);
+        }
+        return make_uint2(bits_of(__hmul2(as_bf2(even), as_bf2(factor))),
+                          bits_of(__hmul2(as_bf2(odd), as_bf2(factor))));
+    } else {
+        uint32_t even, odd;
+        if constexpr (F == POS_CKPT_INT8) {
+            const uint32_t u = w ^ 0x80808080u;
+            even = bits_of(__hsub2(as_h2((u & 0x00ff00ffu) | 0x64006400u), as_h2(0x64806480u)));
+            odd = bits_of(__hsub2(as_h2((u >> 8 & 0x00ff00ffu) | 0x64006400u), as_h2(0x64806480u)));
+        } else {
+            even = (w << 8 & 0x80008000u) | (w << 7 & 0x3f803f80u);
+            odd = (w & 0x80008000u) | (w >> 1 & 0x3f803f80u);
+        }
+        return make_uint2(bits_of(__hmul2(as_h2(even), as_h2(factor))),
+                          bits_of(__hmul2(as_h2(odd), as_h2(factor))));
+    }
+}
+// Eight codes as eight values in column_at's order.
+template <typename T, int F>
+__device__ __forceinline__ uint4 decode8_short(uint2 c, uint32_t factor) {
+    const uint2 a = decode4<T, F>(c.x, factor), b = decode4<T, F>(c.y, factor);
+    return make_uint4(a.x, a.y, b.x, b.y);
+}
+template <typename T, int F>
+__device__ __forceinline__ uint4 decode8_long(uint2 c, int byte) {
+    const Vec8 v = decode8<F>(c, scale_value(byte));
+    Vec8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = v.v[(i & ~3) | (i & 1) << 1 | (i >> 1 & 1)];
+    return from_float<T, true>(o).a;
 }
 
 // ---------------------------------------------------------------------------
@@ -417,10 +464,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         __syncwarp();
     } else if (group <= kDecodeGroups) {
         give_registers<kDecodeRegs>();
-        // A thread decodes 16 columns of four rows of its group's stages.
+        // A thread decodes four pieces of 16 columns: eight lanes take 64
+        // columns of an even row and the other 64 of the odd row after it, so
+        // that both their loads and, the swizzle shifting odd rows by one
+        // piece of 16 bytes, their stores cover all banks.
         const int mine = group - 1;
-        const int i = threadIdx.x % 128, piece = i % 8, row = i / 8;
-        const int block = piece / 4, chunk = piece % 4 * 2;
+        const int i = threadIdx.x % 128, piece = i % 4, odd = i / 4 % 2, rows2 = i / 8;
         const uint32_t leader_full = in_cta(full, 0);
         int s = mine, cs = mine;
         uint32_t ph = 1, cph = 0;
@@ -438,14 +487,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 uint32_t byte[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const int tr = row + 16 * h;
+                    const int row = 2 * (rows2 + 16 * (h / 2)) + odd, at = piece + 4 * (odd ^ h % 2);
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(c[h].x), "=r"(c[h].y), "=r"(c[h].z), "=r"(c[h].w)
-                                 : "r"(c_at + cs * kCodeBytes + tr * kHalf + piece * 16)
+                                 : "r"(c_at + cs * kCodeBytes + row * kHalf + at * 16)
                                  : "memory");
                     asm volatile("ld.shared.u8 %0, [%1];"
                                  : "=r"(byte[h])
-                                 : "r"(s_at + cs * kScaleBytes + tr * 4 + piece / 2)
+                                 : "r"(s_at + cs * kScaleBytes + row * 4 + at / 2)
                                  : "memory");
                 }
                 __syncwarp();
@@ -456,21 +505,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
+                    const int row = 2 * (rows2 + 16 * (h / 2)) + odd, block = odd ^ h % 2;
+                    const uint32_t to = a_at + s * kABytes + block * (kTileK * 128) + row * 128;
                     uint4 v[2];
-                    const int tr = row + 16 * h;
-                    decode16<T, F>(c[h], (int)byte[h], v);
-                    const uint32_t to = a_at + s * kABytes + block * (kTileK * 128) + tr * 128;
-                    // the upper block's lanes store their second half first:
-                    // eight lanes then cover all banks
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int half = q ^ block;
-                        const uint4 x = half ? v[1] : v[0];
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                         to + (((chunk + half) ^ (tr & 7)) << 4)),
-                                     "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
-                                     : "memory");
+                    const uint2 lo = make_uint2(c[h].x, c[h].y), hi = make_uint2(c[h].z, c[h].w);
+                    if (short_way<T, F>((int)byte[h])) {
+                        const uint32_t f = short_factor<T, F>((int)byte[h]);
+                        v[0] = decode8_short<T, F>(lo, f);
+                        v[1] = decode8_short<T, F>(hi, f);
+                    } else {
+                        v[0] = decode8_long<T, F>(lo, (int)byte[h]);
+                        v[1] = decode8_long<T, F>(hi, (int)byte[h]);
                     }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                         to + (((2 * piece + q) ^ (row & 7)) << 4)),
+                                     "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w)
+                                     : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -492,7 +544,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         bool ok = true;
         for (int u = pair; u < p.units; u += pairs) {
             const Unit t = unit_of(p, u);
-            const int m = (int)rank * kHalf + 32 * quarter + lane, j1 = side * 128;
+            const int m = (int)rank * kHalf + 32 * quarter + column_at(lane), j1 = side * 128;
             const int left = t.m0 + m < p.cols ? p.n - t.n0 - j1 : 0;  // rows of dW to write
             // dw_in is read while the first products run: all loads at once
             float sum[128];
