@@ -467,9 +467,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         // A thread decodes four pieces of 16 columns: eight lanes take 64
         // columns of an even row and the other 64 of the odd row after it, so
         // that both their loads and, the swizzle shifting odd rows by one
-        // piece of 16 bytes, their stores cover all banks.
+        // piece of 16 bytes, their stores cover all banks.  Pieces h = 0, 1
+        // are the two blocks of 64 columns, h = 2, 3 the same 32 rows on.
         const int mine = group - 1;
-        const int i = threadIdx.x % 128, piece = i % 4, odd = i / 4 % 2, rows2 = i / 8;
+        const int piece = threadIdx.x % 4, odd = threadIdx.x / 4 % 2;
+        const int row = 2 * (threadIdx.x % 128 / 8) + odd;
+        const uint32_t from[2] = {c_at + row * kHalf + (piece + 4 * odd) * 16,
+                                  c_at + row * kHalf + (piece + 4 * (odd ^ 1)) * 16};
+        const uint32_t scale_at = s_at + row * 4 + piece / 2;
+        const uint32_t to_row = a_at + row * 128 + odd * (kTileK * 128);
+        const uint32_t to[2] = {to_row + (((2 * piece) ^ (row & 7)) << 4),
+                                to_row + (((2 * piece + 1) ^ (row & 7)) << 4)};
+        const uint32_t other = odd ? 0u - kTileK * 128 : kTileK * 128;  // to the other block
         const uint32_t leader_full = in_cta(full, 0);
         int s = mine, cs = mine;
         uint32_t ph = 1, cph = 0;
@@ -487,16 +496,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 uint32_t byte[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const int row = 2 * (rows2 + 16 * (h / 2)) + odd, at = piece + 4 * (odd ^ h % 2);
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(c[h].x), "=r"(c[h].y), "=r"(c[h].z), "=r"(c[h].w)
-                                 : "r"(c_at + cs * kCodeBytes + row * kHalf + at * 16)
-                                 : "memory");
+                                 : "r"(from[h % 2] + cs * kCodeBytes + h / 2 * (32 * kHalf)));
                     asm volatile("ld.shared.u8 %0, [%1];"
                                  : "=r"(byte[h])
-                                 : "r"(s_at + cs * kScaleBytes + row * 4 + at / 2)
-                                 : "memory");
+                                 : "r"(scale_at + 2 * (odd ^ h % 2) + cs * kScaleBytes +
+                                       h / 2 * (32 * 4)));
                 }
+                const bool all_short = __all_sync(
+                    0xffffffffu, short_way<T, F>((int)byte[0]) && short_way<T, F>((int)byte[1]) &&
+                                     short_way<T, F>((int)byte[2]) && short_way<T, F>((int)byte[3]));
                 __syncwarp();
                 if (lane == 0) bar_arrive(code_empty + 8 * cs);
                 cs += kDecodeGroups;
@@ -505,11 +515,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const int row = 2 * (rows2 + 16 * (h / 2)) + odd, block = odd ^ h % 2;
-                    const uint32_t to = a_at + s * kABytes + block * (kTileK * 128) + row * 128;
-                    uint4 v[2];
                     const uint2 lo = make_uint2(c[h].x, c[h].y), hi = make_uint2(c[h].z, c[h].w);
-                    if (short_way<T, F>((int)byte[h])) {
+                    uint4 v[2];
+                    if (all_short) {
                         const uint32_t f = short_factor<T, F>((int)byte[h]);
                         v[0] = decode8_short<T, F>(lo, f);
                         v[1] = decode8_short<T, F>(hi, f);
@@ -520,9 +528,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
-                                         to + (((2 * piece + q) ^ (row & 7)) << 4)),
-                                     "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w)
-                                     : "memory");
+                                         to[q] + s * kABytes + h % 2 * other + h / 2 * (32 * 128)),
+                                     "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
