@@ -224,19 +224,19 @@ __device__ __forceinline__ int column_at(int row) {
 template <typename T, int F>
 __device__ __forceinline__ bool short_way(int byte) {
     if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        return F == POS_CKPT_INT8 || byte <= 127 + 7;  // the factor 2^(120 + e) is finite
+        return byte <= (F == POS_CKPT_INT8 ? 127 + 119   // 256 * 2^e is finite
+                                           : 127 + 7);   // the factor 2^(120 + e) is
     else if constexpr (F == POS_CKPT_INT8)
         return byte >= 127 - 24 && byte <= 127 + 9;    // 2^e is an f16, 127 * 2^9 < 65504
     else
         return byte >= 127 - 32 && byte <= 127 + 7;    // 2^(8 + e) is an f16, 448 * 2^7 < 65504
 }
-// The factor of a short way, in both halves of a word.
+// The factor of a short way in both halves of a word; int8 -> bf16: 128 * 2^e.
 template <typename T, int F>
 __device__ __forceinline__ uint32_t short_factor(int byte) {
     uint32_t f;
     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        f = F == POS_CKPT_INT8 ? (byte == kScaleNan ? 0x7fffu : (uint32_t)byte << 7)
-                               : (uint32_t)(byte + 120) << 7;
+        f = (uint32_t)(byte + (F == POS_CKPT_INT8 ? 7 : 120)) << 7;
     } else {
         const int e = byte - 127 + (F == POS_CKPT_INT8 ? 0 : 8);
         f = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
@@ -244,25 +244,24 @@ __device__ __forceinline__ uint32_t short_factor(int byte) {
     return f | f << 16;
 }
 // Four codes as two words.
-//   int8 -> bf16: byte s m (s = 128, m < 128) gives 128 + m and 128 + s, whose
-//     difference is the code; all steps are exact.
+//   int8 -> bf16: byte s m (s: one bit, m: seven) gives, under the exponent of
+//     128 * 2^e, (128 + m) * 2^e and, s added to the exponent, 128 (1 + s) 2^e;
+//     their difference is the value, exactly.
 //   int8 -> f16: the code + 128 as the last byte of 1024 + it, minus 1152.
 //   e4m3 -> bf16, f16: sign, exponent and mantissa in their places are the
 //     value times 2^-120 or 2^-8, subnormals too.
 template <typename T, int F>
 __device__ __forceinline__ uint2 decode4(uint32_t w, uint32_t factor) {
     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        uint32_t even, odd;
         if constexpr (F == POS_CKPT_INT8) {
             const uint32_t h = w >> 8;
-            even = bits_of(__hsub2(as_bf2((w & 0x007f007fu) | 0x43004300u),
-                                   as_bf2((w & 0x00800080u) | 0x43004300u)));
-            odd = bits_of(__hsub2(as_bf2((h & 0x007f007fu) | 0x43004300u),
-                                  as_bf2((h & 0x00800080u) | 0x43004300u)));
-        } else {
-            even = (w << 8 & 0x80008000u) | (w << 4 & 0x07f007f0u);
-            odd = (w & 0x80008000u) | (w >> 4 & 0x07f007f0u);
+            return make_uint2(bits_of(__hsub2(as_bf2((w & 0x007f007fu) | factor),
+                                              as_bf2((w & 0x00800080u) + factor))),
+                              bits_of(__hsub2(as_bf2((h & 0x007f007fu) | factor),
+                                              as_bf2((h & 0x00800080u) + factor))));
         }
+        const uint32_t even = (w << 8 & 0x80008000u) | (w << 4 & 0x07f007f0u);
+        const uint32_t odd = (w & 0x80008000u) | (w >> 4 & 0x07f007f0u);
         return make_uint2(bits_of(__hmul2(as_bf2(even), as_bf2(factor))),
                           bits_of(__hmul2(as_bf2(odd), as_bf2(factor))));
     } else {
