@@ -227,18 +227,19 @@ __device__ __forceinline__ bool short_way(int byte) {
         return byte <= (F == POS_CKPT_INT8 ? 127 + 119   // 256 * 2^e is finite
                                            : 127 + 7);   // the factor 2^(120 + e) is
     else if constexpr (F == POS_CKPT_INT8)
-        return byte >= 127 - 24 && byte <= 127 + 9;    // 2^e is an f16, 127 * 2^9 < 65504
+        return byte >= 127 - 24 && byte <= 127 + 5;    // 1024 * 2^e to 1280 * 2^e are normal
     else
         return byte >= 127 - 32 && byte <= 127 + 7;    // 2^(8 + e) is an f16, 448 * 2^7 < 65504
 }
-// The factor of a short way in both halves of a word; int8 -> bf16: 128 * 2^e.
+// The factor of a short way in both halves of a word; int8: what
+// the code's zero stands at, 128 * 2^e in bf16 and 1024 * 2^e in f16.
 template <typename T, int F>
 __device__ __forceinline__ uint32_t short_factor(int byte) {
     uint32_t f;
     if constexpr (std::is_same<T, __nv_bfloat16>::value) {
         f = (uint32_t)(byte + (F == POS_CKPT_INT8 ? 7 : 120)) << 7;
     } else {
-        const int e = byte - 127 + (F == POS_CKPT_INT8 ? 0 : 8);
+        const int e = byte - 127 + (F == POS_CKPT_INT8 ? 10 : 8);
         f = e >= -14 ? (uint32_t)(e + 15) << 10 : 1u << (e + 24);
     }
     return f | f << 16;
@@ -247,7 +248,8 @@ __device__ __forceinline__ uint32_t short_factor(int byte) {
 //   int8 -> bf16: byte s m (s: one bit, m: seven) gives, under the exponent of
 //     128 * 2^e, (128 + m) * 2^e and, s added to the exponent, 128 (1 + s) 2^e;
 //     their difference is the value, exactly.
-//   int8 -> f16: the code + 128 as the last byte of 1024 + it, minus 1152.
+//   int8 -> f16: the code + 128 as the last byte of (1024 + it) 2^e, minus
+//     1152 * 2^e: exact, f16 having ten bits after the first.
 //   e4m3 -> bf16, f16: sign, exponent and mantissa in their places are the
 //     value times 2^-120 or 2^-8, subnormals too.
 template <typename T, int F>
@@ -265,15 +267,13 @@ __device__ __forceinline__ uint2 decode4(uint32_t w, uint32_t factor) {
         return make_uint2(bits_of(__hmul2(as_bf2(even), as_bf2(factor))),
                           bits_of(__hmul2(as_bf2(odd), as_bf2(factor))));
     } else {
-        uint32_t even, odd;
         if constexpr (F == POS_CKPT_INT8) {
-            const uint32_t u = w ^ 0x80808080u;
-            even = bits_of(__hsub2(as_h2((u & 0x00ff00ffu) | 0x64006400u), as_h2(0x64806480u)));
-            odd = bits_of(__hsub2(as_h2((u >> 8 & 0x00ff00ffu) | 0x64006400u), as_h2(0x64806480u)));
-        } else {
-            even = (w << 8 & 0x80008000u) | (w << 7 & 0x3f803f80u);
-            odd = (w & 0x80008000u) | (w >> 1 & 0x3f803f80u);
+            const uint32_t u = w ^ 0x80808080u, zero = factor | 0x00800080u;
+            return make_uint2(bits_of(__hsub2(as_h2((u & 0x00ff00ffu) | factor), as_h2(zero))),
+                              bits_of(__hsub2(as_h2((u >> 8 & 0x00ff00ffu) | factor), as_h2(zero))));
         }
+        const uint32_t even = (w << 8 & 0x80008000u) | (w << 7 & 0x3f803f80u);
+        const uint32_t odd = (w & 0x80008000u) | (w >> 1 & 0x3f803f80u);
         return make_uint2(bits_of(__hmul2(as_h2(even), as_h2(factor))),
                           bits_of(__hmul2(as_h2(odd), as_h2(factor))));
     }
