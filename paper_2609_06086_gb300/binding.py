@@ -91,6 +91,16 @@ class pos_heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class qk_pair(C.Structure):
+    """The (queries, keys) array of two pos_heads, its fields in one row: a
+    call builds several, and nested structures take three times as long."""
+    _fields_ = [("q", C.c_void_p), ("q_token", C.c_int64), ("q_head", C.c_int64),
+                ("k", C.c_void_p), ("k_token", C.c_int64), ("k_head", C.c_int64)]
+
+
+assert C.sizeof(qk_pair) == 2 * C.sizeof(pos_heads)
+
+
 class PoseidonError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -121,11 +131,9 @@ def lib():
         L.poseidon_ckpt_pack.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp]
         L.poseidon_ckpt_unpack.argtypes = [vp, i32, i64, i64, vp, i32, i64, vp]
         L.poseidon_ckpt_wgrad.argtypes = [vp, i32, vp, i32, i64, i64, i64, i64, vp, vp, i64, vp]
-        L.poseidon_qk_forward.argtypes = [C.POINTER(pos_qk), C.POINTER(pos_heads),
-                                          C.POINTER(pos_heads), vp, vp, vp, vp, vp]
-        L.poseidon_qk_backward.argtypes = [C.POINTER(pos_qk), C.POINTER(pos_heads), vp, vp, vp,
-                                           vp, C.POINTER(pos_heads), C.POINTER(pos_heads), vp,
-                                           vp, vp]
+        qk, pair = C.POINTER(pos_qk), C.POINTER(qk_pair)
+        L.poseidon_qk_forward.argtypes = [qk, pair, pair, vp, vp, vp, vp, vp]
+        L.poseidon_qk_backward.argtypes = [qk, pair, vp, vp, vp, vp, pair, pair, vp, vp, vp]
         L.poseidon_last_error.restype = C.c_char_p
         L.poseidon_last_error.argtypes = []
         for name in EXPORTS[:-1]:
@@ -323,20 +331,19 @@ def poseidon_ckpt_wgrad(d_ckpt: int, format: int, d_dy: int, dtype: int, ld_dy: 
                                      d_dw_out, ld_dw, stream))
 
 
-def qk_heads(q: int, q_token: int, q_head: int, k: int, k_token: int, k_head: int):
-    """The (queries, keys) pair of pos_heads that the q/k calls take: pointer,
-    token stride and head stride of each."""
-    return (pos_heads * 2)((q, q_token, q_head), (k, k_token, k_head))
+# qk_heads(q, q_token, q_head, k, k_token, k_head): the (queries, keys) pair that
+# the q/k calls take, pointer, token stride and head stride of each
+qk_heads = qk_pair
 
 
 def poseidon_qk_forward(qk: pos_qk, x, y, rstd=(0, 0), ckpt=(0, 0), stream: int = 0):
     """x, y: qk_heads(); rstd, ckpt: (queries, keys) device pointers, 0 = not kept."""
-    _check(lib().poseidon_qk_forward(C.byref(qk), x, y, rstd[0], rstd[1], ckpt[0], ckpt[1],
+    _check(lib().poseidon_qk_forward(qk, x, y, rstd[0], rstd[1], ckpt[0], ckpt[1],
                                      stream))
 
 
 def poseidon_qk_backward(qk: pos_qk, dy, dx, rstd, ckpt=(0, 0), x=None, dw_in: int = 0,
                          dw: int = 0, stream: int = 0):
     """dy, dx: qk_heads(); x: qk_heads() or None (the checkpoints are read)."""
-    _check(lib().poseidon_qk_backward(C.byref(qk), x, ckpt[0], ckpt[1], rstd[0], rstd[1], dy, dx,
+    _check(lib().poseidon_qk_backward(qk, x, ckpt[0], ckpt[1], rstd[0], rstd[1], dy, dx,
                                       dw_in, dw, stream))

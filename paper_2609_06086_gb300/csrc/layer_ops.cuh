@@ -53,43 +53,37 @@ struct Vec8 {
     float v[8];
 };
 
-// Codes of 8 values under one scale byte.  x * 2^-e is exact (or an underflow
+// Codes of 4 values under one scale byte.  x * 2^-e is exact (or an underflow
 // far below half a code), so each code is rounded once: int8 by adding
 // 1.5 * 2^23, whose last bit is a whole number, e4m3 by the conversion.  Only
 // the largest scale can leave values past the top code, which saturate.
 template <int F>
-__device__ __forceinline__ uint2 encode8(const Vec8 &x, int byte) {
-    if (byte == kScaleNan) return make_uint2(0u, 0u);
+__device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, int byte) {
+    if (byte == kScaleNan) return 0u;
     const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
     if constexpr (F == POS_CKPT_INT8) {
-        uint32_t b[8];
         if (byte == Fmt<F>::kScaleHi) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                b[i] = __float_as_uint(fminf(fmaxf(x.v[i] * inv, -127.f), 127.f) + 12582912.f);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(x.v[i], inv, 12582912.f));
+            const float top = 127.f * scale_value(byte);
+            x0 = fminf(fmaxf(x0, -top), top), x1 = fminf(fmaxf(x1, -top), top);
+            x2 = fminf(fmaxf(x2, -top), top), x3 = fminf(fmaxf(x3, -top), top);
         }
-        uint32_t w[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            w[h] = __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040),
-                               __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
-        return make_uint2(w[0], w[1]);
+        const uint32_t a = __float_as_uint(fmaf(x0, inv, 12582912.f));
+        const uint32_t b = __float_as_uint(fmaf(x1, inv, 12582912.f));
+        const uint32_t c = __float_as_uint(fmaf(x2, inv, 12582912.f));
+        const uint32_t d = __float_as_uint(fmaf(x3, inv, 12582912.f));
+        return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
     } else {
-        uint32_t w[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t lo = __nv_cvt_float2_to_fp8x2(
-                make_float2(x.v[4 * h] * inv, x.v[4 * h + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-            const uint32_t hi = __nv_cvt_float2_to_fp8x2(
-                make_float2(x.v[4 * h + 2] * inv, x.v[4 * h + 3] * inv), __NV_SATFINITE,
-                __NV_E4M3);
-            w[h] = lo | hi << 16;
-        }
-        return make_uint2(w[0], w[1]);
+        const uint32_t lo =
+            __nv_cvt_float2_to_fp8x2(make_float2(x0 * inv, x1 * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi =
+            __nv_cvt_float2_to_fp8x2(make_float2(x2 * inv, x3 * inv), __NV_SATFINITE, __NV_E4M3);
+        return lo | hi << 16;
     }
+}
+template <int F>
+__device__ __forceinline__ uint2 encode8(const Vec8 &x, int byte) {
+    return make_uint2(encode4<F>(x.v[0], x.v[1], x.v[2], x.v[3], byte),
+                      encode4<F>(x.v[4], x.v[5], x.v[6], x.v[7], byte));
 }
 
 // The values of 8 codes: exact in f32.

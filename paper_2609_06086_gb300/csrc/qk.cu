@@ -25,104 +25,158 @@ struct QkParams {
     const float *cos, *sin;
     const int32_t *positions;
     float *part;               // backward: [block][2][dim] partial sums, or NULL
-    int64_t tokens, tasks, n_pos;
+    int64_t tokens, tasks[2], n_pos;
     int32_t heads[2], dim, half, pitch, spitch;
-    int32_t chunk, n_chunk;    // heads of a task, tasks of a token
+    int32_t chunk[2], n_chunk[2];  // heads of a task, tasks of a token
     int32_t pairing, format;
-    bool tables16;             // cos and sin rows can be read as 16-byte words
     float eps, inv_dim;
 };
 
-// What a thread knows of its 8 elements i = 8 l .. 8 l + 7 of every head of
-// one token.  turn: element i of Rot u is u_i c_i + u_partner s_i (s with its
-// sign), elements from rot on stay.
-struct Turn {
-    float c[8], s[8];
+// Two f32 operations in one instruction.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
+        "mul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
+        "mov.b64 c, {%6, %7};\nfma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ F2 both(float v) { return {v, v}; }
+
+// A thread's 8 elements of a head, as four pairs.
+struct Eight {
+    F2 v[4];
 };
 
-// POS_ROT_HALF: c, s per element; POS_ROT_ADJACENT: per pair, in [0, 4).
-__device__ __forceinline__ void load_turn(const QkParams &p, int64_t at, int l, Turn &t) {
-    const float *cs = p.cos + at * p.half, *sn = p.sin + at * p.half;
-    if (p.pairing == POS_ROT_HALF) {
-        const int first = 8 * l < p.half ? 8 * l : 8 * l - p.half;
-        if (p.tables16 && p.half % 8 == 0) {
-            if (8 * l < 2 * p.half) {
-                const float4 c0 = *reinterpret_cast<const float4 *>(cs + first);
-                const float4 c1 = *reinterpret_cast<const float4 *>(cs + first + 4);
-                const float4 s0 = *reinterpret_cast<const float4 *>(sn + first);
-                const float4 s1 = *reinterpret_cast<const float4 *>(sn + first + 4);
-                const float sg = 8 * l < p.half ? -1.f : 1.f;
-                const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-                const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    t.c[e] = c[e];
-                    t.s[e] = sg * s[e];
-                }
-            }
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = 8 * l + e;
-            if (i >= 2 * p.half) continue;
-            const int k = i < p.half ? i : i - p.half;
-            t.c[e] = cs[k];
-            t.s[e] = i < p.half ? -sn[k] : sn[k];
-        }
+// Where a thread's elements lie in a head.
+//   kRun: elements 8 l .. 8 l + 7.  The partners of the rotation lie in the
+//     same pair (POS_ROT_ADJACENT), in one other lane (POS_ROT_HALF with
+//     rot / 2 divisible by 8) or anywhere in the row.
+//   kSplit: 4 l .. 4 l + 3 and as many from dim / 2 + 4 l on: under
+//     POS_ROT_HALF with rot = dim a multiple of 64, partners lie in the same
+//     thread and a group of 32 columns in 8 lanes.  8192 tokens of 64 + 8 heads
+//     of 128, bf16, both passes: @SPLIT@ us, kRun @RUN@ us.
+enum Layout { kRun, kSplit };
+
+template <int L>
+__device__ __forceinline__ int element(const QkParams &p, int l, int e) {
+    if (L == kRun) return 8 * l + e;
+    return e < 4 ? 4 * l + e : p.half + 4 * l + (e - 4);
+}
+
+// The words of a thread's elements.  kSplit and ALIGNED: vector loads.
+template <typename T, int L, bool ALIGNED>
+__device__ __forceinline__ Raw8<T> load_row(const QkParams &p, const T *head, int l, bool live) {
+    if constexpr (L == kRun) {
+        return load8<ALIGNED>(head + 8 * l, live ? p.dim - 8 * l : 0);
     } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = 4 * l + e;
-            if (k >= p.half) continue;
-            t.c[e] = cs[k];
-            t.s[e] = sn[k];
+        Raw8<T> r;
+        zero_raw(r.a);
+        if constexpr (sizeof(T) == 4) zero_raw(r.b);
+        if (live && 4 * l < p.half) {
+            if constexpr (sizeof(T) == 4) {
+                r.a = *reinterpret_cast<const uint4 *>(head + 4 * l);
+                r.b = *reinterpret_cast<const uint4 *>(head + p.half + 4 * l);
+            } else {
+                const uint2 a = *reinterpret_cast<const uint2 *>(head + 4 * l);
+                const uint2 b = *reinterpret_cast<const uint2 *>(head + p.half + 4 * l);
+                r.a = make_uint4(a.x, a.y, b.x, b.y);
+            }
+        }
+        return r;
+    }
+}
+template <typename T, int L, bool ALIGNED>
+__device__ __forceinline__ void store_row(const QkParams &p, T *head, int l, bool live,
+                                          const Raw8<T> &r) {
+    if constexpr (L == kRun) {
+        store8<ALIGNED>(head + 8 * l, r, live ? p.dim - 8 * l : 0);
+    } else if (live && 4 * l < p.half) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<uint4 *>(head + 4 * l) = r.a;
+            *reinterpret_cast<uint4 *>(head + p.half + 4 * l) = r.b;
+        } else {
+            *reinterpret_cast<uint2 *>(head + 4 * l) = make_uint2(r.a.x, r.a.y);
+            *reinterpret_cast<uint2 *>(head + p.half + 4 * l) = make_uint2(r.a.z, r.a.w);
         }
     }
 }
 
-// Rot u, or with BACK its transpose, for the G lanes of a row.  Partners lie
-// in the same thread (adjacent pairs), in one other lane at the same slot
-// (half pairs of a half divisible by 8), or anywhere in the row, which then
-// goes through shared memory (`row`, one float per element).  Lanes without
-// a row take part in the exchanges.
-template <int G, bool BACK>
-__device__ __forceinline__ Vec8 turned(const QkParams &p, const Vec8 &u, const Turn &t, int l,
-                                       float *row) {
-    const int rot = 2 * p.half;
-    Vec8 y = u;
+__device__ __forceinline__ Eight pairs_of(const Vec8 &x) {
+    return {{{x.v[0], x.v[1]}, {x.v[2], x.v[3]}, {x.v[4], x.v[5]}, {x.v[6], x.v[7]}}};
+}
+__device__ __forceinline__ Vec8 values_of(const Eight &x) {
+    return {{x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y}};
+}
+
+// Every element's partner in the rotation (elements without one: anything).
+// Lanes without a row take part in the exchanges.
+template <int G, int L>
+__device__ __forceinline__ Eight partners(const QkParams &p, const Eight &u, int l, float *row) {
+    if constexpr (L == kSplit) return {{u.v[2], u.v[3], u.v[0], u.v[1]}};
+    Eight q;
     if (p.pairing == POS_ROT_ADJACENT) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = u.v[2 * e], b = u.v[2 * e + 1], s = BACK ? -t.s[e] : t.s[e];
-            if (8 * l + 2 * e >= rot) continue;
-            y.v[2 * e] = a * t.c[e] - b * s;
-            y.v[2 * e + 1] = b * t.c[e] + a * s;
-        }
-        return y;
-    }
-    Vec8 q;
-    if (p.half % 8 == 0) {
+        for (int i = 0; i < 4; ++i) q.v[i] = {u.v[i].y, u.v[i].x};
+    } else if (p.half % 8 == 0) {
         const int d = p.half / 8;
-        const int from = 8 * l < p.half ? l + d : (8 * l < rot ? l - d : l);
+        const int from = 8 * l < p.half ? l + d : (8 * l < 2 * p.half ? l - d : l);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q.v[e] = __shfl_sync(0xffffffffu, u.v[e], from, G);
+        for (int i = 0; i < 4; ++i)
+            q.v[i] = {__shfl_sync(0xffffffffu, u.v[i].x, from, G),
+                      __shfl_sync(0xffffffffu, u.v[i].y, from, G)};
     } else {
         __syncwarp();
-        *reinterpret_cast<float4 *>(row + 8 * l) = make_float4(u.v[0], u.v[1], u.v[2], u.v[3]);
-        *reinterpret_cast<float4 *>(row + 8 * l + 4) = make_float4(u.v[4], u.v[5], u.v[6], u.v[7]);
+        *reinterpret_cast<float4 *>(row + 8 * l) =
+            make_float4(u.v[0].x, u.v[0].y, u.v[1].x, u.v[1].y);
+        *reinterpret_cast<float4 *>(row + 8 * l + 4) =
+            make_float4(u.v[2].x, u.v[2].y, u.v[3].x, u.v[3].y);
         __syncwarp();
+        float o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int i = 8 * l + e;
-            q.v[e] = i < rot ? row[i < p.half ? i + p.half : i - p.half] : 0.f;
+            o[e] = i < 2 * p.half ? row[i < p.half ? i + p.half : i - p.half] : 0.f;
         }
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (8 * l + e < rot)
-            y.v[e] = u.v[e] * t.c[e] + q.v[e] * (BACK ? -t.s[e] : t.s[e]);
-    return y;
+        for (int i = 0; i < 4; ++i) q.v[i] = {o[2 * i], o[2 * i + 1]};
+    }
+    return q;
+}
+
+// The cosine of an element's pair and its sine with the sign that Rot gives
+// the partner's term; 1 and 0 from rot on.  `other`: the partner's element.
+template <int L>
+__device__ __forceinline__ void angle(const QkParams &p, int64_t at, int i, bool turn, float &c,
+                                      float &s, int &other) {
+    c = 1.f, s = 0.f, other = i;
+    if (i >= 2 * p.half) return;
+    int k;
+    bool first;
+    if (L == kSplit || p.pairing == POS_ROT_HALF) {
+        first = i < p.half;
+        k = first ? i : i - p.half;
+        other = first ? i + p.half : i - p.half;
+    } else {
+        first = i % 2 == 0;
+        k = i / 2;
+        other = i ^ 1;
+    }
+    if (!turn) return;
+    c = p.cos[at * p.half + k];
+    s = p.sin[at * p.half + k];
+    if (first) s = -s;
 }
 
 template <int G>
@@ -131,12 +185,9 @@ __device__ __forceinline__ float row_sum(float v) {
     for (int o = 1; o < G; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-
-__device__ __forceinline__ Vec8 load_weights(const float *w, int l, int dim) {
-    Vec8 v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.v[e] = w && 8 * l + e < dim ? w[8 * l + e] : 1.f;
-    return v;
+__device__ __forceinline__ float dot8(const Eight &a, const Eight &b) {
+    const F2 s = fma2(a.v[3], b.v[3], fma2(a.v[2], b.v[2], fma2(a.v[1], b.v[1], mul2(a.v[0], b.v[0]))));
+    return s.x + s.y;
 }
 
 // A token's place: its position, whether it is padding, whether the position
@@ -153,201 +204,296 @@ __device__ __forceinline__ Place place_of(const QkParams &p, int64_t token) {
     return q;
 }
 
-// A task is one token and a run of its heads (queries, then keys); a warp
-// takes it, G lanes a head with 8 elements a lane, 32 / G heads at once, U of
-// those in flight.  The token's cosines and sines and both weights stay in
-// registers over the task.  Bound by HBM: x is read once, y (and the codes)
-// written once; the sum of squares, the groups' magnitudes and the partners of
-// the rotation come from shuffles.
-template <typename T, int G, int U, bool ALIGNED>
-__global__ void __launch_bounds__(kQkThreads) qk_forward_kernel(const QkParams p) {
+// Keeps a head in 8 bits.
+template <typename T, int L, int F>
+__device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, const Eight &x,
+                                         uint8_t *codes, uint8_t *scales, int l, bool live) {
+    if constexpr (L == kRun) {
+        uint32_t m = amax_bits(raw);
+        m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const int byte = scale_byte<F>(f32_bits<T>(m));
+        if (!live || 8 * l >= p.pitch) return;
+        const Vec8 v = values_of(x);
+        *reinterpret_cast<uint2 *>(codes + 8 * l) = encode8<F>(v, byte);
+        if (l % 4 == 0) scales[l / 4] = (uint8_t)byte;
+    } else {
+        // two groups: of the first and of the second half
+        uint32_t lo, hi;
+        if constexpr (sizeof(T) == 4) {
+            constexpr uint32_t kAbs = 0x7fffffffu;
+            lo = max(max(raw.a.x & kAbs, raw.a.y & kAbs), max(raw.a.z & kAbs, raw.a.w & kAbs));
+            hi = max(max(raw.b.x & kAbs, raw.b.y & kAbs), max(raw.b.z & kAbs, raw.b.w & kAbs));
+#pragma unroll
+            for (int o = 1; o < 8; o *= 2) {
+                lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            }
+        } else {
+            // both magnitudes, 16 bits each, through one shuffle
+            constexpr uint32_t kAbs = 0x7fff7fffu;
+            const uint32_t a = __vmaxu2(raw.a.x & kAbs, raw.a.y & kAbs);
+            const uint32_t b = __vmaxu2(raw.a.z & kAbs, raw.a.w & kAbs);
+            uint32_t m = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+            for (int o = 1; o < 8; o *= 2) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+            lo = f32_bits<T>(m & 0xffffu);
+            hi = f32_bits<T>(m >> 16);
+        }
+        const int b0 = scale_byte<F>(lo), b1 = scale_byte<F>(hi);
+        if (!live || 4 * l >= p.half) return;
+        *reinterpret_cast<uint32_t *>(codes + 4 * l) =
+            encode4<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
+        *reinterpret_cast<uint32_t *>(codes + p.half + 4 * l) =
+            encode4<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
+        if (l % 8 == 0) {
+            scales[l / 8] = (uint8_t)b0;
+            scales[p.half / 32 + l / 8] = (uint8_t)b1;
+        }
+    }
+}
+
+// A task is one token and a run of its query or key heads; a warp takes it, G
+// lanes a head with 8 elements a lane, 32 / G heads at once, U of those in
+// flight.  With the weights in them, the token's cosines and sines make y =
+// r (x c + partner s) with 16 coefficients, kept in registers over the task.
+// Bound by HBM: x is read once, y (and the codes) written once.
+template <typename T, int G, int U, int L, bool ALIGNED>
+__global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
+    qk_forward_kernel(const QkParams p) {
     constexpr int R = 32 / G;
-    __shared__ float4 rows[kQkThreads * 2];
+    __shared__ float4 rows[L == kSplit ? 1 : kQkThreads * 2];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
-    float *row = reinterpret_cast<float *>(rows) + warp * 256 + sub * 8 * G;
-    const int64_t task = blockIdx.x * (int64_t)kQkWarps + warp;
-    if (task >= p.tasks) return;
-    const int64_t token = task / p.n_chunk;
-    const int c0 = (int)(task - token * p.n_chunk) * p.chunk;
-    const int c1 = min(c0 + p.chunk, p.heads[0] + p.heads[1]);
-    const Place at = place_of(p, token);
-    Vec8 w[2];
-    Turn turn;
-    for (int base = c0; base < c1; base += R * U) {
+    float *row = reinterpret_cast<float *>(rows) + (L == kSplit ? 0 : warp * 256 + sub * 8 * G);
+    int64_t task = blockIdx.x * (int64_t)kQkWarps + warp;
+    const int k = task >= p.tasks[0];
+    if (k) task -= p.tasks[0];
+    if (task >= p.tasks[k]) return;
+    const int64_t token = task / p.n_chunk[k];
+    const int h0 = (int)(task - token * p.n_chunk[k]) * p.chunk[k];
+    const int h1 = min(h0 + p.chunk[k], p.heads[k]);
+    const T *x_token = static_cast<const T *>(p.a[k].p) + token * p.a[k].token;
+    T *y_token = static_cast<T *>(p.b[k].p) + token * p.b[k].token;
+    Place at = {};
+    Eight c, s;
+    for (int base = h0 + sub; base - sub < h1; base += R * U) {
         Raw8<T> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = base + u * R + sub, k = c >= p.heads[0], h = k ? c - p.heads[0] : c;
-            const T *x = static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
-                         h * p.a[k].head + 8 * l;
-            raw[u] = load8<ALIGNED>(x, c < c1 ? p.dim - 8 * l : 0);
-        }
-        if (base == c0) {
-            w[0] = load_weights(p.w[0], l, p.dim);
-            w[1] = load_weights(p.w[1], l, p.dim);
+        for (int u = 0; u < U; ++u)
+            raw[u] = load_row<T, L, ALIGNED>(p, x_token + (base + u * R) * p.a[k].head, l,
+                                             base + u * R < h1);
+        if (base - sub == h0) {
+            at = place_of(p, token);
+            float cc[8], ss[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) turn.c[e] = 1.f, turn.s[e] = 0.f;
-            if (!at.padding && !at.outside) load_turn(p, at.at, l, turn);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (base + u * R >= c1) break;  // no row of this step, for the whole warp
-            const int c = base + u * R + sub, k = c >= p.heads[0], h = k ? c - p.heads[0] : c;
-            const bool live = c < c1;
-            const Vec8 x = to_float(raw[u]);
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(x.v[e], x.v[e], ss);
-            float r = __frsqrt_rn(fmaf(row_sum<G>(ss), p.inv_dim, p.eps));
-            const int64_t at_row = token * p.heads[k] + h;
-            if (p.codes[0] || p.codes[1]) {
-                uint32_t m = amax_bits(raw[u]);
-                m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                if (live && p.codes[k] && 8 * l < p.pitch) {
-                    const uint32_t bits = f32_bits<T>(m);
-                    const int byte = p.format == POS_CKPT_INT8 ? scale_byte<POS_CKPT_INT8>(bits)
-                                                               : scale_byte<POS_CKPT_E4M3>(bits);
-                    *reinterpret_cast<uint2 *>(p.codes[k] + at_row * p.pitch + 8 * l) =
-                        p.format == POS_CKPT_INT8 ? encode8<POS_CKPT_INT8>(x, byte)
-                                                  : encode8<POS_CKPT_E4M3>(x, byte);
-                    if (l % 4 == 0) p.scales[k][at_row * p.spitch + l / 4] = (uint8_t)byte;
+            for (int e = 0; e < 8; ++e) {
+                const int i = element<L>(p, l, e);
+                int other;
+                angle<L>(p, at.at, i, !at.padding && !at.outside, cc[e], ss[e], other);
+                if (p.w[k] && i < p.dim) {
+                    cc[e] *= p.w[k][i];
+                    ss[e] *= p.w[k][other];
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c.v[i] = {cc[2 * i], cc[2 * i + 1]};
+                s.v[i] = {ss[2 * i], ss[2 * i + 1]};
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = base + u * R;
+            if (h - sub >= h1) break;  // no row of this step, for the whole warp
+            const bool live = h < h1;
+            const Eight x = pairs_of(to_float(raw[u]));
+            float r = __frsqrt_rn(fmaf(row_sum<G>(dot8(x, x)), p.inv_dim, p.eps));
+            const int64_t at_row = token * p.heads[k] + h;
+            if (p.codes[k]) {
+                uint8_t *codes = p.codes[k] + at_row * p.pitch;
+                uint8_t *scales = p.scales[k] + at_row * p.spitch;
+                if (p.format == POS_CKPT_INT8)
+                    keep_row<T, L, POS_CKPT_INT8>(p, raw[u], x, codes, scales, l, live);
+                else
+                    keep_row<T, L, POS_CKPT_E4M3>(p, raw[u], x, codes, scales, l, live);
             }
             if (live && p.rstd[k] && l == 0) p.rstd[k][at_row] = r;
             if (at.outside) r = __uint_as_float(0x7fffffffu);
-            Vec8 y;
+            const Eight q = partners<G, L>(p, x, l, row);
+            Eight y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y.v[e] = x.v[e] * r * (k ? w[1].v[e] : w[0].v[e]);
-            y = turned<G, false>(p, y, turn, l, row);
+            for (int i = 0; i < 4; ++i)
+                y.v[i] = mul2(fma2(q.v[i], s.v[i], mul2(x.v[i], c.v[i])), both(r));
+            Raw8<T> out = from_float<T>(values_of(y));
             if (at.padding) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y.v[e] = 0.f;
+                zero_raw(out.a);
+                if constexpr (sizeof(T) == 4) zero_raw(out.b);
             }
-            T *out = static_cast<T *>(p.b[k].p) + token * p.b[k].token + h * p.b[k].head + 8 * l;
-            store8<ALIGNED>(out, from_float<T>(y), live ? p.dim - 8 * l : 0);
+            store_row<T, L, ALIGNED>(p, y_token + h * p.b[k].head, l, live, out);
         }
     }
 }
 
-// The same tasks, taken by a resident grid; dw is summed over a thread's rows
-// in registers, over the block in shared memory, and written as one partial
-// sum per block, which qk_dw_kernel adds up in order.
-template <typename T, int G, int U, bool ALIGNED>
-__global__ void __launch_bounds__(kQkThreads) qk_backward_kernel(const QkParams p) {
+// The codes of a thread's elements and their scales times r, as n = x r.
+template <int L, int F>
+__device__ __forceinline__ Eight read_kept(uint2 code, int b0, int b1, float r) {
+    const Vec8 v = decode8<F>(code, 1.f);
+    const F2 s0 = both(scale_value(b0) * r), s1 = L == kSplit ? both(scale_value(b1) * r) : s0;
+    return {{mul2({v.v[0], v.v[1]}, s0), mul2({v.v[2], v.v[3]}, s0), mul2({v.v[4], v.v[5]}, s1),
+             mul2({v.v[6], v.v[7]}, s1)}};
+}
+
+// The same tasks, taken by a resident grid, the queries' first; dw is summed
+// over a thread's rows in registers, over the block in shared memory, and
+// written as one partial sum per block, which qk_dw_kernel adds up in order.
+template <typename T, int G, int U, int L, bool ALIGNED>
+__global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 2 : 3)
+    qk_backward_kernel(const QkParams p) {
     constexpr int R = 32 / G;
-    __shared__ float4 rows[kQkWarps * 2 * kQkMaxDim / 4];
+    __shared__ float4 rows[kQkWarps * kQkMaxDim / 4];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
     float *row = reinterpret_cast<float *>(rows) + warp * 256 + sub * 8 * G;
-    Vec8 w[2], dw[2];
-    w[0] = load_weights(p.w[0], l, p.dim);
-    w[1] = load_weights(p.w[1], l, p.dim);
+    for (int k = 0; k < 2; ++k) {
+        Eight w, dw;
+        {
+            float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[0].v[e] = dw[1].v[e] = 0.f;
-    for (int64_t task = blockIdx.x * (int64_t)kQkWarps + warp; task < p.tasks;
-         task += gridDim.x * (int64_t)kQkWarps) {
-        const int64_t token = task / p.n_chunk;
-        const int c0 = (int)(task - token * p.n_chunk) * p.chunk;
-        const int c1 = min(c0 + p.chunk, p.heads[0] + p.heads[1]);
-        const Place at = place_of(p, token);
-        Turn turn;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) turn.c[e] = 1.f, turn.s[e] = 0.f;
-        if (!at.padding && !at.outside) load_turn(p, at.at, l, turn);
-        for (int base = c0; base < c1; base += R * U) {
-            Raw8<T> raw[U], rawx[U];
-            uint2 code[U];
-            int byte[U];
-            float rs[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = base + u * R + sub, k = c >= p.heads[0], h = k ? c - p.heads[0] : c;
-                const int n = c < c1 && !at.padding ? p.dim - 8 * l : 0;
-                const int64_t at_row = token * p.heads[k] + h;
-                raw[u] = load8<ALIGNED>(static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
-                                            h * p.a[k].head + 8 * l, n);
-                rs[u] = 0.f, byte[u] = 0, code[u] = make_uint2(0u, 0u);
-                if (n > 0) {
-                    rs[u] = p.rstd[k][at_row];
-                    if (!p.x[k].p) {
-                        code[u] = *reinterpret_cast<const uint2 *>(p.codes[k] + at_row * p.pitch +
-                                                                   8 * l);
-                        byte[u] = p.scales[k][at_row * p.spitch + l / 4];
-                    }
-                }
-                if (p.x[k].p)
-                    rawx[u] = load8<ALIGNED>(static_cast<const T *>(p.x[k].p) +
-                                                 token * p.x[k].token + h * p.x[k].head + 8 * l, n);
+            for (int e = 0; e < 8; ++e) {
+                const int i = element<L>(p, l, e);
+                f[e] = p.w[k] && i < p.dim ? p.w[k][i] : 1.f;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (base + u * R >= c1) break;  // no row of this step, for the whole warp
-                const int c = base + u * R + sub, k = c >= p.heads[0], h = k ? c - p.heads[0] : c;
-                const bool live = c < c1;
-                const Vec8 g = turned<G, true>(p, to_float(raw[u]), turn, l, row);
-                Vec8 n = p.x[k].p ? to_float(rawx[u])
-                         : p.format == POS_CKPT_INT8
-                             ? decode8<POS_CKPT_INT8>(code[u], scale_value(byte[u]))
-                             : decode8<POS_CKPT_E4M3>(code[u], scale_value(byte[u]));
-                const float r = at.outside ? __uint_as_float(0x7fffffffu) : rs[u];
-                Vec8 hw;
-                float dot = 0.f;
+            for (int i = 0; i < 4; ++i) w.v[i] = {f[2 * i], f[2 * i + 1]}, dw.v[i] = both(0.f);
+        }
+        for (int64_t task = blockIdx.x * (int64_t)kQkWarps + warp; task < p.tasks[k];
+             task += gridDim.x * (int64_t)kQkWarps) {
+            const int64_t token = task / p.n_chunk[k];
+            const int h0 = (int)(task - token * p.n_chunk[k]) * p.chunk[k];
+            const int h1 = min(h0 + p.chunk[k], p.heads[k]);
+            const Place at = place_of(p, token);
+            const T *dy_token = static_cast<const T *>(p.a[k].p) + token * p.a[k].token;
+            const T *x_token = static_cast<const T *>(p.x[k].p) + token * p.x[k].token;
+            T *dx_token = static_cast<T *>(p.b[k].p) + token * p.b[k].token;
+            Eight c, s;  // s with the sign of the transpose
+            {
+                float cc[8], ss[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    n.v[e] *= r;
-                    hw.v[e] = g.v[e] * (k ? w[1].v[e] : w[0].v[e]);
-                    dot = fmaf(hw.v[e], n.v[e], dot);
-                    if (k) dw[1].v[e] = fmaf(g.v[e], n.v[e], dw[1].v[e]);
-                    else dw[0].v[e] = fmaf(g.v[e], n.v[e], dw[0].v[e]);
+                    int other;
+                    angle<L>(p, at.at, element<L>(p, l, e), !at.padding && !at.outside, cc[e],
+                             ss[e], other);
                 }
-                dot = row_sum<G>(dot) * p.inv_dim;
-                Vec8 dx;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dx.v[e] = r * (hw.v[e] - n.v[e] * dot);
-                T *out = static_cast<T *>(p.b[k].p) + token * p.b[k].token + h * p.b[k].head + 8 * l;
-                store8<ALIGNED>(out, from_float<T>(dx), live ? p.dim - 8 * l : 0);
+                for (int i = 0; i < 4; ++i) {
+                    c.v[i] = {cc[2 * i], cc[2 * i + 1]};
+                    s.v[i] = {-ss[2 * i], -ss[2 * i + 1]};
+                }
+            }
+            for (int base = h0 + sub; base - sub < h1; base += R * U) {
+                Raw8<T> raw[U], rawx[U];
+                uint2 code[U];
+                int b0[U], b1[U];
+                float rs[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int h = base + u * R;
+                    const bool live = h < h1 && !at.padding;
+                    const int64_t at_row = token * p.heads[k] + h;
+                    raw[u] = load_row<T, L, ALIGNED>(p, dy_token + h * p.a[k].head, l, live);
+                    rs[u] = 0.f, b0[u] = b1[u] = 0, code[u] = make_uint2(0u, 0u);
+                    if (live) rs[u] = p.rstd[k][at_row];
+                    if (p.x[k].p) {
+                        rawx[u] = load_row<T, L, ALIGNED>(p, x_token + h * p.x[k].head, l, live);
+                    } else if (live) {
+                        const uint8_t *codes = p.codes[k] + at_row * p.pitch;
+                        const uint8_t *scales = p.scales[k] + at_row * p.spitch;
+                        if (L == kRun && 8 * l < p.dim) {
+                            code[u] = *reinterpret_cast<const uint2 *>(codes + 8 * l);
+                            b0[u] = scales[l / 4];
+                        } else if (L == kSplit && 4 * l < p.half) {
+                            code[u].x = *reinterpret_cast<const uint32_t *>(codes + 4 * l);
+                            code[u].y = *reinterpret_cast<const uint32_t *>(codes + p.half + 4 * l);
+                            b0[u] = scales[l / 8];
+                            b1[u] = scales[p.half / 32 + l / 8];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int h = base + u * R;
+                    if (h - sub >= h1) break;  // no row of this step, for the whole warp
+                    const float r = at.outside ? __uint_as_float(0x7fffffffu) : rs[u];
+                    const Eight dy = pairs_of(to_float(raw[u]));
+                    const Eight q = partners<G, L>(p, dy, l, row);
+                    Eight n, g, hw;
+                    if (p.x[k].p) {
+                        n = pairs_of(to_float(rawx[u]));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) n.v[i] = mul2(n.v[i], both(r));
+                    } else {
+                        n = p.format == POS_CKPT_INT8
+                                ? read_kept<L, POS_CKPT_INT8>(code[u], b0[u], b1[u], r)
+                                : read_kept<L, POS_CKPT_E4M3>(code[u], b0[u], b1[u], r);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        g.v[i] = fma2(q.v[i], s.v[i], mul2(dy.v[i], c.v[i]));
+                        dw.v[i] = fma2(g.v[i], n.v[i], dw.v[i]);
+                        hw.v[i] = mul2(g.v[i], w.v[i]);
+                    }
+                    const F2 t = both(-r * (row_sum<G>(dot8(hw, n)) * p.inv_dim));
+                    Eight dx;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dx.v[i] = fma2(n.v[i], t, mul2(hw.v[i], both(r)));
+                    Raw8<T> out = from_float<T>(values_of(dx));
+                    store_row<T, L, ALIGNED>(p, dx_token + h * p.b[k].head, l, h < h1, out);
+                }
             }
         }
-    }
-    if (!p.part) return;
-    // [warp][2][dim], heads side by side in a warp first
-    float *sum = reinterpret_cast<float *>(rows);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
+        if (!p.part) continue;
+        // [warp][dim], heads side by side in a warp first
+        float *sum = reinterpret_cast<float *>(rows);
+        const Vec8 f = values_of(dw);
+        __syncthreads();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float v = dw[k].v[e];
+            float v = f.v[e];
 #pragma unroll
             for (int o = G; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-            if (sub == 0 && 8 * l + e < p.dim)
-                sum[(warp * 2 + k) * kQkMaxDim + 8 * l + e] = v;
+            const int i = element<L>(p, l, e);
+            if (sub == 0 && i < p.dim && (L == kRun || 4 * l < p.half))
+                sum[warp * kQkMaxDim + i] = v;
         }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * p.dim; i += kQkThreads) {
-        const int k = i >= p.dim, e = k ? i - p.dim : i;
-        float v = 0.f;
-        for (int q = 0; q < kQkWarps; ++q) v += sum[(q * 2 + k) * kQkMaxDim + e];
-        p.part[blockIdx.x * (int64_t)(2 * p.dim) + i] = v;
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.dim; i += kQkThreads) {
+            float v = 0.f;
+            for (int q = 0; q < kQkWarps; ++q) v += sum[q * kQkMaxDim + i];
+            p.part[blockIdx.x * (int64_t)(2 * p.dim) + k * p.dim + i] = v;
+        }
+        __syncthreads();
     }
 }
 
-// dw = dw_in + the blocks' partial sums: a block of 32 x 32 threads takes 32
-// columns, its rows a strided share of the partial sums each.
+// dw = dw_in + the blocks' partial sums: a block takes 32 columns, each of its
+// 32 warps a strided share of the partial sums.
 __global__ void __launch_bounds__(1024) qk_dw_kernel(const float *part, int n_part, int cols,
                                                      const float *dw_in, float *dw) {
+    grid_dep_wait();
     __shared__ float sum[32][33];
-    const int i = blockIdx.x * 32 + threadIdx.x;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int i = blockIdx.x * 32 + lane;
     float v = 0.f;
     if (i < cols)
-        for (int b = threadIdx.y; b < n_part; b += 32) v += part[b * (int64_t)cols + i];
-    sum[threadIdx.y][threadIdx.x] = v;
+#pragma unroll 4
+        for (int b = warp; b < n_part; b += 32) v += part[b * (int64_t)cols + i];
+    sum[warp][lane] = v;
     __syncthreads();
-    v = sum[threadIdx.x][threadIdx.y];
+    v = sum[lane][warp];
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-    const int j = blockIdx.x * 32 + threadIdx.y;
-    if (threadIdx.x == 0 && j < cols) dw[j] = dw_in ? dw_in[j] + v : v;
+    const int j = blockIdx.x * 32 + warp;
+    if (lane == 0 && j < cols) dw[j] = dw_in ? dw_in[j] + v : v;
 }
 
 // ---------------------------------------------------------------------------
@@ -409,7 +555,6 @@ static QkParams make_params(const pos_qk *q) {
     const CkptShape s = ckpt_shape(q->dim);
     p.pitch = (int32_t)s.pitch, p.spitch = (int32_t)s.spitch;
     p.pairing = q->pairing, p.format = q->format;
-    p.tables16 = aligned16(q->cos) && aligned16(q->sin) && p.half % 4 == 0;
     p.eps = q->eps, p.inv_dim = 1.f / q->dim;
     return p;
 }
@@ -420,28 +565,42 @@ static int lanes_per_head(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32
 // Cuts a token's heads into tasks: as few as keep `warps` warps busy (each
 // reads the token's cosines and sines again), at least 32 / G heads a task.
 static void cut_tasks(QkParams &p, int64_t warps) {
-    const int R = 32 / lanes_per_head(p.dim), heads = p.heads[0] + p.heads[1];
-    const int most = (heads + R - 1) / R;
+    const int R = 32 / lanes_per_head(p.dim);
     const int64_t want = p.tokens ? (warps + p.tokens - 1) / p.tokens : 1;
-    const int n = (int)std::max<int64_t>(1, std::min<int64_t>(want, most));
-    p.chunk = ((most + n - 1) / n) * R;
-    p.n_chunk = (heads + p.chunk - 1) / p.chunk;
-    p.tasks = p.tokens * p.n_chunk;
+    for (int k = 0; k < 2; ++k) {
+        const int most = std::max(1, (p.heads[k] + R - 1) / R);
+        const int n = (int)std::max<int64_t>(1, std::min<int64_t>(want, most));
+        p.chunk[k] = ((most + n - 1) / n) * R;
+        p.n_chunk[k] = std::max(1, (p.heads[k] + p.chunk[k] - 1) / p.chunk[k]);
+        p.tasks[k] = p.heads[k] ? p.tokens * p.n_chunk[k] : 0;
+    }
+}
+
+// Which layout and loads a call can use.
+enum Shape { kShapeSplit, kShapeRun, kShapeAny };
+static Shape shape_of(const QkParams &p, bool aligned) {
+    if (!aligned) return kShapeAny;
+    return p.pairing == POS_ROT_HALF && 2 * p.half == p.dim && p.dim % 64 == 0 ? kShapeSplit
+                                                                               : kShapeRun;
 }
 
 template <typename T, int G, int U>
-static pos_status launch_forward(const QkParams &p, bool aligned, cudaStream_t s) {
-    const int64_t grid = (p.tasks + kQkWarps - 1) / kQkWarps;
+static pos_status launch_forward(QkParams &p, bool aligned, cudaStream_t s) {
+    cut_tasks(p, (int64_t)sm_count() * 64);
+    const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
-    if (aligned) qk_forward_kernel<T, G, U, true><<<(unsigned)grid, kQkThreads, 0, s>>>(p);
-    else qk_forward_kernel<T, G, U, false><<<(unsigned)grid, kQkThreads, 0, s>>>(p);
+    const Shape shape = shape_of(p, aligned);
+    auto kern = shape == kShapeSplit ? qk_forward_kernel<T, G, U, kSplit, true>
+                : shape == kShapeRun ? qk_forward_kernel<T, G, U, kRun, true>
+                                     : qk_forward_kernel<T, G, U, kRun, false>;
+    kern<<<(unsigned)grid, kQkThreads, 0, s>>>(p);
     POS_CUDA(cudaGetLastError());
     return POS_OK;
 }
 
 template <typename T>
-static pos_status forward_of(const QkParams &p, bool aligned, cudaStream_t s) {
-    constexpr int U = sizeof(T) == 4 ? 2 : 4;
+static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
+    constexpr int U = sizeof(T) == 4 ? 1 : 2;
     switch (lanes_per_head(p.dim)) {
         case 8: return launch_forward<T, 8, U>(p, aligned, s);
         case 16: return launch_forward<T, 16, U>(p, aligned, s);
@@ -452,13 +611,17 @@ static pos_status forward_of(const QkParams &p, bool aligned, cudaStream_t s) {
 template <typename T, int G, int U>
 static pos_status launch_backward(QkParams &p, bool aligned, const float *dw_in, float *dw,
                                   cudaStream_t s) {
-    auto kern = aligned ? qk_backward_kernel<T, G, U, true> : qk_backward_kernel<T, G, U, false>;
+    const Shape shape = shape_of(p, aligned);
+    auto kern = shape == kShapeSplit ? qk_backward_kernel<T, G, U, kSplit, true>
+                : shape == kShapeRun ? qk_backward_kernel<T, G, U, kRun, true>
+                                     : qk_backward_kernel<T, G, U, kRun, false>;
     int per_sm = 0;
     POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), kQkThreads, 0, &per_sm));
     per_sm = std::max(1, std::min(per_sm, 8));
     cut_tasks(p, (int64_t)sm_count() * per_sm * kQkWarps);
-    const int grid = (int)std::min<int64_t>((p.tasks + kQkWarps - 1) / kQkWarps,
-                                            (int64_t)sm_count() * per_sm);
+    const int64_t tasks = std::max(p.tasks[0], p.tasks[1]);
+    const int grid =
+        (int)std::min<int64_t>((tasks + kQkWarps - 1) / kQkWarps, (int64_t)sm_count() * per_sm);
     const int cols = 2 * p.dim;
     void *scratch = nullptr;
     if (dw && grid > 0) {
@@ -469,10 +632,9 @@ static pos_status launch_backward(QkParams &p, bool aligned, const float *dw_in,
     }
     if (grid > 0) kern<<<grid, kQkThreads, 0, s>>>(p);
     cudaError_t e = cudaGetLastError();
-    if (dw && e == cudaSuccess) {
-        qk_dw_kernel<<<(cols + 31) / 32, dim3(32, 32), 0, s>>>(p.part, grid, cols, dw_in, dw);
-        e = cudaGetLastError();
-    }
+    if (dw && e == cudaSuccess)
+        e = launch_dependent(qk_dw_kernel, (cols + 31) / 32, 1024, 0, s,
+                             (const float *)p.part, grid, cols, dw_in, dw);
     const cudaError_t e2 = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
     if (e == cudaSuccess) e = e2;
     return e == cudaSuccess ? POS_OK : cuda_fail(e, "q/k backward");
@@ -519,7 +681,6 @@ pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_h
         p.b[k] = {y[k].data, y[k].token_stride, y[k].head_stride};
     }
     p.rstd[0] = rstd_q, p.rstd[1] = rstd_k;
-    cut_tasks(p, (int64_t)sm_count() * 64);
     const bool aligned = heads_aligned(qk, x) && heads_aligned(qk, y);
     const auto s = static_cast<cudaStream_t>(stream);
     switch (qk->dtype) {
