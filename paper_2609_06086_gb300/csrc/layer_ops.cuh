@@ -53,20 +53,15 @@ struct Vec8 {
     float v[8];
 };
 
-// Codes of 4 values under one scale byte.  x * 2^-e is exact (or an underflow
-// far below half a code), so each code is rounded once: int8 by adding
-// 1.5 * 2^23, whose last bit is a whole number, e4m3 by the conversion.  Only
-// the largest scale can leave values past the top code, which saturate.
+// Codes of 4 values under one scale byte below the largest.  x * 2^-e is exact
+// (or an underflow far below half a code), so each code is rounded once: int8
+// by adding 1.5 * 2^23, whose last bit is a whole number, e4m3 by the
+// conversion.
 template <int F>
-__device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, int byte) {
-    if (byte == kScaleNan) return 0u;
+__device__ __forceinline__ uint32_t encode4_inside(float x0, float x1, float x2, float x3,
+                                                   int byte) {
     const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
     if constexpr (F == POS_CKPT_INT8) {
-        if (byte == Fmt<F>::kScaleHi) {
-            const float top = 127.f * scale_value(byte);
-            x0 = fminf(fmaxf(x0, -top), top), x1 = fminf(fmaxf(x1, -top), top);
-            x2 = fminf(fmaxf(x2, -top), top), x3 = fminf(fmaxf(x3, -top), top);
-        }
         const uint32_t a = __float_as_uint(fmaf(x0, inv, 12582912.f));
         const uint32_t b = __float_as_uint(fmaf(x1, inv, 12582912.f));
         const uint32_t c = __float_as_uint(fmaf(x2, inv, 12582912.f));
@@ -79,6 +74,18 @@ __device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float 
             __nv_cvt_float2_to_fp8x2(make_float2(x2 * inv, x3 * inv), __NV_SATFINITE, __NV_E4M3);
         return lo | hi << 16;
     }
+}
+// The same under any scale byte: at the largest, values past the top code
+// saturate; a group that is NaN has codes 0.
+template <int F>
+__device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, int byte) {
+    if (byte >= Fmt<F>::kScaleHi) {
+        if (byte == kScaleNan) return 0u;
+        const float top = Fmt<F>::kTop * scale_value(byte);
+        x0 = fminf(fmaxf(x0, -top), top), x1 = fminf(fmaxf(x1, -top), top);
+        x2 = fminf(fmaxf(x2, -top), top), x3 = fminf(fmaxf(x3, -top), top);
+    }
+    return encode4_inside<F>(x0, x1, x2, x3, byte);
 }
 template <int F>
 __device__ __forceinline__ uint2 encode8(const Vec8 &x, int byte) {

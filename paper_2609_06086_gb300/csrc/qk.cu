@@ -29,6 +29,7 @@ struct QkParams {
     int32_t heads[2], dim, half, pitch, spitch;
     int32_t chunk[2], n_chunk[2];  // heads of a task, tasks of a token
     int32_t pairing, format;
+    bool vectors;              // cos, sin and w can be read 16 bytes at a time
     float eps, inv_dim;
 };
 
@@ -155,28 +156,61 @@ __device__ __forceinline__ Eight partners(const QkParams &p, const Eight &u, int
     return q;
 }
 
-// The cosine of an element's pair and its sine with the sign that Rot gives
-// the partner's term; 1 and 0 from rot on.  `other`: the partner's element.
+// A thread's weights; ones where there are none.
 template <int L>
-__device__ __forceinline__ void angle(const QkParams &p, int64_t at, int i, bool turn, float &c,
-                                      float &s, int &other) {
-    c = 1.f, s = 0.f, other = i;
-    if (i >= 2 * p.half) return;
-    int k;
-    bool first;
-    if (L == kSplit || p.pairing == POS_ROT_HALF) {
-        first = i < p.half;
-        k = first ? i : i - p.half;
-        other = first ? i + p.half : i - p.half;
-    } else {
-        first = i % 2 == 0;
-        k = i / 2;
-        other = i ^ 1;
+__device__ __forceinline__ Eight load_weights(const QkParams &p, const float *w, int l) {
+    Eight o;
+    if (L == kSplit && w && p.vectors) {
+        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+        const bool in = 4 * l < p.half;
+        const float4 a = in ? *reinterpret_cast<const float4 *>(w + 4 * l) : one;
+        const float4 b = in ? *reinterpret_cast<const float4 *>(w + p.half + 4 * l) : one;
+        return {{{a.x, a.y}, {a.z, a.w}, {b.x, b.y}, {b.z, b.w}}};
     }
-    if (!turn) return;
-    c = p.cos[at * p.half + k];
-    s = p.sin[at * p.half + k];
-    if (first) s = -s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = element<L>(p, l, 2 * i);
+        o.v[i] = {w && e < p.dim ? w[e] : 1.f, w && e + 1 < p.dim ? w[e + 1] : 1.f};
+    }
+    return o;
+}
+
+// y = x c + partner s is Rot x: the cosine of an element's pair, and its sine
+// with the sign that the partner's term has; 1 and 0 from rot on.
+template <int L>
+__device__ __forceinline__ void load_angles(const QkParams &p, int64_t at, int l, Eight &c,
+                                            Eight &s) {
+    const float *cs = p.cos + at * p.half, *sn = p.sin + at * p.half;
+    if constexpr (L == kSplit) {
+        float4 a = make_float4(1.f, 1.f, 1.f, 1.f), b = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * l < p.half) {
+            if (p.vectors) {
+                a = *reinterpret_cast<const float4 *>(cs + 4 * l);
+                b = *reinterpret_cast<const float4 *>(sn + 4 * l);
+            } else {
+                a = make_float4(cs[4 * l], cs[4 * l + 1], cs[4 * l + 2], cs[4 * l + 3]);
+                b = make_float4(sn[4 * l], sn[4 * l + 1], sn[4 * l + 2], sn[4 * l + 3]);
+            }
+        }
+        c = {{{a.x, a.y}, {a.z, a.w}, {a.x, a.y}, {a.z, a.w}}};
+        s = {{{-b.x, -b.y}, {-b.z, -b.w}, {b.x, b.y}, {b.z, b.w}}};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c.v[i] = both(1.f), s.v[i] = both(0.f);
+            const int e = 8 * l + 2 * i;  // even, as rot is: both elements turn or none
+            if (e >= 2 * p.half) continue;
+            if (p.pairing == POS_ROT_ADJACENT) {
+                const float a = cs[e / 2], b = sn[e / 2];
+                c.v[i] = {a, a}, s.v[i] = {-b, b};
+            } else {
+                const int k0 = e < p.half ? e : e - p.half;
+                const int k1 = e + 1 < p.half ? e + 1 : e + 1 - p.half;
+                c.v[i] = {cs[k0], cs[k1]};
+                s.v[i] = {e < p.half ? -sn[k0] : sn[k0], e + 1 < p.half ? -sn[k1] : sn[k1]};
+            }
+        }
+    }
 }
 
 template <int G>
@@ -242,10 +276,16 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
         }
         const int b0 = scale_byte<F>(lo), b1 = scale_byte<F>(hi);
         if (!live || 4 * l >= p.half) return;
-        *reinterpret_cast<uint32_t *>(codes + 4 * l) =
-            encode4<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
-        *reinterpret_cast<uint32_t *>(codes + p.half + 4 * l) =
-            encode4<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
+        uint32_t c0, c1;
+        if (max(b0, b1) < Fmt<F>::kScaleHi) {
+            c0 = encode4_inside<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
+            c1 = encode4_inside<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
+        } else {
+            c0 = encode4<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
+            c1 = encode4<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
+        }
+        *reinterpret_cast<uint32_t *>(codes + 4 * l) = c0;
+        *reinterpret_cast<uint32_t *>(codes + p.half + 4 * l) = c1;
         if (l % 8 == 0) {
             scales[l / 8] = (uint8_t)b0;
             scales[p.half / 32 + l / 8] = (uint8_t)b1;
@@ -254,11 +294,11 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
 }
 
 // A task is one token and a run of its query or key heads; a warp takes it, G
-// lanes a head with 8 elements a lane, 32 / G heads at once, U of those in
-// flight.  With the weights in them, the token's cosines and sines make y =
+// lanes a head with 8 elements a lane, 32 / G heads at once, the next ones on
+// their way.  With the weights in them, the token's cosines and sines make y =
 // r (x c + partner s) with 16 coefficients, kept in registers over the task.
 // Bound by HBM: x is read once, y (and the codes) written once.
-template <typename T, int G, int U, int L, bool ALIGNED>
+template <typename T, int G, int L, bool ALIGNED>
 __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     qk_forward_kernel(const QkParams p) {
     constexpr int R = 32 / G;
@@ -272,65 +312,61 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     const int64_t token = task / p.n_chunk[k];
     const int h0 = (int)(task - token * p.n_chunk[k]) * p.chunk[k];
     const int h1 = min(h0 + p.chunk[k], p.heads[k]);
-    const T *x_token = static_cast<const T *>(p.a[k].p) + token * p.a[k].token;
-    T *y_token = static_cast<T *>(p.b[k].p) + token * p.b[k].token;
-    Place at = {};
+    const Place at = place_of(p, token);
+    const int64_t row0 = token * p.heads[k] + h0 + sub;
+    const T *x = static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
+                 (h0 + sub) * p.a[k].head;
+    T *y = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head;
+    uint8_t *codes = p.codes[k] ? p.codes[k] + row0 * p.pitch : nullptr;
+    uint8_t *scales = p.scales[k] + row0 * p.spitch;
+    float *rstd = p.rstd[k] && l == 0 ? p.rstd[k] + row0 : nullptr;
+    Raw8<T> next = load_row<T, L, ALIGNED>(p, x, l, h0 + sub < h1);
+    // y = r (x c + partner s): the weights go into c and s
     Eight c, s;
-    for (int base = h0 + sub; base - sub < h1; base += R * U) {
-        Raw8<T> raw[U];
+    const Eight w = load_weights<L>(p, p.w[k], l);
+    if (!at.padding && !at.outside) {
+        load_angles<L>(p, at.at, l, c, s);
+    } else {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            raw[u] = load_row<T, L, ALIGNED>(p, x_token + (base + u * R) * p.a[k].head, l,
-                                             base + u * R < h1);
-        if (base - sub == h0) {
-            at = place_of(p, token);
-            float cc[8], ss[8];
+        for (int i = 0; i < 4; ++i) c.v[i] = both(1.f), s.v[i] = both(0.f);
+    }
+    const Eight w_partner = partners<G, L>(p, w, l, row);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = element<L>(p, l, e);
-                int other;
-                angle<L>(p, at.at, i, !at.padding && !at.outside, cc[e], ss[e], other);
-                if (p.w[k] && i < p.dim) {
-                    cc[e] *= p.w[k][i];
-                    ss[e] *= p.w[k][other];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c.v[i] = {cc[2 * i], cc[2 * i + 1]};
-                s.v[i] = {ss[2 * i], ss[2 * i + 1]};
-            }
+    for (int i = 0; i < 4; ++i) {
+        c.v[i] = mul2(c.v[i], w.v[i]);
+        s.v[i] = mul2(s.v[i], w_partner.v[i]);
+    }
+    const float outside = at.outside ? __uint_as_float(0x7fffffffu) : 1.f;
+    for (int h = h0; h < h1; h += R) {
+        const bool live = h + sub < h1;
+        const Raw8<T> raw = next;
+        x += R * p.a[k].head;
+        next = load_row<T, L, ALIGNED>(p, x, l, h + R + sub < h1);  // while this row is worked on
+        const Eight v = pairs_of(to_float(raw));
+        const float r = rsqrtf(fmaf(row_sum<G>(dot8(v, v)), p.inv_dim, p.eps));
+        if (codes) {
+            if (p.format == POS_CKPT_INT8)
+                keep_row<T, L, POS_CKPT_INT8>(p, raw, v, codes, scales, l, live);
+            else
+                keep_row<T, L, POS_CKPT_E4M3>(p, raw, v, codes, scales, l, live);
+            codes += R * p.pitch, scales += R * p.spitch;
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = base + u * R;
-            if (h - sub >= h1) break;  // no row of this step, for the whole warp
-            const bool live = h < h1;
-            const Eight x = pairs_of(to_float(raw[u]));
-            float r = __frsqrt_rn(fmaf(row_sum<G>(dot8(x, x)), p.inv_dim, p.eps));
-            const int64_t at_row = token * p.heads[k] + h;
-            if (p.codes[k]) {
-                uint8_t *codes = p.codes[k] + at_row * p.pitch;
-                uint8_t *scales = p.scales[k] + at_row * p.spitch;
-                if (p.format == POS_CKPT_INT8)
-                    keep_row<T, L, POS_CKPT_INT8>(p, raw[u], x, codes, scales, l, live);
-                else
-                    keep_row<T, L, POS_CKPT_E4M3>(p, raw[u], x, codes, scales, l, live);
-            }
-            if (live && p.rstd[k] && l == 0) p.rstd[k][at_row] = r;
-            if (at.outside) r = __uint_as_float(0x7fffffffu);
-            const Eight q = partners<G, L>(p, x, l, row);
-            Eight y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                y.v[i] = mul2(fma2(q.v[i], s.v[i], mul2(x.v[i], c.v[i])), both(r));
-            Raw8<T> out = from_float<T>(values_of(y));
-            if (at.padding) {
-                zero_raw(out.a);
-                if constexpr (sizeof(T) == 4) zero_raw(out.b);
-            }
-            store_row<T, L, ALIGNED>(p, y_token + h * p.b[k].head, l, live, out);
+        if (rstd) {
+            if (live) *rstd = r;
+            rstd += R;
         }
+        const Eight q = partners<G, L>(p, v, l, row);
+        Eight o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o.v[i] = mul2(fma2(q.v[i], s.v[i], mul2(v.v[i], c.v[i])), both(r * outside));
+        Raw8<T> out = from_float<T>(values_of(o));
+        if (at.padding) {
+            zero_raw(out.a);
+            if constexpr (sizeof(T) == 4) zero_raw(out.b);
+        }
+        store_row<T, L, ALIGNED>(p, y, l, live, out);
+        y += R * p.b[k].head;
     }
 }
 
@@ -343,28 +379,30 @@ __device__ __forceinline__ Eight read_kept(uint2 code, int b0, int b1, float r) 
              mul2({v.v[6], v.v[7]}, s1)}};
 }
 
+// What a thread reads of a row: dy, x or in its place the codes, their one or
+// two scale bytes, rstd.
+template <typename T>
+struct Fetched {
+    Raw8<T> dy, x;
+    uint32_t scales;
+    float r;
+};
+
 // The same tasks, taken by a resident grid, the queries' first; dw is summed
 // over a thread's rows in registers, over the block in shared memory, and
 // written as one partial sum per block, which qk_dw_kernel adds up in order.
 template <typename T, int G, int U, int L, bool ALIGNED>
-__global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kQkThreads, 2)
     qk_backward_kernel(const QkParams p) {
     constexpr int R = 32 / G;
     __shared__ float4 rows[kQkWarps * kQkMaxDim / 4];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
     float *row = reinterpret_cast<float *>(rows) + warp * 256 + sub * 8 * G;
     for (int k = 0; k < 2; ++k) {
-        Eight w, dw;
-        {
-            float f[8];
+        const Eight w = load_weights<L>(p, p.w[k], l);
+        Eight dw;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int i = element<L>(p, l, e);
-                f[e] = p.w[k] && i < p.dim ? p.w[k][i] : 1.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w.v[i] = {f[2 * i], f[2 * i + 1]}, dw.v[i] = both(0.f);
-        }
+        for (int i = 0; i < 4; ++i) dw.v[i] = both(0.f);
         for (int64_t task = blockIdx.x * (int64_t)kQkWarps + warp; task < p.tasks[k];
              task += gridDim.x * (int64_t)kQkWarps) {
             const int64_t token = task / p.n_chunk[k];
@@ -375,65 +413,65 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 2 : 3)
             const T *x_token = static_cast<const T *>(p.x[k].p) + token * p.x[k].token;
             T *dx_token = static_cast<T *>(p.b[k].p) + token * p.b[k].token;
             Eight c, s;  // s with the sign of the transpose
-            {
-                float cc[8], ss[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    int other;
-                    angle<L>(p, at.at, element<L>(p, l, e), !at.padding && !at.outside, cc[e],
-                             ss[e], other);
-                }
+            for (int i = 0; i < 4; ++i) c.v[i] = both(1.f), s.v[i] = both(0.f);
+            if (!at.padding && !at.outside) load_angles<L>(p, at.at, l, c, s);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c.v[i] = {cc[2 * i], cc[2 * i + 1]};
-                    s.v[i] = {-ss[2 * i], -ss[2 * i + 1]};
-                }
-            }
-            for (int base = h0 + sub; base - sub < h1; base += R * U) {
-                Raw8<T> raw[U], rawx[U];
-                uint2 code[U];
-                int b0[U], b1[U];
-                float rs[U];
+            for (int i = 0; i < 4; ++i) s.v[i] = {-s.v[i].x, -s.v[i].y};
+            Fetched<T> next[U];
+            auto fetch = [&](int base) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int h = base + u * R;
                     const bool live = h < h1 && !at.padding;
                     const int64_t at_row = token * p.heads[k] + h;
-                    raw[u] = load_row<T, L, ALIGNED>(p, dy_token + h * p.a[k].head, l, live);
-                    rs[u] = 0.f, b0[u] = b1[u] = 0, code[u] = make_uint2(0u, 0u);
-                    if (live) rs[u] = p.rstd[k][at_row];
+                    Fetched<T> &f = next[u];
+                    f.dy = load_row<T, L, ALIGNED>(p, dy_token + h * p.a[k].head, l, live);
+                    f.r = 0.f, f.scales = 0u;
+                    zero_raw(f.x.a);
+                    if constexpr (sizeof(T) == 4) zero_raw(f.x.b);
+                    if (live) f.r = p.rstd[k][at_row];
                     if (p.x[k].p) {
-                        rawx[u] = load_row<T, L, ALIGNED>(p, x_token + h * p.x[k].head, l, live);
+                        f.x = load_row<T, L, ALIGNED>(p, x_token + h * p.x[k].head, l, live);
                     } else if (live) {
                         const uint8_t *codes = p.codes[k] + at_row * p.pitch;
                         const uint8_t *scales = p.scales[k] + at_row * p.spitch;
                         if (L == kRun && 8 * l < p.dim) {
-                            code[u] = *reinterpret_cast<const uint2 *>(codes + 8 * l);
-                            b0[u] = scales[l / 4];
+                            const uint2 c = *reinterpret_cast<const uint2 *>(codes + 8 * l);
+                            f.x.a.x = c.x, f.x.a.y = c.y;
+                            f.scales = scales[l / 4];
                         } else if (L == kSplit && 4 * l < p.half) {
-                            code[u].x = *reinterpret_cast<const uint32_t *>(codes + 4 * l);
-                            code[u].y = *reinterpret_cast<const uint32_t *>(codes + p.half + 4 * l);
-                            b0[u] = scales[l / 8];
-                            b1[u] = scales[p.half / 32 + l / 8];
+                            f.x.a.x = *reinterpret_cast<const uint32_t *>(codes + 4 * l);
+                            f.x.a.y = *reinterpret_cast<const uint32_t *>(codes + p.half + 4 * l);
+                            f.scales = scales[l / 8] | (uint32_t)scales[p.half / 32 + l / 8] << 8;
                         }
                     }
                 }
+            };
+            fetch(h0 + sub);
+            for (int base = h0 + sub; base - sub < h1; base += R * U) {
+                Fetched<T> now[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) now[u] = next[u];
+                fetch(base + R * U);  // while these rows are worked on
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int h = base + u * R;
                     if (h - sub >= h1) break;  // no row of this step, for the whole warp
-                    const float r = at.outside ? __uint_as_float(0x7fffffffu) : rs[u];
-                    const Eight dy = pairs_of(to_float(raw[u]));
+                    const float r = at.outside ? __uint_as_float(0x7fffffffu) : now[u].r;
+                    const Eight dy = pairs_of(to_float(now[u].dy));
                     const Eight q = partners<G, L>(p, dy, l, row);
                     Eight n, g, hw;
                     if (p.x[k].p) {
-                        n = pairs_of(to_float(rawx[u]));
+                        n = pairs_of(to_float(now[u].x));
 #pragma unroll
                         for (int i = 0; i < 4; ++i) n.v[i] = mul2(n.v[i], both(r));
                     } else {
+                        const uint2 code = make_uint2(now[u].x.a.x, now[u].x.a.y);
+                        const int b0 = now[u].scales & 255u, b1 = now[u].scales >> 8;
                         n = p.format == POS_CKPT_INT8
-                                ? read_kept<L, POS_CKPT_INT8>(code[u], b0[u], b1[u], r)
-                                : read_kept<L, POS_CKPT_E4M3>(code[u], b0[u], b1[u], r);
+                                ? read_kept<L, POS_CKPT_INT8>(code, b0, b1, r)
+                                : read_kept<L, POS_CKPT_E4M3>(code, b0, b1, r);
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -555,6 +593,8 @@ static QkParams make_params(const pos_qk *q) {
     const CkptShape s = ckpt_shape(q->dim);
     p.pitch = (int32_t)s.pitch, p.spitch = (int32_t)s.spitch;
     p.pairing = q->pairing, p.format = q->format;
+    p.vectors = aligned16(q->cos) && aligned16(q->sin) && aligned16(q->w_q) && aligned16(q->w_k) &&
+                q->dim % 4 == 0;
     p.eps = q->eps, p.inv_dim = 1.f / q->dim;
     return p;
 }
@@ -584,15 +624,15 @@ static Shape shape_of(const QkParams &p, bool aligned) {
                                                                                : kShapeRun;
 }
 
-template <typename T, int G, int U>
+template <typename T, int G>
 static pos_status launch_forward(QkParams &p, bool aligned, cudaStream_t s) {
-    cut_tasks(p, (int64_t)sm_count() * 64);
+    cut_tasks(p, (int64_t)sm_count() * 32);
     const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
     const Shape shape = shape_of(p, aligned);
-    auto kern = shape == kShapeSplit ? qk_forward_kernel<T, G, U, kSplit, true>
-                : shape == kShapeRun ? qk_forward_kernel<T, G, U, kRun, true>
-                                     : qk_forward_kernel<T, G, U, kRun, false>;
+    auto kern = shape == kShapeSplit ? qk_forward_kernel<T, G, kSplit, true>
+                : shape == kShapeRun ? qk_forward_kernel<T, G, kRun, true>
+                                     : qk_forward_kernel<T, G, kRun, false>;
     kern<<<(unsigned)grid, kQkThreads, 0, s>>>(p);
     POS_CUDA(cudaGetLastError());
     return POS_OK;
@@ -600,11 +640,10 @@ static pos_status launch_forward(QkParams &p, bool aligned, cudaStream_t s) {
 
 template <typename T>
 static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
-    constexpr int U = sizeof(T) == 4 ? 1 : 2;
     switch (lanes_per_head(p.dim)) {
-        case 8: return launch_forward<T, 8, U>(p, aligned, s);
-        case 16: return launch_forward<T, 16, U>(p, aligned, s);
-        default: return launch_forward<T, 32, U>(p, aligned, s);
+        case 8: return launch_forward<T, 8>(p, aligned, s);
+        case 16: return launch_forward<T, 16>(p, aligned, s);
+        default: return launch_forward<T, 32>(p, aligned, s);
     }
 }
 
