@@ -25,9 +25,12 @@ struct QkParams {
     const float *cos, *sin;
     const int32_t *positions;
     float *part;               // backward: [block][2][dim] partial sums, or NULL
-    int64_t tokens, tasks[2], n_pos;
+    int64_t tokens, n_pos;
     int32_t heads[2], dim, half, pitch, spitch;
+    int64_t tasks[2];              // forward: all tasks,
     int32_t chunk[2], n_chunk[2];  // heads of a task, tasks of a token
+    int32_t steps[2];          // backward: of a token, its heads by what a warp takes at once
+    int32_t step_bytes;        // backward: shared memory of a step
     int32_t pairing, format;
     bool vectors;              // cos, sin and w can be read 16 bytes at a time
     float eps, inv_dim;
@@ -138,17 +141,17 @@ __device__ __forceinline__ Eight partners(const QkParams &p, const Eight &u, int
             q.v[i] = {__shfl_sync(0xffffffffu, u.v[i].x, from, G),
                       __shfl_sync(0xffffffffu, u.v[i].y, from, G)};
     } else {
+        // row: the warp's 256 floats
+        float *own = row + 8 * (threadIdx.x % 32);
         __syncwarp();
-        *reinterpret_cast<float4 *>(row + 8 * l) =
-            make_float4(u.v[0].x, u.v[0].y, u.v[1].x, u.v[1].y);
-        *reinterpret_cast<float4 *>(row + 8 * l + 4) =
-            make_float4(u.v[2].x, u.v[2].y, u.v[3].x, u.v[3].y);
+        *reinterpret_cast<float4 *>(own) = make_float4(u.v[0].x, u.v[0].y, u.v[1].x, u.v[1].y);
+        *reinterpret_cast<float4 *>(own + 4) = make_float4(u.v[2].x, u.v[2].y, u.v[3].x, u.v[3].y);
         __syncwarp();
         float o[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int i = 8 * l + e;
-            o[e] = i < 2 * p.half ? row[i < p.half ? i + p.half : i - p.half] : 0.f;
+            o[e] = i < 2 * p.half ? own[i < p.half ? e + p.half : e - p.half] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) q.v[i] = {o[2 * i], o[2 * i + 1]};
@@ -213,6 +216,7 @@ __device__ __forceinline__ void load_angles(const QkParams &p, int64_t at, int l
     }
 }
 
+// The sum over a head's lanes, in each of them.
 template <int G>
 __device__ __forceinline__ float row_sum(float v) {
 #pragma unroll
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     constexpr int R = 32 / G;
     __shared__ float4 rows[L == kSplit ? 1 : kQkThreads * 2];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
-    float *row = reinterpret_cast<float *>(rows) + (L == kSplit ? 0 : warp * 256 + sub * 8 * G);
+    float *row = reinterpret_cast<float *>(rows) + (L == kSplit ? 0 : warp * 256);
     int64_t task = blockIdx.x * (int64_t)kQkWarps + warp;
     const int k = task >= p.tasks[0];
     if (k) task -= p.tasks[0];
@@ -379,118 +383,192 @@ __device__ __forceinline__ Eight read_kept(uint2 code, int b0, int b1, float r) 
              mul2({v.v[6], v.v[7]}, s1)}};
 }
 
-// What a thread reads of a row: dy, x or in its place the codes, their one or
-// two scale bytes, rstd.
-template <typename T>
-struct Fetched {
-    Raw8<T> dy, x;
-    uint32_t scales;
-    float r;
-};
+// Asynchronous copies of 4, 8 or 16 bytes; zeros where `there` is false.
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool there) {
+    if constexpr (N == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+                     "r"(there ? 16 : 0)
+                     : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N),
+                     "r"(there ? N : 0)
+                     : "memory");
+}
 
-// The same tasks, taken by a resident grid, the queries' first; dw is summed
-// over a thread's rows in registers, over the block in shared memory, and
-// written as one partial sum per block, which qk_dw_kernel adds up in order.
-template <typename T, int G, int U, int L, bool ALIGNED>
+// What a warp holds of one step in shared memory (p.step_bytes): 256 elements of
+// dy, as many codes or elements of x, and for each of its heads 16 bytes with up
+// to 8 scale bytes and rstd.
+template <typename T>
+constexpr int kStepDy = 256 * (int)sizeof(T);
+constexpr int kSteps = 4;
+
+// A step is 32 / G query or key heads of one token, G lanes a head.  The
+// steps of all tokens, the queries' and then the keys', are cut into as many
+// equal runs as there are warps.
+struct Run {
+    int64_t at, end;
+};
+__device__ __forceinline__ Run run_of(const QkParams &p, int k) {
+    const int64_t total = p.tokens * p.steps[k], warps = gridDim.x * (int64_t)kQkWarps;
+    const int64_t w = blockIdx.x * (int64_t)kQkWarps + threadIdx.x / 32;
+    const int64_t each = total / warps, more = total % warps;
+    return {w * each + min(w, more), (w + 1) * each + min(w + 1, more)};
+}
+
+// A warp goes through its run, token by token.  ALIGNED: its rows are on their
+// way to shared memory three steps ahead, which takes no registers (with rows prefetched in registers @REG@ us instead of @ASYNC@ for 8192
+// tokens of 64 + 8 heads of 128, bf16).  dw is summed over a thread's rows in
+// registers, over the block in shared memory, and written as one partial sum
+// per block, which qk_dw_kernel adds up in order.
+template <typename T, int G, int L, bool ALIGNED>
 __global__ void __launch_bounds__(kQkThreads, 2)
     qk_backward_kernel(const QkParams p) {
-    constexpr int R = 32 / G;
+    extern __shared__ float4 steps[];
     __shared__ float4 rows[kQkWarps * kQkMaxDim / 4];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
-    float *row = reinterpret_cast<float *>(rows) + warp * 256 + sub * 8 * G;
+    constexpr int R = 32 / G;
+    const int warp = threadIdx.x / 32, l = threadIdx.x % G, sub = threadIdx.x % 32 / G;
+    float *row = reinterpret_cast<float *>(rows) + warp * 256;
+    const int bytes = p.step_bytes;
+    unsigned char *const mine = reinterpret_cast<unsigned char *>(steps) + warp * kSteps * bytes;
     for (int k = 0; k < 2; ++k) {
         const Eight w = load_weights<L>(p, p.w[k], l);
+        const bool from_x = p.x[k].p != nullptr;
         Eight dw;
 #pragma unroll
         for (int i = 0; i < 4; ++i) dw.v[i] = both(0.f);
-        for (int64_t task = blockIdx.x * (int64_t)kQkWarps + warp; task < p.tasks[k];
-             task += gridDim.x * (int64_t)kQkWarps) {
-            const int64_t token = task / p.n_chunk[k];
-            const int h0 = (int)(task - token * p.n_chunk[k]) * p.chunk[k];
-            const int h1 = min(h0 + p.chunk[k], p.heads[k]);
+        for (Run run = run_of(p, k); run.at < run.end;) {
+            const int64_t token = run.at / p.steps[k];
+            const int h0 = (int)(run.at - token * p.steps[k]) * R;
+            const int h1 = (int)min((int64_t)p.heads[k], h0 + (run.end - run.at) * R);
+            run.at = min(run.end, (token + 1) * p.steps[k]);
             const Place at = place_of(p, token);
-            const T *dy_token = static_cast<const T *>(p.a[k].p) + token * p.a[k].token;
-            const T *x_token = static_cast<const T *>(p.x[k].p) + token * p.x[k].token;
-            T *dx_token = static_cast<T *>(p.b[k].p) + token * p.b[k].token;
+            const int64_t row0 = token * p.heads[k] + h0 + sub;
+            const T *dy = static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
+                          (h0 + sub) * p.a[k].head;
+            T *dx = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head;
+            const T *x = static_cast<const T *>(p.x[k].p) + token * p.x[k].token +
+                         (h0 + sub) * p.x[k].head;
+            const uint8_t *codes = p.codes[k] + row0 * p.pitch;
+            const uint8_t *scales = p.scales[k] + row0 * p.spitch;
+            const float *rstd = p.rstd[k] + row0;
+            int ahead = h0 + sub, slot = 0;  // head and slot of the next copies
+            if constexpr (ALIGNED) {
+                dy += 8 * l, x += 8 * l, codes += 8 * l, scales += 4 * l;
+                __syncwarp();  // the last token's rows have been read
+            }
+            // (ALIGNED) starts the copies of one step, if there is one
+            auto start = [&]() {
+                const bool there = ahead < h1 && !at.padding;
+                if (ahead - sub < h1) {
+                    const uint32_t to =
+                        (uint32_t)__cvta_generic_to_shared(mine + slot * bytes);
+                    const uint32_t el = 8 * (threadIdx.x % 32);
+                    if (8 * l < p.dim) {
+                        copy_async<16>(to + el * sizeof(T), dy, there);
+                        if constexpr (sizeof(T) == 4) copy_async<16>(to + el * 4 + 16, dy + 4, there);
+                        if (from_x) {
+                            copy_async<16>(to + kStepDy<T> + el * sizeof(T), x, there);
+                            if constexpr (sizeof(T) == 4)
+                                copy_async<16>(to + kStepDy<T> + el * 4 + 16, x + 4, there);
+                        } else {
+                            copy_async<8>(to + kStepDy<T> + el, codes, there);
+                        }
+                    }
+                    const uint32_t aux = to + bytes - 16 * R + sub * 16;
+                    if (!from_x && 4 * l < p.spitch) copy_async<4>(aux + 4 * l, scales, there);
+                    if (l == 2) copy_async<4>(aux + 8, rstd, there);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                dy += R * p.a[k].head, x += R * p.x[k].head;
+                codes += R * p.pitch, scales += R * p.spitch, rstd += R;
+                ahead += R;
+                slot = slot + 1 == kSteps ? 0 : slot + 1;
+            };
+            if constexpr (ALIGNED) {
+#pragma unroll
+                for (int i = 0; i < kSteps - 1; ++i) start();
+            }
             Eight c, s;  // s with the sign of the transpose
 #pragma unroll
             for (int i = 0; i < 4; ++i) c.v[i] = both(1.f), s.v[i] = both(0.f);
             if (!at.padding && !at.outside) load_angles<L>(p, at.at, l, c, s);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s.v[i] = {-s.v[i].x, -s.v[i].y};
-            Fetched<T> next[U];
-            auto fetch = [&](int base) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int h = base + u * R;
-                    const bool live = h < h1 && !at.padding;
-                    const int64_t at_row = token * p.heads[k] + h;
-                    Fetched<T> &f = next[u];
-                    f.dy = load_row<T, L, ALIGNED>(p, dy_token + h * p.a[k].head, l, live);
-                    f.r = 0.f, f.scales = 0u;
-                    zero_raw(f.x.a);
-                    if constexpr (sizeof(T) == 4) zero_raw(f.x.b);
-                    if (live) f.r = p.rstd[k][at_row];
-                    if (p.x[k].p) {
-                        f.x = load_row<T, L, ALIGNED>(p, x_token + h * p.x[k].head, l, live);
-                    } else if (live) {
-                        const uint8_t *codes = p.codes[k] + at_row * p.pitch;
-                        const uint8_t *scales = p.scales[k] + at_row * p.spitch;
+            const float outside = at.outside ? __uint_as_float(0x7fffffffu) : 1.f;
+            int at_slot = 0;
+            for (int h = h0; h < h1; h += R) {
+                Raw8<T> raw, raw_x;
+                uint2 code = make_uint2(0u, 0u);
+                int b0 = 0, b1 = 0;
+                float r = 0.f;
+                const int g0 = L == kSplit ? l / 8 : l / 4, g1 = p.half / 32 + l / 8;
+                if constexpr (ALIGNED) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kSteps - 2) : "memory");
+                    __syncwarp();
+                    const unsigned char *from = mine + at_slot * bytes;
+                    const T *row_dy = reinterpret_cast<const T *>(from) + sub * 8 * G;
+                    const unsigned char *aux = from + bytes - 16 * R + sub * 16;
+                    raw = load_row<T, L, true>(p, row_dy, l, true);
+                    r = *reinterpret_cast<const float *>(aux + 8);
+                    if (from_x) {
+                        raw_x = load_row<T, L, true>(p, row_dy + 256, l, true);
+                    } else {
+                        const unsigned char *row_code = from + kStepDy<T> + sub * 8 * G;
                         if (L == kRun && 8 * l < p.dim) {
-                            const uint2 c = *reinterpret_cast<const uint2 *>(codes + 8 * l);
-                            f.x.a.x = c.x, f.x.a.y = c.y;
-                            f.scales = scales[l / 4];
+                            code = *reinterpret_cast<const uint2 *>(row_code + 8 * l);
+                            b0 = aux[g0];
                         } else if (L == kSplit && 4 * l < p.half) {
-                            f.x.a.x = *reinterpret_cast<const uint32_t *>(codes + 4 * l);
-                            f.x.a.y = *reinterpret_cast<const uint32_t *>(codes + p.half + 4 * l);
-                            f.scales = scales[l / 8] | (uint32_t)scales[p.half / 32 + l / 8] << 8;
+                            code.x = *reinterpret_cast<const uint32_t *>(row_code + 4 * l);
+                            code.y = *reinterpret_cast<const uint32_t *>(row_code + p.half + 4 * l);
+                            b0 = aux[g0], b1 = aux[g1];
                         }
                     }
-                }
-            };
-            fetch(h0 + sub);
-            for (int base = h0 + sub; base - sub < h1; base += R * U) {
-                Fetched<T> now[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) now[u] = next[u];
-                fetch(base + R * U);  // while these rows are worked on
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int h = base + u * R;
-                    if (h - sub >= h1) break;  // no row of this step, for the whole warp
-                    const float r = at.outside ? __uint_as_float(0x7fffffffu) : now[u].r;
-                    const Eight dy = pairs_of(to_float(now[u].dy));
-                    const Eight q = partners<G, L>(p, dy, l, row);
-                    Eight n, g, hw;
-                    if (p.x[k].p) {
-                        n = pairs_of(to_float(now[u].x));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) n.v[i] = mul2(n.v[i], both(r));
-                    } else {
-                        const uint2 code = make_uint2(now[u].x.a.x, now[u].x.a.y);
-                        const int b0 = now[u].scales & 255u, b1 = now[u].scales >> 8;
-                        n = p.format == POS_CKPT_INT8
-                                ? read_kept<L, POS_CKPT_INT8>(code, b0, b1, r)
-                                : read_kept<L, POS_CKPT_E4M3>(code, b0, b1, r);
+                    at_slot = at_slot + 1 == kSteps ? 0 : at_slot + 1;
+                    start();
+                } else {
+                    const bool live = h + sub < h1 && !at.padding;
+                    raw = load_row<T, L, false>(p, dy, l, live);
+                    if (from_x) raw_x = load_row<T, L, false>(p, x, l, live);
+                    if (live) {
+                        r = *rstd;
+                        if (!from_x && 8 * l < p.dim) {
+                            code = *reinterpret_cast<const uint2 *>(codes + 8 * l);
+                            b0 = scales[g0];
+                        }
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        g.v[i] = fma2(q.v[i], s.v[i], mul2(dy.v[i], c.v[i]));
-                        dw.v[i] = fma2(g.v[i], n.v[i], dw.v[i]);
-                        hw.v[i] = mul2(g.v[i], w.v[i]);
-                    }
-                    const F2 t = both(-r * (row_sum<G>(dot8(hw, n)) * p.inv_dim));
-                    Eight dx;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        dx.v[i] = fma2(n.v[i], t, mul2(hw.v[i], both(r)));
-                    Raw8<T> out = from_float<T>(values_of(dx));
-                    store_row<T, L, ALIGNED>(p, dx_token + h * p.b[k].head, l, h < h1, out);
+                    dy += R * p.a[k].head, x += R * p.x[k].head;
+                    codes += R * p.pitch, scales += R * p.spitch, rstd += R;
                 }
+                r *= outside;
+                const Eight v = pairs_of(to_float(raw));
+                const Eight q = partners<G, L>(p, v, l, row);
+                Eight n, hw;
+                if (from_x) {
+                    n = pairs_of(to_float(raw_x));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) n.v[i] = mul2(n.v[i], both(r));
+                } else {
+                    n = p.format == POS_CKPT_INT8 ? read_kept<L, POS_CKPT_INT8>(code, b0, b1, r)
+                                                  : read_kept<L, POS_CKPT_E4M3>(code, b0, b1, r);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const F2 gi = fma2(q.v[i], s.v[i], mul2(v.v[i], c.v[i]));
+                    dw.v[i] = fma2(gi, n.v[i], dw.v[i]);
+                    hw.v[i] = mul2(gi, w.v[i]);
+                }
+                const F2 t = both(-r * (row_sum<G>(dot8(hw, n)) * p.inv_dim));
+                Eight o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o.v[i] = fma2(n.v[i], t, mul2(hw.v[i], both(r)));
+                store_row<T, L, ALIGNED>(p, dx, l, h + sub < h1,
+                                         from_float<T>(values_of(o)));
+                dx += R * p.b[k].head;
             }
         }
         if (!p.part) continue;
-        // [warp][dim], heads side by side in a warp first
+        // [warp][dim], the heads side by side in a warp first
         float *sum = reinterpret_cast<float *>(rows);
         const Vec8 f = values_of(dw);
         __syncthreads();
@@ -599,8 +677,34 @@ static QkParams make_params(const pos_qk *q) {
     return p;
 }
 
-// Lanes per head: 8 elements a lane, a power of two.
+// Lanes of a head: 8 elements a lane, a power of two.  (With as many lanes as a
+// head of 80 needs, ten, three heads fit a warp instead of two, but sums over
+// ten lanes cost what that gains: 63 us either way for 4096 tokens of 72.)
 static int lanes_per_head(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
+
+// The kernel for a call: layout, lanes of a head, loads.
+template <typename T, template <typename, int, int, bool> class Kernel, int G>
+static auto pick_layout(const QkParams &p, bool aligned) {
+    const bool split = p.pairing == POS_ROT_HALF && 2 * p.half == p.dim && p.dim % 64 == 0;
+    return !aligned ? Kernel<T, G, kRun, false>::fn()
+           : split  ? Kernel<T, G, kSplit, true>::fn()
+                    : Kernel<T, G, kRun, true>::fn();
+}
+template <typename T, template <typename, int, int, bool> class Kernel>
+static auto pick(const QkParams &p, bool aligned) {
+    const int g = lanes_per_head(p.dim);
+    return g == 8    ? pick_layout<T, Kernel, 8>(p, aligned)
+           : g == 16 ? pick_layout<T, Kernel, 16>(p, aligned)
+                     : pick_layout<T, Kernel, 32>(p, aligned);
+}
+template <typename T, int G, int L, bool ALIGNED>
+struct Forward {
+    static auto fn() { return qk_forward_kernel<T, G, L, ALIGNED>; }
+};
+template <typename T, int G, int L, bool ALIGNED>
+struct Backward {
+    static auto fn() { return qk_backward_kernel<T, G, L, ALIGNED>; }
+};
 
 // Cuts a token's heads into tasks: as few as keep `warps` warps busy (each
 // reads the token's cosines and sines again), at least 32 / G heads a task.
@@ -616,52 +720,38 @@ static void cut_tasks(QkParams &p, int64_t warps) {
     }
 }
 
-// Which layout and loads a call can use.
-enum Shape { kShapeSplit, kShapeRun, kShapeAny };
-static Shape shape_of(const QkParams &p, bool aligned) {
-    if (!aligned) return kShapeAny;
-    return p.pairing == POS_ROT_HALF && 2 * p.half == p.dim && p.dim % 64 == 0 ? kShapeSplit
-                                                                               : kShapeRun;
+static void set_steps(QkParams &p) {
+    const int heads = 32 / lanes_per_head(p.dim);
+    for (int k = 0; k < 2; ++k) p.steps[k] = (p.heads[k] + heads - 1) / heads;
+}
+// Blocks: what the GPU holds at once, or fewer where there are fewer steps.
+static int grid_of(const QkParams &p, int per_sm) {
+    const int64_t steps = p.tokens * std::max(p.steps[0], p.steps[1]);
+    return (int)std::min<int64_t>((steps + kQkWarps - 1) / kQkWarps,
+                                  (int64_t)sm_count() * per_sm);
 }
 
-template <typename T, int G>
-static pos_status launch_forward(QkParams &p, bool aligned, cudaStream_t s) {
+template <typename T>
+static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
     cut_tasks(p, (int64_t)sm_count() * 32);
     const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
-    const Shape shape = shape_of(p, aligned);
-    auto kern = shape == kShapeSplit ? qk_forward_kernel<T, G, kSplit, true>
-                : shape == kShapeRun ? qk_forward_kernel<T, G, kRun, true>
-                                     : qk_forward_kernel<T, G, kRun, false>;
-    kern<<<(unsigned)grid, kQkThreads, 0, s>>>(p);
+    pick<T, Forward>(p, aligned)<<<(unsigned)grid, kQkThreads, 0, s>>>(p);
     POS_CUDA(cudaGetLastError());
     return POS_OK;
 }
 
 template <typename T>
-static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
-    switch (lanes_per_head(p.dim)) {
-        case 8: return launch_forward<T, 8>(p, aligned, s);
-        case 16: return launch_forward<T, 16>(p, aligned, s);
-        default: return launch_forward<T, 32>(p, aligned, s);
-    }
-}
-
-template <typename T, int G, int U>
-static pos_status launch_backward(QkParams &p, bool aligned, const float *dw_in, float *dw,
-                                  cudaStream_t s) {
-    const Shape shape = shape_of(p, aligned);
-    auto kern = shape == kShapeSplit ? qk_backward_kernel<T, G, U, kSplit, true>
-                : shape == kShapeRun ? qk_backward_kernel<T, G, U, kRun, true>
-                                     : qk_backward_kernel<T, G, U, kRun, false>;
+static pos_status backward_of(QkParams &p, bool aligned, const float *dw_in, float *dw,
+                              cudaStream_t s) {
+    set_steps(p);
+    auto kern = pick<T, Backward>(p, aligned);
+    p.step_bytes = kStepDy<T> + (p.x[0].p || p.x[1].p ? kStepDy<T> : 256) + 16 * (32 / lanes_per_head(p.dim));
+    const int smem = aligned ? kQkWarps * kSteps * p.step_bytes : 0;
+    POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), smem));
     int per_sm = 0;
-    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), kQkThreads, 0, &per_sm));
-    per_sm = std::max(1, std::min(per_sm, 8));
-    cut_tasks(p, (int64_t)sm_count() * per_sm * kQkWarps);
-    const int64_t tasks = std::max(p.tasks[0], p.tasks[1]);
-    const int grid =
-        (int)std::min<int64_t>((tasks + kQkWarps - 1) / kQkWarps, (int64_t)sm_count() * per_sm);
-    const int cols = 2 * p.dim;
+    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), kQkThreads, smem, &per_sm));
+    const int grid = grid_of(p, std::min(per_sm, 8)), cols = 2 * p.dim;
     void *scratch = nullptr;
     if (dw && grid > 0) {
         cudaMemPool_t pool;
@@ -669,25 +759,14 @@ static pos_status launch_backward(QkParams &p, bool aligned, const float *dw_in,
         POS_CUDA(cudaMallocFromPoolAsync(&scratch, (size_t)grid * cols * 4, pool, s));
         p.part = static_cast<float *>(scratch);
     }
-    if (grid > 0) kern<<<grid, kQkThreads, 0, s>>>(p);
+    if (grid > 0) kern<<<grid, kQkThreads, smem, s>>>(p);
     cudaError_t e = cudaGetLastError();
     if (dw && e == cudaSuccess)
-        e = launch_dependent(qk_dw_kernel, (cols + 31) / 32, 1024, 0, s,
-                             (const float *)p.part, grid, cols, dw_in, dw);
+        e = launch_dependent(qk_dw_kernel, (cols + 31) / 32, 1024, 0, s, (const float *)p.part,
+                             grid, cols, dw_in, dw);
     const cudaError_t e2 = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
     if (e == cudaSuccess) e = e2;
     return e == cudaSuccess ? POS_OK : cuda_fail(e, "q/k backward");
-}
-
-template <typename T>
-static pos_status backward_of(QkParams &p, bool aligned, const float *dw_in, float *dw,
-                              cudaStream_t s) {
-    constexpr int U = sizeof(T) == 4 ? 1 : 2;
-    switch (lanes_per_head(p.dim)) {
-        case 8: return launch_backward<T, 8, U>(p, aligned, dw_in, dw, s);
-        case 16: return launch_backward<T, 16, U>(p, aligned, dw_in, dw, s);
-        default: return launch_backward<T, 32, U>(p, aligned, dw_in, dw, s);
-    }
 }
 
 static pos_status set_ckpt(QkParams &p, const void *ckpt_q, const void *ckpt_k) {
