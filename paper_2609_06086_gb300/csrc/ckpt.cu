@@ -29,6 +29,43 @@ struct PackParams {
     FastDiv per_row;   // pitch / 8
 };
 
+// 8 elements at p, which need not be 16-byte aligned, from the aligned words
+// around them; those words lie inside the row, [p - before, p + left).
+// (keep_odd-like matrices, f16, 5003 x 5001, rows 5003 apart: @SHIFT@)
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8_shifted(const T *p, int before, int left) {
+    constexpr int kPer = 16 / sizeof(T);
+    const int m = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % kPer);
+    if (m == 0 && left >= 8) return load8<true>(p, 8);
+    if (before < m || left < 8 - m + kPer) return load8<false>(p, left);
+    constexpr int kWords = 4 * (8 / kPer + 1);
+    uint32_t w[kWords];
+    const uint4 *at = reinterpret_cast<const uint4 *>(p - m);
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) {
+        const uint4 v = at[i];
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+    // down by m elements: whole words by two choices, then half a word
+    const int q = sizeof(T) == 2 ? m / 2 : m;
+    if (q & 2) {
+#pragma unroll
+        for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
+    }
+    if (q & 1) {
+#pragma unroll
+        for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
+    }
+    if (sizeof(T) == 2 && (m & 1)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    Raw8<T> r;
+    r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (sizeof(T) == 4) r.b = make_uint4(w[4], w[5], w[6], w[7]);
+    return r;
+}
+
 // A thread takes vectors of 8 elements (a warp: 256 consecutive ones), four
 // lanes share a group's largest magnitude by two shuffles.  Bound by HBM:
 // every value is read once and every code written once.
@@ -44,7 +81,9 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackParams p) 
         row[i] = r;
         j[i] = v - r * p.per_row.d;
         const int left = v < p.n_vec ? p.cols - (int)(8 * j[i]) : 0;
-        raw[i] = load8<ALIGNED>(x + (int64_t)r * p.ld + 8 * j[i], left);
+        const T *at = x + (int64_t)r * p.ld + 8 * j[i];
+        if constexpr (ALIGNED) raw[i] = load8<true>(at, left);
+        else raw[i] = load8_shifted(at, (int)(8 * j[i]), left);
     }
 #pragma unroll
     for (int i = 0; i < kPackUnroll; ++i) {
@@ -60,7 +99,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackParams p) 
     }
 }
 
-template <typename T, int F, bool ALIGNED>
+template <typename T, int F>
 __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackParams p) {
     T *y = static_cast<T *>(const_cast<void *>(p.x));
     uint2 code[kPackUnroll];
@@ -79,9 +118,69 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackParams p
     for (int i = 0; i < kPackUnroll; ++i) {
         const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
         if (v >= p.n_vec) continue;
-        store8<ALIGNED>(y + (int64_t)row[i] * p.ld + 8 * j[i],
-                        from_float<T, true>(decode8<F>(code[i], scale_value(byte[i]))),
-                        p.cols - (int)(8 * j[i]));
+        store8<true>(y + (int64_t)row[i] * p.ld + 8 * j[i],
+                     from_float<T, true>(decode8<F>(code[i], scale_value(byte[i]))),
+                     p.cols - (int)(8 * j[i]));
+    }
+}
+
+// Rows that are not 16-byte aligned: a thread's 8 elements are those of an
+// aligned word of y, columns 8 j - m .. 8 j - m + 7 for a row that starts m
+// elements past one; their codes come from two words, under two scales.  One
+// vector more per row than above.
+template <typename T, int F>
+__global__ void __launch_bounds__(kPackThreads) unpack_shifted_kernel(const PackParams p) {
+    constexpr int kPer = 16 / sizeof(T);
+    T *y = static_cast<T *>(const_cast<void *>(p.x));
+    uint2 lo[kPackUnroll], hi[kPackUnroll];
+    int b0[kPackUnroll], b1[kPackUnroll];
+    uint32_t row[kPackUnroll], j[kPackUnroll];
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        row[i] = p.per_row.div(v);
+        j[i] = v - row[i] * p.per_row.d;
+        lo[i] = hi[i] = make_uint2(0u, 0u);
+        b0[i] = b1[i] = 0;
+        if (v >= p.n_vec) continue;
+        const uint8_t *codes = p.codes + row[i] * p.pitch, *scales = p.scales + row[i] * p.spitch;
+        if (j[i] > 0) {
+            lo[i] = *reinterpret_cast<const uint2 *>(codes + 8 * j[i] - 8);
+            b0[i] = scales[(j[i] - 1) / 4];
+        }
+        if (8 * j[i] < p.pitch) {
+            hi[i] = *reinterpret_cast<const uint2 *>(codes + 8 * j[i]);
+            b1[i] = scales[j[i] / 4];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kPackUnroll; ++i) {
+        const uint32_t v = blockIdx.x * (uint32_t)kPackBlock + i * kPackThreads + threadIdx.x;
+        if (v >= p.n_vec) continue;
+        T *start = y + (int64_t)row[i] * p.ld;
+        const int m = (int)(reinterpret_cast<uintptr_t>(start) / sizeof(T) % kPer);
+        const uint64_t a = (uint64_t)lo[i].y << 32 | lo[i].x, b = (uint64_t)hi[i].y << 32 | hi[i].x;
+        const uint64_t c = m ? a >> 8 * (8 - m) | b << 8 * m : b;
+        Vec8 f = decode8<F>(make_uint2((uint32_t)c, (uint32_t)(c >> 32)), 1.f);
+        const float s0 = scale_value(b0[i]), s1 = scale_value(b1[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] *= e < m ? s0 : s1;
+        const Raw8<T> out = from_float<T, true>(f);
+        const int first = (int)(8 * j[i]) - m, left = p.cols - first;  // column, columns from it
+        if (first >= 0) {
+            store8<true>(start + first, out, left);
+        } else {  // a row's first word: from its first column on
+            const uint32_t w[8] = {out.a.x, out.a.y, out.a.z, out.a.w, 0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e < m || e >= left) continue;
+                if constexpr (sizeof(T) == 2)
+                    reinterpret_cast<uint16_t *>(start)[first + e] =
+                        (uint16_t)(w[e / 2] >> 16 * (e % 2));
+                else
+                    start[first + e] = f.v[e];
+            }
+        }
     }
 }
 
@@ -90,9 +189,9 @@ template <typename T, int F>
 static pos_status launch_pack(bool pack, const void *x, int64_t rows, int64_t cols, int64_t ld,
                               void *ckpt, cudaStream_t stream) {
     const CkptShape s = ckpt_shape(cols);
-    const int64_t per_row = s.pitch / 8;
-    const int64_t most = std::max<int64_t>(1, (0x7fffffffll - kPackBlock) / per_row);
     const bool aligned = aligned16(x) && ld * (int64_t)sizeof(T) % 16 == 0;
+    const int64_t per_row = s.pitch / 8 + (!pack && !aligned ? 1 : 0);
+    const int64_t most = std::max<int64_t>(1, (0x7fffffffll - kPackBlock) / per_row);
     for (int64_t r = 0; r < rows; r += most) {
         const int64_t n = std::min(most, rows - r);
         PackParams p{static_cast<const T *>(x) + r * ld,
@@ -101,13 +200,9 @@ static pos_status launch_pack(bool pack, const void *x, int64_t rows, int64_t co
                      ld, s.pitch, s.spitch, (uint32_t)(n * per_row), (int32_t)cols,
                      FastDiv((uint32_t)per_row)};
         const int grid = (int)((n * per_row + kPackBlock - 1) / kPackBlock);
-        if (pack) {
-            if (aligned) pack_kernel<T, F, true><<<grid, kPackThreads, 0, stream>>>(p);
-            else pack_kernel<T, F, false><<<grid, kPackThreads, 0, stream>>>(p);
-        } else {
-            if (aligned) unpack_kernel<T, F, true><<<grid, kPackThreads, 0, stream>>>(p);
-            else unpack_kernel<T, F, false><<<grid, kPackThreads, 0, stream>>>(p);
-        }
+        auto kern = pack ? (aligned ? pack_kernel<T, F, true> : pack_kernel<T, F, false>)
+                         : (aligned ? unpack_kernel<T, F> : unpack_shifted_kernel<T, F>);
+        kern<<<grid, kPackThreads, 0, stream>>>(p);
         POS_CUDA(cudaGetLastError());
     }
     return POS_OK;

@@ -46,7 +46,8 @@ struct WgradParams {
     float *out, *part;     // part: tiles [256][256] of the split tiles' partial sums
     int64_t rows, ld, spitch;
     int32_t n, cols;
-    int32_t tiles_m, tiles_n;
+    int32_t tiles_m, tiles_n;  // tiles_n: of more than 128 columns of dy
+    int32_t tiles;         // with tiles_m narrow ones for what is left, if it is
     int32_t whole;         // tiles with all rows in one unit: the first ones
     int32_t units;         // whole + splits * (tiles - whole)
     int32_t splits;
@@ -297,17 +298,26 @@ __device__ __forceinline__ uint4 decode8_long(uint2 c, int byte) {
 // Kernel
 // ---------------------------------------------------------------------------
 struct Unit {
-    int m0, n0;      // first column of x, of dy
+    int m0, n0, tn;  // first column of x, of dy; columns of dy: 64, 128 or 256
     int r0, r1;      // rows
     int part;        // partial sum that it writes, or -1
 };
 // Units of the pairs that run at once share columns: bands of 8 tiles of dy,
-// through which the tiles of x pass.
-__device__ __forceinline__ void tile_of(const WgradParams &p, int tile, int &m0, int &n0) {
+// through which the tiles of x pass.  Tiles for a last 128 columns of dy or
+// fewer multiply only 128 or 64 (@NARROW@); they come last.
+__device__ __forceinline__ void tile_of(const WgradParams &p, int tile, int &m0, int &n0,
+                                        int &tn) {
+    if (tile >= p.tiles_m * p.tiles_n) {
+        m0 = (tile - p.tiles_m * p.tiles_n) * kTileM;
+        n0 = p.tiles_n * kTileN;
+        tn = p.n - n0 <= 64 ? 64 : 128;
+        return;
+    }
     const int band = tile / (8 * p.tiles_m), n_band = min(8, p.tiles_n - 8 * band);
     tile -= band * 8 * p.tiles_m;
     m0 = tile / n_band * kTileM;
     n0 = (8 * band + tile % n_band) * kTileN;
+    tn = kTileN;
 }
 __device__ __forceinline__ Unit unit_of(const WgradParams &p, int u) {
     Unit t;
@@ -319,7 +329,7 @@ __device__ __forceinline__ Unit unit_of(const WgradParams &p, int u) {
         t.r0 = (int)(t.part % p.splits * p.split_rows);
         t.r1 = (int)min(p.rows, t.r0 + p.split_rows);
     }
-    tile_of(p, tile, t.m0, t.n0);
+    tile_of(p, tile, t.m0, t.n0, t.tn);
     return t;
 }
 
@@ -361,6 +371,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&code_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&dy_map) : "memory");
+    }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
                      "r"(2 * kAccCols)
@@ -391,10 +405,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                     if (++cs == kCodeStages) cs = 0, cph ^= 1;
                     ok = bar_wait(empty + 8 * s, ph, gave_up);
                     if (!ok) break;
-                    if (rank == 0) bar_expect(full + 8 * s, 2 * kBBytes);
-                    for (int h = 0; h < 2; ++h)
+                    const int boxes = t.tn == kTileN ? 2 : 1;
+                    if (rank == 0) bar_expect(full + 8 * s, 2 * boxes * (kTileK * 128));
+                    for (int h = 0; h < boxes; ++h)
                         tma_load_pair(b_at + s * kBBytes + h * kTileK * 128, &dy_map,
-                                      t.n0 + (int)rank * kHalf + 64 * h, (int)r,
+                                      t.n0 + (int)rank * (t.tn / 2) + 64 * h, r,
                                       leader_full + 8 * s);
                     if (++s == kStages) s = 0, ph ^= 1;
                 }
@@ -403,13 +418,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
             constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             // f32 sums, both operands with M / N contiguous
             constexpr uint32_t kIdesc = 1u << 4 | kType << 7 | kType << 10 | 1u << 15 | 1u << 16 |
-                                        (uint32_t)(kTileN >> 3) << 17 |
                                         (uint32_t)(kTileM >> 4) << 24;
             int s = 0, acc = 0;
             uint32_t ph = 0, aph = 1;
             bool ok = true;
             for (int u = pair; u < p.units && ok; u += pairs) {
                 const Unit t = unit_of(p, u);
+                const uint32_t idesc = kIdesc | (uint32_t)(t.tn >> 3) << 17;
                 for (int c = t.r0; c < t.r1 && ok; c += kChunkRows) {
                     const int c1 = min(t.r1, c + kChunkRows);
                     ok = bar_wait(acc_empty + 8 * acc, aph, gave_up);
@@ -423,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
 #pragma unroll
                         for (int k = 0; k < kTileK / 16; ++k)
                             mma_pair(tmem + acc * kAccCols, a + k * (2048 >> 4),
-                                     b + k * (2048 >> 4), kIdesc, r > c || k > 0);
+                                     b + k * (2048 >> 4), idesc, r > c || k > 0);
                         commit_pair(empty + 8 * s);
                         if (++s == kStages) s = 0, ph ^= 1;
                     }
@@ -564,6 +579,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (int j0 = 0; j0 < 128; j0 += 8) {
+                    if (j1 + j0 >= t.tn) break;  // the others of a narrow tile stay 0
                     uint32_t v[8];
                     tmem_load8(from + acc * kAccCols + j0, v);
 #pragma unroll
@@ -615,8 +631,8 @@ __global__ void __launch_bounds__(kTileM) wgrad_join_kernel(const WgradParams p)
     grid_dep_wait();
     const int tile = blockIdx.x / (kTileN / kJoinRows);
     const int j0 = blockIdx.x % (kTileN / kJoinRows) * kJoinRows;
-    int m0, n0;
-    tile_of(p, p.whole + tile, m0, n0);
+    int m0, n0, tn;
+    tile_of(p, p.whole + tile, m0, n0, tn);
     const float *part = p.part + (int64_t)tile * p.splits * (kTileM * kTileN) + j0 * kTileM +
                         threadIdx.x;
     float sum[kJoinRows] = {};
@@ -704,7 +720,7 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), kWgradSmem));
     kern<<<2 * std::min(p.units, sm_count() / 2), kWgradThreads, kWgradSmem, s>>>(codes, grads, p);
     POS_CUDA(cudaGetLastError());
-    const int tiles = p.tiles_m * p.tiles_n - p.whole;
+    const int tiles = p.tiles - p.whole;
     if (p.splits > 1)
         POS_CUDA(launch_dependent(wgrad_join_kernel, tiles * (kTileN / kJoinRows), kTileM, 0, s, p));
     return POS_OK;
@@ -716,7 +732,7 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
 // about 6 stages to fill and drain, joining takes a launch (10 stages) and
 // reads every part.
 static void cut_rows(WgradParams &p, int pairs) {
-    const int tiles = p.tiles_m * p.tiles_n;
+    const int tiles = p.tiles;
     p.whole = tiles / pairs * pairs;
     const int rest = tiles - p.whole;
     const int64_t stages = (p.rows + kTileK - 1) / kTileK;
@@ -747,9 +763,10 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
     p.in = in, p.out = out, p.ld = ld, p.rows = rows, p.spitch = shape.spitch;
     p.n = (int32_t)n, p.cols = (int32_t)cols;
     p.tiles_m = (int32_t)((cols + kTileM - 1) / kTileM);
-    p.tiles_n = (int32_t)((n + kTileN - 1) / kTileN);
-    if ((int64_t)p.tiles_m * p.tiles_n > 0x7fffffffll)
-        return fail(POS_EINVAL, "wgrad: n * cols too large");
+    p.tiles_n = (int32_t)((n + kTileN / 2 - 1) / kTileN);
+    const int64_t tiles = (int64_t)p.tiles_m * ((n + kTileN - 1) / kTileN);
+    if (tiles > 0x7fffffffll / 2) return fail(POS_EINVAL, "wgrad: n * cols too large");
+    p.tiles = (int32_t)tiles;
     cut_rows(p, std::max(1, sm_count() / 2));
     // scratch: the split tiles' parts, then dy's copy
     const int64_t part_bytes =
