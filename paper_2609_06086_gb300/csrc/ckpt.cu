@@ -29,48 +29,13 @@ struct PackParams {
     FastDiv per_row;   // pitch / 8
 };
 
-// 8 elements at p, which need not be 16-byte aligned, from the aligned words
-// around them; those words lie inside the row, [p - before, p + left).
-// (keep_odd-like matrices, f16, 5003 x 5001, rows 5003 apart: @SHIFT@)
-template <typename T>
-__device__ __forceinline__ Raw8<T> load8_shifted(const T *p, int before, int left) {
-    constexpr int kPer = 16 / sizeof(T);
-    const int m = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % kPer);
-    if (m == 0 && left >= 8) return load8<true>(p, 8);
-    if (before < m || left < 8 - m + kPer) return load8<false>(p, left);
-    constexpr int kWords = 4 * (8 / kPer + 1);
-    uint32_t w[kWords];
-    const uint4 *at = reinterpret_cast<const uint4 *>(p - m);
-#pragma unroll
-    for (int i = 0; i < kWords / 4; ++i) {
-        const uint4 v = at[i];
-        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-    }
-    // down by m elements: whole words by two choices, then half a word
-    const int q = sizeof(T) == 2 ? m / 2 : m;
-    if (q & 2) {
-#pragma unroll
-        for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
-    }
-    if (q & 1) {
-#pragma unroll
-        for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
-    }
-    if (sizeof(T) == 2 && (m & 1)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-    }
-    Raw8<T> r;
-    r.a = make_uint4(w[0], w[1], w[2], w[3]);
-    if constexpr (sizeof(T) == 4) r.b = make_uint4(w[4], w[5], w[6], w[7]);
-    return r;
-}
-
 // A thread takes vectors of 8 elements (a warp: 256 consecutive ones), four
 // lanes share a group's largest magnitude by two shuffles.  Bound by HBM:
 // every value is read once and every code written once.
 template <typename T, int F, bool ALIGNED>
 __global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
     const T *x = static_cast<const T *>(p.x);
     Raw8<T> raw[kPackUnroll];
     uint32_t row[kPackUnroll], j[kPackUnroll];
@@ -101,6 +66,8 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackParams p) 
 
 template <typename T, int F>
 __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
     T *y = static_cast<T *>(const_cast<void *>(p.x));
     uint2 code[kPackUnroll];
     int byte[kPackUnroll];
@@ -130,6 +97,8 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackParams p
 // vector more per row than above.
 template <typename T, int F>
 __global__ void __launch_bounds__(kPackThreads) unpack_shifted_kernel(const PackParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
     constexpr int kPer = 16 / sizeof(T);
     T *y = static_cast<T *>(const_cast<void *>(p.x));
     uint2 lo[kPackUnroll], hi[kPackUnroll];
@@ -202,8 +171,7 @@ static pos_status launch_pack(bool pack, const void *x, int64_t rows, int64_t co
         const int grid = (int)((n * per_row + kPackBlock - 1) / kPackBlock);
         auto kern = pack ? (aligned ? pack_kernel<T, F, true> : pack_kernel<T, F, false>)
                          : (aligned ? unpack_kernel<T, F> : unpack_shifted_kernel<T, F>);
-        kern<<<grid, kPackThreads, 0, stream>>>(p);
-        POS_CUDA(cudaGetLastError());
+        POS_CUDA(launch_dependent(kern, grid, kPackThreads, 0, stream, p));
     }
     return POS_OK;
 }

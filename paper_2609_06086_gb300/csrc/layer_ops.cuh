@@ -170,6 +170,42 @@ __device__ __forceinline__ Raw8<T> load8(const T *p, int n) {
     return r;
 }
 
+// 8 elements at p, which need not be 16-byte aligned, from the aligned words
+// around them; those words lie inside the row, [p - before, p + left).
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8_shifted(const T *p, int before, int left) {
+    constexpr int kPer = 16 / sizeof(T);
+    const int m = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % kPer);
+    if (m == 0 && left >= 8) return load8<true>(p, 8);
+    if (before < m || left < 8 - m + kPer) return load8<false>(p, left);
+    constexpr int kWords = 4 * (8 / kPer + 1);
+    uint32_t w[kWords];
+    const uint4 *at = reinterpret_cast<const uint4 *>(p - m);
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) {
+        const uint4 v = at[i];
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+    // down by m elements: whole words by two choices, then half a word
+    const int q = sizeof(T) == 2 ? m / 2 : m;
+    if (q & 2) {
+#pragma unroll
+        for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
+    }
+    if (q & 1) {
+#pragma unroll
+        for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
+    }
+    if (sizeof(T) == 2 && (m & 1)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    Raw8<T> r;
+    r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (sizeof(T) == 4) r.b = make_uint4(w[4], w[5], w[6], w[7]);
+    return r;
+}
+
 template <bool ALIGNED, typename T>
 __device__ __forceinline__ void store8(T *p, const Raw8<T> &r, int n) {
     if constexpr (ALIGNED) {

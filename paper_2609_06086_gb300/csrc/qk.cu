@@ -305,6 +305,8 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
 template <typename T, int G, int L, bool ALIGNED>
 __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     qk_forward_kernel(const QkParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
     constexpr int R = 32 / G;
     __shared__ float4 rows[L == kSplit ? 1 : kQkThreads * 2];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, l = lane % G, sub = lane / G;
@@ -424,6 +426,8 @@ __device__ __forceinline__ Run run_of(const QkParams &p, int k) {
 template <typename T, int G, int L, bool ALIGNED>
 __global__ void __launch_bounds__(kQkThreads, 2)
     qk_backward_kernel(const QkParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
     extern __shared__ float4 steps[];
     __shared__ float4 rows[kQkWarps * kQkMaxDim / 4];
     constexpr int R = 32 / G;
@@ -596,6 +600,7 @@ __global__ void __launch_bounds__(kQkThreads, 2)
 __global__ void __launch_bounds__(1024) qk_dw_kernel(const float *part, int n_part, int cols,
                                                      const float *dw_in, float *dw) {
     grid_dep_wait();
+    grid_dep_trigger();
     __shared__ float sum[32][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int i = blockIdx.x * 32 + lane;
@@ -736,8 +741,7 @@ static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
     cut_tasks(p, (int64_t)sm_count() * 32);
     const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
-    pick<T, Forward>(p, aligned)<<<(unsigned)grid, kQkThreads, 0, s>>>(p);
-    POS_CUDA(cudaGetLastError());
+    POS_CUDA(launch_dependent(pick<T, Forward>(p, aligned), (int)grid, kQkThreads, 0, s, p));
     return POS_OK;
 }
 
@@ -759,8 +763,7 @@ static pos_status backward_of(QkParams &p, bool aligned, const float *dw_in, flo
         POS_CUDA(cudaMallocFromPoolAsync(&scratch, (size_t)grid * cols * 4, pool, s));
         p.part = static_cast<float *>(scratch);
     }
-    if (grid > 0) kern<<<grid, kQkThreads, smem, s>>>(p);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = grid > 0 ? launch_dependent(kern, grid, kQkThreads, smem, s, p) : cudaSuccess;
     if (dw && e == cudaSuccess)
         e = launch_dependent(qk_dw_kernel, (cols + 31) / 32, 1024, 0, s, (const float *)p.part,
                              grid, cols, dw_in, dw);

@@ -385,6 +385,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
     __syncthreads();
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    grid_dep_wait();
+    grid_dep_trigger();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
 
     if (group == 0) {
@@ -629,6 +631,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
 constexpr int kJoinRows = 4;
 __global__ void __launch_bounds__(kTileM) wgrad_join_kernel(const WgradParams p) {
     grid_dep_wait();
+    grid_dep_trigger();
     const int tile = blockIdx.x / (kTileN / kJoinRows);
     const int j0 = blockIdx.x % (kTileN / kJoinRows) * kJoinRows;
     int m0, n0, tn;
@@ -659,11 +662,16 @@ __global__ void wgrad_fill_kernel(const float *in, float *out, int64_t n, int64_
             out[i * ld + j] = in ? in[i * ld + j] : 0.f;
 }
 
-// dy into rows that tensor copies can read (16-byte aligned).
-__global__ void wgrad_copy_kernel(const uint16_t *x, int64_t ldx, uint16_t *y, int64_t ldy,
-                                  int64_t rows, int64_t n) {
-    for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
-        for (int64_t j = threadIdx.x; j < n; j += blockDim.x) y[i * ldy + j] = x[i * ldx + j];
+// dy into rows that tensor copies can read (16-byte aligned, a multiple of 8
+// elements, zeros past the last column): 8 elements a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) wgrad_copy_kernel(const T *x, int64_t ldx, T *y,
+                                                         int64_t ldy, int64_t rows, int n) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    for (int64_t j = 8 * (blockIdx.y * 256ll + threadIdx.x); j < n; j += 2048ll * gridDim.y)
+        for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
+            store8<true>(y + i * ldy + j, load8_shifted(x + i * ldx + j, (int)j, n - (int)j), 8);
 }
 
 // ---------------------------------------------------------------------------
@@ -718,8 +726,8 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
                      dy, p.rows, p.n, ld_dy * 2, 64, CU_TENSOR_MAP_SWIZZLE_128B));
     auto kern = wgrad_kernel<T, F>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), kWgradSmem));
-    kern<<<2 * std::min(p.units, sm_count() / 2), kWgradThreads, kWgradSmem, s>>>(codes, grads, p);
-    POS_CUDA(cudaGetLastError());
+    POS_CUDA(launch_dependent(kern, 2 * std::min(p.units, std::max(1, sm_count() / 2)),
+                              kWgradThreads, kWgradSmem, s, codes, grads, p));
     const int tiles = p.tiles - p.whole;
     if (p.splits > 1)
         POS_CUDA(launch_dependent(wgrad_join_kernel, tiles * (kTileN / kJoinRows), kTileM, 0, s, p));
@@ -728,21 +736,20 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
 
 // Full rounds of tiles take all rows each; the tiles of the last round are cut
 // along the rows where that ends sooner.  In units of a stage (64 rows of a
-// tile, 0.28 us): a round of `splits` parts takes its share of the rows and
-// about 6 stages to fill and drain, joining takes a launch (10 stages) and
-// reads every part.
+// tile, 0.4 us): a round takes its share of the rows and about one stage to
+// change tiles, joining takes a launch (8 stages) and reads every part.
 static void cut_rows(WgradParams &p, int pairs) {
     const int tiles = p.tiles;
     p.whole = tiles / pairs * pairs;
     const int rest = tiles - p.whole;
     const int64_t stages = (p.rows + kTileK - 1) / kTileK;
     p.splits = 1, p.split_rows = stages * kTileK;
-    double best = stages + 6.;
+    double best = stages + 1.;
     for (int s = 2; rest > 0 && s <= stages && rest * s <= 3 * pairs; ++s) {
         const int64_t each = (stages + s - 1) / s;
         if ((s - 1) * each >= stages) continue;  // the last part would be empty
-        const double t = (double)((rest * s + pairs - 1) / pairs) * (each + 6.) + 10. +
-                         0.2 * rest * s * 4. / pairs;
+        const double t = (double)((rest * s + pairs - 1) / pairs) * (each + 1.) + 8. +
+                         0.8 * rest * s / pairs;
         if (t < best) best = t, p.splits = s, p.split_rows = each * kTileK;
     }
     if (p.splits == 1) p.whole = tiles;
@@ -781,9 +788,18 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
         p.part = static_cast<float *>(scratch);
     }
     if (copy) {
-        uint16_t *to = reinterpret_cast<uint16_t *>(static_cast<char *>(scratch) + part_bytes);
-        wgrad_copy_kernel<<<(int)std::min<int64_t>(rows, 65535), 256, 0, s>>>(
-            static_cast<const uint16_t *>(dy), ld_dy, to, ld2, rows, n);
+        void *to = static_cast<char *>(scratch) + part_bytes;
+        const dim3 grid((unsigned)std::min<int64_t>(rows, 8192),
+                        (unsigned)std::min<int64_t>((ld2 / 8 + 255) / 256, 65535));
+        // (either type: 16 bits are copied)
+        wgrad_copy_kernel<__half><<<grid, 256, 0, s>>>(static_cast<const __half *>(dy), ld_dy,
+                                                       static_cast<__half *>(to), ld2, rows,
+                                                       (int)n);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) {
+            cudaFreeAsync(scratch, s);
+            return cuda_fail(e, "wgrad copy");
+        }
         dy = to, ld_dy = ld2;
     }
     pos_status st;
