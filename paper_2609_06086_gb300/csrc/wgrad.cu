@@ -46,7 +46,8 @@ struct WgradParams {
     float *out, *part;     // part: tiles [256][256] of the split tiles' partial sums
     int64_t rows, ld, spitch;
     int32_t n, cols;
-    int32_t tiles_m, tiles_n;  // tiles_n: of more than 128 columns of dy
+    int32_t tile_n;        // columns of dy of a tile: 64, 128 or 256
+    int32_t tiles_m, tiles_n;  // under tile_n = 256, tiles_n has more than 128 columns each
     int32_t tiles;         // with tiles_m narrow ones for what is left, if it is
     int32_t whole;         // tiles with all rows in one unit: the first ones
     int32_t units;         // whole + splits * (tiles - whole)
@@ -310,14 +311,14 @@ __device__ __forceinline__ void tile_of(const WgradParams &p, int tile, int &m0,
     if (tile >= p.tiles_m * p.tiles_n) {
         m0 = (tile - p.tiles_m * p.tiles_n) * kTileM;
         n0 = p.tiles_n * kTileN;
-        tn = p.n - n0 <= 64 ? 64 : 128;
+        tn = p.n - n0 <= 64 ? 64 : 128;  // (only under tile_n = 256)
         return;
     }
     const int band = tile / (8 * p.tiles_m), n_band = min(8, p.tiles_n - 8 * band);
     tile -= band * 8 * p.tiles_m;
     m0 = tile / n_band * kTileM;
-    n0 = (8 * band + tile % n_band) * kTileN;
-    tn = kTileN;
+    n0 = (8 * band + tile % n_band) * p.tile_n;
+    tn = p.tile_n;
 }
 __device__ __forceinline__ Unit unit_of(const WgradParams &p, int u) {
     Unit t;
@@ -353,24 +354,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
 
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            // both SMs' decoding warps, and the arrival that expects both
-            // halves of dy (in the first SM only)
-            bar_init(full + 8 * i, 1 + 2 * kDecodeWarps);
-            bar_init(empty + 8 * i, 1);
-        }
-        for (int i = 0; i < kCodeStages; ++i) {
-            bar_init(code_full + 8 * i, 1 + 32);  // codes, a warp's copies of scales
-            bar_init(code_empty + 8 * i, kDecodeWarps);
-        }
-        for (int i = 0; i < 2; ++i) {
-            bar_init(acc_full + 8 * i, 1);
-            bar_init(acc_empty + 8 * i, 2 * kSumWarps);
-        }
-        *gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = threadIdx.x; i < kBars; i += kWgradThreads) {
+        int count = 1;  // empty, acc_full: one commit
+        // full: both SMs' decoding warps, and the arrival that expects both
+        // halves of dy (in the first SM only)
+        if (i < kStages) count = 1 + 2 * kDecodeWarps;
+        const int j = i - 2 * kStages, k = j - 2 * kCodeStages;
+        if (j >= 0 && j < kCodeStages) count = 1 + 32;  // codes, a warp's copies of scales
+        if (j >= kCodeStages && k < 0) count = kDecodeWarps;
+        if (k >= 2) count = 2 * kSumWarps;
+        bar_init(bars + 8 * i, count);
     }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (threadIdx.x == 0) *gave_up = 0;
     if (warp == 0 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&code_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&dy_map) : "memory");
@@ -568,7 +564,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         for (int u = pair; u < p.units; u += pairs) {
             const Unit t = unit_of(p, u);
             const int m = (int)rank * kHalf + 32 * quarter + column_at(lane), j1 = side * 128;
-            const int left = t.m0 + m < p.cols ? p.n - t.n0 - j1 : 0;  // rows of dW to write
+            const int left = t.m0 + m < p.cols ? min(t.tn, p.n - t.n0) - j1 : 0;  // rows to write
             // dw_in is read while the first products run: all loads at once
             float sum[128];
             const float *in = p.in + (t.n0 + j1) * p.ld + t.m0 + m;
@@ -639,6 +635,7 @@ __global__ void __launch_bounds__(kTileM) wgrad_join_kernel(const WgradParams p)
     const float *part = p.part + (int64_t)tile * p.splits * (kTileM * kTileN) + j0 * kTileM +
                         threadIdx.x;
     float sum[kJoinRows] = {};
+    if (j0 >= tn) return;
     for (int s = 0; s < p.splits; ++s) {
 #pragma unroll
         for (int j = 0; j < kJoinRows; ++j)
@@ -734,26 +731,38 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
     return POS_OK;
 }
 
-// Full rounds of tiles take all rows each; the tiles of the last round are cut
-// along the rows where that ends sooner.  In units of a stage (64 rows of a
-// tile, 0.4 us): a round takes its share of the rows and about one stage to
-// change tiles, joining takes a launch (8 stages) and reads every part.
-static void cut_rows(WgradParams &p, int pairs) {
-    const int tiles = p.tiles;
-    p.whole = tiles / pairs * pairs;
-    const int rest = tiles - p.whole;
+// Tiles and cuts along the rows.  Full rounds of tiles take all rows each; the
+// tiles of the last round are cut where that ends sooner, and where there are
+// few tiles they are narrower.  In units of a stage of 256 columns (64 rows,
+// 0.4 us): a stage of fewer is bound by decoding; a tile's sums leave the SM
+// at 32 bytes a cycle, which the last one of all shows; joining parts takes a
+// launch (8 units) and reads each of them.
+static void cut(WgradParams &p, int pairs) {
     const int64_t stages = (p.rows + kTileK - 1) / kTileK;
-    p.splits = 1, p.split_rows = stages * kTileK;
-    double best = stages + 1.;
-    for (int s = 2; rest > 0 && s <= stages && rest * s <= 3 * pairs; ++s) {
-        const int64_t each = (stages + s - 1) / s;
-        if ((s - 1) * each >= stages) continue;  // the last part would be empty
-        const double t = (double)((rest * s + pairs - 1) / pairs) * (each + 1.) + 8. +
-                         0.8 * rest * s / pairs;
-        if (t < best) best = t, p.splits = s, p.split_rows = each * kTileK;
+    double best = 1e300;
+    for (int tn = kTileN; tn >= 64; tn /= 2) {
+        const double stage = tn == 256 ? 1. : tn == 128 ? 0.75 : 0.7, drain = 5. * tn / 256;
+        const int64_t n_tiles = (p.n + tn - 1) / tn, tiles = p.tiles_m * n_tiles;
+        if (tn < kTileN && tiles > 4 * pairs) break;
+        const int64_t whole = tiles / pairs * pairs, rest = tiles - whole;
+        const double base = (double)(tiles / pairs) * stages * stage + drain;
+        for (int64_t s = 1; s == 1 || (s <= stages && rest * s <= 3 * pairs && rest > 0); ++s) {
+            const int64_t each = (stages + s - 1) / s;
+            if ((s - 1) * each >= stages) continue;  // the last part would be empty
+            const double last = (double)((rest * s + pairs - 1) / pairs) * (each * stage + 1.);
+            const double t =
+                base + last + (s > 1 ? 8. + 0.8 * tn / 256 * (double)(rest * s) / pairs : 0.);
+            if (t >= best) continue;
+            best = t;
+            p.tile_n = tn;
+            p.tiles_n = (int32_t)(tn == kTileN ? (p.n + kTileN / 2 - 1) / kTileN : n_tiles);
+            p.tiles = (int32_t)tiles;
+            p.splits = (int32_t)s;
+            p.split_rows = each * kTileK;
+            p.whole = (int32_t)(s > 1 ? whole : tiles);
+        }
     }
-    if (p.splits == 1) p.whole = tiles;
-    p.units = p.whole + (tiles - p.whole) * p.splits;
+    p.units = p.whole + (p.tiles - p.whole) * p.splits;
 }
 
 static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int32_t dtype,
@@ -770,11 +779,9 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
     p.in = in, p.out = out, p.ld = ld, p.rows = rows, p.spitch = shape.spitch;
     p.n = (int32_t)n, p.cols = (int32_t)cols;
     p.tiles_m = (int32_t)((cols + kTileM - 1) / kTileM);
-    p.tiles_n = (int32_t)((n + kTileN / 2 - 1) / kTileN);
-    const int64_t tiles = (int64_t)p.tiles_m * ((n + kTileN - 1) / kTileN);
-    if (tiles > 0x7fffffffll / 2) return fail(POS_EINVAL, "wgrad: n * cols too large");
-    p.tiles = (int32_t)tiles;
-    cut_rows(p, std::max(1, sm_count() / 2));
+    if ((int64_t)p.tiles_m * ((n + kTileN - 1) / kTileN) > 0x7fffffffll / 2)
+        return fail(POS_EINVAL, "wgrad: n * cols too large");
+    cut(p, std::max(1, sm_count() / 2));
     // scratch: the split tiles' parts, then dy's copy
     const int64_t part_bytes =
         p.splits > 1 ? (int64_t)(p.units - p.whole) * (kTileM * kTileN) * 4 : 0;
