@@ -388,19 +388,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
     if (group == 0) {
         give_registers<kLoadRegs>();
         if (warp == 0 && lane == 0) {
-            int s = 0, cs = 0;
-            uint32_t ph = 1, cph = 1;  // an empty buffer's first wait passes
+            int s = 0;
+            uint32_t ph = 1;  // an empty buffer's first wait passes
             const uint32_t leader_full = in_cta(full, 0);
             bool ok = true;
             for (int u = pair; u < p.units && ok; u += pairs) {
                 const Unit t = unit_of(p, u);
                 for (int r = t.r0; r < t.r1; r += kTileK) {
-                    ok = bar_wait(code_empty + 8 * cs, cph, gave_up);
-                    if (!ok) break;
-                    bar_expect(code_full + 8 * cs, kCodeBytes);
-                    tma_load(c_at + cs * kCodeBytes, &code_map, t.m0 + (int)rank * kHalf, (int)r,
-                             code_full + 8 * cs);
-                    if (++cs == kCodeStages) cs = 0, cph ^= 1;
                     ok = bar_wait(empty + 8 * s, ph, gave_up);
                     if (!ok) break;
                     const int boxes = t.tn == kTileN ? 2 : 1;
@@ -447,8 +441,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 }
             }
         } else if (warp == 2) {
-            // The scales of a stage's rows, four groups (a word) each: plain
-            // asynchronous copies, since their rows may start at any word.
+            // Codes, and the scales of a stage's rows, four groups (a word) each:
+            // plain asynchronous copies, since their rows may start at any word.
+            // Their own warp: they are wanted some stages before dy, and waiting
+            // for its place too made them late (@LATE@).
             int cs = 0;
             uint32_t cph = 1;
             bool ok = true;
@@ -460,6 +456,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                     ok = bar_wait(code_empty + 8 * cs, cph, gave_up);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
+                    if (lane == 0) {
+                        bar_expect(code_full + 8 * cs, kCodeBytes);
+                        tma_load(c_at + cs * kCodeBytes, &code_map, m0, r, code_full + 8 * cs);
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int at = r + lane + 32 * h;
