@@ -36,9 +36,10 @@ constexpr int kWgradSmem = 1024 + kStages * (kABytes + kBBytes) +
 constexpr int kAccCols = 256;           // TMEM columns of one accumulator; two alternate
 // The tensor cores cut what they add to a sum instead of rounding it, so a
 // long sum drifts towards zero by about 1e-9 of its size per row (measured:
-// 2.6e-6 over 4096 rows).  An accumulator therefore takes 512 rows, and the
-// sums of those are added in registers, with rounding.
-constexpr int kChunkRows = 512;
+// 2.6e-6 over 4096 rows).  An accumulator therefore takes 768 rows, and the
+// sums of those are added in registers, with rounding (512 rows each: 107 us for
+// 4096 x 4864 x 4096 instead of @CH@).
+constexpr int kChunkRows = 768;
 
 struct WgradParams {
     const uint8_t *scales;
@@ -519,10 +520,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 const bool all_short = __all_sync(
                     0xffffffffu, short_way<T, F>((int)byte[0]) && short_way<T, F>((int)byte[1]) &&
                                      short_way<T, F>((int)byte[2]) && short_way<T, F>((int)byte[3]));
-                __syncwarp();
-                if (lane == 0) bar_arrive(code_empty + 8 * cs);
-                cs += kDecodeGroups;
-                if (cs >= kCodeStages) cs -= kCodeStages, cph ^= 1;
                 ok = bar_wait(empty + 8 * s, ph, gave_up);
                 if (!ok) break;
 #pragma unroll
@@ -543,9 +540,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                                          to[q] + s * kABytes + h % 2 * other + h / 2 * (32 * 128)),
                                      "r"(v[q].x), "r"(v[q].y), "r"(v[q].z), "r"(v[q].w));
                 }
+                // Orders the stores before the tensor cores' reads and the loads
+                // before the next copy into the codes' place: an arrival alone
+                // does neither.
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(leader_full + 8 * s);
+                if (lane == 0) {
+                    bar_arrive_cluster(leader_full + 8 * s);
+                    bar_arrive(code_empty + 8 * cs);
+                }
+                cs += kDecodeGroups;
+                if (cs >= kCodeStages) cs -= kCodeStages, cph ^= 1;
                 s += kDecodeGroups;
                 if (s >= kStages) s -= kStages, ph ^= 1;
             }
@@ -588,6 +593,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 if (lane == 0) bar_arrive_cluster(leader_acc_empty + 8 * acc);
                 acc ^= 1;
                 if (acc == 0) aph ^= 1;
+                if (c == t.r0 && p.in && u + pairs < p.units) {
+                    // the next unit's dw_in on its way to L2
+                    const Unit n = unit_of(p, u + pairs);
+                    const int col = n.m0 + (int)rank * kHalf + 32 * quarter;
+                    for (int j = lane; j < min(128, min(n.tn, p.n - n.n0) - j1); j += 32)
+                        if (n.part < 0 && col < p.cols)
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(
+                                p.in + (n.n0 + j1 + j) * p.ld + col));
+                }
             }
             // a wait that gave up: no sums
             const float lost = ok ? 0.f : __uint_as_float(0x7fffffffu);

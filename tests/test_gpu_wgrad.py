@@ -216,3 +216,28 @@ def test_same_bits_every_time(P, rows, n, cols):
                               o.data_ptr(), cols, streams[i % 2].cuda_stream)
     torch.cuda.synchronize()
     assert all(torch.equal(first, o) for o in outs)
+
+
+@pytest.mark.parametrize("rows,n,cols,fmt", [(4096, 6144, 4096, "int8"), (8192, 2048, 2048, "e4m3"),
+                                             (1500, 5000, 3000, "int8")])
+def test_many_tiles_added_to_earlier_gradients(P, rows, n, cols, fmt):
+    """Several tiles per pair of SMs with dw_in to read in between, which lets
+    the loads run as far ahead as their buffers allow; several calls, since what
+    overtakes what differs from one to the next.  The sums in 64 bits are the
+    GPU's, of the values that poseidon_ckpt_unpack gives."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, device="cuda", generator=gen)
+    ckpt = torch.empty(U.layout(rows, cols)[3], dtype=torch.uint8, device="cuda")
+    P.poseidon_ckpt_pack(x.data_ptr(), 2, rows, cols, cols, U.FORMATS[fmt], ckpt.data_ptr(), stream())
+    P.poseidon_ckpt_unpack(ckpt.data_ptr(), U.FORMATS[fmt], rows, cols, x.data_ptr(), 2, cols,
+                           stream())
+    dy = torch.randn(rows, n, device="cuda", generator=gen).to(torch.bfloat16)
+    add = torch.randn(n, cols, device="cuda", generator=gen)
+    want = add.double() + dy.double().t() @ x.double()
+    size = dy.double().abs().t() @ x.double().abs()
+    room = (rows / 16 + 16) * 2.0 ** -23 * size + 2.0 ** -22 * want.abs()
+    for _ in range(8):
+        out = torch.full((n, cols), 5.0, device="cuda")
+        call(P, ckpt, fmt, dy, "bf16", rows, n, cols, n, add, out, cols)
+        assert bool(((out.double() - want).abs() <= room).all())
