@@ -53,6 +53,28 @@ struct Vec8 {
     float v[8];
 };
 
+// Two f32 operations in one instruction.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
+        "mul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
+        "mov.b64 c, {%6, %7};\nfma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ F2 both(float v) { return {v, v}; }
+
 // Codes of 4 values under one scale byte below the largest.  x * 2^-e is exact
 // (or an underflow far below half a code), so each code is rounded once: int8
 // by adding 1.5 * 2^23, whose last bit is a whole number, e4m3 by the
@@ -62,16 +84,17 @@ __device__ __forceinline__ uint32_t encode4_inside(float x0, float x1, float x2,
                                                    int byte) {
     const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
     if constexpr (F == POS_CKPT_INT8) {
-        const uint32_t a = __float_as_uint(fmaf(x0, inv, 12582912.f));
-        const uint32_t b = __float_as_uint(fmaf(x1, inv, 12582912.f));
-        const uint32_t c = __float_as_uint(fmaf(x2, inv, 12582912.f));
-        const uint32_t d = __float_as_uint(fmaf(x3, inv, 12582912.f));
-        return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+        const F2 u = fma2({x0, x1}, both(inv), both(12582912.f));
+        const F2 v = fma2({x2, x3}, both(inv), both(12582912.f));
+        return __byte_perm(__byte_perm(__float_as_uint(u.x), __float_as_uint(u.y), 0x0040),
+                           __byte_perm(__float_as_uint(v.x), __float_as_uint(v.y), 0x0040),
+                           0x5410);
     } else {
+        const F2 u = mul2({x0, x1}, both(inv)), v = mul2({x2, x3}, both(inv));
         const uint32_t lo =
-            __nv_cvt_float2_to_fp8x2(make_float2(x0 * inv, x1 * inv), __NV_SATFINITE, __NV_E4M3);
+            __nv_cvt_float2_to_fp8x2(make_float2(u.x, u.y), __NV_SATFINITE, __NV_E4M3);
         const uint32_t hi =
-            __nv_cvt_float2_to_fp8x2(make_float2(x2 * inv, x3 * inv), __NV_SATFINITE, __NV_E4M3);
+            __nv_cvt_float2_to_fp8x2(make_float2(v.x, v.y), __NV_SATFINITE, __NV_E4M3);
         return lo | hi << 16;
     }
 }

@@ -36,83 +36,85 @@ struct QkParams {
     float eps, inv_dim;
 };
 
-// Two f32 operations in one instruction.
-struct F2 {
-    float x, y;
-};
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-    F2 r;
-    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
-        "mul.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("{\n.reg .b64 a, b, c, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
-        "mov.b64 c, {%6, %7};\nfma.rn.f32x2 r, a, b, c;\nmov.b64 {%0, %1}, r;\n}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-__device__ __forceinline__ F2 both(float v) { return {v, v}; }
-
 // A thread's 8 elements of a head, as four pairs.
 struct Eight {
     F2 v[4];
 };
 
+// How a kernel reads heads: kAny one element at a time, kAligned 16 bytes at a
+// time, kFull likewise heads of exactly 8 G elements, G lanes a head, so that
+// sizes and offsets are constants.
+enum Loads { kAny, kAligned, kFull };
+template <int G, int A>
+__device__ __forceinline__ int dim_of(const QkParams &p) {
+    return A == kFull ? 8 * G : p.dim;
+}
+template <int G, int A>
+__device__ __forceinline__ int pitch_of(const QkParams &p) {
+    return A == kFull ? 8 * G : p.pitch;
+}
+template <int G, int A>
+__device__ __forceinline__ int spitch_of(const QkParams &p) {
+    return A == kFull ? (G + 15) / 16 * 4 : p.spitch;
+}
+
 // Where a thread's elements lie in a head.
 //   kRun: elements 8 l .. 8 l + 7.  The partners of the rotation lie in the
 //     same pair (POS_ROT_ADJACENT), in one other lane (POS_ROT_HALF with
 //     rot / 2 divisible by 8) or anywhere in the row.
-//   kSplit: 4 l .. 4 l + 3 and as many from dim / 2 + 4 l on: under
-//     POS_ROT_HALF with rot = dim a multiple of 64, partners lie in the same
-//     thread and a group of 32 columns in 8 lanes.  8192 tokens of 64 + 8 heads
-//     of 128, bf16: 75.5 us forward and 80.5 us backward, kRun 83.7 and 99.3.
+//   kSplit (kFull, POS_ROT_HALF, rot = dim): 4 l .. 4 l + 3 and as many from
+//     dim / 2 + 4 l on, so that partners lie in the same thread and a group of 32
+//     columns in 8 lanes.  8192 tokens of 64 + 8 heads of 128, bf16: 73.7 us
+//     forward and 79.0 us backward; exchanging kRun's partners by shuffles took
+//     8 us and 19 us more.
 enum Layout { kRun, kSplit };
-
 template <int L>
-__device__ __forceinline__ int element(const QkParams &p, int l, int e) {
-    if (L == kRun) return 8 * l + e;
-    return e < 4 ? 4 * l + e : p.half + 4 * l + (e - 4);
+__device__ __forceinline__ int first_of(int l) {  // the thread's first element
+    return (L == kSplit ? 4 : 8) * l;
+}
+template <int G, int L>
+__device__ __forceinline__ int element(int l, int e) {
+    return L == kSplit && e >= 4 ? 4 * G + 4 * l + (e - 4) : first_of<L>(l) + e;
 }
 
-// The words of a thread's elements.  kSplit and ALIGNED: vector loads.
-template <typename T, int L, bool ALIGNED>
-__device__ __forceinline__ Raw8<T> load_row(const QkParams &p, const T *head, int l, bool live) {
-    if constexpr (L == kRun) {
-        return load8<ALIGNED>(head + 8 * l, live ? p.dim - 8 * l : 0);
+// The words of a thread's elements, the first of them at `at`.
+template <typename T, int G, int L, int A>
+__device__ __forceinline__ Raw8<T> load_row(const QkParams &p, const T *at, int l, bool live) {
+    if constexpr (A != kFull) {
+        return load8<A == kAligned>(at, live ? p.dim - 8 * l : 0);
     } else {
         Raw8<T> r;
         zero_raw(r.a);
         if constexpr (sizeof(T) == 4) zero_raw(r.b);
-        if (live && 4 * l < p.half) {
+        if (live) {
             if constexpr (sizeof(T) == 4) {
-                r.a = *reinterpret_cast<const uint4 *>(head + 4 * l);
-                r.b = *reinterpret_cast<const uint4 *>(head + p.half + 4 * l);
+                r.a = *reinterpret_cast<const uint4 *>(at);
+                r.b = *reinterpret_cast<const uint4 *>(at + (L == kSplit ? 4 * G : 4));
+            } else if constexpr (L == kRun) {
+                r.a = *reinterpret_cast<const uint4 *>(at);
             } else {
-                const uint2 a = *reinterpret_cast<const uint2 *>(head + 4 * l);
-                const uint2 b = *reinterpret_cast<const uint2 *>(head + p.half + 4 * l);
+                const uint2 a = *reinterpret_cast<const uint2 *>(at);
+                const uint2 b = *reinterpret_cast<const uint2 *>(at + 4 * G);
                 r.a = make_uint4(a.x, a.y, b.x, b.y);
             }
         }
         return r;
     }
 }
-template <typename T, int L, bool ALIGNED>
-__device__ __forceinline__ void store_row(const QkParams &p, T *head, int l, bool live,
+template <typename T, int G, int L, int A>
+__device__ __forceinline__ void store_row(const QkParams &p, T *at, int l, bool live,
                                           const Raw8<T> &r) {
-    if constexpr (L == kRun) {
-        store8<ALIGNED>(head + 8 * l, r, live ? p.dim - 8 * l : 0);
-    } else if (live && 4 * l < p.half) {
+    if constexpr (A != kFull) {
+        store8<A == kAligned>(at, r, live ? p.dim - 8 * l : 0);
+    } else if (live) {
         if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<uint4 *>(head + 4 * l) = r.a;
-            *reinterpret_cast<uint4 *>(head + p.half + 4 * l) = r.b;
+            *reinterpret_cast<uint4 *>(at) = r.a;
+            *reinterpret_cast<uint4 *>(at + (L == kSplit ? 4 * G : 4)) = r.b;
+        } else if constexpr (L == kRun) {
+            *reinterpret_cast<uint4 *>(at) = r.a;
         } else {
-            *reinterpret_cast<uint2 *>(head + 4 * l) = make_uint2(r.a.x, r.a.y);
-            *reinterpret_cast<uint2 *>(head + p.half + 4 * l) = make_uint2(r.a.z, r.a.w);
+            *reinterpret_cast<uint2 *>(at) = make_uint2(r.a.x, r.a.y);
+            *reinterpret_cast<uint2 *>(at + 4 * G) = make_uint2(r.a.z, r.a.w);
         }
     }
 }
@@ -160,40 +162,36 @@ __device__ __forceinline__ Eight partners(const QkParams &p, const Eight &u, int
 }
 
 // A thread's weights; ones where there are none.
-template <int L>
+template <int G, int L, int A>
 __device__ __forceinline__ Eight load_weights(const QkParams &p, const float *w, int l) {
     Eight o;
     if (L == kSplit && w && p.vectors) {
-        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-        const bool in = 4 * l < p.half;
-        const float4 a = in ? *reinterpret_cast<const float4 *>(w + 4 * l) : one;
-        const float4 b = in ? *reinterpret_cast<const float4 *>(w + p.half + 4 * l) : one;
+        const float4 a = *reinterpret_cast<const float4 *>(w + 4 * l);
+        const float4 b = *reinterpret_cast<const float4 *>(w + 4 * G + 4 * l);
         return {{{a.x, a.y}, {a.z, a.w}, {b.x, b.y}, {b.z, b.w}}};
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int e = element<L>(p, l, 2 * i);
-        o.v[i] = {w && e < p.dim ? w[e] : 1.f, w && e + 1 < p.dim ? w[e + 1] : 1.f};
+        const int e = element<G, L>(l, 2 * i), dim = dim_of<G, A>(p);
+        o.v[i] = {w && e < dim ? w[e] : 1.f, w && e + 1 < dim ? w[e + 1] : 1.f};
     }
     return o;
 }
 
 // y = x c + partner s is Rot x: the cosine of an element's pair, and its sine
 // with the sign that the partner's term has; 1 and 0 from rot on.
-template <int L>
+template <int G, int L>
 __device__ __forceinline__ void load_angles(const QkParams &p, int64_t at, int l, Eight &c,
                                             Eight &s) {
     const float *cs = p.cos + at * p.half, *sn = p.sin + at * p.half;
     if constexpr (L == kSplit) {
-        float4 a = make_float4(1.f, 1.f, 1.f, 1.f), b = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (4 * l < p.half) {
-            if (p.vectors) {
-                a = *reinterpret_cast<const float4 *>(cs + 4 * l);
-                b = *reinterpret_cast<const float4 *>(sn + 4 * l);
-            } else {
-                a = make_float4(cs[4 * l], cs[4 * l + 1], cs[4 * l + 2], cs[4 * l + 3]);
-                b = make_float4(sn[4 * l], sn[4 * l + 1], sn[4 * l + 2], sn[4 * l + 3]);
-            }
+        float4 a, b;
+        if (p.vectors) {
+            a = *reinterpret_cast<const float4 *>(cs + 4 * l);
+            b = *reinterpret_cast<const float4 *>(sn + 4 * l);
+        } else {
+            a = make_float4(cs[4 * l], cs[4 * l + 1], cs[4 * l + 2], cs[4 * l + 3]);
+            b = make_float4(sn[4 * l], sn[4 * l + 1], sn[4 * l + 2], sn[4 * l + 3]);
         }
         c = {{{a.x, a.y}, {a.z, a.w}, {a.x, a.y}, {a.z, a.w}}};
         s = {{{-b.x, -b.y}, {-b.z, -b.w}, {b.x, b.y}, {b.z, b.w}}};
@@ -242,8 +240,25 @@ __device__ __forceinline__ Place place_of(const QkParams &p, int64_t token) {
     return q;
 }
 
-// Keeps a head in 8 bits.
-template <typename T, int L, int F>
+// The scale bytes of the two groups whose largest magnitudes are the halves of
+// m, in the halves of a word.  bf16: exponent and mantissa are the same as f32's,
+// so both at once; a group with an infinity or a NaN gets the largest one.
+template <typename T, int F>
+__device__ __forceinline__ uint32_t scale_bytes2(uint32_t m) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        constexpr uint32_t kBoth = 0x00010001u, kLead = Fmt<F>::kLead;
+        const uint32_t b = (m + (Fmt<F>::kCarry >> 16) * kBoth) >> 7 & 0x01ff01ffu;
+        return __vminu2(__vmaxu2(b, (kScaleLo + kLead) * kBoth),
+                        (Fmt<F>::kScaleHi + kLead) * kBoth) - kLead * kBoth;
+    } else {
+        const int b0 = scale_byte<F>(f32_bits<T>(m & 0xffffu));
+        const int b1 = scale_byte<F>(f32_bits<T>(m >> 16));
+        return (uint32_t)b0 | (uint32_t)b1 << 16;
+    }
+}
+
+// Keeps a head in 8 bits; codes and scales at the thread's first columns.
+template <typename T, int G, int L, int A, int F>
 __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, const Eight &x,
                                          uint8_t *codes, uint8_t *scales, int l, bool live) {
     if constexpr (L == kRun) {
@@ -251,13 +266,13 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
         m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = max_bits<T>(m, __shfl_xor_sync(0xffffffffu, m, 2));
         const int byte = scale_byte<F>(f32_bits<T>(m));
-        if (!live || 8 * l >= p.pitch) return;
-        const Vec8 v = values_of(x);
-        *reinterpret_cast<uint2 *>(codes + 8 * l) = encode8<F>(v, byte);
-        if (l % 4 == 0) scales[l / 4] = (uint8_t)byte;
+        if (!live || 8 * l >= pitch_of<G, A>(p)) return;
+        *reinterpret_cast<uint2 *>(codes) = encode8<F>(values_of(x), byte);
+        if (l % 4 == 0) *scales = (uint8_t)byte;
     } else {
         // two groups: of the first and of the second half
-        uint32_t lo, hi;
+        int b0, b1;
+        uint32_t lo, hi;  // their largest magnitudes, as f32 bits or as T's
         if constexpr (sizeof(T) == 4) {
             constexpr uint32_t kAbs = 0x7fffffffu;
             lo = max(max(raw.a.x & kAbs, raw.a.y & kAbs), max(raw.a.z & kAbs, raw.a.w & kAbs));
@@ -267,6 +282,7 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
                 lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, o));
                 hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
             }
+            b0 = scale_byte<F>(lo), b1 = scale_byte<F>(hi);
         } else {
             // both magnitudes, 16 bits each, through one shuffle
             constexpr uint32_t kAbs = 0x7fff7fffu;
@@ -275,24 +291,25 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
             uint32_t m = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
 #pragma unroll
             for (int o = 1; o < 8; o *= 2) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-            lo = f32_bits<T>(m & 0xffffu);
-            hi = f32_bits<T>(m >> 16);
+            lo = m & 0xffffu, hi = m >> 16;
+            const uint32_t bytes = scale_bytes2<T, F>(m);
+            b0 = bytes & 0xffffu, b1 = bytes >> 16;
         }
-        const int b0 = scale_byte<F>(lo), b1 = scale_byte<F>(hi);
-        if (!live || 4 * l >= p.half) return;
+        if (!live) return;
         uint32_t c0, c1;
         if (max(b0, b1) < Fmt<F>::kScaleHi) {
             c0 = encode4_inside<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
             c1 = encode4_inside<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
         } else {
+            b0 = scale_byte<F>(f32_bits<T>(lo)), b1 = scale_byte<F>(f32_bits<T>(hi));
             c0 = encode4<F>(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y, b0);
             c1 = encode4<F>(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y, b1);
         }
-        *reinterpret_cast<uint32_t *>(codes + 4 * l) = c0;
-        *reinterpret_cast<uint32_t *>(codes + p.half + 4 * l) = c1;
+        *reinterpret_cast<uint32_t *>(codes) = c0;
+        *reinterpret_cast<uint32_t *>(codes + 4 * G) = c1;
         if (l % 8 == 0) {
-            scales[l / 8] = (uint8_t)b0;
-            scales[p.half / 32 + l / 8] = (uint8_t)b1;
+            scales[0] = (uint8_t)b0;
+            scales[G / 8] = (uint8_t)b1;
         }
     }
 }
@@ -301,10 +318,11 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
 // lanes a head with 8 elements a lane, 32 / G heads at once, the next ones on
 // their way.  With the weights in them, the token's cosines and sines make y =
 // r (x c + partner s) with 16 coefficients, kept in registers over the task.
-// Bound by HBM: x is read once, y (and the codes) written once (8192 tokens of
-// 64 + 8 heads of 128, bf16: 75.5 us, 75% of HBM's rate).  64 registers and 32
-// warps an SM: with 80 and 24 warps 88.5 us.
-template <typename T, int G, int L, bool ALIGNED>
+// Bound by HBM and by issuing its instructions: x is read once, y (and the codes)
+// written once (8192 tokens of 64 + 8 heads of 128: bf16 73.7 us, 77% of HBM's
+// rate; 4096 in f32 58.8 us, 87%).  64 registers and 32 warps an SM: with 80 and
+// 24 warps it took 10 us more.
+template <typename T, int G, int L, int A>
 __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     qk_forward_kernel(const QkParams p) {
     grid_dep_wait();
@@ -322,18 +340,22 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     const int h1 = min(h0 + p.chunk[k], p.heads[k]);
     const Place at = place_of(p, token);
     const int64_t row0 = token * p.heads[k] + h0 + sub;
+    const int pitch = pitch_of<G, A>(p), spitch = spitch_of<G, A>(p);
+    // all at the thread's first element
     const T *x = static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
-                 (h0 + sub) * p.a[k].head;
-    T *y = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head;
-    uint8_t *codes = p.codes[k] ? p.codes[k] + row0 * p.pitch : nullptr;
-    uint8_t *scales = p.scales[k] + row0 * p.spitch;
+                 (h0 + sub) * p.a[k].head + first_of<L>(l);
+    T *y = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head +
+           first_of<L>(l);
+    const bool keep = p.codes[k] != nullptr;
+    uint8_t *codes = p.codes[k] + row0 * pitch + first_of<L>(l);
+    uint8_t *scales = p.scales[k] + row0 * spitch + first_of<L>(l) / kGroup;
     float *rstd = p.rstd[k] && l == 0 ? p.rstd[k] + row0 : nullptr;
-    Raw8<T> next = load_row<T, L, ALIGNED>(p, x, l, h0 + sub < h1);
+    Raw8<T> next = load_row<T, G, L, A>(p, x, l, h0 + sub < h1);
     // y = r (x c + partner s): the weights go into c and s
     Eight c, s;
-    const Eight w = load_weights<L>(p, p.w[k], l);
+    const Eight w = load_weights<G, L, A>(p, p.w[k], l);
     if (!at.padding && !at.outside) {
-        load_angles<L>(p, at.at, l, c, s);
+        load_angles<G, L>(p, at.at, l, c, s);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) c.v[i] = both(1.f), s.v[i] = both(0.f);
@@ -349,15 +371,15 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
         const bool live = h + sub < h1;
         const Raw8<T> raw = next;
         x += R * p.a[k].head;
-        next = load_row<T, L, ALIGNED>(p, x, l, h + R + sub < h1);  // while this row is worked on
+        next = load_row<T, G, L, A>(p, x, l, h + R + sub < h1);  // while this row is worked on
         const Eight v = pairs_of(to_float(raw));
         const float r = rsqrtf(fmaf(row_sum<G>(dot8(v, v)), p.inv_dim, p.eps));
-        if (codes) {
+        if (keep) {
             if (p.format == POS_CKPT_INT8)
-                keep_row<T, L, POS_CKPT_INT8>(p, raw, v, codes, scales, l, live);
+                keep_row<T, G, L, A, POS_CKPT_INT8>(p, raw, v, codes, scales, l, live);
             else
-                keep_row<T, L, POS_CKPT_E4M3>(p, raw, v, codes, scales, l, live);
-            codes += R * p.pitch, scales += R * p.spitch;
+                keep_row<T, G, L, A, POS_CKPT_E4M3>(p, raw, v, codes, scales, l, live);
+            codes += R * pitch, scales += R * spitch;
         }
         if (rstd) {
             if (live) *rstd = r;
@@ -373,7 +395,7 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
             zero_raw(out.a);
             if constexpr (sizeof(T) == 4) zero_raw(out.b);
         }
-        store_row<T, L, ALIGNED>(p, y, l, live, out);
+        store_row<T, G, L, A>(p, y, l, live, out);
         y += R * p.b[k].head;
     }
 }
@@ -420,14 +442,14 @@ __device__ __forceinline__ Run run_of(const QkParams &p, int k) {
     return {w * each + min(w, more), (w + 1) * each + min(w + 1, more)};
 }
 
-// A warp goes through its run, token by token.  ALIGNED: its rows are on their
-// way to shared memory three steps ahead, which takes no registers (two rows
+// A warp goes through its run, token by token.  kAligned, kFull: its rows are on
+// their way to shared memory three steps ahead, which takes no registers (two rows
 // prefetched in registers instead: 111 us for 8192 tokens of 64 + 8 heads of 128,
-// bf16; so 80.5 us, 71% of HBM's rate).  Bound by issuing its instructions and
+// bf16; so 79.0 us, 72% of HBM's rate, 86% from x).  Bound by issuing its instructions and
 // by HBM: 16 warps an SM, since fewer than 128 registers spill.  dw is summed
 // over a thread's rows in registers, over the block in shared memory, and
 // written as one partial sum per block, which qk_dw_kernel adds up in order.
-template <typename T, int G, int L, bool ALIGNED>
+template <typename T, int G, int L, int A>
 __global__ void __launch_bounds__(kQkThreads, 2)
     qk_backward_kernel(const QkParams p) {
     grid_dep_wait();
@@ -440,7 +462,7 @@ __global__ void __launch_bounds__(kQkThreads, 2)
     const int bytes = p.step_bytes;
     unsigned char *const mine = reinterpret_cast<unsigned char *>(steps) + warp * kSteps * bytes;
     for (int k = 0; k < 2; ++k) {
-        const Eight w = load_weights<L>(p, p.w[k], l);
+        const Eight w = load_weights<G, L, A>(p, p.w[k], l);
         const bool from_x = p.x[k].p != nullptr;
         Eight dw;
 #pragma unroll
@@ -454,25 +476,25 @@ __global__ void __launch_bounds__(kQkThreads, 2)
             const int64_t row0 = token * p.heads[k] + h0 + sub;
             const T *dy = static_cast<const T *>(p.a[k].p) + token * p.a[k].token +
                           (h0 + sub) * p.a[k].head;
-            T *dx = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head;
+            T *dx = static_cast<T *>(p.b[k].p) + token * p.b[k].token + (h0 + sub) * p.b[k].head +
+                    first_of<L>(l);
             const T *x = static_cast<const T *>(p.x[k].p) + token * p.x[k].token +
                          (h0 + sub) * p.x[k].head;
-            const uint8_t *codes = p.codes[k] + row0 * p.pitch;
-            const uint8_t *scales = p.scales[k] + row0 * p.spitch;
+            const int pitch = pitch_of<G, A>(p), spitch = spitch_of<G, A>(p);
+            const uint8_t *codes = p.codes[k] + row0 * pitch + 8 * l;
+            const uint8_t *scales = p.scales[k] + row0 * spitch + (A == kAny ? l / 4 : 4 * l);
             const float *rstd = p.rstd[k] + row0;
             int ahead = h0 + sub, slot = 0;  // head and slot of the next copies
-            if constexpr (ALIGNED) {
-                dy += 8 * l, x += 8 * l, codes += 8 * l, scales += 4 * l;
-                __syncwarp();  // the last token's rows have been read
-            }
-            // (ALIGNED) starts the copies of one step, if there is one
+            dy += 8 * l, x += 8 * l;
+            if constexpr (A != kAny) __syncwarp();  // the last token's rows have been read
+            // (not kAny) starts the copies of one step, if there is one
             auto start = [&]() {
                 const bool there = ahead < h1 && !at.padding;
                 if (ahead - sub < h1) {
                     const uint32_t to =
                         (uint32_t)__cvta_generic_to_shared(mine + slot * bytes);
                     const uint32_t el = 8 * (threadIdx.x % 32);
-                    if (8 * l < p.dim) {
+                    if (8 * l < dim_of<G, A>(p)) {
                         copy_async<16>(to + el * sizeof(T), dy, there);
                         if constexpr (sizeof(T) == 4) copy_async<16>(to + el * 4 + 16, dy + 4, there);
                         if (from_x) {
@@ -484,23 +506,23 @@ __global__ void __launch_bounds__(kQkThreads, 2)
                         }
                     }
                     const uint32_t aux = to + bytes - 16 * R + sub * 16;
-                    if (!from_x && 4 * l < p.spitch) copy_async<4>(aux + 4 * l, scales, there);
+                    if (!from_x && 4 * l < spitch) copy_async<4>(aux + 4 * l, scales, there);
                     if (l == 2) copy_async<4>(aux + 8, rstd, there);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 dy += R * p.a[k].head, x += R * p.x[k].head;
-                codes += R * p.pitch, scales += R * p.spitch, rstd += R;
+                codes += R * pitch, scales += R * spitch, rstd += R;
                 ahead += R;
                 slot = slot + 1 == kSteps ? 0 : slot + 1;
             };
-            if constexpr (ALIGNED) {
+            if constexpr (A != kAny) {
 #pragma unroll
                 for (int i = 0; i < kSteps - 1; ++i) start();
             }
             Eight c, s;  // s with the sign of the transpose
 #pragma unroll
             for (int i = 0; i < 4; ++i) c.v[i] = both(1.f), s.v[i] = both(0.f);
-            if (!at.padding && !at.outside) load_angles<L>(p, at.at, l, c, s);
+            if (!at.padding && !at.outside) load_angles<G, L>(p, at.at, l, c, s);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s.v[i] = {-s.v[i].x, -s.v[i].y};
             const float outside = at.outside ? __uint_as_float(0x7fffffffu) : 1.f;
@@ -510,43 +532,44 @@ __global__ void __launch_bounds__(kQkThreads, 2)
                 uint2 code = make_uint2(0u, 0u);
                 int b0 = 0, b1 = 0;
                 float r = 0.f;
-                const int g0 = L == kSplit ? l / 8 : l / 4, g1 = p.half / 32 + l / 8;
-                if constexpr (ALIGNED) {
+                if constexpr (A != kAny) {
                     asm volatile("cp.async.wait_group %0;" ::"n"(kSteps - 2) : "memory");
                     __syncwarp();
                     const unsigned char *from = mine + at_slot * bytes;
-                    const T *row_dy = reinterpret_cast<const T *>(from) + sub * 8 * G;
+                    const T *row_dy =
+                        reinterpret_cast<const T *>(from) + sub * 8 * G + first_of<L>(l);
                     const unsigned char *aux = from + bytes - 16 * R + sub * 16;
-                    raw = load_row<T, L, true>(p, row_dy, l, true);
+                    raw = load_row<T, G, L, A>(p, row_dy, l, true);
                     r = *reinterpret_cast<const float *>(aux + 8);
                     if (from_x) {
-                        raw_x = load_row<T, L, true>(p, row_dy + 256, l, true);
+                        raw_x = load_row<T, G, L, A>(p, row_dy + 256, l, true);
                     } else {
-                        const unsigned char *row_code = from + kStepDy<T> + sub * 8 * G;
-                        if (L == kRun && 8 * l < p.dim) {
-                            code = *reinterpret_cast<const uint2 *>(row_code + 8 * l);
-                            b0 = aux[g0];
-                        } else if (L == kSplit && 4 * l < p.half) {
-                            code.x = *reinterpret_cast<const uint32_t *>(row_code + 4 * l);
-                            code.y = *reinterpret_cast<const uint32_t *>(row_code + p.half + 4 * l);
-                            b0 = aux[g0], b1 = aux[g1];
+                        const unsigned char *row_code =
+                            from + kStepDy<T> + sub * 8 * G + first_of<L>(l);
+                        if (L == kSplit) {
+                            code.x = *reinterpret_cast<const uint32_t *>(row_code);
+                            code.y = *reinterpret_cast<const uint32_t *>(row_code + 4 * G);
+                            b0 = aux[l / 8], b1 = aux[G / 8 + l / 8];
+                        } else if (8 * l < dim_of<G, A>(p)) {
+                            code = *reinterpret_cast<const uint2 *>(row_code);
+                            b0 = aux[l / 4];
                         }
                     }
                     at_slot = at_slot + 1 == kSteps ? 0 : at_slot + 1;
                     start();
                 } else {
                     const bool live = h + sub < h1 && !at.padding;
-                    raw = load_row<T, L, false>(p, dy, l, live);
-                    if (from_x) raw_x = load_row<T, L, false>(p, x, l, live);
+                    raw = load_row<T, G, L, A>(p, dy, l, live);
+                    if (from_x) raw_x = load_row<T, G, L, A>(p, x, l, live);
                     if (live) {
                         r = *rstd;
                         if (!from_x && 8 * l < p.dim) {
-                            code = *reinterpret_cast<const uint2 *>(codes + 8 * l);
-                            b0 = scales[g0];
+                            code = *reinterpret_cast<const uint2 *>(codes);
+                            b0 = *scales;
                         }
                     }
                     dy += R * p.a[k].head, x += R * p.x[k].head;
-                    codes += R * p.pitch, scales += R * p.spitch, rstd += R;
+                    codes += R * pitch, scales += R * spitch, rstd += R;
                 }
                 r *= outside;
                 const Eight v = pairs_of(to_float(raw));
@@ -570,8 +593,7 @@ __global__ void __launch_bounds__(kQkThreads, 2)
                 Eight o;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o.v[i] = fma2(n.v[i], t, mul2(hw.v[i], both(r)));
-                store_row<T, L, ALIGNED>(p, dx, l, h + sub < h1,
-                                         from_float<T>(values_of(o)));
+                store_row<T, G, L, A>(p, dx, l, h + sub < h1, from_float<T>(values_of(o)));
                 dx += R * p.b[k].head;
             }
         }
@@ -585,9 +607,8 @@ __global__ void __launch_bounds__(kQkThreads, 2)
             float v = f.v[e];
 #pragma unroll
             for (int o = G; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-            const int i = element<L>(p, l, e);
-            if (sub == 0 && i < p.dim && (L == kRun || 4 * l < p.half))
-                sum[warp * kQkMaxDim + i] = v;
+            const int i = element<G, L>(l, e);
+            if (sub == 0 && i < dim_of<G, A>(p)) sum[warp * kQkMaxDim + i] = v;
         }
         __syncthreads();
         for (int i = threadIdx.x; i < p.dim; i += kQkThreads) {
@@ -691,28 +712,28 @@ static QkParams make_params(const pos_qk *q) {
 // ten lanes cost what that gains: 63 us either way for 4096 tokens of 72.)
 static int lanes_per_head(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
 
-// The kernel for a call: layout, lanes of a head, loads.
-template <typename T, template <typename, int, int, bool> class Kernel, int G>
+// The kernel for a call: lanes of a head, layout, loads.
+template <typename T, template <typename, int, int, int> class Kernel, int G>
 static auto pick_layout(const QkParams &p, bool aligned) {
-    const bool split = p.pairing == POS_ROT_HALF && 2 * p.half == p.dim && p.dim % 64 == 0;
-    return !aligned ? Kernel<T, G, kRun, false>::fn()
-           : split  ? Kernel<T, G, kSplit, true>::fn()
-                    : Kernel<T, G, kRun, true>::fn();
+    if (!aligned) return Kernel<T, G, kRun, kAny>::fn();
+    if (p.dim != 8 * G) return Kernel<T, G, kRun, kAligned>::fn();
+    return p.pairing == POS_ROT_HALF && 2 * p.half == p.dim ? Kernel<T, G, kSplit, kFull>::fn()
+                                                            : Kernel<T, G, kRun, kFull>::fn();
 }
-template <typename T, template <typename, int, int, bool> class Kernel>
+template <typename T, template <typename, int, int, int> class Kernel>
 static auto pick(const QkParams &p, bool aligned) {
     const int g = lanes_per_head(p.dim);
     return g == 8    ? pick_layout<T, Kernel, 8>(p, aligned)
            : g == 16 ? pick_layout<T, Kernel, 16>(p, aligned)
                      : pick_layout<T, Kernel, 32>(p, aligned);
 }
-template <typename T, int G, int L, bool ALIGNED>
+template <typename T, int G, int L, int A>
 struct Forward {
-    static auto fn() { return qk_forward_kernel<T, G, L, ALIGNED>; }
+    static auto fn() { return qk_forward_kernel<T, G, L, A>; }
 };
-template <typename T, int G, int L, bool ALIGNED>
+template <typename T, int G, int L, int A>
 struct Backward {
-    static auto fn() { return qk_backward_kernel<T, G, L, ALIGNED>; }
+    static auto fn() { return qk_backward_kernel<T, G, L, A>; }
 };
 
 // Cuts a token's heads into tasks: as few as keep `warps` warps busy (each
