@@ -741,25 +741,30 @@ static pos_status launch_wgrad(const uint8_t *ckpt, const void *dy, int64_t ld_d
 
 // Tiles and cuts along the rows.  Full rounds of tiles take all rows each; the
 // tiles of the last round are cut where that ends sooner, and where there are
-// few tiles they are narrower.  In units of a stage of 256 columns (64 rows,
-// 0.4 us): a stage of fewer is bound by decoding; a tile's sums leave the SM
-// at 32 bytes a cycle, which the last one of all shows; joining parts takes a
-// launch (8 units) and reads each of them.
+// few tiles they are narrower.  In units of a stage (64 rows of a tile, 0.37 us,
+// hardly less for a narrow tile, whose decoding is the same): a tile's sums
+// leave the SM at 32 bytes a cycle, which the last one of all shows, or every
+// one where there are few rows; joining takes a launch and writes and reads each
+// part.  The best of all tiles and up to 24 parts, and the chosen: 8192 x 512 x 512
+// 14.7 and 15.2 us, 4000 x 256 x 512 11.4 and 11.4, 4096 x 6144 x 4096 139.0 and
+// 139.5, 512 x 1024 x 1024 8.2 and 8.7.
 static void cut(WgradParams &p, int pairs) {
     const int64_t stages = (p.rows + kTileK - 1) / kTileK;
     double best = 1e300;
     for (int tn = kTileN; tn >= 64; tn /= 2) {
-        const double stage = tn == 256 ? 1. : tn == 128 ? 0.75 : 0.7, drain = 5. * tn / 256;
+        const double stage = tn == 256 ? 1. : tn == 128 ? 0.97 : 0.95, drain = 5.5 * tn / 256;
         const int64_t n_tiles = (p.n + tn - 1) / tn, tiles = p.tiles_m * n_tiles;
         if (tn < kTileN && tiles > 4 * pairs) break;
         const int64_t whole = tiles / pairs * pairs, rest = tiles - whole;
-        const double base = (double)(tiles / pairs) * stages * stage + drain;
+        const double round = std::max(stages * stage, drain) + 1.;
+        const double base = (double)(tiles / pairs) * round + drain;
         for (int64_t s = 1; s == 1 || (s <= stages && rest * s <= 3 * pairs && rest > 0); ++s) {
             const int64_t each = (stages + s - 1) / s;
             if ((s - 1) * each >= stages) continue;  // the last part would be empty
-            const double last = (double)((rest * s + pairs - 1) / pairs) * (each * stage + 1.);
-            const double t =
-                base + last + (s > 1 ? 8. + 0.8 * tn / 256 * (double)(rest * s) / pairs : 0.);
+            const double last =
+                (double)((rest * s + pairs - 1) / pairs) * (std::max(each * stage, drain) + 1.);
+            const double join = 8. + 0.17 * (0.5 + 0.5 * tn / 256) * (double)(rest * s);
+            const double t = base + last + (s > 1 ? join : 0.);
             if (t >= best) continue;
             best = t;
             p.tile_n = tn;
