@@ -208,22 +208,29 @@ static pos_status pack_or_unpack(bool pack, const void *x, int32_t dtype, int64_
 extern "C" {
 
 pos_status poseidon_ckpt_bytes(int64_t rows, int64_t cols, int64_t *bytes) {
-    if (!bytes) return pos::fail(POS_EINVAL, "checkpoint: NULL pointer");
-    if (!pos::ckpt_size_ok(rows, cols)) return pos::fail(POS_EINVAL, "checkpoint: bad rows or cols");
-    const pos::CkptShape s = pos::ckpt_shape(cols);
-    *bytes = rows * (s.pitch + s.spitch);
-    return POS_OK;
+    return pos::guarded([&] {
+        if (!bytes) return pos::fail(POS_EINVAL, "checkpoint: NULL pointer");
+        if (!pos::ckpt_size_ok(rows, cols))
+            return pos::fail(POS_EINVAL, "checkpoint: bad rows or cols");
+        const pos::CkptShape s = pos::ckpt_shape(cols);
+        *bytes = rows * (s.pitch + s.spitch);
+        return (pos_status)POS_OK;
+    });
 }
 
 pos_status poseidon_ckpt_pack(const void *d_x, int32_t dtype, int64_t rows, int64_t cols,
                               int64_t ldx, int32_t format, void *d_ckpt, void *stream) {
-    return pos::pack_or_unpack(true, d_x, dtype, rows, cols, ldx, format, d_ckpt, stream);
+    return pos::guarded([&] {
+        return pos::pack_or_unpack(true, d_x, dtype, rows, cols, ldx, format, d_ckpt, stream);
+    });
 }
 
 pos_status poseidon_ckpt_unpack(const void *d_ckpt, int32_t format, int64_t rows, int64_t cols,
                                 void *d_y, int32_t dtype, int64_t ldy, void *stream) {
-    return pos::pack_or_unpack(false, d_y, dtype, rows, cols, ldy, format,
-                               const_cast<void *>(d_ckpt), stream);
+    return pos::guarded([&] {
+        return pos::pack_or_unpack(false, d_y, dtype, rows, cols, ldy, format,
+                                   const_cast<void *>(d_ckpt), stream);
+    });
 }
 
 }  // extern "C"

@@ -354,6 +354,15 @@ inline bool ckpt_size_ok(int64_t rows, int64_t cols) {
     const CkptShape s = ckpt_shape(cols);
     return s.pitch == 0 || rows < (1ll << 62) / (s.pitch + s.spitch);
 }
+// Runs an entry point's work: no C++ exception leaves the library.
+template <typename F>
+pos_status guarded(F work) noexcept {
+    try {
+        return work();
+    } catch (...) {  // only allocations of host memory throw here
+        return POS_ENOMEM;
+    }
+}
 inline bool dtype_ok(int32_t d) { return d == POS_BF16 || d == POS_F16 || d == POS_F32; }
 inline bool format_ok(int32_t f) { return f == POS_CKPT_INT8 || f == POS_CKPT_E4M3; }
 inline int dtype_size(int32_t d) { return d == POS_F32 ? 4 : 2; }

@@ -620,26 +620,29 @@ __global__ void __launch_bounds__(kQkThreads, 2)
     }
 }
 
-// dw = dw_in + the blocks' partial sums: a block takes 32 columns, each of its
-// 32 warps a strided share of the partial sums.
-__global__ void __launch_bounds__(1024) qk_dw_kernel(const float *part, int n_part, int cols,
-                                                     const float *dw_in, float *dw) {
+// dw = dw_in + the blocks' partial sums: a block takes 8 columns, 32 threads a
+// column a strided share of the partial sums each.  Small blocks find room
+// beside the last ones of the kernel before.
+constexpr int kDwCols = 8, kDwThreads = 32 * kDwCols;
+__global__ void __launch_bounds__(kDwThreads) qk_dw_kernel(const float *part, int n_part, int cols,
+                                                           const float *dw_in, float *dw) {
     grid_dep_wait();
     grid_dep_trigger();
-    __shared__ float sum[32][33];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int i = blockIdx.x * 32 + lane;
+    __shared__ float sum[kDwThreads / 32][kDwCols];
+    const int c = threadIdx.x % kDwCols, i = blockIdx.x * kDwCols + c;
     float v = 0.f;
     if (i < cols)
-#pragma unroll 4
-        for (int b = warp; b < n_part; b += 32) v += part[b * (int64_t)cols + i];
-    sum[warp][lane] = v;
+#pragma unroll 5
+        for (int b = threadIdx.x / kDwCols; b < n_part; b += 32) v += part[b * (int64_t)cols + i];
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+    if (threadIdx.x % 32 < kDwCols) sum[threadIdx.x / 32][c] = v;
     __syncthreads();
-    v = sum[lane][warp];
+    if (threadIdx.x >= kDwCols || i >= cols) return;
+    v = 0.f;
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-    const int j = blockIdx.x * 32 + warp;
-    if (lane == 0 && j < cols) dw[j] = dw_in ? dw_in[j] + v : v;
+    for (int q = 0; q < kDwThreads / 32; ++q) v += sum[q][c];
+    dw[i] = dw_in ? dw_in[i] + v : v;
 }
 
 // ---------------------------------------------------------------------------
@@ -736,11 +739,14 @@ struct Backward {
     static auto fn() { return qk_backward_kernel<T, G, L, A>; }
 };
 
-// Cuts a token's heads into tasks: as few as keep `warps` warps busy (each
-// reads the token's cosines and sines again), at least 32 / G heads a task.
+// Cuts a token's heads into tasks: as few as give `warps` of them (each reads the
+// token's cosines and sines again), at least 32 / G heads a task.  One and a half
+// times what the GPU holds at once: 3001 tokens of 24 heads of 80 take 15.3 us,
+// with once 16.8; 4096 of 72 heads of 128 39.3, with twice 39.6.
 static void cut_tasks(QkParams &p, int64_t warps) {
     const int R = 32 / lanes_per_head(p.dim);
-    const int64_t want = p.tokens ? (warps + p.tokens - 1) / p.tokens : 1;
+    const int64_t least = p.tokens * ((p.heads[0] > 0) + (p.heads[1] > 0));
+    const int64_t want = least ? (warps + least - 1) / least : 1;
     for (int k = 0; k < 2; ++k) {
         const int most = std::max(1, (p.heads[k] + R - 1) / R);
         const int n = (int)std::max<int64_t>(1, std::min<int64_t>(want, most));
@@ -763,7 +769,7 @@ static int grid_of(const QkParams &p, int per_sm) {
 
 template <typename T>
 static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
-    cut_tasks(p, (int64_t)sm_count() * 32);
+    cut_tasks(p, (int64_t)sm_count() * 48);
     const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
     POS_CUDA(launch_dependent(pick<T, Forward>(p, aligned), (int)grid, kQkThreads, 0, s, p));
@@ -791,7 +797,8 @@ static pos_status backward_of(QkParams &p, bool aligned, const float *dw_in, flo
     }
     cudaError_t e = grid > 0 ? launch_dependent(kern, grid, kQkThreads, smem, s, p) : cudaSuccess;
     if (dw && e == cudaSuccess)
-        e = launch_dependent(qk_dw_kernel, (cols + 31) / 32, 1024, 0, s, (const float *)p.part,
+        e = launch_dependent(qk_dw_kernel, (cols + kDwCols - 1) / kDwCols, kDwThreads, 0, s,
+                             (const float *)p.part,
                              grid, cols, dw_in, dw);
     const cudaError_t e2 = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
     if (e == cudaSuccess) e = e2;
@@ -817,24 +824,26 @@ pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_h
                                float *rstd_q, float *rstd_k, void *ckpt_q, void *ckpt_k,
                                void *stream) {
     using namespace pos;
-    POS_TRY(check_qk(qk));
-    POS_TRY(check_heads(qk, x, "x", false));
-    POS_TRY(check_heads(qk, y, "y", true));
-    QkParams p = make_params(qk);
-    POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
-    if (p.tokens == 0 || p.heads[0] + p.heads[1] == 0) return POS_OK;
-    for (int k = 0; k < 2; ++k) {
-        p.a[k] = {x[k].data, x[k].token_stride, x[k].head_stride};
-        p.b[k] = {y[k].data, y[k].token_stride, y[k].head_stride};
-    }
-    p.rstd[0] = rstd_q, p.rstd[1] = rstd_k;
-    const bool aligned = heads_aligned(qk, x) && heads_aligned(qk, y);
-    const auto s = static_cast<cudaStream_t>(stream);
-    switch (qk->dtype) {
-        case POS_BF16: return forward_of<__nv_bfloat16>(p, aligned, s);
-        case POS_F16: return forward_of<__half>(p, aligned, s);
-        default: return forward_of<float>(p, aligned, s);
-    }
+    return guarded([&]() -> pos_status {
+        POS_TRY(check_qk(qk));
+        POS_TRY(check_heads(qk, x, "x", false));
+        POS_TRY(check_heads(qk, y, "y", true));
+        QkParams p = make_params(qk);
+        POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
+        if (p.tokens == 0 || p.heads[0] + p.heads[1] == 0) return POS_OK;
+        for (int k = 0; k < 2; ++k) {
+            p.a[k] = {x[k].data, x[k].token_stride, x[k].head_stride};
+            p.b[k] = {y[k].data, y[k].token_stride, y[k].head_stride};
+        }
+        p.rstd[0] = rstd_q, p.rstd[1] = rstd_k;
+        const bool aligned = heads_aligned(qk, x) && heads_aligned(qk, y);
+        const auto s = static_cast<cudaStream_t>(stream);
+        switch (qk->dtype) {
+            case POS_BF16: return forward_of<__nv_bfloat16>(p, aligned, s);
+            case POS_F16: return forward_of<__half>(p, aligned, s);
+            default: return forward_of<float>(p, aligned, s);
+        }
+    });
 }
 
 pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void *ckpt_q,
@@ -842,30 +851,32 @@ pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void
                                 const pos_heads *dy, const pos_heads *dx, const float *d_dw_in,
                                 float *d_dw, void *stream) {
     using namespace pos;
-    POS_TRY(check_qk(qk));
-    if (x) POS_TRY(check_heads(qk, x, "x", false));
-    POS_TRY(check_heads(qk, dy, "dy", false));
-    POS_TRY(check_heads(qk, dx, "dx", true));
-    QkParams p = make_params(qk);
-    POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
-    if (d_dw_in && !d_dw) return fail(POS_EINVAL, "q/k: dw_in without dw");
-    p.rstd[0] = const_cast<float *>(rstd_q), p.rstd[1] = const_cast<float *>(rstd_k);
-    for (int k = 0; k < 2; ++k) {
-        p.a[k] = {dy[k].data, dy[k].token_stride, dy[k].head_stride};
-        p.b[k] = {dx[k].data, dx[k].token_stride, dx[k].head_stride};
-        if (x) p.x[k] = {x[k].data, x[k].token_stride, x[k].head_stride};
-        if (p.tokens == 0 || p.heads[k] == 0) continue;
-        if (!x && !p.codes[k]) return fail(POS_EINVAL, "q/k: neither x nor its checkpoint");
-        if (!p.rstd[k]) return fail(POS_EINVAL, "q/k: NULL rstd");
-    }
-    const bool aligned =
-        heads_aligned(qk, dy) && heads_aligned(qk, dx) && (!x || heads_aligned(qk, x));
-    const auto s = static_cast<cudaStream_t>(stream);
-    switch (qk->dtype) {
-        case POS_BF16: return backward_of<__nv_bfloat16>(p, aligned, d_dw_in, d_dw, s);
-        case POS_F16: return backward_of<__half>(p, aligned, d_dw_in, d_dw, s);
-        default: return backward_of<float>(p, aligned, d_dw_in, d_dw, s);
-    }
+    return guarded([&]() -> pos_status {
+        POS_TRY(check_qk(qk));
+        if (x) POS_TRY(check_heads(qk, x, "x", false));
+        POS_TRY(check_heads(qk, dy, "dy", false));
+        POS_TRY(check_heads(qk, dx, "dx", true));
+        QkParams p = make_params(qk);
+        POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
+        if (d_dw_in && !d_dw) return fail(POS_EINVAL, "q/k: dw_in without dw");
+        p.rstd[0] = const_cast<float *>(rstd_q), p.rstd[1] = const_cast<float *>(rstd_k);
+        for (int k = 0; k < 2; ++k) {
+            p.a[k] = {dy[k].data, dy[k].token_stride, dy[k].head_stride};
+            p.b[k] = {dx[k].data, dx[k].token_stride, dx[k].head_stride};
+            if (x) p.x[k] = {x[k].data, x[k].token_stride, x[k].head_stride};
+            if (p.tokens == 0 || p.heads[k] == 0) continue;
+            if (!x && !p.codes[k]) return fail(POS_EINVAL, "q/k: neither x nor its checkpoint");
+            if (!p.rstd[k]) return fail(POS_EINVAL, "q/k: NULL rstd");
+        }
+        const bool aligned =
+            heads_aligned(qk, dy) && heads_aligned(qk, dx) && (!x || heads_aligned(qk, x));
+        const auto s = static_cast<cudaStream_t>(stream);
+        switch (qk->dtype) {
+            case POS_BF16: return backward_of<__nv_bfloat16>(p, aligned, d_dw_in, d_dw, s);
+            case POS_F16: return backward_of<__half>(p, aligned, d_dw_in, d_dw, s);
+            default: return backward_of<float>(p, aligned, d_dw_in, d_dw, s);
+        }
+    });
 }
 
 }  // extern "C"

@@ -843,21 +843,23 @@ extern "C" pos_status poseidon_ckpt_wgrad(const void *d_ckpt, int32_t format, co
                                           int64_t cols, const float *d_dw_in, float *d_dw_out,
                                           int64_t ld_dw, void *stream) {
     using namespace pos;
-    if (!ckpt_size_ok(rows, cols) || n < 0 || rows >= (1ll << 31) - kTileK ||
-        n >= (1ll << 31) - kTileN || cols >= (1ll << 31) - kTileM)
-        return fail(POS_EINVAL, "wgrad: bad rows, n or cols");
-    if (dtype != POS_BF16 && dtype != POS_F16)
-        return fail(POS_EINVAL, "wgrad: dy must be bf16 or f16");
-    if (!format_ok(format)) return fail(POS_EINVAL, "wgrad: unknown format");
-    if (ld_dy < 0 || ld_dw < 0 || ld_dy >= (1ll << 38) || ld_dw >= (1ll << 31) || ld_dw < cols)
-        return fail(POS_EINVAL, "wgrad: bad row stride");
-    if (n == 0 || cols == 0) return POS_OK;
-    if (!d_dw_out || (rows > 0 && (!d_ckpt || !d_dy)))
-        return fail(POS_EINVAL, "wgrad: NULL pointer");
-    if (!aligned16(d_ckpt)) return fail(POS_EINVAL, "wgrad: checkpoint not 16-byte aligned");
-    if (reinterpret_cast<uintptr_t>(d_dy) % 2 || reinterpret_cast<uintptr_t>(d_dw_in) % 4 ||
-        reinterpret_cast<uintptr_t>(d_dw_out) % 4)
-        return fail(POS_EINVAL, "wgrad: matrix not aligned to its elements");
-    return wgrad(static_cast<const uint8_t *>(d_ckpt), format, d_dy, dtype, ld_dy, rows, n, cols,
-                 d_dw_in, d_dw_out, ld_dw, static_cast<cudaStream_t>(stream));
+    return guarded([&]() -> pos_status {
+        if (!ckpt_size_ok(rows, cols) || n < 0 || rows >= (1ll << 31) - kTileK ||
+            n >= (1ll << 31) - kTileN || cols >= (1ll << 31) - kTileM)
+            return fail(POS_EINVAL, "wgrad: bad rows, n or cols");
+        if (dtype != POS_BF16 && dtype != POS_F16)
+            return fail(POS_EINVAL, "wgrad: dy must be bf16 or f16");
+        if (!format_ok(format)) return fail(POS_EINVAL, "wgrad: unknown format");
+        if (ld_dy < 0 || ld_dw < 0 || ld_dy >= (1ll << 38) || ld_dw >= (1ll << 31) || ld_dw < cols)
+            return fail(POS_EINVAL, "wgrad: bad row stride");
+        if (n == 0 || cols == 0) return POS_OK;
+        if (!d_dw_out || (rows > 0 && (!d_ckpt || !d_dy)))
+            return fail(POS_EINVAL, "wgrad: NULL pointer");
+        if (!aligned16(d_ckpt)) return fail(POS_EINVAL, "wgrad: checkpoint not 16-byte aligned");
+        if (reinterpret_cast<uintptr_t>(d_dy) % 2 || reinterpret_cast<uintptr_t>(d_dw_in) % 4 ||
+            reinterpret_cast<uintptr_t>(d_dw_out) % 4)
+            return fail(POS_EINVAL, "wgrad: matrix not aligned to its elements");
+        return wgrad(static_cast<const uint8_t *>(d_ckpt), format, d_dy, dtype, ld_dy, rows, n, cols,
+                     d_dw_in, d_dw_out, ld_dw, static_cast<cudaStream_t>(stream));
+    });
 }
