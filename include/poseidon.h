@@ -15,8 +15,8 @@
  *  - every call returns a pos_status; no C++ exception crosses the ABI;
  *    poseidon_last_error() describes the last failure of the calling thread;
  *  - the caller owns every buffer it passes; the library copies what it keeps;
- *  - costs are int32 microseconds, memory int64 bytes; all arithmetic is
- *    integer, so results are exact and reproducible;
+ *  - costs are int32 microseconds, memory int64 bytes; the planner's
+ *    arithmetic is integer, so its results are exact and reproducible;
  *  - class k = type * n_tp + tp_idx indexes every per-class table.
  */
 #ifndef POSEIDON_H
