@@ -742,7 +742,10 @@ struct Backward {
 // Cuts a token's heads into tasks: as few as give `warps` of them (each reads the
 // token's cosines and sines again), at least 32 / G heads a task.  One and a half
 // times what the GPU holds at once: 3001 tokens of 24 heads of 80 take 15.3 us,
-// with once 16.8; 4096 of 72 heads of 128 39.3, with twice 39.6.
+// with once 16.8; 4096 of 72 heads of 128 39.0, with twice 39.6.  Three times in f32,
+// whose tasks are longer, so that the last round leaves more of the GPU idle: 4096
+// tokens of 72 heads of 128 take 59.0 us, with one and a half 66.5; of 256 115.7 and
+// 133.8; 5000 of 128 69.8 and 74.2.  (Three times in bf16 is slower: 39.6.)
 static void cut_tasks(QkParams &p, int64_t warps) {
     const int R = 32 / lanes_per_head(p.dim);
     const int64_t least = p.tokens * ((p.heads[0] > 0) + (p.heads[1] > 0));
@@ -769,7 +772,7 @@ static int grid_of(const QkParams &p, int per_sm) {
 
 template <typename T>
 static pos_status forward_of(QkParams &p, bool aligned, cudaStream_t s) {
-    cut_tasks(p, (int64_t)sm_count() * 48);
+    cut_tasks(p, (int64_t)sm_count() * (sizeof(T) == 4 ? 96 : 48));
     const int64_t grid = (p.tasks[0] + p.tasks[1] + kQkWarps - 1) / kQkWarps;
     if (grid > 0x7fffffffll) return fail(POS_EINVAL, "q/k: too many tokens");
     POS_CUDA(launch_dependent(pick<T, Forward>(p, aligned), (int)grid, kQkThreads, 0, s, p));
