@@ -42,8 +42,9 @@ struct Eight {
 };
 
 // How a kernel reads heads: kAny one element at a time, kAligned 16 bytes at a
-// time, kFull likewise heads of exactly 8 G elements, G lanes a head, so that
-// sizes and offsets are constants.
+// time (dim is a multiple of 8: a lane has 8 elements or none), kFull likewise
+// heads of exactly 8 G elements, G lanes a head, so that sizes and offsets are
+// constants.
 enum Loads { kAny, kAligned, kFull };
 template <int G, int A>
 __device__ __forceinline__ int dim_of(const QkParams &p) {
@@ -80,13 +81,13 @@ __device__ __forceinline__ int element(int l, int e) {
 // The words of a thread's elements, the first of them at `at`.
 template <typename T, int G, int L, int A>
 __device__ __forceinline__ Raw8<T> load_row(const QkParams &p, const T *at, int l, bool live) {
-    if constexpr (A != kFull) {
-        return load8<A == kAligned>(at, live ? p.dim - 8 * l : 0);
+    if constexpr (A == kAny) {
+        return load8<false>(at, live ? p.dim - 8 * l : 0);
     } else {
         Raw8<T> r;
         zero_raw(r.a);
         if constexpr (sizeof(T) == 4) zero_raw(r.b);
-        if (live) {
+        if (live && 8 * l < dim_of<G, A>(p)) {
             if constexpr (sizeof(T) == 4) {
                 r.a = *reinterpret_cast<const uint4 *>(at);
                 r.b = *reinterpret_cast<const uint4 *>(at + (L == kSplit ? 4 * G : 4));
@@ -104,9 +105,9 @@ __device__ __forceinline__ Raw8<T> load_row(const QkParams &p, const T *at, int 
 template <typename T, int G, int L, int A>
 __device__ __forceinline__ void store_row(const QkParams &p, T *at, int l, bool live,
                                           const Raw8<T> &r) {
-    if constexpr (A != kFull) {
-        store8<A == kAligned>(at, r, live ? p.dim - 8 * l : 0);
-    } else if (live) {
+    if constexpr (A == kAny) {
+        store8<false>(at, r, live ? p.dim - 8 * l : 0);
+    } else if (live && 8 * l < dim_of<G, A>(p)) {
         if constexpr (sizeof(T) == 4) {
             *reinterpret_cast<uint4 *>(at) = r.a;
             *reinterpret_cast<uint4 *>(at + (L == kSplit ? 4 * G : 4)) = r.b;
@@ -710,9 +711,8 @@ static QkParams make_params(const pos_qk *q) {
     return p;
 }
 
-// Lanes of a head: 8 elements a lane, a power of two.  (With as many lanes as a
-// head of 80 needs, ten, three heads fit a warp instead of two, but sums over
-// ten lanes cost what that gains: 63 us either way for 4096 tokens of 72.)
+// Lanes of a head: 8 elements a lane, a power of two, so that sums over a head are
+// four shuffles in place; 10 of 16 hold a head of 80, the others are idle.
 static int lanes_per_head(int dim) { return dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
 
 // The kernel for a call: lanes of a head, layout, loads.
@@ -741,11 +741,11 @@ struct Backward {
 
 // Cuts a token's heads into tasks: as few as give `warps` of them (each reads the
 // token's cosines and sines again), at least 32 / G heads a task.  One and a half
-// times what the GPU holds at once: 3001 tokens of 24 heads of 80 take 15.3 us,
-// with once 16.8; 4096 of 72 heads of 128 39.0, with twice 39.6.  Three times in f32,
-// whose tasks are longer, so that the last round leaves more of the GPU idle: 4096
-// tokens of 72 heads of 128 take 59.0 us, with one and a half 66.5; of 256 115.7 and
-// 133.8; 5000 of 128 69.8 and 74.2.  (Three times in bf16 is slower: 39.6.)
+// times what the GPU holds at once: 1000 tokens of 72 heads of 128 take 10.1 us,
+// with once 12.1; 4096 of them 39.0, with twice 39.5.  Three times in f32, whose
+// tasks are longer, so that the last round leaves more of the GPU idle: 4096 tokens
+// of 72 heads of 128 take 59.0 us, with one and a half 66.5; of 256 115.7 and 133.8;
+// 5000 of 128 69.8 and 74.2.
 static void cut_tasks(QkParams &p, int64_t warps) {
     const int R = 32 / lanes_per_head(p.dim);
     const int64_t least = p.tokens * ((p.heads[0] > 0) + (p.heads[1] > 0));
