@@ -527,7 +527,8 @@ typedef struct pos_heads {
  * (the same pointers and strides).  rstd_q, rstd_k ([tokens][heads], float)
  * and ckpt_q, ckpt_k (16-byte aligned checkpoints of x as a matrix
  * [tokens * heads][dim]) are what the backward pass reads; each may be NULL.
- * Errors: POS_EINVAL, POS_ECUDA.
+ * Errors: POS_EINVAL (NULL, sizes, strides, rows of y that overlap, dtype,
+ * pairing, format, a pointer off its elements), POS_ECUDA.
  */
 pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_heads *y,
                                float *rstd_q, float *rstd_k, void *ckpt_q, void *ckpt_k,
@@ -542,7 +543,8 @@ pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_h
  * is NULL for zeros or may be d_dw itself.  The sums' order depends on the
  * sizes and the GPU alone.  Scratch from the library's pool: 8 * dim bytes for
  * each block of the grid (at most 8 per SM) when d_dw is not NULL.
- * Errors: POS_EINVAL, POS_ENOMEM, POS_ECUDA.
+ * Errors: POS_EINVAL (as above; neither x nor checkpoints, d_dw_in without
+ * d_dw), POS_ENOMEM, POS_ECUDA.
  */
 pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void *ckpt_q,
                                 const void *ckpt_k, const float *rstd_q, const float *rstd_k,

@@ -662,6 +662,8 @@ __global__ void __launch_bounds__(kDwThreads) qk_dw_kernel(const float *part, in
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+static bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
 static pos_status check_qk(const pos_qk *q) {
     if (!q) return fail(POS_EINVAL, "q/k: NULL pointer");
     if (q->tokens < 0 || q->heads_q < 0 || q->heads_k < 0 || q->tokens >= (1ll << 40) ||
@@ -678,7 +680,26 @@ static pos_status check_qk(const pos_qk *q) {
     if (q->n_pos < 0) return fail(POS_EINVAL, "q/k: n_pos must be >= 0");
     if (q->rot > 0 && q->n_pos > 0 && (!q->cos || !q->sin))
         return fail(POS_EINVAL, "q/k: NULL tables");
+    if (!aligned4(q->w_q) || !aligned4(q->w_k) || !aligned4(q->cos) || !aligned4(q->sin) ||
+        !aligned4(q->positions))
+        return fail(POS_EINVAL, "q/k: misaligned weights, tables or positions");
     return POS_OK;
+}
+
+// Whether two rows of a tensor share an element.
+static bool rows_overlap(int64_t tokens, int64_t heads, int64_t dim, int64_t token_stride,
+                         int64_t head_stride) {
+    if ((heads > 1 && head_stride < dim) || (tokens > 1 && token_stride < dim)) return true;
+    if (heads <= 1 || tokens <= 1) return false;
+    // one token's rows before the next token's, or one head's before the next head's
+    if (token_stride >= (heads - 1) * head_stride + dim) return false;
+    if ((head_stride - dim) / token_stride >= tokens - 1) return false;
+    for (int64_t h = 1; h < heads; ++h) {  // against head 0 of the tokens beside it
+        const int64_t at = h * head_stride, t = at / token_stride;
+        if (t > 0 && t < tokens && at - t * token_stride < dim) return true;
+        if (t + 1 < tokens && (t + 1) * token_stride - at < dim) return true;
+    }
+    return false;
 }
 
 // A host array of two tensors; data may be NULL where there is nothing.
@@ -693,8 +714,8 @@ static pos_status check_heads(const pos_qk *q, const pos_heads *t, const char *w
         if (!t[k].data) return fail(POS_EINVAL, std::string("q/k: NULL ") + what);
         if (reinterpret_cast<uintptr_t>(t[k].data) % dtype_size(q->dtype))
             return fail(POS_EINVAL, std::string("q/k: misaligned ") + what);
-        if (written && ((heads > 1 && t[k].head_stride < q->dim) ||
-                        (q->tokens > 1 && t[k].token_stride < q->dim)))
+        if (written &&
+            rows_overlap(q->tokens, heads, q->dim, t[k].token_stride, t[k].head_stride))
             return fail(POS_EINVAL, std::string("q/k: overlapping rows of ") + what);
     }
     return POS_OK;
@@ -844,6 +865,7 @@ pos_status poseidon_qk_forward(const pos_qk *qk, const pos_heads *x, const pos_h
         POS_TRY(check_qk(qk));
         POS_TRY(check_heads(qk, x, "x", false));
         POS_TRY(check_heads(qk, y, "y", true));
+        if (!aligned4(rstd_q) || !aligned4(rstd_k)) return fail(POS_EINVAL, "q/k: misaligned rstd");
         QkParams p = make_params(qk);
         POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
         if (p.tokens == 0 || p.heads[0] + p.heads[1] == 0) return POS_OK;
@@ -874,6 +896,8 @@ pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void
         POS_TRY(check_heads(qk, dx, "dx", true));
         QkParams p = make_params(qk);
         POS_TRY(set_ckpt(p, ckpt_q, ckpt_k));
+        if (!aligned4(rstd_q) || !aligned4(rstd_k)) return fail(POS_EINVAL, "q/k: misaligned rstd");
+        if (!aligned4(d_dw_in) || !aligned4(d_dw)) return fail(POS_EINVAL, "q/k: misaligned dw");
         if (d_dw_in && !d_dw) return fail(POS_EINVAL, "q/k: dw_in without dw");
         p.rstd[0] = const_cast<float *>(rstd_q), p.rstd[1] = const_cast<float *>(rstd_k);
         for (int k = 0; k < 2; ++k) {

@@ -121,6 +121,50 @@ def test_qk_refused(P):
     refused(P, backward(qk(), dx=P.qk_heads(P16, 24, 0, P16, 24, 8)), "overlapping rows of dx")
 
 
+def test_qk_misaligned_refused(P):
+    """Weights, tables, positions, rstd and dw off their elements."""
+    t = P.qk_heads(P16, 24, 8, P16, 24, 8)
+    for name in ("w_q", "w_k", "cos", "sin", "positions"):
+        f = dict(tokens=2, heads_q=2, heads_k=1, dim=8, rot=8, pairing=0, dtype=0, format=0,
+                 eps=1e-6, w_q=P16, w_k=P16, cos=P16, sin=P16, n_pos=4, positions=P16)
+        f[name] += 2
+        refused(P, P.lib().poseidon_qk_forward(C.byref(P.pos_qk(*f.values())), t, t, None, None,
+                                               None, None, None), "misaligned weights, tables")
+        f[name] -= 2
+    q = C.byref(P.pos_qk(*f.values()))
+
+    def forward(rq=P16, rk=P16):
+        return P.lib().poseidon_qk_forward(q, t, t, rq, rk, None, None, None)
+
+    def backward(rq=P16, rk=P16, add=P16, dw=P16):
+        return P.lib().poseidon_qk_backward(q, t, None, None, rq, rk, t, t, add, dw, None)
+
+    for call in (forward, backward):
+        refused(P, call(rq=P16 + 2), "misaligned rstd")
+        refused(P, call(rk=ODD), "misaligned rstd")
+    refused(P, backward(add=P16 + 2), "misaligned dw")
+    refused(P, backward(dw=P16 + 2), "misaligned dw")
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_written_rows_that_overlap_are_refused(P, seed):
+    """Against all pairs of rows, for small shapes and strides; the checkpoint that is
+    refused next shows that a tensor whose rows are apart got past."""
+    rng = np.random.default_rng(seed)
+    met = set()
+    for _ in range(400):
+        tokens, heads, dim = (int(v) for v in rng.integers(1, 6, 3))
+        ts, hs = (int(v) for v in rng.integers(0, 24, 2))
+        starts = sorted(i * ts + j * hs for i in range(tokens) for j in range(heads))
+        apart = all(b - a >= dim for a, b in zip(starts, starts[1:]))
+        met.add(apart)
+        q = P.pos_qk(tokens, heads, 0, dim, 0, 0, 0, 0, 1e-6, None, None, None, None, 0, None)
+        t = P.qk_heads(P16, ts, hs, 0, 0, 0)
+        refused(P, P.lib().poseidon_qk_forward(C.byref(q), t, t, None, None, P16 + 8, None, None),
+                "16-byte" if apart else "overlapping rows of y")
+    assert met == {True, False}
+
+
 def test_struct_layouts(P, tmp_path):
     structs = {"pos_qk": P.pos_qk, "pos_heads": P.pos_heads}
     lines = ['#include <stdio.h>', '#include <stddef.h>',
