@@ -179,6 +179,21 @@ def test_against_64_bits(P, T, hq, hk, dim, rot, half, dtype, fmt):
         near(dw, want_dw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim,rot", [(64, 36), (72, 72), (80, 34), (88, 84), (128, 100), (256, 124),
+                                     (192, 190)])
+def test_partners_that_are_not_whole_vectors_apart(P, dtype, dim, rot):
+    """rot / 2 = 18, 36, 17, 42, 50, 62 and 95: partners by pairs or one by one, heads of
+    whole vectors that fill their lanes or leave some idle."""
+    c = Case(P, 21, 9, 2, dim, rot, dtype, "e4m3", seed=rot)
+    near(c.forward(), c.want_forward())
+    for from_x in (False, True):
+        dx, dw = c.backward(from_x)
+        want_dx, want_dw = c.want_backward(from_x)
+        near(dx, want_dx)
+        near(dw, want_dw)
+
+
 @pytest.mark.parametrize("half", [True, False])
 @pytest.mark.parametrize("dim,rot", [(24, 24), (128, 64), (36, 20)])
 def test_gradients_against_differences(P, half, dim, rot):
