@@ -228,6 +228,15 @@ __device__ __forceinline__ void load_angles(const QkParams &p, int64_t at, int l
     }
 }
 
+// x c + partner s for a lane's pair i.  Elements from rot on have no partner term: with a
+// sine of 0 an infinity or NaN of theirs, or in the pair's other half, would still make
+// a NaN.  turning: how many of the lane's pairs lie below rot (any number, <= 0: none).
+template <int L>
+__device__ __forceinline__ F2 turn(F2 x, F2 c, F2 partner, F2 s, int i, int turning) {
+    const F2 y = mul2(x, c);
+    return L == kSplit || i < turning ? fma2(partner, s, y) : y;
+}
+
 // The sum over a head's lanes, in each of them.
 template <int G>
 __device__ __forceinline__ float row_sum(float v) {
@@ -381,6 +390,7 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
         s.v[i] = mul2(s.v[i], w_partner.v[i]);
     }
     const float outside = at.outside ? __uint_as_float(0x7fffffffu) : 1.f;
+    const int turning = p.half - 4 * l;
     for (int h = h0; h < h1; h += R) {
         const bool live = h + sub < h1;
         const Raw8<T> raw = next;
@@ -403,7 +413,7 @@ __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
         Eight o;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            o.v[i] = mul2(fma2(q.v[i], s.v[i], mul2(v.v[i], c.v[i])), both(r * outside));
+            o.v[i] = mul2(turn<L>(v.v[i], c.v[i], q.v[i], s.v[i], i, turning), both(r * outside));
         Raw8<T> out = from_float<T>(values_of(o));
         if (at.padding) {
             zero_raw(out.a);
@@ -474,6 +484,7 @@ __global__ void __launch_bounds__(kQkThreads, 2)
     const int warp = threadIdx.x / 32, l = threadIdx.x % G, sub = threadIdx.x % 32 / G;
     float *row = reinterpret_cast<float *>(rows) + warp * 256;
     const int bytes = p.step_bytes;
+    const int turning = p.half - 4 * l;
     unsigned char *const mine = reinterpret_cast<unsigned char *>(steps) + warp * kSteps * bytes;
     for (int k = 0; k < 2; ++k) {
         const Eight w = load_weights<G, L, A>(p, p.w[k], l);
@@ -610,7 +621,7 @@ __global__ void __launch_bounds__(kQkThreads, 2)
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const F2 gi = fma2(q.v[i], s.v[i], mul2(v.v[i], c.v[i]));
+                    const F2 gi = turn<L>(v.v[i], c.v[i], q.v[i], s.v[i], i, turning);
                     dw.v[i] = fma2(gi, n.v[i], dw.v[i]);
                     hw.v[i] = mul2(gi, w.v[i]);
                 }
