@@ -439,7 +439,7 @@ pos_status launch_decode(const EvalParams &p, cudaStream_t stream) {
 // keeps its memory between calls (release threshold: unlimited), so what is
 // taken from it is bounded: 39 bytes per candidate of a chunk of 2^24, an
 // argmin's partial results, host batches up to kHostPoolBytes, and the layer
-// operators' scratch (poseidon.h).
+// operators' scratch (at most 320 MB a call, see poseidon.h).
 constexpr size_t kHostPoolBytes = 64ull << 20;
 static std::mutex g_pool_mutex;
 static cudaMemPool_t g_pool[64];
