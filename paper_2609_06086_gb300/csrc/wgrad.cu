@@ -838,6 +838,8 @@ static pos_status wgrad_block(const uint8_t *codes, const uint8_t *scales, int32
 // of each kernel and an end with idle SMs: in blocks of 64 MB 8192 x 5121 x 512 takes
 // 99 us instead of 86, 8192 x 4097 x 4096 253 instead of 241.
 constexpr int64_t kCopyBytes = 256ll << 20;
+// Rows of a block: the kernel counts them in 32 bits, up to kChunkRows past the last.
+constexpr int64_t kBlockRows = 1ll << 30;
 static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int32_t dtype,
                         int64_t ld_dy, int64_t rows, int64_t n, int64_t cols, const float *in,
                         float *out, int64_t ld, cudaStream_t s) {
@@ -848,10 +850,11 @@ static pos_status wgrad(const uint8_t *ckpt, int32_t format, const void *dy, int
     }
     const CkptShape shape = ckpt_shape(cols);
     const bool copy = !aligned16(dy) || ld_dy % 8 || ld_dy < n;
-    int64_t n_each = n, rows_each = rows;
+    int64_t n_each = n, rows_each = std::min(rows, kBlockRows);
     if (copy) {
         const int64_t n8 = (n + 7) / 8 * 8;
-        rows_each = std::min(rows, kCopyBytes / (2 * std::min<int64_t>(n8, kTileN)) / kTileK * kTileK);
+        rows_each = std::min(
+            rows_each, kCopyBytes / (2 * std::min<int64_t>(n8, kTileN)) / kTileK * kTileK);
         if (rows_each * n8 * 2 > kCopyBytes) {
             const int64_t most = kCopyBytes / (2 * rows_each) / kTileN * kTileN;
             const int64_t blocks = (n + most - 1) / most;

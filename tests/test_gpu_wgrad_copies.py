@@ -1,5 +1,5 @@
-"""poseidon_ckpt_wgrad where dy has to be copied first, in blocks of at most 256 MB: of
-columns, and of rows where there are many.  Values are whole numbers and sums stay
+"""poseidon_ckpt_wgrad in blocks: where dy has to be copied first, 256 MB at a time, of
+columns, and of rows where there are many; and of the largest row counts.  Values are whole numbers and sums stay
 below 2^24, so that gradients are exact in any order of the sums."""
 import pytest
 
@@ -82,3 +82,32 @@ def test_blocks(P, rows, n, cols):
     same(add[:n, :cols], ckpt, dy, cols, before[:n, :cols])
     for a, b in ((out, torch.full_like(out, 9.0)), (add, before)):  # nothing else is written
         assert torch.equal(a[n:], b[n:]) and torch.equal(a[:, cols:], b[:, cols:])
+
+
+def test_most_rows(P):
+    """The largest row count: all zeros but for rows on either side of the places where
+    sums begin and end.  111 GB: skipped where they are not free."""
+    import torch
+    rows, n, cols = 2 ** 31 - 65, 8, 32
+    pitch, size = U.layout(rows, cols)[1], U.layout(rows, cols)[3]
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 130 << 30:
+        pytest.skip("needs 130 GB of device memory")
+    ckpt = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    dy = torch.zeros(rows, n, dtype=torch.bfloat16, device="cuda")
+    want = torch.zeros(n, cols, dtype=torch.float64)
+    gen = torch.Generator().manual_seed(5)
+    marked = [0, 1, 767, 768, 2 ** 30 - 1, 2 ** 30, 2 ** 30 + 768, 2 ** 31 - 833, 2 ** 31 - 769,
+              2 ** 31 - 768, rows - 64, rows - 1]
+    for r in marked:
+        code = torch.randint(-127, 128, (cols,), dtype=torch.int8, generator=gen)
+        g = torch.randint(-8, 9, (n,), generator=gen).bfloat16()
+        ckpt[r * pitch:(r + 1) * pitch] = code.view(torch.uint8).cuda()
+        ckpt[rows * pitch + 4 * r] = 127
+        dy[r] = g.cuda()
+        want += torch.outer(g.double(), code.double())
+    out = torch.full((n, cols), 5.0, device="cuda")
+    call(P, ckpt, dy, cols, None, out)
+    del ckpt, dy
+    torch.cuda.empty_cache()
+    assert torch.equal(out.double().cpu(), want)
