@@ -130,6 +130,13 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     if (bar_try(bar, parity)) return true;
     return bar_wait_long(bar, parity, gave_up);
 }
+// The same by a whole warp.  Where a wait gives up its lanes may not agree (one sees
+// the phase on its last try, another that the block has given up), and lanes that went
+// on would wait in the warp's next vote for those that left: all go on or none does.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity,
+                                              volatile int *gave_up) {
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+}
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y,
                                          uint32_t bar) {
     asm volatile(
@@ -457,8 +464,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 const int m0 = t.m0 + (int)rank * kHalf;
                 const uint8_t *sc = p.scales + (m0 < p.cols ? m0 / kGroup : 0);
                 for (int r = t.r0; r < t.r1; r += kTileK) {
-                    ok = bar_wait(code_empty + 8 * cs, cph, gave_up);
-                    ok = __all_sync(0xffffffffu, ok);
+                    ok = bar_wait_warp(code_empty + 8 * cs, cph, gave_up);
                     if (!ok) break;
                     if (lane == 0) {
                         bar_expect(code_full + 8 * cs, kCodeBytes);
@@ -499,15 +505,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         int s = mine, cs = mine;
         uint32_t ph = 1, cph = 0;
         int turn = 0;  // of the groups, over all stages
-        bool ok = true;
-        for (int u = pair; u < p.units && ok; u += pairs) {
+        // Lanes may differ in whether a wait gave up; none leaves alone, since the
+        // others would wait for it in the next vote.  One that gave up on its place
+        // among the operands goes on to that vote, and lane 0 then announces nothing:
+        // what it wrote is in sums that are lost (a vote of its own after that wait:
+        // registers spill, 109 us instead of 103 for 4096^3 in f16, e4m3).
+        bool ok = true, going = true;
+        for (int u = pair; u < p.units && going; u += pairs) {
             const Unit t = unit_of(p, u);
             for (int r = t.r0; r < t.r1; r += kTileK) {
                 const bool skip = turn != mine;
                 if (++turn == kDecodeGroups) turn = 0;
                 if (skip) continue;
-                ok = bar_wait(code_full + 8 * cs, cph, gave_up);
-                if (!ok) break;
+                ok = ok && bar_wait(code_full + 8 * cs, cph, gave_up);
                 uint4 c[4];
                 uint32_t byte[4];
 #pragma unroll
@@ -521,10 +531,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                                        h / 2 * (32 * 4)));
                 }
                 const bool all_short = __all_sync(
-                    0xffffffffu, short_way<T, F>((int)byte[0]) && short_way<T, F>((int)byte[1]) &&
-                                     short_way<T, F>((int)byte[2]) && short_way<T, F>((int)byte[3]));
+                    0xffffffffu, ok && short_way<T, F>((int)byte[0]) &&
+                                     short_way<T, F>((int)byte[1]) &&
+                                     short_way<T, F>((int)byte[2]) &&
+                                     short_way<T, F>((int)byte[3]));
+                if (!all_short) {
+                    going = __all_sync(0xffffffffu, ok);
+                    if (!going) break;
+                }
                 ok = bar_wait(empty + 8 * s, ph, gave_up);
-                if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     const uint2 lo = make_uint2(c[h].x, c[h].y), hi = make_uint2(c[h].z, c[h].w);
@@ -548,7 +563,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 // does neither.
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
+                if (lane == 0 && ok) {
                     bar_arrive_cluster(leader_full + 8 * s);
                     bar_arrive(code_empty + 8 * cs);
                 }
@@ -580,8 +595,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
             for (int j = 0; j < 128; ++j, in += p.ld)
                 sum[j] = p.in && t.part < 0 && j < left ? *in : 0.f;
             for (int c = t.r0; c < t.r1; c += kChunkRows) {
-                if (ok) ok = bar_wait(acc_full + 8 * acc, aph, gave_up);
-                ok = __all_sync(0xffffffffu, ok);
+                if (ok) ok = bar_wait_warp(acc_full + 8 * acc, aph, gave_up);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (int j0 = 0; j0 < 128; j0 += 8) {
@@ -597,8 +611,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 acc ^= 1;
                 if (acc == 0) aph ^= 1;
             }
-            // a wait that gave up: no sums
-            const float lost = ok ? 0.f : __uint_as_float(0x7fffffffu);
+            // a wait that gave up, here or in a warp that these sums come from: no sums
+            const float lost = ok && !*gave_up ? 0.f : __uint_as_float(0x7fffffffu);
             if (t.part >= 0) {
                 float *out = p.part + (int64_t)t.part * (kTileM * kTileN) + j1 * kTileM + m;
 #pragma unroll

@@ -1,0 +1,42 @@
+"""The weight gradient kernel's bounded waits.  One that runs out would need a GPU whose
+copies or products never come, so what happens then is looked for in the source."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                    "paper_2609_06086_gb300", "csrc")
+
+
+def kernel():
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "wgrad.cu")).read())
+    body = text[text.index("    wgrad_kernel(const __grid_constant__"):]
+    return text, body[:body.index("\n}\n")]
+
+
+def test_a_warp_gives_up_as_a_whole():
+    """Lanes of a warp may differ in whether a wait gave up, and one that left its loop
+    would be waited for by the others' next vote.  So a wait belongs to a single lane, or
+    it ends in a vote, or (the decoding warps) nothing but a vote's result ends a loop."""
+    text, body = kernel()
+    wait = r"\bbar_wait\("
+    alone = re.findall(r"if \(warp == \d[^{]*lane == 0\) \{(.*?)(?=\n        \} else if)", body,
+                       re.S)
+    assert sum(len(re.findall(wait, a)) for a in alone) == 3
+    decode = body[body.index("group <= kDecodeGroups"):body.index("take_registers<kSumRegs>")]
+    assert len(re.findall(wait, decode)) == 2
+    assert len(re.findall(wait, body)) == 5 and len(re.findall(r"\bbar_wait_warp\(", body)) == 2
+    vote = text[text.index("bool bar_wait_warp("):]
+    assert "__all_sync(0xffffffffu, bar_wait(" in vote[:vote.index("}")]
+    assert re.findall(r"if \(([^;{]*)\) break;", decode) == ["!going"]
+    assert re.findall(r"going = ([^;]*);", decode) == ["true", "__all_sync(0xffffffffu, ok)"]
+    assert re.findall(r"for \(int [ur] [^;]*;([^;]*);", decode) == [" u < p.units && going",
+                                                                  " r < t.r1"]
+
+
+def test_no_sums_of_what_was_given_up():
+    """A decoding warp announces no stage whose place it gave up on, and sums that its
+    stores may have reached are marked."""
+    _, body = kernel()
+    decode = body[body.index("group <= kDecodeGroups"):body.index("take_registers<kSumRegs>")]
+    assert re.search(r"if \(lane == 0 && ok\) \{\s*bar_arrive_cluster\(leader_full", decode)
+    assert "lost = ok && !*gave_up ? 0.f : __uint_as_float(0x7fffffffu)" in body
