@@ -477,7 +477,8 @@ pos_status poseidon_ckpt_unpack(const void *d_ckpt, int32_t format, int64_t rows
  * Scratch from the library's pool (stream-ordered): partial sums where the
  * rows are split, at most 64 MB; when dy is not 16-byte aligned (base and
  * ld_dy) or ld_dy < n, a copy of it, a block of at most 256 MB at a time.
- * A bounded wait that ran out inside the kernel makes the gradients NaN.
+ * Waits inside the kernel are bounded: two seconds, not counting time in which
+ * the GPU ran something else.  One that ran out makes the gradients NaN.
  * Errors: POS_EINVAL (NULL, negative sizes or strides, ld_dw < cols, dtype,
  * format, rows, n or cols of 2^31 or more, alignment), POS_ENOMEM, POS_ECUDA.
  */

@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "layer_ops.cuh"
+#include "wait_limit.h"
 
 namespace pos {
 
@@ -112,15 +113,14 @@ __device__ __forceinline__ uint64_t now_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a phase, two seconds at most; false: it did not come, or another
-// wait of the block has already given up.
-constexpr uint64_t kWaitNs = 2000000000ull;
+// Waits for a phase, two seconds at most (WaitLimit); false: it did not come, or
+// another wait of the block has already given up.
 __device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *gave_up) {
-    const uint64_t t0 = now_ns();
+    WaitLimit limit(now_ns());
     for (;;) {
         if (bar_try(bar, parity)) return true;
         if (*gave_up) return false;
-        if (now_ns() - t0 > kWaitNs) {
+        if (limit.reached(now_ns())) {
             *gave_up = 1;
             return false;
         }

@@ -2,6 +2,7 @@
 copies or products never come, so what happens then is looked for in the source."""
 import os
 import re
+import subprocess
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                     "paper_2609_06086_gb300", "csrc")
@@ -40,3 +41,35 @@ def test_no_sums_of_what_was_given_up():
     decode = body[body.index("group <= kDecodeGroups"):body.index("take_registers<kSumRegs>")]
     assert re.search(r"if \(lane == 0 && ok\) \{\s*bar_arrive_cluster\(leader_full", decode)
     assert "lost = ok && !*gave_up ? 0.f : __uint_as_float(0x7fffffffu)" in body
+
+
+def test_only_a_waits_own_time_counts(tmp_path):
+    """The limit against a clock of the test's: two seconds of tries a millisecond or a
+    microsecond apart run out, and not before; gaps of ten seconds, in which the GPU ran
+    something else, do not use them up."""
+    src = tmp_path / "limit.cpp"
+    src.write_text("""
+#include <cstdio>
+#include "%s"
+// tries until the limit, the clock moving by `step`, at every `every`-th try by `jump`
+static long tries(uint64_t step, long every, uint64_t jump) {
+    uint64_t now = 12345;
+    pos::WaitLimit limit(now);
+    for (long i = 1;; ++i) {
+        now += every && i %% every == 0 ? jump : step;
+        if (limit.reached(now)) return i;
+        if (i > 100000000) return -1;
+    }
+}
+int main() {
+    const uint64_t us = 1000, ms = 1000000, s = 1000000000;
+    std::printf("%%ld %%ld %%ld %%ld\\n", tries(ms, 0, 0), tries(us, 0, 0), tries(ms, 100, 10 * s),
+                tries(10 * s, 0, 0));
+}
+""" % os.path.join(CSRC, "wait_limit.h"))
+    subprocess.run(["g++", "-std=c++17", "-O2", "-o", str(tmp_path / "limit"), str(src)], check=True)
+    out = subprocess.run([str(tmp_path / "limit")], capture_output=True, text=True, check=True).stdout
+    each_ms, each_us, jumps, all_jumps = map(int, out.split())
+    assert each_ms == 2001 and each_us == 2000001
+    assert 1900 <= jumps <= 2000   # 19 gaps of four milliseconds among them
+    assert all_jumps == 501
