@@ -505,19 +505,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
         int s = mine, cs = mine;
         uint32_t ph = 1, cph = 0;
         int turn = 0;  // of the groups, over all stages
-        // Lanes may differ in whether a wait gave up; none leaves alone, since the
-        // others would wait for it in the next vote.  One that gave up on its place
-        // among the operands goes on to that vote, and lane 0 then announces nothing:
-        // what it wrote is in sums that are lost (a vote of its own after that wait:
-        // registers spill, 109 us instead of 103 for 4096^3 in f16, e4m3).
-        bool ok = true, going = true;
-        for (int u = pair; u < p.units && going; u += pairs) {
+        bool ok = true;
+        for (int u = pair; u < p.units && ok; u += pairs) {
             const Unit t = unit_of(p, u);
             for (int r = t.r0; r < t.r1; r += kTileK) {
                 const bool skip = turn != mine;
                 if (++turn == kDecodeGroups) turn = 0;
                 if (skip) continue;
-                ok = ok && bar_wait(code_full + 8 * cs, cph, gave_up);
+                // Lanes may differ in whether a wait gave up: the vote below is all lanes',
+                // and only its result ends the loop (votes of their own after either
+                // wait: registers spill, 109 us instead of 103 for 4096^3 in f16, e4m3).
+                ok = bar_wait(code_full + 8 * cs, cph, gave_up) &&
+                     bar_wait(empty + 8 * s, ph, gave_up);
                 uint4 c[4];
                 uint32_t byte[4];
 #pragma unroll
@@ -536,10 +535,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                                      short_way<T, F>((int)byte[2]) &&
                                      short_way<T, F>((int)byte[3]));
                 if (!all_short) {
-                    going = __all_sync(0xffffffffu, ok);
-                    if (!going) break;
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
                 }
-                ok = bar_wait(empty + 8 * s, ph, gave_up);
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     const uint2 lo = make_uint2(c[h].x, c[h].y), hi = make_uint2(c[h].z, c[h].w);
@@ -563,7 +561,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 // does neither.
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0 && ok) {
+                if (lane == 0) {
                     bar_arrive_cluster(leader_full + 8 * s);
                     bar_arrive(code_empty + 8 * cs);
                 }
@@ -611,8 +609,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 acc ^= 1;
                 if (acc == 0) aph ^= 1;
             }
-            // a wait that gave up, here or in a warp that these sums come from: no sums
-            const float lost = ok && !*gave_up ? 0.f : __uint_as_float(0x7fffffffu);
+            // a wait that gave up: no sums
+            const float lost = ok ? 0.f : __uint_as_float(0x7fffffffu);
             if (t.part >= 0) {
                 float *out = p.part + (int64_t)t.part * (kTileM * kTileN) + j1 * kTileM + m;
 #pragma unroll

@@ -28,19 +28,12 @@ def test_a_warp_gives_up_as_a_whole():
     assert len(re.findall(wait, body)) == 5 and len(re.findall(r"\bbar_wait_warp\(", body)) == 2
     vote = text[text.index("bool bar_wait_warp("):]
     assert "__all_sync(0xffffffffu, bar_wait(" in vote[:vote.index("}")]
-    assert re.findall(r"if \(([^;{]*)\) break;", decode) == ["!going"]
-    assert re.findall(r"going = ([^;]*);", decode) == ["true", "__all_sync(0xffffffffu, ok)"]
-    assert re.findall(r"for \(int [ur] [^;]*;([^;]*);", decode) == [" u < p.units && going",
-                                                                  " r < t.r1"]
-
-
-def test_no_sums_of_what_was_given_up():
-    """A decoding warp announces no stage whose place it gave up on, and sums that its
-    stores may have reached are marked."""
-    _, body = kernel()
-    decode = body[body.index("group <= kDecodeGroups"):body.index("take_registers<kSumRegs>")]
-    assert re.search(r"if \(lane == 0 && ok\) \{\s*bar_arrive_cluster\(leader_full", decode)
-    assert "lost = ok && !*gave_up ? 0.f : __uint_as_float(0x7fffffffu)" in body
+    assert re.findall(r"if \(([^;{]*)\) break;", decode) == ["!ok"]
+    # what is between the waits and that break: loads and votes of all lanes
+    between = decode[decode.rindex("bar_wait("):decode.index("if (!ok) break;")]
+    assert re.findall(r"__all_sync\(\s*0xffffffffu, (ok)", between) == ["ok", "ok"]
+    assert between.count("if (") == 1 and "if (!all_short) {" in between
+    assert "st.shared" not in between and "arrive" not in between
 
 
 def test_only_a_waits_own_time_counts(tmp_path):
