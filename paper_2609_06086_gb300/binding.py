@@ -336,14 +336,24 @@ def poseidon_ckpt_wgrad(d_ckpt: int, format: int, d_dy: int, dtype: int, ld_dy: 
 qk_heads = qk_pair
 
 
+def _pair(t):
+    """A (queries, keys) pair: qk_heads(), or two pos_heads as an array or a sequence."""
+    if t is None or type(t) is qk_pair:
+        return t
+    if len(t) != 2:
+        raise ValueError("q/k: a pair of pos_heads is wanted")
+    return qk_pair.from_buffer_copy((pos_heads * 2)(*t))
+
+
 def poseidon_qk_forward(qk: pos_qk, x, y, rstd=(0, 0), ckpt=(0, 0), stream: int = 0):
-    """x, y: qk_heads(); rstd, ckpt: (queries, keys) device pointers, 0 = not kept."""
-    _check(lib().poseidon_qk_forward(qk, x, y, rstd[0], rstd[1], ckpt[0], ckpt[1],
+    """x, y: qk_heads() or two pos_heads; rstd, ckpt: (queries, keys) device pointers, 0 =
+    not kept."""
+    _check(lib().poseidon_qk_forward(qk, _pair(x), _pair(y), rstd[0], rstd[1], ckpt[0], ckpt[1],
                                      stream))
 
 
 def poseidon_qk_backward(qk: pos_qk, dy, dx, rstd, ckpt=(0, 0), x=None, dw_in: int = 0,
                          dw: int = 0, stream: int = 0):
-    """dy, dx: qk_heads(); x: qk_heads() or None (the checkpoints are read)."""
-    _check(lib().poseidon_qk_backward(qk, x, ckpt[0], ckpt[1], rstd[0], rstd[1], dy, dx,
-                                      dw_in, dw, stream))
+    """dy, dx: qk_heads() or two pos_heads; x: the same or None (the checkpoints are read)."""
+    _check(lib().poseidon_qk_backward(qk, _pair(x), ckpt[0], ckpt[1], rstd[0], rstd[1], _pair(dy),
+                                      _pair(dx), dw_in, dw, stream))

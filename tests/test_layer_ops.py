@@ -146,6 +146,29 @@ def test_qk_misaligned_refused(P):
     refused(P, backward(dw=P16 + 2), "misaligned dw")
 
 
+@pytest.mark.parametrize("make", [lambda P, q, k: (P.pos_heads * 2)(q, k), lambda P, q, k: (q, k),
+                                  lambda P, q, k: [q, k]])
+def test_pairs_of_pos_heads(P, make):
+    """Both q/k calls take two pos_heads as they take qk_heads(): every field arrives,
+    which the refusal of one field after another shows."""
+    q = P.pos_qk(2, 2, 1, 8, 8, 0, 0, 0, 1e-6, None, None, P16, P16, 4, None)
+    good = make(P, P.pos_heads(P16, 24, 8), P.pos_heads(P16, 24, 8))
+    for over, text in ((dict(), "16-byte"), (dict(q=(ODD, 24, 8)), "misaligned"),
+                       (dict(q=(P16, -1, 8)), "stride"), (dict(q=(P16, 24, 4)), "overlapping"),
+                       (dict(k=(ODD, 24, 8)), "misaligned"), (dict(k=(P16, 0, 8)), "overlapping"),
+                       (dict(k=(P16, 24, -1)), "stride")):
+        f = dict(q=(P16, 24, 8), k=(P16, 24, 8))
+        f.update(over)
+        t = make(P, *(P.pos_heads(*v) for v in f.values()))
+        for x, y in ((good, t), (t, t)):
+            with pytest.raises(P.PoseidonError, match=text):
+                P.poseidon_qk_forward(q, x, y, ckpt=(P16 + 8, 0))
+            with pytest.raises(P.PoseidonError, match=text):
+                P.poseidon_qk_backward(q, x, t, (P16, P16), x=x, ckpt=(P16 + 8, 0))
+    with pytest.raises(ValueError):
+        P.poseidon_qk_forward(q, [P.pos_heads(P16, 24, 8)], good)
+
+
 @pytest.mark.parametrize("seed", range(3))
 def test_written_rows_that_overlap_are_refused(P, seed):
     """Against all pairs of rows, for small shapes and strides; the checkpoint that is
