@@ -3,8 +3,10 @@
 1. Searches the pipeline plan of a 7B-like model on one device of 80 GB and three
    slower ones of 24 GB twice: with the tables as profiled (activations in bf16),
    and with the memory per micro-batch that is left when the inputs of a layer's
-   four linear operations, the queries and the keys are kept as 8-bit
-   checkpoints.  The second search may use plans that did not fit before.
+   four linear operations are kept as 8-bit checkpoints.  The queries and keys that
+   attention's backward pass reads stay as they are; those before their norm, which
+   the profile has no norm for, are kept in 8 bits besides.  The second search may
+   use plans that did not fit before.
 2. Runs the q/k/v projections of the first stage of that plan in its 1F1B order
    on the GPU: W_s slots of checkpoints, one per micro-batch in flight; the
    forward pass fills a slot, the backward pass reads it, and the weights'
@@ -45,9 +47,11 @@ def workload(checkpoints):
     w = gen.config2()
     w.placement, w.type_counts = gen.workloads.PLACE_EXACT, [1, 3]
     w.cap = np.array([80, 24], np.int64) * 10 ** 9
-    if checkpoints:  # inputs of the q/k/v and output projections, of the MLP's two
-        plain, packed = kept_bytes(4096, (4096, 4096, 4096, 4 * 4096), (32, 8), 128)
-        w.mem_a = w.mem_a - (plain - packed)
+    if checkpoints:
+        # instead of bf16: inputs of the q/k/v and output projections, of the MLP's two
+        plain, packed = kept_bytes(4096, (4096, 4096, 4096, 4 * 4096), (), 128)
+        # besides: q and k before their norm
+        w.mem_a = w.mem_a - (plain - packed) + kept_bytes(4096, (), (32, 8), 128)[1]
     return w
 
 

@@ -42,6 +42,20 @@ def test_checkpoints_take_about_half(example):
     assert packed < 0.54 * plain
 
 
+def test_memory_of_the_planned_layer(example):
+    """What 8 bits save of 34 s h (2 s h the inputs of three linear operations, 8 s h the
+    fourth's) and what the norm of q and k adds; q and k as attention reads them (2 s
+    each of their widths) stay.  The plans' times are the oracle's."""
+    import oracle
+    s, h, width = 4096, 4096, (32 + 8) * 128
+    plain, packed = example.workload(False), example.workload(True)
+    saved = 14 * s * h - 7 * s * h * 33 // 32          # a byte and a scale of 32 instead of two
+    norm = s * width * 33 // 32 + 4 * s * (32 + 8)     # their codes, scales and 1 / rms
+    assert (plain.mem_a - packed.mem_a == saved - norm).all()
+    times = [oracle.search(w, prune=False)[0]["T"] for w in (plain, packed)]
+    assert times == [11078885, 10480313]
+
+
 @pytest.mark.gpu
 def test_plan_and_stage(example):
     """Smaller activations let the search find a faster plan, and the gradients
