@@ -512,11 +512,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                 const bool skip = turn != mine;
                 if (++turn == kDecodeGroups) turn = 0;
                 if (skip) continue;
-                // Lanes may differ in whether a wait gave up: the vote below is all lanes',
-                // and only its result ends the loop (votes of their own after either
-                // wait: registers spill, 109 us instead of 103 for 4096^3 in f16, e4m3).
-                ok = bar_wait(code_full + 8 * cs, cph, gave_up) &&
-                     bar_wait(empty + 8 * s, ph, gave_up);
+                // Lanes may differ in whether a wait gave up, so all of them vote before
+                // the loads, on their first tries alone where those pass: 154.2 us for
+                // 4096 x 6144 x 4096 with dw_in, 155.5 with one vote on both waits (whose
+                // loops are then in the way), 154.8 with the loads before the second
+                // wait; 152.9 without any vote.
+                ok = __all_sync(0xffffffffu, bar_try(code_full + 8 * cs, cph) &&
+                                                 bar_try(empty + 8 * s, ph));
+                if (!ok) {
+                    ok = __all_sync(0xffffffffu, bar_wait(code_full + 8 * cs, cph, gave_up) &&
+                                                     bar_wait(empty + 8 * s, ph, gave_up));
+                    if (!ok) break;
+                }
                 uint4 c[4];
                 uint32_t byte[4];
 #pragma unroll
@@ -530,14 +537,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWgradThreads, 1)
                                        h / 2 * (32 * 4)));
                 }
                 const bool all_short = __all_sync(
-                    0xffffffffu, ok && short_way<T, F>((int)byte[0]) &&
-                                     short_way<T, F>((int)byte[1]) &&
-                                     short_way<T, F>((int)byte[2]) &&
-                                     short_way<T, F>((int)byte[3]));
-                if (!all_short) {
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                }
+                    0xffffffffu, short_way<T, F>((int)byte[0]) && short_way<T, F>((int)byte[1]) &&
+                                     short_way<T, F>((int)byte[2]) && short_way<T, F>((int)byte[3]));
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     const uint2 lo = make_uint2(c[h].x, c[h].y), hi = make_uint2(c[h].z, c[h].w);

@@ -17,7 +17,7 @@ def kernel():
 def test_a_warp_gives_up_as_a_whole():
     """Lanes of a warp may differ in whether a wait gave up, and one that left its loop
     would be waited for by the others' next vote.  So a wait belongs to a single lane, or
-    it ends in a vote, or (the decoding warps) nothing but a vote's result ends a loop."""
+    its outcome is voted on at once, and nothing but a vote's result ends a loop."""
     text, body = kernel()
     wait = r"\bbar_wait\("
     alone = re.findall(r"if \(warp == \d[^{]*lane == 0\) \{(.*?)(?=\n        \} else if)", body,
@@ -29,11 +29,9 @@ def test_a_warp_gives_up_as_a_whole():
     vote = text[text.index("bool bar_wait_warp("):]
     assert "__all_sync(0xffffffffu, bar_wait(" in vote[:vote.index("}")]
     assert re.findall(r"if \(([^;{]*)\) break;", decode) == ["!ok"]
-    # what is between the waits and that break: loads and votes of all lanes
-    between = decode[decode.rindex("bar_wait("):decode.index("if (!ok) break;")]
-    assert re.findall(r"__all_sync\(\s*0xffffffffu, (ok)", between) == ["ok", "ok"]
-    assert between.count("if (") == 1 and "if (!all_short) {" in between
-    assert "st.shared" not in between and "arrive" not in between
+    votes = re.findall(r"ok = __all_sync\(0xffffffffu, (\w+)\([^;]*&&\s*(\w+)\([^;]*;", decode)
+    assert votes == [("bar_try", "bar_try"), ("bar_wait", "bar_wait")]
+    assert len(re.findall(r"\bok = ", decode)) == 3  # true, and the votes
 
 
 def test_only_a_waits_own_time_counts(tmp_path):
