@@ -344,7 +344,8 @@ __device__ __forceinline__ void keep_row(const QkParams &p, const Raw8<T> &raw, 
 // Bound by HBM and by issuing its instructions: x is read once, y (and the codes)
 // written once (8192 tokens of 64 + 8 heads of 128: bf16 73.7 us, 77% of HBM's
 // rate; 4096 in f32 58.8 us, 87%).  64 registers and 32 warps an SM: with 80 and
-// 24 warps it took 10 us more.
+// 24 warps it took 10 us more, at that size.  kRun's 16-bit kernels spill a little
+// so: 40 to 52 bytes in f16, 4 to 28 in bf16.
 template <typename T, int G, int L, int A>
 __global__ void __launch_bounds__(kQkThreads, sizeof(T) == 4 ? 3 : 4)
     qk_forward_kernel(const QkParams p) {
@@ -469,7 +470,7 @@ __device__ __forceinline__ Run run_of(const QkParams &p, int k) {
 // A warp goes through its run, token by token.  kAligned, kFull: its rows are on
 // their way to shared memory three steps ahead, which takes no registers (two rows
 // prefetched in registers instead: 111 us for 8192 tokens of 64 + 8 heads of 128,
-// bf16; so 79.0 us, 72% of HBM's rate, 86% from x).  Bound by issuing its instructions and
+// bf16; so 78.7 us, 72% of HBM's rate, 86% from x).  Bound by issuing its instructions and
 // by HBM: 16 warps an SM, since fewer than 128 registers spill.  dw is summed
 // over a thread's rows in registers, over the block in shared memory, and
 // written as one partial sum per block, which qk_dw_kernel adds up in order.

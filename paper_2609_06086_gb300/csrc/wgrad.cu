@@ -39,8 +39,8 @@ constexpr int kAccCols = 256;           // TMEM columns of one accumulator; two 
 // long sum drifts towards zero by about 1e-9 of its size per row (measured:
 // 2.6e-6 over 4096 rows).  An accumulator therefore takes 768 rows, and the
 // sums of those are added in registers, with rounding: 3.4e-7 over 4096 rows.
-// 4096 x 4864 x 4096 takes 103.6 us; 106.0 with 512 rows each, 102 with 1024
-// and half as much error again.
+// 4096 x 4864 x 4096 took 103.6 us so; 106.0 with 512 rows each, 102 with 1024
+// and half as much error again (now 106.6: the votes on the decoding warps' waits).
 constexpr int kChunkRows = 768;
 
 struct WgradParams {
