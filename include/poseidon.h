@@ -552,6 +552,87 @@ pos_status poseidon_qk_backward(const pos_qk *qk, const pos_heads *x, const void
                                 const pos_heads *dy, const pos_heads *dx, const float *d_dw_in,
                                 float *d_dw, void *stream);
 
+/*
+ * Dropout whose mask is computed where it is needed and never stored: the backward
+ * pass is the same call on the gradient.  Element (r, c) of a matrix is kept where
+ * its 16 random bits, a whole number, are at least t = p * 65536 (rounded to nearest),
+ * and then multiplied by 65536 / (65536 - t), so the mean is kept exactly.  The bits
+ * are half word c % 8 (low halves first) of the four words that Philox-4x32 of ten
+ * rounds gives for the counter (c / 8, r, low and high word of offset + *d_offset)
+ * under the key (low and high word of seed).  One offset per tensor, layer and
+ * micro-batch makes their masks independent.  d_offset is read when the kernel runs:
+ * a captured graph whose program advances it draws new masks at every replay.
+ * What a dropped element holds has no effect, a NaN neither.
+ */
+typedef struct pos_dropout {
+    float p;                    /* 0..1; below 2^-17 nothing is dropped */
+    uint64_t seed, offset;
+    const uint64_t *d_offset;   /* device, 8-byte aligned; NULL = 0 */
+} pos_dropout;
+
+/*
+ * y = residual + dropout(x), [rows][cols]; one rounding in 32 bits, one to y's type.
+ * d_res (y's type) may be NULL: y = dropout(x).  x and y may have any two types.  y may
+ * be x or d_res itself (the same pointer, stride and type) and must not overlap them
+ * otherwise.
+ * Errors: POS_EINVAL (NULL, p, rows or cols < 0 or of 2^31 - 8 or more, strides < 0 or
+ * of 2^31 or more, ldy < cols, dtype, a pointer off its elements), POS_ECUDA.
+ */
+pos_status poseidon_dropout(const pos_dropout *drop, int64_t rows, int64_t cols, const void *d_x,
+                            int32_t dtype, int64_t ldx, const void *d_res, int64_t ldr, void *d_y,
+                            int32_t dtype_y, int64_t ldy, void *stream);
+
+/*
+ * The residual's addition and the RMS norm of the sum, row by row:
+ *   h = residual + dropout(x)   rounded once in 32 bits, then to dtype_h,
+ *   r = 1 / sqrt(mean(h^2) + eps),  y = h * r * w   of h as it is written,
+ * sums in 32 bits.
+ */
+typedef struct pos_norm {
+    int64_t rows;               /* 0..2^31 - 1 */
+    int32_t cols;               /* 1..32768 */
+    int32_t dtype;              /* of x, y and their gradients */
+    int32_t dtype_h;            /* of the residual, h and their gradients: dtype or POS_F32 */
+    int32_t format;             /* of the checkpoints */
+    float eps;                  /* >= 0 */
+    const float *w;             /* [cols]; NULL = ones */
+    pos_dropout drop;           /* of x; p = 0: none */
+} pos_norm;
+
+/*
+ * Forward pass.  d_res may be NULL (h = dropout(x)).  Each output may be NULL: h, y,
+ * the checkpoints (16-byte aligned) of h, which the backward pass can read in h's
+ * place, and of y, which poseidon_ckpt_wgrad reads (both as poseidon_ckpt_pack makes
+ * them of the tensor written), rstd [rows] (r).  h may be d_res and y may be x
+ * itself (the same pointers and strides); other overlaps are not allowed.
+ * Errors: POS_EINVAL (NULL, sizes, strides, dtypes, format, eps, p, alignment),
+ * POS_ECUDA.
+ */
+pos_status poseidon_norm_forward(const pos_norm *norm, const void *d_x, int64_t ldx,
+                                 const void *d_res, int64_t ldr, void *d_h, int64_t ldh, void *d_y,
+                                 int64_t ldy, void *d_ckpt_h, void *d_ckpt_y, float *d_rstd,
+                                 void *stream);
+
+/*
+ * Backward pass.  With n = h * r (h, or where it is NULL its checkpoint, and the
+ * forward pass's rstd) and a = dy * w:
+ *   dh = dh_in + r * (a - n * mean(a * n)),  dx = dropout(dh),
+ *   dw = dw_in + sum over the rows of dy * n,
+ * dh_in the gradient that reaches h on other ways (NULL: zeros).  dh is the
+ * gradient of the residual too.  dx is dropped from dh before its rounding.  dh, dx and
+ * d_dw ([cols]) may be NULL; dh may be dh_in, dx may be dy and d_dw may be d_dw_in
+ * itself.  The sums' order depends on the sizes and the GPU alone.  Scratch from the
+ * library's pool where d_dw is not NULL: 4 * cols bytes for each block of the grid (what
+ * the GPU holds at once, at most 16 an SM).
+ * Errors: POS_EINVAL (as above; neither h nor its checkpoint, d_dw_in without d_dw),
+ * POS_ENOMEM, POS_ECUDA.
+ */
+pos_status poseidon_norm_backward(const pos_norm *norm, const void *d_h, int64_t ldh,
+                                  const void *d_ckpt_h, const float *d_rstd, const void *d_dy,
+                                  int64_t lddy, const void *d_dh_in, int64_t lddh_in, void *d_dh,
+                                  int64_t lddh, void *d_dx, int64_t lddx, const float *d_dw_in,
+                                  float *d_dw, void *stream);
+
 /* Message describing the last error of the calling thread ("" if none). */
 const char *poseidon_last_error(void);
 

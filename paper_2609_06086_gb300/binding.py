@@ -30,7 +30,8 @@ EXPORTS = ["poseidon_tables_create", "poseidon_tables_destroy", "poseidon_eval_b
            "poseidon_eval_batch_ex", "poseidon_eval_batch_host", "poseidon_argmin",
            "poseidon_argmin_noalloc", "poseidon_search", "poseidon_ckpt_bytes",
            "poseidon_ckpt_pack", "poseidon_ckpt_unpack", "poseidon_ckpt_wgrad",
-           "poseidon_qk_forward", "poseidon_qk_backward", "poseidon_last_error"]
+           "poseidon_qk_forward", "poseidon_qk_backward", "poseidon_dropout",
+           "poseidon_norm_forward", "poseidon_norm_backward", "poseidon_last_error"]
 
 
 class pos_tables(C.Structure):
@@ -101,6 +102,17 @@ class qk_pair(C.Structure):
 assert C.sizeof(qk_pair) == 2 * C.sizeof(pos_heads)
 
 
+class pos_dropout(C.Structure):
+    _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("d_offset", C.c_void_p)]
+
+
+class pos_norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32),
+                ("dtype_h", C.c_int32), ("format", C.c_int32), ("eps", C.c_float),
+                ("w", C.c_void_p), ("drop", pos_dropout)]
+
+
 class PoseidonError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -134,6 +146,12 @@ def lib():
         qk, pair = C.POINTER(pos_qk), C.POINTER(qk_pair)
         L.poseidon_qk_forward.argtypes = [qk, pair, pair, vp, vp, vp, vp, vp]
         L.poseidon_qk_backward.argtypes = [qk, pair, vp, vp, vp, vp, pair, pair, vp, vp, vp]
+        drop, norm = C.POINTER(pos_dropout), C.POINTER(pos_norm)
+        L.poseidon_dropout.argtypes = [drop, i64, i64, vp, i32, i64, vp, i64, vp, i32, i64, vp]
+        L.poseidon_norm_forward.argtypes = [norm, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp,
+                                            vp]
+        L.poseidon_norm_backward.argtypes = [norm, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp,
+                                             i64, vp, vp, vp]
         L.poseidon_last_error.restype = C.c_char_p
         L.poseidon_last_error.argtypes = []
         for name in EXPORTS[:-1]:
@@ -357,3 +375,27 @@ def poseidon_qk_backward(qk: pos_qk, dy, dx, rstd, ckpt=(0, 0), x=None, dw_in: i
     """dy, dx: qk_heads() or two pos_heads; x: the same or None (the checkpoints are read)."""
     _check(lib().poseidon_qk_backward(qk, _pair(x), ckpt[0], ckpt[1], rstd[0], rstd[1], _pair(dy),
                                       _pair(dx), dw_in, dw, stream))
+
+
+def poseidon_dropout(drop: pos_dropout, rows: int, cols: int, d_x: int, dtype: int, ldx: int,
+                     d_res: int, ldr: int, d_y: int, dtype_y: int, ldy: int, stream: int = 0):
+    """y = residual (0: zeros) + dropout(x); the gradient of x is the same call on y's."""
+    _check(lib().poseidon_dropout(drop, rows, cols, d_x, dtype, ldx, d_res, ldr, d_y, dtype_y, ldy,
+                                  stream))
+
+
+def poseidon_norm_forward(norm: pos_norm, d_x: int, ldx: int, d_res: int = 0, ldr: int = 0,
+                          d_h: int = 0, ldh: int = 0, d_y: int = 0, ldy: int = 0,
+                          d_ckpt_h: int = 0, d_ckpt_y: int = 0, d_rstd: int = 0, stream: int = 0):
+    """h = residual + dropout(x), y = its RMS norm; 0 = not there or not wanted."""
+    _check(lib().poseidon_norm_forward(norm, d_x, ldx, d_res, ldr, d_h, ldh, d_y, ldy, d_ckpt_h,
+                                       d_ckpt_y, d_rstd, stream))
+
+
+def poseidon_norm_backward(norm: pos_norm, d_h: int, ldh: int, d_ckpt_h: int, d_rstd: int,
+                           d_dy: int, lddy: int, d_dh_in: int = 0, lddh_in: int = 0,
+                           d_dh: int = 0, lddh: int = 0, d_dx: int = 0, lddx: int = 0,
+                           d_dw_in: int = 0, d_dw: int = 0, stream: int = 0):
+    """The gradients of h, x and w; d_h = 0: h is read from its checkpoint."""
+    _check(lib().poseidon_norm_backward(norm, d_h, ldh, d_ckpt_h, d_rstd, d_dy, lddy, d_dh_in,
+                                        lddh_in, d_dh, lddh, d_dx, lddx, d_dw_in, d_dw, stream))

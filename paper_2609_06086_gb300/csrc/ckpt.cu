@@ -8,18 +8,6 @@ constexpr int kPackThreads = 256;
 constexpr int kPackUnroll = 4;  // vectors of 8 elements in flight per thread
 constexpr int kPackBlock = kPackThreads * kPackUnroll;
 
-// n / d for n < 2^31 by a multiplication (round-up method).
-struct FastDiv {
-    uint32_t d, mul, shift;
-    explicit FastDiv(uint32_t v) : d(v), mul(0), shift(0) {
-        while ((1ull << shift) < v) ++shift;
-        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - v)) / v + 1);
-    }
-    __device__ __forceinline__ uint32_t div(uint32_t n) const {
-        return (__umulhi(n, mul) + n) >> shift;
-    }
-};
-
 struct PackParams {
     const void *x;     // pack: input; unpack: output
     uint8_t *codes, *scales;

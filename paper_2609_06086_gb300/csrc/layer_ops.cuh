@@ -49,6 +49,18 @@ __device__ __forceinline__ float scale_value(int byte) {
     return __uint_as_float(byte == kScaleNan ? 0x7fffffffu : (uint32_t)byte << 23);
 }
 
+// n / d for n < 2^31 by a multiplication (round-up method).
+struct FastDiv {
+    uint32_t d, mul, shift;
+    explicit FastDiv(uint32_t v) : d(v), mul(0), shift(0) {
+        while ((1ull << shift) < v) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - v)) / v + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const {
+        return (__umulhi(n, mul) + n) >> shift;
+    }
+};
+
 struct Vec8 {
     float v[8];
 };

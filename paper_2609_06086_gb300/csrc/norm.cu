@@ -1,0 +1,174 @@
+// poseidon_norm_forward: the residual's addition (with dropout) and the RMS norm of
+// the sum in one pass, with 8-bit checkpoints of both (formulas: poseidon.h).
+#include "norm.cuh"
+
+namespace pos {
+
+// A team takes a row at a time and holds it in registers, so that every matrix goes
+// through HBM once.  h is rounded to its type before it is squared, kept or
+// normalised: what the backward pass reads is what the forward pass used.
+template <typename T, typename H, class TEAM, bool ALIGNED>
+__global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    __shared__ float shared[2][32];
+    constexpr int V = TEAM::V;
+    const int rank = TEAM::rank(), step = TEAM::threads();
+    const uint64_t offset = drop_offset(p.drop);
+    Vec8 w[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = load_w(p, rank + i * step);
+    int turn = 0;
+    for (int64_t r = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index(); r < p.rows;
+         r += (int64_t)gridDim.x * TEAM::teams(), turn ^= 1) {
+        const T *x = static_cast<const T *>(p.x) + r * p.ldx;
+        const H *res = static_cast<const H *>(p.res) + r * p.ldr;
+        Raw8<T> xr[V];
+        Raw8<H> hr[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            xr[i] = load_vec<ALIGNED>(x, rank + i * step, p.cols);
+            if (p.res) hr[i] = load_vec<ALIGNED>(res, rank + i * step, p.cols);
+        }
+        float squares = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int j = rank + i * step;
+            Vec8 v = to_float(xr[i]);
+            if (p.res) {
+                add_dropped8(p.drop, offset, (uint32_t)r, (uint32_t)j, v, to_float(hr[i]));
+            } else if (p.drop.threshold) {
+                drop8(p.drop, offset, (uint32_t)r, (uint32_t)j, v);
+            }
+            hr[i] = from_float<H>(v);
+            if (p.h && 8 * j < p.cols)
+                store8<ALIGNED>(static_cast<H *>(p.h) + r * p.ldh + 8 * j, hr[i], p.cols - 8 * j);
+            if (p.codes_h)
+                keep8(p.format, hr[i], p.codes_h + r * p.pitch, p.scales_h + r * p.spitch, j,
+                      8 * j < p.pitch);
+            v = to_float(hr[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) squares += v.v[e] * v.v[e];
+        }
+        squares = TEAM::sum(squares, shared, turn);
+        const float rstd = rsqrtf(squares * p.inv_cols + p.eps);
+        if (p.rstd && rank == 0) p.rstd[r] = rstd;
+        if (!p.y && !p.codes_y) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int j = rank + i * step;
+            Vec8 v = to_float(hr[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)  // (past the last column 0, also under a norm that is NaN)
+                v.v[e] = 8 * j + e < p.cols ? v.v[e] * rstd * w[i].v[e] : 0.f;
+            const Raw8<T> y = from_float<T>(v);
+            if (p.y && 8 * j < p.cols)
+                store8<ALIGNED>(static_cast<T *>(p.y) + r * p.ldy + 8 * j, y, p.cols - 8 * j);
+            if (p.codes_y)
+                keep8(p.format, y, p.codes_y + r * p.pitch, p.scales_y + r * p.spitch, j,
+                      8 * j < p.pitch);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+pos_status check_norm(const pos_norm *n, NormParams *p) {
+    if (!n) return fail(POS_EINVAL, "norm: NULL pointer");
+    if (n->rows < 0 || n->rows >= (1ll << 31)) return fail(POS_EINVAL, "norm: bad rows");
+    if (n->cols < 1 || n->cols > kNormMaxCols)
+        return fail(POS_EINVAL, "norm: cols must be 1..32768");
+    if (!dtype_ok(n->dtype)) return fail(POS_EINVAL, "norm: unknown dtype");
+    if (n->dtype_h != n->dtype && n->dtype_h != POS_F32)
+        return fail(POS_EINVAL, "norm: dtype_h must be dtype or f32");
+    if (!format_ok(n->format)) return fail(POS_EINVAL, "norm: unknown format");
+    if (!(n->eps >= 0.f)) return fail(POS_EINVAL, "norm: eps must be >= 0");
+    if (reinterpret_cast<uintptr_t>(n->w) % 4) return fail(POS_EINVAL, "norm: misaligned w");
+    POS_TRY(make_drop(n->drop, "norm", &p->drop));
+    const CkptShape s = ckpt_shape(n->cols);
+    p->pitch = s.pitch, p->spitch = s.spitch;
+    p->rows = n->rows, p->cols = n->cols, p->format = n->format;
+    p->eps = n->eps, p->inv_cols = 1.f / n->cols;
+    p->w = n->w, p->w_vectors = aligned16(n->w);
+    return POS_OK;
+}
+
+// One matrix of a call, if it is there; aligned: whether all so far allow 16-byte
+// accesses.
+pos_status check_matrix(const char *what, const void *d, int32_t dtype, int64_t rows, int64_t cols,
+                        int64_t ld, bool written, bool *aligned) {
+    if (!d) return POS_OK;
+    const int size = dtype_size(dtype);
+    if (ld < 0 || ld >= (1ll << 31) || (written && rows > 1 && ld < cols))
+        return fail(POS_EINVAL, std::string("norm: bad row stride of ") + what);
+    if (reinterpret_cast<uintptr_t>(d) % size)
+        return fail(POS_EINVAL, std::string("norm: misaligned ") + what);
+    if (!aligned16(d) || ld * size % 16) *aligned = false;
+    return POS_OK;
+}
+
+template <typename T, typename H, class TEAM>
+static pos_status launch_forward(const NormParams &p, const NormShape &shape, bool aligned,
+                                 cudaStream_t s) {
+    auto kern = aligned ? norm_forward_kernel<T, H, TEAM, true>
+                        : norm_forward_kernel<T, H, TEAM, false>;
+    int per_sm = 0;
+    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), shape.threads, 0, &per_sm));
+    const int64_t blocks = (p.rows + shape.rows - 1) / shape.rows;
+    POS_CUDA(launch_dependent(kern, (int)std::min<int64_t>(blocks, (int64_t)sm_count() * per_sm),
+                              shape.threads, 0, s, p));
+    return POS_OK;
+}
+
+template <typename T, typename H>
+static pos_status forward_of(const NormParams &p, bool aligned, cudaStream_t s) {
+    const NormShape shape = norm_shape(p.cols);
+    switch (shape.team) {
+        case 0: return launch_forward<T, H, Team<true, 1, 256>>(p, shape, aligned, s);
+        case 1: return launch_forward<T, H, Team<true, 4, 256>>(p, shape, aligned, s);
+        case 2: return launch_forward<T, H, Team<false, 2, 512>>(p, shape, aligned, s);
+        case 3: return launch_forward<T, H, Team<false, 4, 512>>(p, shape, aligned, s);
+        default: return launch_forward<T, H, Team<false, 4, 1024>>(p, shape, aligned, s);
+    }
+}
+
+}  // namespace pos
+
+extern "C" pos_status poseidon_norm_forward(const pos_norm *norm, const void *d_x, int64_t ldx,
+                                            const void *d_res, int64_t ldr, void *d_h, int64_t ldh,
+                                            void *d_y, int64_t ldy, void *d_ckpt_h,
+                                            void *d_ckpt_y, float *d_rstd, void *stream) {
+    using namespace pos;
+    return guarded([&]() -> pos_status {
+        NormParams p = {};
+        bool aligned = true;
+        POS_TRY(check_norm(norm, &p));
+        const int64_t rows = norm->rows, cols = norm->cols;
+        POS_TRY(check_matrix("x", d_x, norm->dtype, rows, cols, ldx, false, &aligned));
+        POS_TRY(check_matrix("the residual", d_res, norm->dtype_h, rows, cols, ldr, false, &aligned));
+        POS_TRY(check_matrix("h", d_h, norm->dtype_h, rows, cols, ldh, true, &aligned));
+        POS_TRY(check_matrix("y", d_y, norm->dtype, rows, cols, ldy, true, &aligned));
+        if (!aligned16(d_ckpt_h) || !aligned16(d_ckpt_y))
+            return fail(POS_EINVAL, "norm: checkpoint not 16-byte aligned");
+        if (reinterpret_cast<uintptr_t>(d_rstd) % 4)
+            return fail(POS_EINVAL, "norm: misaligned rstd");
+        if (rows == 0) return POS_OK;
+        if (!d_x) return fail(POS_EINVAL, "norm: NULL x");
+        p.x = d_x, p.ldx = ldx, p.res = d_res, p.ldr = ldr, p.h = d_h, p.ldh = ldh;
+        p.y = d_y, p.ldy = ldy, p.rstd = d_rstd;
+        p.codes_h = static_cast<uint8_t *>(d_ckpt_h);
+        p.codes_y = static_cast<uint8_t *>(d_ckpt_y);
+        p.scales_h = p.codes_h ? p.codes_h + rows * p.pitch : nullptr;
+        p.scales_y = p.codes_y ? p.codes_y + rows * p.pitch : nullptr;
+        const auto s = static_cast<cudaStream_t>(stream);
+        const bool wide = norm->dtype_h == POS_F32;
+        if (norm->dtype == POS_BF16)
+            return wide ? forward_of<__nv_bfloat16, float>(p, aligned, s)
+                        : forward_of<__nv_bfloat16, __nv_bfloat16>(p, aligned, s);
+        if (norm->dtype == POS_F16)
+            return wide ? forward_of<__half, float>(p, aligned, s)
+                        : forward_of<__half, __half>(p, aligned, s);
+        return forward_of<float, float>(p, aligned, s);
+    });
+}
