@@ -633,6 +633,43 @@ pos_status poseidon_norm_backward(const pos_norm *norm, const void *d_h, int64_t
                                   int64_t lddh, void *d_dx, int64_t lddx, const float *d_dw_in,
                                   float *d_dw, void *stream);
 
+/*
+ * Causal attention with grouped heads over packed sequences.  Token i of a sequence
+ * sees its tokens j <= i; query head h reads key head h / (heads_q / heads_k):
+ *   s_ij = scale * q_i k_j,  lse_i = log(sum_j exp(s_ij)),
+ *   o_i = sum_j exp(s_ij - lse_i) v_j.
+ * Sequence n is the tokens starts[n] .. starts[n + 1] - 1 and may be empty; what lies
+ * before the first and behind the last is left as it was and may hold anything, and
+ * so may later tokens and other sequences: an infinity or a NaN reaches only those
+ * rows that see it.  A start below one before it counts as that one, one outside
+ * 0..tokens as the nearest of these.
+ */
+typedef struct pos_attn {
+    int64_t tokens;             /* below 2^31 - 512 */
+    int32_t heads_q, heads_k;   /* 0..65536; heads_q a multiple of heads_k */
+    int32_t dim;                /* 1..128 */
+    int32_t dtype;              /* POS_BF16 or POS_F16 */
+    float scale;                /* above 0 */
+    int32_t sequences;          /* at most 2^24 */
+    const int32_t *starts;      /* device [sequences + 1]; NULL = one sequence of all tokens */
+} pos_attn;
+
+/*
+ * Forward pass.  x: host array of three (queries, keys, values), o: one; lse
+ * [heads_q][tokens], which the backward pass reads, may be NULL.  o must not overlap x.
+ * Scores and sums are in 32 bits; probabilities, relative to a reference within 2^8 of
+ * the row's largest, are rounded to dtype for the product with the values, and o once
+ * on output.
+ * Scratch from the library's pool (stream-ordered): 16 bytes a tile of 256 tokens and
+ * sequence where starts is not NULL; a copy of each of x that is off the 16-byte
+ * alignment (base, strides and dim) or has a stride of 0.  Waits inside the kernel are
+ * bounded as poseidon_ckpt_wgrad's are; one that ran out makes its rows NaN.
+ * Errors: POS_EINVAL (NULL, sizes, heads, dim, dtype, scale, strides, rows of o that
+ * overlap, a pointer off its elements), POS_ENOMEM, POS_ECUDA.
+ */
+pos_status poseidon_attn_forward(const pos_attn *attn, const pos_heads *x, const pos_heads *o,
+                                 float *d_lse, void *stream);
+
 /* Message describing the last error of the calling thread ("" if none). */
 const char *poseidon_last_error(void);
 

@@ -8,9 +8,9 @@ The Python side is the ctypes binding in ``binding``; it loads the in-tree
 library and never computes anything itself.
 """
 from .binding import (  # noqa: F401
-    EXPORTS, Handle, PoseidonError, Tables, lib, make_problem, pos_dropout, pos_heads, pos_norm,
-    pos_qk, poseidon_argmin, poseidon_ckpt_bytes, poseidon_ckpt_pack, poseidon_ckpt_unpack,
-    poseidon_ckpt_wgrad, poseidon_dropout, poseidon_eval_batch, poseidon_eval_batch_ex,
-    poseidon_eval_batch_host, poseidon_norm_backward, poseidon_norm_forward, poseidon_qk_backward,
-    poseidon_qk_forward, poseidon_search, qk_heads,
+    EXPORTS, Handle, PoseidonError, Tables, attn_heads, lib, make_problem, pos_attn, pos_dropout,
+    pos_heads, pos_norm, pos_qk, poseidon_argmin, poseidon_attn_forward, poseidon_ckpt_bytes,
+    poseidon_ckpt_pack, poseidon_ckpt_unpack, poseidon_ckpt_wgrad, poseidon_dropout,
+    poseidon_eval_batch, poseidon_eval_batch_ex, poseidon_eval_batch_host, poseidon_norm_backward,
+    poseidon_norm_forward, poseidon_qk_backward, poseidon_qk_forward, poseidon_search, qk_heads,
 )

@@ -31,7 +31,8 @@ EXPORTS = ["poseidon_tables_create", "poseidon_tables_destroy", "poseidon_eval_b
            "poseidon_argmin_noalloc", "poseidon_search", "poseidon_ckpt_bytes",
            "poseidon_ckpt_pack", "poseidon_ckpt_unpack", "poseidon_ckpt_wgrad",
            "poseidon_qk_forward", "poseidon_qk_backward", "poseidon_dropout",
-           "poseidon_norm_forward", "poseidon_norm_backward", "poseidon_last_error"]
+           "poseidon_norm_forward", "poseidon_norm_backward", "poseidon_attn_forward",
+           "poseidon_last_error"]
 
 
 class pos_tables(C.Structure):
@@ -113,6 +114,21 @@ class pos_norm(C.Structure):
                 ("w", C.c_void_p), ("drop", pos_dropout)]
 
 
+class pos_attn(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("heads_q", C.c_int32), ("heads_k", C.c_int32),
+                ("dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("sequences", C.c_int32), ("starts", C.c_void_p)]
+
+
+class attn_triple(C.Structure):
+    """The (queries, keys, values) array of three pos_heads, its fields in one row."""
+    _fields_ = [(f"{t}{f}", C.c_void_p if not f else C.c_int64) for t in "qkv"
+                for f in ("", "_token", "_head")]
+
+
+assert C.sizeof(attn_triple) == 3 * C.sizeof(pos_heads)
+
+
 class PoseidonError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -152,6 +168,8 @@ def lib():
                                             vp]
         L.poseidon_norm_backward.argtypes = [norm, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp,
                                              i64, vp, vp, vp]
+        attn, triple, one = C.POINTER(pos_attn), C.POINTER(attn_triple), C.POINTER(pos_heads)
+        L.poseidon_attn_forward.argtypes = [attn, triple, one, vp, vp]
         L.poseidon_last_error.restype = C.c_char_p
         L.poseidon_last_error.argtypes = []
         for name in EXPORTS[:-1]:
@@ -399,3 +417,22 @@ def poseidon_norm_backward(norm: pos_norm, d_h: int, ldh: int, d_ckpt_h: int, d_
     """The gradients of h, x and w; d_h = 0: h is read from its checkpoint."""
     _check(lib().poseidon_norm_backward(norm, d_h, ldh, d_ckpt_h, d_rstd, d_dy, lddy, d_dh_in,
                                         lddh_in, d_dh, lddh, d_dx, lddx, d_dw_in, d_dw, stream))
+
+
+# attn_heads(q, q_token, q_head, k, k_token, k_head, v, v_token, v_head): the (queries,
+# keys, values) that the attention calls take
+attn_heads = attn_triple
+
+
+def _triple(t):
+    """(queries, keys, values): attn_heads(), or three pos_heads as an array or a sequence."""
+    if t is None or type(t) is attn_triple:
+        return t
+    if len(t) != 3:
+        raise ValueError("attention: three pos_heads are wanted")
+    return attn_triple.from_buffer_copy((pos_heads * 3)(*t))
+
+
+def poseidon_attn_forward(attn: pos_attn, x, o: pos_heads, lse: int = 0, stream: int = 0):
+    """x: attn_heads() or three pos_heads; lse: device pointer, 0 = not kept."""
+    _check(lib().poseidon_attn_forward(attn, _triple(x), o, lse, stream))

@@ -1,0 +1,266 @@
+// Shared by attn.cu and attn_backward.cu: causal attention over packed sequences
+// (formulas: poseidon.h).
+#pragma once
+#include <algorithm>
+#include <type_traits>
+
+#include "layer_ops.cuh"
+#include "tensor_core.cuh"
+
+namespace pos {
+
+constexpr int kAttnMaxDim = 128;
+constexpr int kTile = 128;                   // rows of queries or keys of a product
+constexpr int kBox = kTile * 128;            // bytes of 64 columns of a tile
+constexpr int kTileBytes = 2 * kBox;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A tensor [tokens][heads][dim] of 16-bit elements.
+struct AttnTensor {
+    const void *p;
+    int64_t token, head;  // strides in elements
+};
+
+struct AttnParams {
+    AttnTensor q, k, v, o, g;   // g: o's gradient; read 16 bytes at a time (except o)
+    void *out, *dq, *dk, *dv;   // outputs and their strides
+    int64_t out_token, out_head;
+    int64_t d_token[3], d_head[3];
+    float *lse;                 // [heads_q][tokens] or NULL
+    float2 *stats;              // backward: [heads_q][tokens]: lse in powers of two, D
+    const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
+    const int32_t *n_tiles;
+    int64_t tokens;
+    int32_t heads_q, heads_k, group, dim;  // dim: a multiple of 8
+    int32_t dim_out;            // elements of a row that are written
+    bool out_vectors, d_vectors[3];  // rows that can be written 16 bytes at a time
+    float scale, scale2;        // scale2 = scale * log2(e)
+};
+
+// A tile of queries or keys: the first token of its sequence, the sequence's
+// length, and which tile of it.
+struct AttnUnit {
+    int start, len, tile;
+};
+template <int ROWS>
+__device__ __forceinline__ bool unit_at(const AttnParams &p, int i, AttnUnit &u) {
+    if (!p.tiles) {  // longest first, as the list is
+        u.start = 0, u.len = (int)p.tokens;
+        u.tile = (u.len + ROWS - 1) / ROWS - 1 - i;
+        return u.tile >= 0;
+    }
+    if (i >= *p.n_tiles) return false;
+    const int4 t = p.tiles[i];
+    u.start = t.x, u.len = t.y, u.tile = t.z;
+    return true;
+}
+
+// ---------------------------------------------------------------------------
+// PTX
+// ---------------------------------------------------------------------------
+// A wait of a whole warp: all lanes go on or none does.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+}
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *map, int x, int head,
+                                         int token, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], "
+        "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar)
+        : "memory");
+}
+// Operand descriptors of a tile in shared memory: blocks of 64 columns, 128 bytes a
+// row, swizzled.  by_rows: the row's elements are the products' inner index (16 of
+// them 32 bytes on); by_columns: the rows are (16 of them 2048 bytes on).
+__device__ __forceinline__ uint64_t by_rows(uint32_t addr) {
+    return (uint64_t)(addr >> 4 & 0x3fffu) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
+           2ull << 61;
+}
+__device__ __forceinline__ uint64_t by_columns(uint32_t addr) {
+    return (uint64_t)(addr >> 4 & 0x3fffu) | (uint64_t)(kBox >> 4) << 16 |
+           (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// f32 sums of 16-bit products, 128 rows, n columns.
+template <typename T>
+__device__ __forceinline__ uint32_t product_of(int n, bool b_by_columns) {
+    constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return 1u << 4 | kType << 7 | kType << 10 | (b_by_columns ? 1u << 16 : 0u) |
+           (uint32_t)(n >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
+}
+// Both operands in shared memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t add) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+// The first operand in TMEM: two elements of a row in a column's word.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t add) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+// d (+)= A B^T over `dim` elements of the rows of two tiles.
+template <typename T>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, int dim) {
+    const uint32_t idesc = product_of<T>(kTile, false);
+    const uint64_t da = by_rows(a), db = by_rows(b);
+    for (int k = 0; k < dim; k += 16) {
+        const uint32_t at = (k / 64 * kBox + k % 64 * 2) >> 4;
+        mma_ss(d, da + at, db + at, idesc, k > 0);
+    }
+}
+// d (+)= A B, A [128][128] in TMEM, B the rows of a tile, `dim` columns of it.
+template <typename T>
+__device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b, int dim, bool add) {
+    const uint32_t idesc = product_of<T>((dim + 15) / 16 * 16, true);
+    const uint64_t db = by_columns(b);
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        mma_ts(d, a + 8 * k, db + k * (2048 >> 4), idesc, add || k > 0);
+}
+// Arrives on a barrier once the products issued so far are done.
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_before() {
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_after() {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_wait_loads() {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_wait_stores() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// 16 or 32 columns of the warp's lanes; the loads are there after tmem_wait_loads().
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+        "%11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+        "%11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+        "%28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+        "%11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15])
+        : "memory");
+}
+// 2^x, both halves of the result within two units of its last place.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two values rounded to 16 bits, the first in the low half.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Rows from `first` on of a tile become zeros: what belongs to another sequence, or
+// to none and may hold anything, would make a NaN of a probability of 0.
+__device__ __forceinline__ void zero_rows(uint32_t tile, int first, int boxes, int lane) {
+    for (int i = first * 8 + lane; i < kTile * 8; i += 32)
+        for (int b = 0; b < boxes; ++b)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + b * kBox + 16 * i),
+                         "r"(0)
+                         : "memory");
+    // before the tensor cores' reads
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < __uint_as_float(0x7f800000u); }
+
+// ---------------------------------------------------------------------------
+// One row by the formulas alone, by a warp: where a tensor-core product gave an
+// infinity or a NaN.  Those multiply what is masked by 0 and so let a later token's
+// infinities into an earlier one's row; here only what a row sees is read.
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ const T *row_at(const AttnTensor &t, int64_t token, int head) {
+    return static_cast<const T *>(t.p) + token * t.token + head * t.head;
+}
+template <typename T>
+__device__ __forceinline__ Vec8 load_row8(const T *at) {
+    return to_float(load8<true>(at, 8));
+}
+template <typename T>
+__device__ __forceinline__ float dot_rows(const T *a, const T *b, int dim) {
+    float s = 0.f;
+    for (int d = 0; d < dim; d += 8) {
+        const Vec8 x = load_row8(a + d), y = load_row8(b + d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += x.v[e] * y.v[e];
+    }
+    return s;
+}
+// A lane's part of a row: elements lane + 32 i.
+struct RowPart {
+    float v[kAttnMaxDim / 32];
+};
+template <typename T>
+__device__ __forceinline__ void add_row(RowPart &sum, float w, const T *row, int dim, int lane) {
+#pragma unroll
+    for (int i = 0; i < kAttnMaxDim / 32; ++i)
+        if (lane + 32 * i < dim) sum.v[i] += w * static_cast<float>(row[lane + 32 * i]);
+}
+template <typename T>
+__device__ __forceinline__ void write_row(void *out, int64_t at, const RowPart &sum, float factor,
+                                          int dim, int lane) {
+#pragma unroll
+    for (int i = 0; i < kAttnMaxDim / 32; ++i)
+        if (lane + 32 * i < dim) static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
+}
+
+// ---------------------------------------------------------------------------
+// Host side (attn.cu)
+// ---------------------------------------------------------------------------
+pos_status check_attn(const pos_attn *a, AttnParams *p);
+pos_status check_attn_tensor(const pos_attn *a, const pos_heads &t, int64_t heads, const char *what,
+                             bool written);
+pos_status attn_scratch(int64_t bytes, cudaStream_t s, void **out);
+bool attn_direct(const pos_attn *a, const pos_heads &t, int64_t heads);
+int64_t attn_copy_bytes(const pos_attn *a, int64_t heads);
+pos_status attn_input(const pos_attn *a, const pos_heads &t, int64_t heads, char **copy,
+                      cudaStream_t s, AttnTensor *out);
+pos_status attn_map(CUtensorMap *map, const pos_attn *a, const AttnTensor &t, int64_t heads,
+                    int32_t dim);
+int64_t attn_list_bytes(const pos_attn *a, int rows);
+pos_status attn_list(const pos_attn *a, int rows, char **at, cudaStream_t s, AttnParams *p);
+pos_status attn_grid(const pos_attn *a, int rows, int64_t heads, int *grid);
+
+}  // namespace pos

@@ -710,22 +710,6 @@ static pos_status check_qk(const pos_qk *q) {
     return POS_OK;
 }
 
-// Whether two rows of a tensor share an element.
-static bool rows_overlap(int64_t tokens, int64_t heads, int64_t dim, int64_t token_stride,
-                         int64_t head_stride) {
-    if ((heads > 1 && head_stride < dim) || (tokens > 1 && token_stride < dim)) return true;
-    if (heads <= 1 || tokens <= 1) return false;
-    // one token's rows before the next token's, or one head's before the next head's
-    if (token_stride >= (heads - 1) * head_stride + dim) return false;
-    if ((head_stride - dim) / token_stride >= tokens - 1) return false;
-    for (int64_t h = 1; h < heads; ++h) {  // against head 0 of the tokens beside it
-        const int64_t at = h * head_stride, t = at / token_stride;
-        if (t > 0 && t < tokens && at - t * token_stride < dim) return true;
-        if (t + 1 < tokens && (t + 1) * token_stride - at < dim) return true;
-    }
-    return false;
-}
-
 // A host array of two tensors; data may be NULL where there is nothing.
 static pos_status check_heads(const pos_qk *q, const pos_heads *t, const char *what, bool written) {
     if (!t) return fail(POS_EINVAL, std::string("q/k: NULL ") + what);

@@ -1,12 +1,9 @@
 // poseidon_ckpt_wgrad: weight gradient of a linear layer from the 8-bit
 // checkpoint of its input (formulas: poseidon.h).
-#include <cuda.h>
-
 #include <algorithm>
-#include <mutex>
 
 #include "layer_ops.cuh"
-#include "wait_limit.h"
+#include "tensor_core.cuh"
 
 namespace pos {
 
@@ -61,9 +58,6 @@ struct WgradParams {
 // ---------------------------------------------------------------------------
 // PTX
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void *p) {
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -78,12 +72,6 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {  // own CTA
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 // A barrier in either CTA of the pair.  The default scope (the CTA) is enough:
 // what the arrival orders is this SM's own shared memory or TMEM, which this
 // SM's tensor core reads or writes; a release to the whole cluster waits for
@@ -92,43 +80,6 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {  // own CTA
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar)
                  : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
-                 : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-        "selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(1000000)  // sleeps for up to 1 ms
-        : "memory");
-    return ok;
-}
-__device__ __forceinline__ uint64_t now_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-// Waits for a phase, two seconds at most (WaitLimit); false: it did not come, or
-// another wait of the block has already given up.
-__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *gave_up) {
-    WaitLimit limit(now_ns());
-    for (;;) {
-        if (bar_try(bar, parity)) return true;
-        if (*gave_up) return false;
-        if (limit.reached(now_ns())) {
-            *gave_up = 1;
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up) {
-    if (bar_try(bar, parity)) return true;
-    return bar_wait_long(bar, parity, gave_up);
 }
 // The same by a whole warp.  Where a wait gives up its lanes may not agree (one sees
 // the phase on its last try, another that the block has given up), and lanes that went
@@ -195,15 +146,6 @@ __device__ __forceinline__ void copy_word(uint32_t dst, const void *src, bool th
 __device__ __forceinline__ void bar_arrive_copies(uint32_t bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
-template <int R>
-__device__ __forceinline__ void give_registers() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R));
-}
-template <int R>
-__device__ __forceinline__ void take_registers() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
-}
-
 // ---------------------------------------------------------------------------
 // Decoding codes into 16-bit values
 // ---------------------------------------------------------------------------
@@ -695,24 +637,6 @@ __global__ void __launch_bounds__(256) wgrad_copy_kernel(const T *x, int64_t ldx
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
-static pos_status encode_fn(EncodeTiled *out) {
-    static std::mutex mu;
-    static EncodeTiled fn;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!fn) {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        POS_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
-                                                  cudaEnableDefault, &found));
-        if (found != cudaDriverEntryPointSuccess || !f)
-            return fail(POS_ECUDA, "the driver has no cuTensorMapEncodeTiled");
-        fn = reinterpret_cast<EncodeTiled>(f);
-    }
-    *out = fn;
-    return POS_OK;
-}
-
 // A matrix [rows][cols] of `type`, rows `stride` bytes apart, in boxes of
 // box_cols x kTileK; what lies outside reads as zeros.
 static pos_status make_map(CUtensorMap *map, CUtensorMapDataType type, const void *p, int64_t rows,
