@@ -670,6 +670,21 @@ typedef struct pos_attn {
 pos_status poseidon_attn_forward(const pos_attn *attn, const pos_heads *x, const pos_heads *o,
                                  float *d_lse, void *stream);
 
+/*
+ * Backward pass.  lse and o are the forward pass's.  With p_ij = exp(s_ij - lse_i),
+ * D_i = do_i o_i and ds_ij = p_ij (do_i v_j - D_i):
+ *   dq_i = scale * sum_j ds_ij k_j,  dk_j = scale * sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
+ * the keys' and values' summed over the query heads of their group.  x, dx: host arrays of
+ * three, o and d_o: one; dx must not overlap what is read.  Sums are in 32 bits, in an
+ * order that depends on the sizes alone; p and ds are rounded to dtype for their products.
+ * Scratch from the library's pool: 8 bytes a token and query head, and what the
+ * forward pass takes (16 bytes a tile of 128; a copy of d_o too where it needs one).
+ * Errors: as above (NULL lse; rows of dx that overlap).
+ */
+pos_status poseidon_attn_backward(const pos_attn *attn, const pos_heads *x, const pos_heads *o,
+                                  const float *d_lse, const pos_heads *d_o, const pos_heads *dx,
+                                  void *stream);
+
 /* Message describing the last error of the calling thread ("" if none). */
 const char *poseidon_last_error(void);
 

@@ -9,8 +9,9 @@ library and never computes anything itself.
 """
 from .binding import (  # noqa: F401
     EXPORTS, Handle, PoseidonError, Tables, attn_heads, lib, make_problem, pos_attn, pos_dropout,
-    pos_heads, pos_norm, pos_qk, poseidon_argmin, poseidon_attn_forward, poseidon_ckpt_bytes,
-    poseidon_ckpt_pack, poseidon_ckpt_unpack, poseidon_ckpt_wgrad, poseidon_dropout,
-    poseidon_eval_batch, poseidon_eval_batch_ex, poseidon_eval_batch_host, poseidon_norm_backward,
-    poseidon_norm_forward, poseidon_qk_backward, poseidon_qk_forward, poseidon_search, qk_heads,
+    pos_heads, pos_norm, pos_qk, poseidon_argmin, poseidon_attn_backward, poseidon_attn_forward,
+    poseidon_ckpt_bytes, poseidon_ckpt_pack, poseidon_ckpt_unpack, poseidon_ckpt_wgrad,
+    poseidon_dropout, poseidon_eval_batch, poseidon_eval_batch_ex, poseidon_eval_batch_host,
+    poseidon_norm_backward, poseidon_norm_forward, poseidon_qk_backward, poseidon_qk_forward,
+    poseidon_search, qk_heads,
 )

@@ -32,7 +32,7 @@ EXPORTS = ["poseidon_tables_create", "poseidon_tables_destroy", "poseidon_eval_b
            "poseidon_ckpt_pack", "poseidon_ckpt_unpack", "poseidon_ckpt_wgrad",
            "poseidon_qk_forward", "poseidon_qk_backward", "poseidon_dropout",
            "poseidon_norm_forward", "poseidon_norm_backward", "poseidon_attn_forward",
-           "poseidon_last_error"]
+           "poseidon_attn_backward", "poseidon_last_error"]
 
 
 class pos_tables(C.Structure):
@@ -170,6 +170,7 @@ def lib():
                                              i64, vp, vp, vp]
         attn, triple, one = C.POINTER(pos_attn), C.POINTER(attn_triple), C.POINTER(pos_heads)
         L.poseidon_attn_forward.argtypes = [attn, triple, one, vp, vp]
+        L.poseidon_attn_backward.argtypes = [attn, triple, one, vp, one, triple, vp]
         L.poseidon_last_error.restype = C.c_char_p
         L.poseidon_last_error.argtypes = []
         for name in EXPORTS[:-1]:
@@ -436,3 +437,9 @@ def _triple(t):
 def poseidon_attn_forward(attn: pos_attn, x, o: pos_heads, lse: int = 0, stream: int = 0):
     """x: attn_heads() or three pos_heads; lse: device pointer, 0 = not kept."""
     _check(lib().poseidon_attn_forward(attn, _triple(x), o, lse, stream))
+
+
+def poseidon_attn_backward(attn: pos_attn, x, o: pos_heads, lse: int, d_o: pos_heads, dx,
+                           stream: int = 0):
+    """x, dx: attn_heads() or three pos_heads (queries, keys, values)."""
+    _check(lib().poseidon_attn_backward(attn, _triple(x), o, lse, d_o, _triple(dx), stream))

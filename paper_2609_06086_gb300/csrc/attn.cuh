@@ -28,6 +28,7 @@ struct AttnParams {
     int64_t d_token[3], d_head[3];
     float *lse;                 // [heads_q][tokens] or NULL
     float2 *stats;              // backward: [heads_q][tokens]: lse in powers of two, D
+    uint32_t *largest;          // backward in f16: bits of dO's largest magnitude
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
     const int32_t *n_tiles;
     int64_t tokens;

@@ -1,0 +1,772 @@
+// poseidon_attn_backward (formulas: poseidon.h).
+#include "attn.cuh"
+
+namespace pos {
+
+// Two kernels, so that every sum has one place and one order: the queries' gradients
+// by blocks that go over the keys, the keys' and values' by blocks that go over the
+// queries.  Scores and their gradients are computed in both: seven products instead of
+// the five of a single pass, which would add up the queries' gradients across blocks.
+constexpr int kBackThreads = 3 * 128;  // two warpgroups of sums, one of loads and products
+constexpr int kBackRegs = 208, kBackIssueRegs = 88;  // 2 * 208 + 88 = 3 * 168
+
+// f16 holds probabilities of long rows and small gradients badly (below 2^-14 with
+// fewer bits, below 2^-25 not at all).  There P is multiplied by 2^12 and dS by 2^k, k the
+// same for a whole call: the largest magnitude of dO becomes 2^8 to 2^9.  A dS that is
+// too large all the same gives an infinity and its rows are done again in 32 bits.
+template <typename T>
+struct Shift {
+    static constexpr float kProbs = std::is_same<T, __half>::value ? 12.f : 0.f;
+    float grads, undo;  // of dP - D, so that P (dP - D) has its factor; 2^-k
+    __device__ __forceinline__ explicit Shift(const AttnParams &p) : grads(1.f), undo(1.f) {
+        if constexpr (std::is_same<T, __half>::value) {
+            const uint32_t big = *p.largest;  // bits of an f32
+            const int k = big ? 8 - ((int)(big >> 23) - 127) : 0;
+            grads = __uint_as_float((uint32_t)(127 + k - 12) << 23);
+            undo = __uint_as_float((uint32_t)(127 - k) << 23);
+        }
+    }
+    static constexpr float kUndoProbs = std::is_same<T, __half>::value ? 1.f / 4096.f : 1.f;
+};
+
+// Of the queries of a tile: lse in powers of two (less the probabilities' factor), and
+// D = dO . O; f16: the largest finite magnitude of dO.  16 lanes a row.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_stats_kernel(const AttnParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    AttnUnit u;
+    if (!unit_at<kTile>(p, blockIdx.x / p.heads_q, u)) return;
+    const int l = threadIdx.x % 16, head = blockIdx.x % p.heads_q;
+    uint32_t big = 0;
+#pragma unroll 4
+    for (int r = threadIdx.x / 16; r < kTile; r += 16) {
+        const int row = u.tile * kTile + r;
+        const int64_t token = u.start + (int64_t)row;
+        float d = 0.f;
+        if (row < u.len && 8 * l < p.dim) {
+            // (o may lie anywhere; past its last element dO's copy holds zeros)
+            const Vec8 a = to_float(load8_shifted(row_at<T>(p.o, token, head) + 8 * l, 8 * l,
+                                                  p.dim_out - 8 * l));
+            const Vec8 b = load_row8(row_at<T>(p.g, token, head) + 8 * l);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                d += a.v[e] * b.v[e];
+                if (finite(b.v[e])) big = max(big, __float_as_uint(fabsf(b.v[e])));
+            }
+        }
+#pragma unroll
+        for (int o = 8; o; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
+        if (l == 0 && row < u.len)
+            p.stats[head * p.tokens + token] =
+                make_float2(p.lse[head * p.tokens + token] * kLog2e - Shift<T>::kProbs, d);
+    }
+    if constexpr (std::is_same<T, __half>::value) {
+        big = __reduce_max_sync(0xffffffffu, big);
+        if (threadIdx.x % 32 == 0 && big) atomicMax(p.largest, big);
+    }
+}
+
+// d (+)= A B, A [128][128] in TMEM: each half of its columns from where the warps
+// that computed it had read their scores.
+template <typename T>
+__device__ __forceinline__ void mma_halves(uint32_t d, uint32_t a, uint32_t b, int dim, bool add) {
+    const uint32_t idesc = product_of<T>((dim + 15) / 16 * 16, true);
+    const uint64_t db = by_columns(b);
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        mma_ts(d, a + (k / 4 * 64 + k % 4 * 8), db + k * (2048 >> 4), idesc, add || k > 0);
+}
+
+// Sums from TMEM to a row of the output: 16 columns at a time, those of half `side` of
+// the pairs of 16.  Whether all are finite.
+template <typename T>
+__device__ __forceinline__ bool write_sums(uint32_t tm, int side, float factor, T *out, bool live,
+                                           bool vectors, int dim, int dim_out) {
+    bool good = true;
+    for (int c = 16 * side; c < dim; c += 32) {
+        uint32_t v[16];
+        tmem_load16(tm + c, v);
+        tmem_wait_loads();
+        if (!live) continue;
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
+            Vec8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x.v[e] = __uint_as_float(v[h + e]) * factor;
+                if (c + h + e < dim) good = good && finite(__uint_as_float(v[h + e]));
+            }
+            if (vectors) store8<true>(out + c + h, from_float<T>(x), dim_out - c - h);
+            else store8<false>(out + c + h, from_float<T>(x), dim_out - c - h);
+        }
+    }
+    return good;
+}
+__device__ __forceinline__ void sums_barrier() {  // of the two warpgroups of sums
+    asm volatile("barrier.sync 1, 256;" ::: "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of the queries
+// ---------------------------------------------------------------------------
+// A block takes 128 queries of a head and goes over the keys from the diagonal down.
+// TMEM: two places of scores, one of dP = dO V^T, the sums.  While two warpgroups
+// (64 columns of a row a thread) make dS = P (dP - D) of a tile, the tensor cores compute
+// the next scores, and dP as soon as the last one has been read.
+constexpr int kKeySlots = 3, kValueSlots = 2;
+constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
+constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 32;
+
+template <typename T>
+__device__ __forceinline__ void dq_row(const AttnParams &p, const AttnUnit &u, int row, int head,
+                                       int lane) {
+    const int g = head / p.group;
+    const T *q = row_at<T>(p.q, u.start + row, head), *dy = row_at<T>(p.g, u.start + row, head);
+    const float2 st = p.stats[head * p.tokens + u.start + row];
+    RowPart sum = {};
+    for (int j0 = 0; j0 <= row; j0 += 32) {
+        const int j = j0 + lane, n = min(32, row + 1 - j0);
+        float ds = 0.f;
+        if (j <= row) {
+            const float s = dot_rows(q, row_at<T>(p.k, u.start + j, g), p.dim) * p.scale2;
+            if (row)
+                ds = exp2f(s - (st.x + Shift<T>::kProbs)) *
+                     (dot_rows(dy, row_at<T>(p.v, u.start + j, g), p.dim) - st.y);
+        }
+        for (int t = 0; t < n; ++t)
+            add_row(sum, __shfl_sync(0xffffffffu, ds, t), row_at<T>(p.k, u.start + j0 + t, g),
+                    p.dim, lane);
+    }
+    write_row<T>(p.dq, (u.start + row) * p.d_token[0] + head * p.d_head[0], sum, p.scale,
+                 p.dim_out, lane);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBackThreads, 1)
+    attn_dq_kernel(const __grid_constant__ CUtensorMap q_map,
+                   const __grid_constant__ CUtensorMap k_map,
+                   const __grid_constant__ CUtensorMap v_map,
+                   const __grid_constant__ CUtensorMap g_map, const AttnParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char *aligned = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t q_at = base, g_at = q_at + kTileBytes, k_at = g_at + kTileBytes;
+    const uint32_t v_at = k_at + kKeySlots * kTileBytes;
+    const uint32_t bars = v_at + kValueSlots * kTileBytes;
+    const uint32_t k_full = bars, k_empty = k_full + 8 * kKeySlots;
+    const uint32_t v_full = k_empty + 8 * kKeySlots, v_empty = v_full + 8 * kValueSlots;
+    const uint32_t in_full = v_empty + 8 * kValueSlots, s_full = in_full + 8, dp_full = s_full + 16;
+    const uint32_t dp_read = dp_full + 8, ds_full = dp_read + 8, dq_full = ds_full + 8;
+    const uint32_t slot = dq_full + 8;
+    unsigned char *tail = aligned + (slot - base);
+    volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
+    uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);  // rows to do again
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kDqBars; ++i) {
+            const bool sums = bars + 8 * i == dp_read || bars + 8 * i == ds_full;
+            bar_init(bars + 8 * i, sums ? 8 : 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gave_up = 0;
+        for (int i = 0; i < 4; ++i) bad[i] = 0;
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
+                     "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tmem_before();
+    }
+    __syncthreads();
+    tmem_after();
+    grid_dep_wait();
+    grid_dep_trigger();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
+    const uint32_t dp_tm = tmem + 2 * kTile, dq_tm = tmem + 3 * kTile;
+
+    const int head = blockIdx.x % p.heads_q;
+    AttnUnit u;
+    const bool any = unit_at<kTile>(p, blockIdx.x / p.heads_q, u);
+    const int n = any ? u.tile + 1 : 0;  // tiles of keys
+    const int boxes = p.dim > 64 ? 2 : 1;
+    bool ok = true;
+
+    if (group == 2) {
+        give_registers<kBackIssueRegs>();
+        if (warp == 8) {
+            if (lane == 0 && any) {
+                bar_expect(in_full, 2 * boxes * kBox);
+                for (int b = 0; b < boxes; ++b) {
+                    const int token = u.start + u.tile * kTile;
+                    tma_rows(q_at + b * kBox, &q_map, 64 * b, head, token, in_full);
+                    tma_rows(g_at + b * kBox, &g_map, 64 * b, head, token, in_full);
+                }
+                int sk = 0, sv = 0;
+                uint32_t phk = 1, phv = 1;
+                const auto load = [&](uint32_t full, uint32_t empty, uint32_t at,
+                                      const CUtensorMap *map, int &s, uint32_t &ph, int slots,
+                                      int j) {
+                    if (!bar_wait(empty + 8 * s, ph, gave_up)) return false;
+                    bar_expect(full + 8 * s, boxes * kBox);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_rows(at + s * kTileBytes + b * kBox, map, 64 * b, head / p.group,
+                                 u.start + j * kTile, full + 8 * s);
+                    if (++s == slots) s = 0, ph ^= 1;
+                    return true;
+                };
+                // keys a step ahead of values
+                for (int i = 0; i <= n && ok; ++i) {
+                    if (i < n)
+                        ok = load(k_full, k_empty, k_at, &k_map, sk, phk, kKeySlots, n - 1 - i);
+                    if (i > 0 && ok)
+                        ok = load(v_full, v_empty, v_at, &v_map, sv, phv, kValueSlots, n - i);
+                }
+            }
+        } else if (warp == 9) {
+            const auto scores = [&](int i) {
+                if (!wait_warp(k_full + 8 * (i % kKeySlots), i / kKeySlots & 1, gave_up))
+                    return false;
+                const uint32_t at = k_at + i % kKeySlots * kTileBytes;
+                const int seen = u.len - (n - 1 - i) * kTile;
+                if (seen < kTile) zero_rows(at, seen, boxes, lane);
+                if (lane == 0) {
+                    mma_rows<T>(tmem + i % 2 * kTile, q_at, at, p.dim);
+                    commit(s_full + 8 * (i % 2));
+                }
+                return true;
+            };
+            const auto grads = [&](int i) {  // dP
+                if (!wait_warp(v_full + 8 * (i % kValueSlots), i / kValueSlots & 1, gave_up))
+                    return false;
+                if (lane == 0) {
+                    mma_rows<T>(dp_tm, g_at, v_at + i % kValueSlots * kTileBytes, p.dim);
+                    commit(dp_full);
+                    commit(v_empty + 8 * (i % kValueSlots));
+                }
+                return true;
+            };
+            if (any) {
+                ok = wait_warp(in_full, 0, gave_up);
+                tmem_after();
+                ok = ok && scores(0) && grads(0) && (n == 1 || scores(1));
+            }
+            for (int i = 0; i < n && ok; ++i) {
+                if (i + 1 < n) {
+                    ok = wait_warp(dp_read, i & 1, gave_up);
+                    tmem_after();
+                    ok = ok && grads(i + 1);
+                    if (!ok) break;
+                }
+                ok = wait_warp(ds_full, i & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                if (lane == 0) {
+                    mma_halves<T>(dq_tm, tmem + i % 2 * kTile, k_at + i % kKeySlots * kTileBytes,
+                                  p.dim, i > 0);
+                    commit(k_empty + 8 * (i % kKeySlots));
+                    if (i == n - 1) commit(dq_full);
+                }
+                __syncwarp();
+                if (i + 2 < n) ok = scores(i + 2);
+            }
+        }
+        __syncwarp();
+    } else {
+        take_registers<kBackRegs>();
+        const int side = group, row = u.tile * kTile + warp % 4 * 32 + lane;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const bool live = any && row < u.len;
+        float2 st = make_float2(0.f, 0.f);
+        const Shift<T> shift(p);
+        if (live) st = p.stats[head * p.tokens + u.start + row];
+        for (int i = 0; i < n; ++i) {
+            const uint32_t s_tm = tmem + i % 2 * kTile + 64 * side + lanes;
+            ok = ok && wait_warp(s_full + 8 * (i % 2), i / 2 & 1, gave_up);
+            if (!ok) break;
+            tmem_after();
+            uint32_t s[64], d[64];
+            tmem_load32(s_tm, s);
+            tmem_load32(s_tm + 32, s + 32);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) {
+                const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
+                                  both(p.scale2), both(-st.x));
+                s[c] = __float_as_uint(exp2_fast(x.x));
+                s[c + 1] = __float_as_uint(exp2_fast(x.y));
+            }
+            ok = wait_warp(dp_full, i & 1, gave_up);
+            if (!ok) break;
+            tmem_after();
+            tmem_load32(dp_tm + 64 * side + lanes, d);
+            tmem_load32(dp_tm + 64 * side + 32 + lanes, d + 32);
+            tmem_wait_loads();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(dp_read);
+            uint32_t w[32];
+            // the last key of this half that the row sees; a row that sees one has P = 1 and
+            // dS = 0, and D, of the rounded o, would leave a rounding
+            const int seen = i ? 64 : row ? row - (n - 1) * kTile - 64 * side : -1;
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) {
+                const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
+                                  both(shift.grads), both(-st.y * shift.grads));
+                F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
+                if (c > seen) v.x = 0.f;
+                if (c + 1 > seen) v.y = 0.f;
+                w[c / 2] = pack2<T>(v.x, v.y);
+            }
+            tmem_store16(s_tm, w);
+            tmem_store16(s_tm + 16, w + 16);
+            tmem_wait_stores();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(ds_full);
+        }
+        if (any) {
+            if (ok) ok = wait_warp(dq_full, 0, gave_up);
+            tmem_after();
+            T *out = static_cast<T *>(p.dq) + (u.start + (int64_t)row) * p.d_token[0] +
+                     head * p.d_head[0];
+            const bool good =
+                write_sums<T>(dq_tm + lanes, side,
+                              ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu), out, live,
+                              p.d_vectors[0], p.dim, p.dim_out);
+            const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
+            if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            sums_barrier();
+            uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
+            while (rows) {
+                const int i = __ffs(rows) - 1;
+                rows &= rows - 1;
+                dq_row<T>(p, u, row - lane + i, head, lane);
+            }
+        }
+    }
+    __syncthreads();
+    if (*gave_up) {  // copies and products may still be on their way
+        const uint64_t t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    tmem_before();
+    __syncthreads();
+    if (warp == 9) {
+        tmem_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of the keys and values
+// ---------------------------------------------------------------------------
+// A block takes 128 keys of a key head and goes over the queries that see them, one
+// query head of the group after another.  Everything is transposed: a thread's row is
+// a key, so P and dS are the products' first operands as they stand in TMEM.  TMEM holds
+// scores, dP, and both sums, and is full: P takes the scores' place and dS that of dP,
+// and while one of them is made, the tensor cores use up the other and compute what
+// comes next in its place.
+constexpr int kQuerySlots = 2;
+constexpr int kStatBytes = kTile * 8;
+constexpr int kDkvBars = 6 * kQuerySlots + 6;
+constexpr int kDkvSmem = 1024 + (2 + 2 * kQuerySlots) * kTileBytes + kQuerySlots * kStatBytes +
+                         8 * kDkvBars + 32;
+
+template <typename T>
+__device__ __forceinline__ void dkv_row(const AttnParams &p, const AttnUnit &u, int row, int g,
+                                        int lane) {
+    const T *k = row_at<T>(p.k, u.start + row, g), *v = row_at<T>(p.v, u.start + row, g);
+    RowPart dk = {}, dv = {};
+    for (int head = g * p.group; head < (g + 1) * p.group; ++head)
+        for (int i0 = row; i0 < u.len; i0 += 32) {
+            const int i = i0 + lane, n = min(32, u.len - i0);
+            float e = 0.f, ds = 0.f;
+            if (i < u.len) {
+                const float2 st = p.stats[head * p.tokens + u.start + i];
+                e = exp2f(dot_rows(row_at<T>(p.q, u.start + i, head), k, p.dim) * p.scale2 -
+                          (st.x + Shift<T>::kProbs));
+                if (i) ds = e * (dot_rows(row_at<T>(p.g, u.start + i, head), v, p.dim) - st.y);
+            }
+            for (int t = 0; t < n; ++t) {
+                add_row(dv, __shfl_sync(0xffffffffu, e, t), row_at<T>(p.g, u.start + i0 + t, head),
+                        p.dim, lane);
+                add_row(dk, __shfl_sync(0xffffffffu, ds, t), row_at<T>(p.q, u.start + i0 + t, head),
+                        p.dim, lane);
+            }
+        }
+    write_row<T>(p.dk, (u.start + row) * p.d_token[1] + g * p.d_head[1], dk, p.scale, p.dim_out,
+                 lane);
+    write_row<T>(p.dv, (u.start + row) * p.d_token[2] + g * p.d_head[2], dv, 1.f, p.dim_out, lane);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBackThreads, 1)
+    attn_dkv_kernel(const __grid_constant__ CUtensorMap q_map,
+                    const __grid_constant__ CUtensorMap k_map,
+                    const __grid_constant__ CUtensorMap v_map,
+                    const __grid_constant__ CUtensorMap g_map, const AttnParams p) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char *aligned = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t k_at = base, v_at = k_at + kTileBytes, q_at = v_at + kTileBytes;
+    const uint32_t g_at = q_at + kQuerySlots * kTileBytes;
+    const uint32_t st_at = g_at + kQuerySlots * kTileBytes;
+    const uint32_t bars = st_at + kQuerySlots * kStatBytes;
+    const uint32_t q_full = bars, q_empty = q_full + 8 * kQuerySlots;
+    const uint32_t g_full = q_empty + 8 * kQuerySlots, g_empty = g_full + 8 * kQuerySlots;
+    const uint32_t st_full = g_empty + 8 * kQuerySlots, st_empty = st_full + 8 * kQuerySlots;
+    const uint32_t in_full = st_empty + 8 * kQuerySlots, s_full = in_full + 8, dp_full = s_full + 8;
+    const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, out_full = ds_full + 8;
+    const uint32_t slot = out_full + 8;
+    unsigned char *tail = aligned + (slot - base);
+    volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
+    uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kDkvBars; ++i) {
+            const uint32_t b = bars + 8 * i;
+            bar_init(b, b == p_full || b == ds_full || (b >= st_empty && b < in_full) ? 8 : 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gave_up = 0;
+        for (int i = 0; i < 4; ++i) bad[i] = 0;
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
+                     "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        tmem_before();
+    }
+    __syncthreads();
+    tmem_after();
+    grid_dep_wait();
+    grid_dep_trigger();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
+    const uint32_t dp_tm = tmem + kTile, dv_tm = tmem + 2 * kTile, dk_tm = tmem + 3 * kTile;
+
+    const int g = blockIdx.x % p.heads_k;
+    AttnUnit u;
+    const bool any = unit_at<kTile>(p, blockIdx.x / p.heads_k, u);
+    // the list is in the order of a query tile's keys; of a key tile's queries it is this
+    const int tiles = any ? (u.len + kTile - 1) / kTile : 0;
+    if (any) u.tile = tiles - 1 - u.tile;
+    const int each = any ? tiles - u.tile : 0;  // tiles of queries of a head
+    const int n = each * p.group;
+    const int boxes = p.dim > 64 ? 2 : 1;
+    bool ok = true;
+
+    if (group == 2) {
+        give_registers<kBackIssueRegs>();
+        if (warp == 8) {
+            if (lane == 0 && any) {
+                bar_expect(in_full, 2 * boxes * kBox);
+                for (int b = 0; b < boxes; ++b) {
+                    const int token = u.start + u.tile * kTile;
+                    tma_rows(k_at + b * kBox, &k_map, 64 * b, g, token, in_full);
+                    tma_rows(v_at + b * kBox, &v_map, 64 * b, g, token, in_full);
+                }
+                int s = 0;
+                uint32_t ph = 1;
+                for (int i = 0; i < n && ok; ++i) {
+                    const int head = g * p.group + i / each;
+                    const int token = u.start + (u.tile + i % each) * kTile;
+                    for (int w = 0; w < 2 && ok; ++w) {
+                        const uint32_t full = (w ? g_full : q_full) + 8 * s;
+                        ok = bar_wait((w ? g_empty : q_empty) + 8 * s, ph, gave_up);
+                        if (!ok) break;
+                        bar_expect(full, boxes * kBox);
+                        for (int b = 0; b < boxes; ++b)
+                            tma_rows((w ? g_at : q_at) + s * kTileBytes + b * kBox,
+                                     w ? &g_map : &q_map, 64 * b, head, token, full);
+                    }
+                    if (++s == kQuerySlots) s = 0, ph ^= 1;
+                }
+            }
+        } else if (warp == 9) {
+            const auto arrived = [&](uint32_t full, uint32_t at, int i) {
+                const int s = i % kQuerySlots;
+                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, gave_up)) return false;
+                const int seen = u.len - (u.tile + i % each) * kTile;
+                if (seen < kTile) zero_rows(at + s * kTileBytes, seen, boxes, lane);
+                return true;
+            };
+            const auto scores = [&](int i) {
+                if (!arrived(q_full, q_at, i)) return false;
+                if (lane == 0) {
+                    mma_rows<T>(tmem, k_at, q_at + i % kQuerySlots * kTileBytes, p.dim);
+                    commit(s_full);
+                }
+                return true;
+            };
+            const auto grads = [&](int i) {  // dP
+                if (!arrived(g_full, g_at, i)) return false;
+                if (lane == 0) {
+                    mma_rows<T>(dp_tm, v_at, g_at + i % kQuerySlots * kTileBytes, p.dim);
+                    commit(dp_full);
+                }
+                return true;
+            };
+            if (any) {
+                ok = wait_warp(in_full, 0, gave_up);
+                tmem_after();
+                ok = ok && scores(0) && grads(0);
+            }
+            for (int i = 0; i < n && ok; ++i) {
+                const int s = i % kQuerySlots;
+                ok = wait_warp(p_full, i & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                if (lane == 0) {
+                    mma_halves<T>(dv_tm, tmem, g_at + s * kTileBytes, p.dim, i > 0);
+                    commit(g_empty + 8 * s);
+                }
+                __syncwarp();
+                if (i + 1 < n) ok = scores(i + 1);
+                ok = ok && wait_warp(ds_full, i & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                if (lane == 0) {
+                    mma_halves<T>(dk_tm, dp_tm, q_at + s * kTileBytes, p.dim, i > 0);
+                    commit(q_empty + 8 * s);
+                    if (i == n - 1) commit(out_full);
+                }
+                __syncwarp();
+                if (i + 1 < n) ok = grads(i + 1);
+            }
+        } else if (warp == 10) {
+            // lse and D of the queries; none for rows past the sequence: their
+            // probabilities are 2^(0 - inf) = 0
+            const Shift<T> shift(p);
+            for (int i = 0; i < n && ok; ++i) {
+                const int s = i % kQuerySlots, head = g * p.group + i / each;
+                const int row = (u.tile + i % each) * kTile;
+                const float2 *from = p.stats + head * p.tokens + u.start + row;
+                float2 st[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    st[h] = row + lane + 32 * h < u.len
+                                ? from[lane + 32 * h]
+                                : make_float2(__uint_as_float(0x7f800000u), 0.f);
+                ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, gave_up);
+                if (!ok) break;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)  // -lse in the first half, -D in the second
+                    asm volatile("st.shared.f32 [%0], %1;\nst.shared.f32 [%0 + 512], %2;" ::"r"(
+                                     st_at + s * kStatBytes + 4 * (lane + 32 * h)),
+                                 "f"(-st[h].x), "f"(-st[h].y * shift.grads)
+                                 : "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(st_full + 8 * s);
+            }
+        }
+        __syncwarp();
+    } else {
+        take_registers<kBackRegs>();
+        const Shift<T> shift(p);
+        const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t s_tm = tmem + 64 * side + lanes, d_tm = dp_tm + 64 * side + lanes;
+        const bool live = any && row < u.len;
+        for (int i = 0; i < n; ++i) {
+            const int slot_i = i % kQuerySlots;
+            const uint32_t st = st_at + slot_i * kStatBytes + 256 * side;
+            // queries of this half before the first that sees the key
+            const int unseen = i % each ? 0 : mine - 64 * side;
+            // (dS of the row that sees one key is 0, as above)
+            const int no_grad = row ? unseen : i % each ? 0 : 1 - 64 * side;
+            ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, gave_up) &&
+                 wait_warp(s_full, i & 1, gave_up);
+            if (!ok) break;
+            tmem_after();
+            uint32_t s[64], d[64], w[32];
+            tmem_load32(s_tm, s);
+            tmem_load32(s_tm + 32, s + 32);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                float4 l;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
+                             : "r"(st + 4 * c));
+                const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
+                                  both(p.scale2), {l.x, l.y});
+                const F2 y = fma2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])},
+                                  both(p.scale2), {l.z, l.w});
+                float e[4] = {exp2_fast(x.x), exp2_fast(x.y), exp2_fast(y.x), exp2_fast(y.y)};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    if (c + h < unseen) e[h] = 0.f;
+                    s[c + h] = __float_as_uint(e[h]);
+                }
+                w[c / 2] = pack2<T>(e[0], e[1]);
+                w[c / 2 + 1] = pack2<T>(e[2], e[3]);
+            }
+            tmem_store16(s_tm, w);
+            tmem_store16(s_tm + 16, w + 16);
+            tmem_wait_stores();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full);
+            ok = wait_warp(dp_full, i & 1, gave_up);
+            if (!ok) break;
+            tmem_after();
+            tmem_load32(d_tm, d);
+            tmem_load32(d_tm + 32, d + 32);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                float4 l;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
+                             : "r"(st + 512 + 4 * c));
+                const F2 x = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
+                                  both(shift.grads), {l.x, l.y});
+                const F2 y = fma2({__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])},
+                                  both(shift.grads), {l.z, l.w});
+                const F2 a = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, x);
+                const F2 b = mul2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])}, y);
+                float e[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (c + h < no_grad) e[h] = 0.f;
+                w[c / 2] = pack2<T>(e[0], e[1]);
+                w[c / 2 + 1] = pack2<T>(e[2], e[3]);
+            }
+            tmem_store16(d_tm, w);
+            tmem_store16(d_tm + 16, w + 16);
+            tmem_wait_stores();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive(ds_full);
+                bar_arrive(st_empty + 8 * slot_i);
+            }
+        }
+        if (any) {
+            if (ok) ok = wait_warp(out_full, 0, gave_up);
+            tmem_after();
+            const int64_t token = u.start + (int64_t)row;
+            const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
+            bool good = write_sums<T>(dk_tm + lanes, side, ok ? p.scale * shift.undo : lost,
+                                      static_cast<T *>(p.dk) + token * p.d_token[1] + g * p.d_head[1],
+                                      live, p.d_vectors[1], p.dim, p.dim_out);
+            good &= write_sums<T>(dv_tm + lanes, side, ok ? Shift<T>::kUndoProbs : lost,
+                                  static_cast<T *>(p.dv) + token * p.d_token[2] + g * p.d_head[2],
+                                  live, p.d_vectors[2], p.dim, p.dim_out);
+            const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
+            if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            sums_barrier();
+            uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
+            while (rows) {
+                const int i = __ffs(rows) - 1;
+                rows &= rows - 1;
+                dkv_row<T>(p, u, row - lane + i, g, lane);
+            }
+        }
+    }
+    __syncthreads();
+    if (*gave_up) {  // copies and products may still be on their way
+        const uint64_t t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    tmem_before();
+    __syncthreads();
+    if (warp == 9) {
+        tmem_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+template <typename T>
+static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaStream_t s) {
+    CUtensorMap q, k, v, g;
+    POS_TRY(attn_map(&q, a, p.q, p.heads_q, p.dim));
+    POS_TRY(attn_map(&k, a, p.k, p.heads_k, p.dim));
+    POS_TRY(attn_map(&v, a, p.v, p.heads_k, p.dim));
+    POS_TRY(attn_map(&g, a, p.g, p.heads_q, p.dim));
+    int grid_q = 0, grid_k = 0;
+    POS_TRY(attn_grid(a, kTile, a->heads_q, &grid_q));
+    POS_TRY(attn_grid(a, kTile, a->heads_k, &grid_k));
+    if (grid_q == 0) return POS_OK;
+    if (std::is_same<T, __half>::value) POS_CUDA(cudaMemsetAsync(p.largest, 0, 4, s));
+    POS_CUDA(launch_dependent(attn_stats_kernel<T>, grid_q, 256, 0, s, p));
+    auto dq = attn_dq_kernel<T>;
+    POS_TRY(ensure_smem(reinterpret_cast<const void *>(dq), kDqSmem));
+    POS_CUDA(launch_dependent(dq, grid_q, kBackThreads, kDqSmem, s, q, k, v, g, p));
+    auto dkv = attn_dkv_kernel<T>;
+    POS_TRY(ensure_smem(reinterpret_cast<const void *>(dkv), kDkvSmem));
+    POS_CUDA(launch_dependent(dkv, grid_k, kBackThreads, kDkvSmem, s, q, k, v, g, p));
+    return POS_OK;
+}
+
+static int64_t stats_bytes(const pos_attn *a) {
+    return 16 + (a->tokens * a->heads_q * 8 + 15) / 16 * 16;
+}
+
+static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_heads &d_o,
+                           AttnParams p, char *at, cudaStream_t s) {
+    p.largest = reinterpret_cast<uint32_t *>(at);
+    p.stats = reinterpret_cast<float2 *>(at + 16);
+    at += stats_bytes(a);
+    const pos_heads t[4] = {x[0], x[1], x[2], d_o};
+    const int64_t heads[4] = {a->heads_q, a->heads_k, a->heads_k, a->heads_q};
+    AttnTensor *to[4] = {&p.q, &p.k, &p.v, &p.g};
+    for (int i = 0; i < 4; ++i) POS_TRY(attn_input(a, t[i], heads[i], &at, s, to[i]));
+    POS_TRY(attn_list(a, kTile, &at, s, &p));
+    return a->dtype == POS_BF16 ? launch_backward<__nv_bfloat16>(a, p, s)
+                                : launch_backward<__half>(a, p, s);
+}
+
+}  // namespace pos
+
+extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_heads *x,
+                                             const pos_heads *o, const float *d_lse,
+                                             const pos_heads *d_o, const pos_heads *dx,
+                                             void *stream) {
+    using namespace pos;
+    return guarded([&]() -> pos_status {
+        AttnParams p = {};
+        POS_TRY(check_attn(attn, &p));
+        if (!x || !o || !d_o || !dx) return fail(POS_EINVAL, "attention: NULL pointer");
+        const int64_t heads[4] = {attn->heads_q, attn->heads_k, attn->heads_k, attn->heads_q};
+        const char *names[3] = {"the queries", "the keys", "the values"};
+        for (int i = 0; i < 3; ++i) {
+            POS_TRY(check_attn_tensor(attn, x[i], heads[i], names[i], false));
+            POS_TRY(check_attn_tensor(attn, dx[i], heads[i],
+                                      (std::string("the gradients of ") + names[i]).c_str(), true));
+        }
+        POS_TRY(check_attn_tensor(attn, *o, attn->heads_q, "o", false));
+        POS_TRY(check_attn_tensor(attn, *d_o, attn->heads_q, "o's gradient", false));
+        if (reinterpret_cast<uintptr_t>(d_lse) % 4)
+            return fail(POS_EINVAL, "attention: misaligned lse");
+        if (attn->tokens == 0 || attn->heads_q == 0) return POS_OK;
+        if (!d_lse) return fail(POS_EINVAL, "attention: NULL lse");
+        p.o = {o->data, o->token_stride, o->head_stride};
+        p.lse = const_cast<float *>(d_lse);
+        void **out[3] = {&p.dq, &p.dk, &p.dv};
+        for (int i = 0; i < 3; ++i) {
+            *out[i] = dx[i].data, p.d_token[i] = dx[i].token_stride, p.d_head[i] = dx[i].head_stride;
+            p.d_vectors[i] = aligned16(dx[i].data) && dx[i].token_stride % 8 == 0 &&
+                             dx[i].head_stride % 8 == 0;
+        }
+        int64_t bytes = stats_bytes(attn) + attn_list_bytes(attn, kTile);
+        for (int i = 0; i < 4; ++i)
+            if (!attn_direct(attn, i < 3 ? x[i] : *d_o, heads[i]))
+                bytes += attn_copy_bytes(attn, heads[i]);
+        const auto s = static_cast<cudaStream_t>(stream);
+        void *scratch = nullptr;
+        POS_TRY(attn_scratch(bytes, s, &scratch));
+        const pos_status st = backward(attn, x, *d_o, p, static_cast<char *>(scratch), s);
+        const cudaError_t e = cudaFreeAsync(scratch, s);
+        if (st != POS_OK) return st;
+        return e == cudaSuccess ? POS_OK : cuda_fail(e, "attention scratch");
+    });
+}
