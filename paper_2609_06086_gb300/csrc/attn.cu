@@ -228,16 +228,16 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     }
             }
         } else if (warp == 9) {
+            const uint32_t mine = one_lane();
+            const int steps = (p.dim + 15) / 16;
             // the i-th tile of keys or values to arrive: keys 2 i, values 2 i + 1
             const auto arrived = [&](int i) {
                 return wait_warp(kv_full + 8 * (i % kSlots), i / kSlots & 1, gave_up);
             };
             const auto scores = [&](int t, int i) {  // i: steps of keys from the first on
-                if (lane == 0) {
-                    mma_rows<T>(tmem + t * kTile, q_at + t * kTileBytes,
-                                kv_at + 2 * i % kSlots * kTileBytes, p.dim);
-                    commit(s_full + 8 * t);
-                }
+                mma_rows<T>(tmem + t * kTile, q_at + t * kTileBytes,
+                            kv_at + 2 * i % kSlots * kTileBytes, steps, mine);
+                commit(s_full + 8 * t, mine);
             };
             if (any) {
                 ok = wait_warp(q_full, 0, gave_up) && (!n1 || wait_warp(q_full + 8, 0, gave_up)) &&
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 if (ok) {
                     if (first < n0) scores(0, 0);
                     if (first < n1) scores(1, 0);
-                    if (lane == 0) commit(kv_empty);
+                    commit(kv_empty, mine);
                 }
             }
             uint32_t ph[2] = {0, 0};
@@ -257,26 +257,22 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 const int seen = u.len - j * kTile;
                 if (seen < kTile) zero_rows(v_at, seen, boxes, lane);
                 if (j > 0) ok = arrived(2 * i + 2);
-                for (int t = 0; t < 2 && ok; ++t) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
                     const int n = t ? n1 : n0;
-                    if (j < n) {
+                    if (j < n && ok) {
                         ok = wait_warp(p_full + 8 * t, ph[t], gave_up);
                         if (!ok) break;
                         ph[t] ^= 1;
                         tmem_after();
-                        if (lane == 0) {
-                            mma_columns<T>(tmem + 2 * kTile + t * kTile, tmem + t * kTile, v_at,
-                                           p.dim, j < n - 1);
-                            if (j == 0) commit(o_full + 8 * t);
-                        }
+                        mma_columns<T>(tmem + 2 * kTile + t * kTile, tmem + t * kTile, v_at, steps,
+                                       j < n - 1, mine);
+                        if (j == 0) commit(o_full + 8 * t, mine);
                     }
-                    if (j > 0 && j - 1 < n) scores(t, i + 1);
+                    if (j > 0 && j - 1 < n && ok) scores(t, i + 1);
                 }
-                if (lane == 0) {
-                    commit(kv_empty + 8 * ((2 * i + 1) % kSlots));
-                    if (j > 0) commit(kv_empty + 8 * ((2 * i + 2) % kSlots));
-                }
-                __syncwarp();
+                commit(kv_empty + 8 * ((2 * i + 1) % kSlots), mine);
+                if (j > 0) commit(kv_empty + 8 * ((2 * i + 2) % kSlots), mine);
             }
         }
         __syncwarp();
@@ -304,10 +300,18 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 for (int c = 0; c < kTile; ++c)
                     if (c > seen) s[c] = 0xff800000u;
             }
-            float m = __uint_as_float(s[0]);
+            float part[4];  // (four chains: one of 128 steps is longer than the exponentials)
 #pragma unroll
-            for (int c = 1; c < kTile; ++c) m = fmaxf(m, __uint_as_float(s[c]));
-            m *= p.scale2;
+            for (int c = 0; c < 4; ++c) part[c] = max3(s[c], s[c + 4], s[c + 8]);
+#pragma unroll
+            for (int c = 12; c + 8 <= kTile; c += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    part[e] = max3(__float_as_uint(part[e]), s[c + e], s[c + e + 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[e] = fmaxf(part[e], __uint_as_float(s[kTile - 4 + e]));
+            const float m =
+                fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * p.scale2;
             if (j == n - 1) {
                 top = m;
             } else {
@@ -329,7 +333,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     }
                 }
             }
-            F2 sum = both(0.f);
+            F2 sum[4] = {};
 #pragma unroll
             for (int c = 0; c < kTile; c += 32) {
                 uint32_t w[16];
@@ -338,12 +342,13 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     const F2 x = fma2({__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])},
                                       both(p.scale2), both(-top));
                     const F2 y = {exp2_fast(x.x), exp2_fast(x.y)};
-                    sum = fma2(y, both(1.f), sum);
+                    sum[e % 4] = add2(sum[e % 4], y);
                     w[e] = pack2<T>(y.x, y.y);
                 }
                 tmem_store16(s_tm + c / 2, w);
             }
-            total += sum.x + sum.y;
+            const F2 a = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+            total += a.x + a.y;
             tmem_wait_stores();
             tmem_before();
             __syncwarp();

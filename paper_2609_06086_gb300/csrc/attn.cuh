@@ -72,16 +72,23 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *map, i
         "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar)
         : "memory");
 }
-// Operand descriptors of a tile in shared memory: blocks of 64 columns, 128 bytes a
-// row, swizzled.  by_rows: the row's elements are the products' inner index (16 of
-// them 32 bytes on); by_columns: the rows are (16 of them 2048 bytes on).
-__device__ __forceinline__ uint64_t by_rows(uint32_t addr) {
-    return (uint64_t)(addr >> 4 & 0x3fffu) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
-           2ull << 61;
+// Products are issued by one thread of a warp whose lanes all run the code, so that
+// the operands' descriptors are computed in uniform registers: issued in a branch that
+// one lane takes, a product of 128 x 128 x 16 took 90 to 130 cycles to issue, and 64 to
+// compute.
+__device__ __forceinline__ uint32_t one_lane() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r;
 }
-__device__ __forceinline__ uint64_t by_columns(uint32_t addr) {
-    return (uint64_t)(addr >> 4 & 0x3fffu) | (uint64_t)(kBox >> 4) << 16 |
-           (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// Operand descriptors of a tile in shared memory: blocks of 64 columns, 128 bytes a
+// row, swizzled.  Low words: rows whose elements are the products' inner index (16 of
+// them 32 bytes on), and rows that are the inner index themselves (16 of them 2048
+// bytes on, the next 64 columns a block on).  High words are alike.
+constexpr uint32_t kDescHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t by_rows(uint32_t addr) { return addr >> 4 | 1u << 16; }
+__device__ __forceinline__ uint32_t by_columns(uint32_t addr) {
+    return addr >> 4 | (uint32_t)(kBox >> 4) << 16;
 }
 // f32 sums of 16-bit products, 128 rows, n columns.
 template <typename T>
@@ -91,46 +98,53 @@ __device__ __forceinline__ uint32_t product_of(int n, bool b_by_columns) {
            (uint32_t)(n >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
 }
 // Both operands in shared memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t add) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       uint32_t add, uint32_t mine) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        "{\n.reg .pred p, q;\n.reg .b64 a, b;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+        "mov.b64 a, {%1, %6};\nmov.b64 b, {%2, %6};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(mine), "r"(kDescHigh)
         : "memory");
 }
 // The first operand in TMEM: two elements of a row in a column's word.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       uint32_t add, uint32_t mine) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(add)
+        "{\n.reg .pred p, q;\n.reg .b64 b;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+        "mov.b64 b, {%2, %6};\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(mine), "r"(kDescHigh)
         : "memory");
 }
-// d (+)= A B^T over `dim` elements of the rows of two tiles.
+// d = A B^T over 16 `steps` elements of the rows of two tiles.
 template <typename T>
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, int dim) {
-    const uint32_t idesc = product_of<T>(kTile, false);
-    const uint64_t da = by_rows(a), db = by_rows(b);
-    for (int k = 0; k < dim; k += 16) {
-        const uint32_t at = (k / 64 * kBox + k % 64 * 2) >> 4;
-        mma_ss(d, da + at, db + at, idesc, k > 0);
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, int steps,
+                                         uint32_t mine) {
+    const uint32_t idesc = product_of<T>(kTile, false), da = by_rows(a), db = by_rows(b);
+#pragma unroll
+    for (int k = 0; k < kAttnMaxDim / 16; ++k) {
+        const uint32_t at = (k / 4 * kBox + k % 4 * 32) >> 4;
+        if (k < steps) mma_ss(d, da + at, db + at, idesc, k > 0, mine);
     }
 }
-// d (+)= A B, A [128][128] in TMEM, B the rows of a tile, `dim` columns of it.
-template <typename T>
-__device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b, int dim, bool add) {
-    const uint32_t idesc = product_of<T>((dim + 15) / 16 * 16, true);
-    const uint64_t db = by_columns(b);
+// d (+)= A B, A [128][128] in TMEM, `part` columns of it one after another and then as many
+// unused, B the rows of a tile, 16 `steps` columns of it.
+template <typename T, int PART = kTile>
+__device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b, int steps, bool add,
+                                            uint32_t mine) {
+    const uint32_t idesc = product_of<T>(16 * steps, true), db = by_columns(b);
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        mma_ts(d, a + 8 * k, db + k * (2048 >> 4), idesc, add || k > 0);
+        mma_ts(d, a + (16 * k / PART * PART + 16 * k % PART / 2), db + k * (2048 >> 4), idesc,
+               add || k > 0, mine);
 }
 // Arrives on a barrier once the products issued so far are done.
-__device__ __forceinline__ void commit(uint32_t bar) {
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t mine) {
     asm volatile(
-        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+        "{\n.reg .pred q;\nsetp.ne.u32 q, %1, 0;\n"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+        "r"(mine)
         : "memory");
 }
 __device__ __forceinline__ void tmem_before() {
@@ -181,6 +195,21 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c) {  // bits of f32
+    float r;
+    asm("max.f32 %0, %1, %2, %3;"
+        : "=f"(r)
+        : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("{\n.reg .b64 a, b, r;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\n"
+        "add.rn.f32x2 r, a, b;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
 }
 // Two values rounded to 16 bits, the first in the low half.
 template <typename T>

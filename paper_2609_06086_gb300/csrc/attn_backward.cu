@@ -7,8 +7,12 @@ namespace pos {
 // by blocks that go over the keys, the keys' and values' by blocks that go over the
 // queries.  Scores and their gradients are computed in both: seven products instead of
 // the five of a single pass, which would add up the queries' gradients across blocks.
-constexpr int kBackThreads = 3 * 128;  // two warpgroups of sums, one of loads and products
-constexpr int kBackRegs = 208, kBackIssueRegs = 88;  // 2 * 208 + 88 = 3 * 168
+constexpr int kSumGroups = 4;            // warpgroups of sums, a quarter of the columns each
+constexpr int kCols = kTile / kSumGroups;  // columns of a tile that a thread takes
+constexpr int kBackThreads = 128 * (kSumGroups + 1);  // and one of loads and products
+// 4 * 104 + 64 = 480 = 5 * 96, what the block is launched with
+constexpr int kBackRegs = 104, kBackIssueRegs = 64;
+constexpr int kLoadWarp = 4 * kSumGroups, kIssueWarp = kLoadWarp + 1, kStatsWarp = kLoadWarp + 2;
 
 // f16 holds probabilities of long rows and small gradients badly (below 2^-14 with
 // fewer bits, below 2^-25 not at all).  There P is multiplied by 2^12 and dS by 2^k, k the
@@ -67,24 +71,13 @@ __global__ void __launch_bounds__(256) attn_stats_kernel(const AttnParams p) {
     }
 }
 
-// d (+)= A B, A [128][128] in TMEM: each half of its columns from where the warps
-// that computed it had read their scores.
-template <typename T>
-__device__ __forceinline__ void mma_halves(uint32_t d, uint32_t a, uint32_t b, int dim, bool add) {
-    const uint32_t idesc = product_of<T>((dim + 15) / 16 * 16, true);
-    const uint64_t db = by_columns(b);
-#pragma unroll
-    for (int k = 0; k < kTile / 16; ++k)
-        mma_ts(d, a + (k / 4 * 64 + k % 4 * 8), db + k * (2048 >> 4), idesc, add || k > 0);
-}
-
-// Sums from TMEM to a row of the output: 16 columns at a time, those of half `side` of
-// the pairs of 16.  Whether all are finite.
+// Sums from TMEM to a row of the output: 16 columns at a time, every kSumGroups-th of
+// them.  Whether all are finite.
 template <typename T>
 __device__ __forceinline__ bool write_sums(uint32_t tm, int side, float factor, T *out, bool live,
                                            bool vectors, int dim, int dim_out) {
     bool good = true;
-    for (int c = 16 * side; c < dim; c += 32) {
+    for (int c = 16 * side; c < dim; c += 16 * kSumGroups) {
         uint32_t v[16];
         tmem_load16(tm + c, v);
         tmem_wait_loads();
@@ -103,16 +96,16 @@ __device__ __forceinline__ bool write_sums(uint32_t tm, int side, float factor, 
     }
     return good;
 }
-__device__ __forceinline__ void sums_barrier() {  // of the two warpgroups of sums
-    asm volatile("barrier.sync 1, 256;" ::: "memory");
+__device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
+    asm volatile("barrier.sync 1, %0;" ::"n"(128 * kSumGroups) : "memory");
 }
 
 // ---------------------------------------------------------------------------
 // Gradients of the queries
 // ---------------------------------------------------------------------------
 // A block takes 128 queries of a head and goes over the keys from the diagonal down.
-// TMEM: two places of scores, one of dP = dO V^T, the sums.  While two warpgroups
-// (64 columns of a row a thread) make dS = P (dP - D) of a tile, the tensor cores compute
+// TMEM: two places of scores, one of dP = dO V^T, the sums.  While four warpgroups
+// (32 columns of a row a thread) make dS = P (dP - D) of a tile, the tensor cores compute
 // the next scores, and dP as soon as the last one has been read.
 constexpr int kKeySlots = 3, kValueSlots = 2;
 constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
@@ -167,13 +160,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDqBars; ++i) {
             const bool sums = bars + 8 * i == dp_read || bars + 8 * i == ds_full;
-            bar_init(bars + 8 * i, sums ? 8 : 1);
+            bar_init(bars + 8 * i, sums ? 4 * kSumGroups : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gave_up = 0;
         for (int i = 0; i < 4; ++i) bad[i] = 0;
     }
-    if (warp == 9) {
+    if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
                      "r"(512)
                      : "memory");
@@ -194,9 +187,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const int boxes = p.dim > 64 ? 2 : 1;
     bool ok = true;
 
-    if (group == 2) {
+    if (group == kSumGroups) {
         give_registers<kBackIssueRegs>();
-        if (warp == 8) {
+        if (warp == kLoadWarp) {
             if (lane == 0 && any) {
                 bar_expect(in_full, 2 * boxes * kBox);
                 for (int b = 0; b < boxes; ++b) {
@@ -225,27 +218,25 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                         ok = load(v_full, v_empty, v_at, &v_map, sv, phv, kValueSlots, n - i);
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == kIssueWarp) {
+            const uint32_t mine = one_lane();
+            const int steps = (p.dim + 15) / 16;
             const auto scores = [&](int i) {
                 if (!wait_warp(k_full + 8 * (i % kKeySlots), i / kKeySlots & 1, gave_up))
                     return false;
                 const uint32_t at = k_at + i % kKeySlots * kTileBytes;
                 const int seen = u.len - (n - 1 - i) * kTile;
                 if (seen < kTile) zero_rows(at, seen, boxes, lane);
-                if (lane == 0) {
-                    mma_rows<T>(tmem + i % 2 * kTile, q_at, at, p.dim);
-                    commit(s_full + 8 * (i % 2));
-                }
+                mma_rows<T>(tmem + i % 2 * kTile, q_at, at, steps, mine);
+                commit(s_full + 8 * (i % 2), mine);
                 return true;
             };
             const auto grads = [&](int i) {  // dP
                 if (!wait_warp(v_full + 8 * (i % kValueSlots), i / kValueSlots & 1, gave_up))
                     return false;
-                if (lane == 0) {
-                    mma_rows<T>(dp_tm, g_at, v_at + i % kValueSlots * kTileBytes, p.dim);
-                    commit(dp_full);
-                    commit(v_empty + 8 * (i % kValueSlots));
-                }
+                mma_rows<T>(dp_tm, g_at, v_at + i % kValueSlots * kTileBytes, steps, mine);
+                commit(dp_full, mine);
+                commit(v_empty + 8 * (i % kValueSlots), mine);
                 return true;
             };
             if (any) {
@@ -263,13 +254,10 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 ok = wait_warp(ds_full, i & 1, gave_up);
                 if (!ok) break;
                 tmem_after();
-                if (lane == 0) {
-                    mma_halves<T>(dq_tm, tmem + i % 2 * kTile, k_at + i % kKeySlots * kTileBytes,
-                                  p.dim, i > 0);
-                    commit(k_empty + 8 * (i % kKeySlots));
-                    if (i == n - 1) commit(dq_full);
-                }
-                __syncwarp();
+                mma_columns<T, kCols>(dq_tm, tmem + i % 2 * kTile,
+                                      k_at + i % kKeySlots * kTileBytes, steps, i > 0, mine);
+                commit(k_empty + 8 * (i % kKeySlots), mine);
+                if (i == n - 1) commit(dq_full, mine);
                 if (i + 2 < n) ok = scores(i + 2);
             }
         }
@@ -283,16 +271,15 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const Shift<T> shift(p);
         if (live) st = p.stats[head * p.tokens + u.start + row];
         for (int i = 0; i < n; ++i) {
-            const uint32_t s_tm = tmem + i % 2 * kTile + 64 * side + lanes;
+            const uint32_t s_tm = tmem + i % 2 * kTile + kCols * side + lanes;
             ok = ok && wait_warp(s_full + 8 * (i % 2), i / 2 & 1, gave_up);
             if (!ok) break;
             tmem_after();
-            uint32_t s[64], d[64];
+            uint32_t s[kCols], d[kCols];
             tmem_load32(s_tm, s);
-            tmem_load32(s_tm + 32, s + 32);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
+            for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
                                   both(p.scale2), both(-st.x));
                 s[c] = __float_as_uint(exp2_fast(x.x));
@@ -301,27 +288,31 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             ok = wait_warp(dp_full, i & 1, gave_up);
             if (!ok) break;
             tmem_after();
-            tmem_load32(dp_tm + 64 * side + lanes, d);
-            tmem_load32(dp_tm + 64 * side + 32 + lanes, d + 32);
+            tmem_load32(dp_tm + kCols * side + lanes, d);
             tmem_wait_loads();
             tmem_before();
             __syncwarp();
             if (lane == 0) bar_arrive(dp_read);
-            uint32_t w[32];
-            // the last key of this half that the row sees; a row that sees one has P = 1 and
+            uint32_t w[kCols / 2];
+            // the last key of this part that the row sees; a row that sees one has P = 1 and
             // dS = 0, and D, of the rounded o, would leave a rounding
-            const int seen = i ? 64 : row ? row - (n - 1) * kTile - 64 * side : -1;
+            const int seen = i ? kCols : row ? row - (n - 1) * kTile - kCols * side : -1;
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
+            for (int c = 0; c < kCols; c += 2) {
                 const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
                                   both(shift.grads), both(-st.y * shift.grads));
-                F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
-                if (c > seen) v.x = 0.f;
-                if (c + 1 > seen) v.y = 0.f;
-                w[c / 2] = pack2<T>(v.x, v.y);
+                const F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
+                s[c] = __float_as_uint(v.x), s[c + 1] = __float_as_uint(v.y);
             }
+            if (i == 0) {
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (c > seen) s[c] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2)
+                w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
             tmem_store16(s_tm, w);
-            tmem_store16(s_tm + 16, w + 16);
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
@@ -354,7 +345,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     }
     tmem_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kIssueWarp) {
         tmem_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
     }
@@ -374,6 +365,14 @@ constexpr int kStatBytes = kTile * 8;
 constexpr int kDkvBars = 6 * kQuerySlots + 6;
 constexpr int kDkvSmem = 1024 + (2 + 2 * kQuerySlots) * kTileBytes + kQuerySlots * kStatBytes +
                          8 * kDkvBars + 32;
+
+__device__ __forceinline__ float4 load_stats(uint32_t at) {
+    float4 l;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
+                 : "r"(at));
+    return l;
+}
 
 template <typename T>
 __device__ __forceinline__ void dkv_row(const AttnParams &p, const AttnUnit &u, int row, int g,
@@ -429,13 +428,15 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDkvBars; ++i) {
             const uint32_t b = bars + 8 * i;
-            bar_init(b, b == p_full || b == ds_full || (b >= st_empty && b < in_full) ? 8 : 1);
+            bar_init(b, b == p_full || b == ds_full || (b >= st_empty && b < in_full)
+                            ? 4 * kSumGroups
+                            : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gave_up = 0;
         for (int i = 0; i < 4; ++i) bad[i] = 0;
     }
-    if (warp == 9) {
+    if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
                      "r"(512)
                      : "memory");
@@ -460,9 +461,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const int boxes = p.dim > 64 ? 2 : 1;
     bool ok = true;
 
-    if (group == 2) {
+    if (group == kSumGroups) {
         give_registers<kBackIssueRegs>();
-        if (warp == 8) {
+        if (warp == kLoadWarp) {
             if (lane == 0 && any) {
                 bar_expect(in_full, 2 * boxes * kBox);
                 for (int b = 0; b < boxes; ++b) {
@@ -487,7 +488,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (++s == kQuerySlots) s = 0, ph ^= 1;
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == kIssueWarp) {
+            const uint32_t mine = one_lane();
+            const int steps = (p.dim + 15) / 16;
             const auto arrived = [&](uint32_t full, uint32_t at, int i) {
                 const int s = i % kQuerySlots;
                 if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, gave_up)) return false;
@@ -497,18 +500,14 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             };
             const auto scores = [&](int i) {
                 if (!arrived(q_full, q_at, i)) return false;
-                if (lane == 0) {
-                    mma_rows<T>(tmem, k_at, q_at + i % kQuerySlots * kTileBytes, p.dim);
-                    commit(s_full);
-                }
+                mma_rows<T>(tmem, k_at, q_at + i % kQuerySlots * kTileBytes, steps, mine);
+                commit(s_full, mine);
                 return true;
             };
             const auto grads = [&](int i) {  // dP
                 if (!arrived(g_full, g_at, i)) return false;
-                if (lane == 0) {
-                    mma_rows<T>(dp_tm, v_at, g_at + i % kQuerySlots * kTileBytes, p.dim);
-                    commit(dp_full);
-                }
+                mma_rows<T>(dp_tm, v_at, g_at + i % kQuerySlots * kTileBytes, steps, mine);
+                commit(dp_full, mine);
                 return true;
             };
             if (any) {
@@ -521,24 +520,18 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 ok = wait_warp(p_full, i & 1, gave_up);
                 if (!ok) break;
                 tmem_after();
-                if (lane == 0) {
-                    mma_halves<T>(dv_tm, tmem, g_at + s * kTileBytes, p.dim, i > 0);
-                    commit(g_empty + 8 * s);
-                }
-                __syncwarp();
+                mma_columns<T, kCols>(dv_tm, tmem, g_at + s * kTileBytes, steps, i > 0, mine);
+                commit(g_empty + 8 * s, mine);
                 if (i + 1 < n) ok = scores(i + 1);
                 ok = ok && wait_warp(ds_full, i & 1, gave_up);
                 if (!ok) break;
                 tmem_after();
-                if (lane == 0) {
-                    mma_halves<T>(dk_tm, dp_tm, q_at + s * kTileBytes, p.dim, i > 0);
-                    commit(q_empty + 8 * s);
-                    if (i == n - 1) commit(out_full);
-                }
-                __syncwarp();
+                mma_columns<T, kCols>(dk_tm, dp_tm, q_at + s * kTileBytes, steps, i > 0, mine);
+                commit(q_empty + 8 * s, mine);
+                if (i == n - 1) commit(out_full, mine);
                 if (i + 1 < n) ok = grads(i + 1);
             }
-        } else if (warp == 10) {
+        } else if (warp == kStatsWarp) {
             // lse and D of the queries; none for rows past the sequence: their
             // probabilities are 2^(0 - inf) = 0
             const Shift<T> shift(p);
@@ -570,44 +563,43 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const Shift<T> shift(p);
         const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const uint32_t s_tm = tmem + 64 * side + lanes, d_tm = dp_tm + 64 * side + lanes;
+        const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
         const bool live = any && row < u.len;
         for (int i = 0; i < n; ++i) {
             const int slot_i = i % kQuerySlots;
-            const uint32_t st = st_at + slot_i * kStatBytes + 256 * side;
-            // queries of this half before the first that sees the key
-            const int unseen = i % each ? 0 : mine - 64 * side;
+            const uint32_t st = st_at + slot_i * kStatBytes + 4 * kCols * side;
+            // queries of this part before the first that sees the key
+            const int unseen = i % each ? 0 : mine - kCols * side;
             // (dS of the row that sees one key is 0, as above)
-            const int no_grad = row ? unseen : i % each ? 0 : 1 - 64 * side;
+            const int no_grad = row ? unseen : i % each ? 0 : 1 - kCols * side;
             ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, gave_up) &&
                  wait_warp(s_full, i & 1, gave_up);
             if (!ok) break;
             tmem_after();
-            uint32_t s[64], d[64], w[32];
+            uint32_t s[kCols], d[kCols], w[kCols / 2];
             tmem_load32(s_tm, s);
-            tmem_load32(s_tm + 32, s + 32);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                float4 l;
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                             : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
-                             : "r"(st + 4 * c));
+            for (int c = 0; c < kCols; c += 4) {
+                const float4 l = load_stats(st + 4 * c);
                 const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
                                   both(p.scale2), {l.x, l.y});
                 const F2 y = fma2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])},
                                   both(p.scale2), {l.z, l.w});
-                float e[4] = {exp2_fast(x.x), exp2_fast(x.y), exp2_fast(y.x), exp2_fast(y.y)};
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    if (c + h < unseen) e[h] = 0.f;
-                    s[c + h] = __float_as_uint(e[h]);
-                }
-                w[c / 2] = pack2<T>(e[0], e[1]);
-                w[c / 2 + 1] = pack2<T>(e[2], e[3]);
+                s[c] = __float_as_uint(exp2_fast(x.x));
+                s[c + 1] = __float_as_uint(exp2_fast(x.y));
+                s[c + 2] = __float_as_uint(exp2_fast(y.x));
+                s[c + 3] = __float_as_uint(exp2_fast(y.y));
             }
+            if (i % each == 0) {
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (c < unseen) s[c] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2)
+                w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
             tmem_store16(s_tm, w);
-            tmem_store16(s_tm + 16, w + 16);
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
@@ -616,29 +608,28 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (!ok) break;
             tmem_after();
             tmem_load32(d_tm, d);
-            tmem_load32(d_tm + 32, d + 32);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                float4 l;
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                             : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
-                             : "r"(st + 512 + 4 * c));
+            for (int c = 0; c < kCols; c += 4) {
+                const float4 l = load_stats(st + 512 + 4 * c);
                 const F2 x = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
                                   both(shift.grads), {l.x, l.y});
                 const F2 y = fma2({__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])},
                                   both(shift.grads), {l.z, l.w});
                 const F2 a = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, x);
                 const F2 b = mul2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])}, y);
-                float e[4] = {a.x, a.y, b.x, b.y};
-#pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    if (c + h < no_grad) e[h] = 0.f;
-                w[c / 2] = pack2<T>(e[0], e[1]);
-                w[c / 2 + 1] = pack2<T>(e[2], e[3]);
+                d[c] = __float_as_uint(a.x), d[c + 1] = __float_as_uint(a.y);
+                d[c + 2] = __float_as_uint(b.x), d[c + 3] = __float_as_uint(b.y);
             }
+            if (i % each == 0) {
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (c < no_grad) d[c] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2)
+                w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
             tmem_store16(d_tm, w);
-            tmem_store16(d_tm + 16, w + 16);
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
@@ -676,7 +667,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     }
     tmem_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kIssueWarp) {
         tmem_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
     }
