@@ -672,7 +672,8 @@ pos_status poseidon_attn_forward(const pos_attn *attn, const pos_heads *x, const
 
 /*
  * Backward pass.  lse and o are the forward pass's.  With p_ij = exp(s_ij - lse_i),
- * D_i = do_i o_i and ds_ij = p_ij (do_i v_j - D_i):
+ * dp_ij = do_i v_j, D_i = sum_j p_ij dp_ij (which is do_i o_i, but for the rounding of o,
+ * that the gradients are freed from) and ds_ij = p_ij (dp_ij - D_i):
  *   dq_i = scale * sum_j ds_ij k_j,  dk_j = scale * sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
  * the keys' and values' summed over the query heads of their group.  x, dx: host arrays of
  * three, o and d_o: one; dx must not overlap what is read.  Sums are in 32 bits, in an

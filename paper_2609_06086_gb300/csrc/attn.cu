@@ -361,8 +361,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             bool good = finite(top) && finite(total);
             float factor = 1.f / total;
             if (!ok) factor = __uint_as_float(0x7fffffffu);  // a wait that gave up: no result
-            T *out = static_cast<T *>(p.out) + (u.start + (int64_t)row) * p.out_token +
-                     head * p.out_head;
+            // the queries' tile has been used: its place holds the results
+            const uint32_t out_at = q_at + t * kTileBytes;
             for (int c = 0; c < dim16; c += 16) {
                 uint32_t o[16];
                 tmem_load16(o_tm + c, o);
@@ -371,20 +371,22 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
-                    if (c + e < p.dim) good = good && finite(__uint_as_float(o[e]));
+                    good = good && finite(__uint_as_float(o[e]));
                 }
-                if (!live) continue;
-#pragma unroll
-                for (int e = 0; e < 16; e += 8) {
-                    if (p.out_vectors) store8<true>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
-                    else store8<false>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
-                }
+                put_columns<T>(out_at, threadIdx.x % kTile, c, x);
             }
+            asm volatile("barrier.sync %0, 128;" ::"r"(t + 1) : "memory");
+            const int row0 = r0 + t * kTile;
+            write_tile(out_at, min(kTile, u.len - row0),
+                       static_cast<T *>(p.out) + (u.start + (int64_t)row0) * p.out_token +
+                           head * p.out_head,
+                       p.out_token, p.out_vectors, p.dim, p.dim_out, (int)threadIdx.x % kTile,
+                       kTile);
             if (p.lse && live)
                 p.lse[head * p.tokens + u.start + row] =
                     ok ? (top + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);
             uint32_t again = __ballot_sync(0xffffffffu, ok && live && !good);
-            __syncwarp();
+            asm volatile("barrier.sync %0, 128;" ::"r"(t + 1) : "memory");
             while (again) {
                 const int i = __ffs(again) - 1;
                 again &= again - 1;

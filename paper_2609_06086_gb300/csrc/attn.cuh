@@ -190,6 +190,29 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t *r) {
         "r"(r[15])
         : "memory");
 }
+// 32 columns of the warp's 32 lanes, 8 values of each of four rows a thread: value
+// 16 h + 4 b + 2 r + e is that of row 16 h + 8 r + lane / 4, column 8 b + lane % 4 * 2 + e;
+// and 16 columns of pairs of 16-bit values in the same places.
+__device__ __forceinline__ void tmem_load_block(uint32_t addr, uint32_t *r) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h, r += 16)
+        asm volatile(
+            "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+            "%11, %12, %13, %14, %15}, [%16];"
+            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+              "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+              "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+            : "r"(addr + ((uint32_t)(16 * h) << 16)));
+}
+__device__ __forceinline__ void tmem_store_block(uint32_t addr, const uint32_t *r) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h, r += 8)
+        asm volatile(
+            "tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(
+                addr + ((uint32_t)(16 * h) << 16)),
+            "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+            : "memory");
+}
 // 2^x, both halves of the result within two units of its last place.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -220,6 +243,36 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+// Results on their way out: a thread's 16 columns from c on of a row, into a tile of
+// shared memory (256 bytes a row, pieces of 16 bytes exchanged so that neither side's
+// accesses meet in a bank) ...
+template <typename T>
+__device__ __forceinline__ void put_columns(uint32_t tile, int row, int c, const Vec8 (&x)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint4 v = from_float<T>(x[h]).a;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                         tile + row * 256 + (((c / 8 + h) ^ (row & 7)) << 4)),
+                     "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                     : "memory");
+    }
+}
+// ... and from there whole rows at a time to memory.
+template <typename T>
+__device__ __forceinline__ void write_tile(uint32_t tile, int rows, T *out, int64_t token,
+                                           bool vectors, int dim, int dim_out, int thread,
+                                           int threads) {
+    const int per = dim / 8;
+    for (int i = thread; i < rows * per; i += threads) {
+        const int row = i / per, c = i - row * per;
+        Raw8<T> r;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w)
+                     : "r"(tile + row * 256 + ((c ^ (row & 7)) << 4)));
+        if (vectors) store8<true>(out + row * token + 8 * c, r, dim_out - 8 * c);
+        else store8<false>(out + row * token + 8 * c, r, dim_out - 8 * c);
+    }
 }
 // Rows from `first` on of a tile become zeros: what belongs to another sequence, or
 // to none and may hold anything, would make a NaN of a probability of 0.

@@ -71,31 +71,6 @@ __global__ void __launch_bounds__(256) attn_stats_kernel(const AttnParams p) {
     }
 }
 
-// Sums from TMEM to a row of the output: 16 columns at a time, every kSumGroups-th of
-// them.  Whether all are finite.
-template <typename T>
-__device__ __forceinline__ bool write_sums(uint32_t tm, int side, float factor, T *out, bool live,
-                                           bool vectors, int dim, int dim_out) {
-    bool good = true;
-    for (int c = 16 * side; c < dim; c += 16 * kSumGroups) {
-        uint32_t v[16];
-        tmem_load16(tm + c, v);
-        tmem_wait_loads();
-        if (!live) continue;
-#pragma unroll
-        for (int h = 0; h < 16; h += 8) {
-            Vec8 x;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x.v[e] = __uint_as_float(v[h + e]) * factor;
-                if (c + h + e < dim) good = good && finite(__uint_as_float(v[h + e]));
-            }
-            if (vectors) store8<true>(out + c + h, from_float<T>(x), dim_out - c - h);
-            else store8<false>(out + c + h, from_float<T>(x), dim_out - c - h);
-        }
-    }
-    return good;
-}
 __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
     asm volatile("barrier.sync 1, %0;" ::"n"(128 * kSumGroups) : "memory");
 }
@@ -104,11 +79,16 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // Gradients of the queries
 // ---------------------------------------------------------------------------
 // A block takes 128 queries of a head and goes over the keys from the diagonal down.
-// TMEM: two places of scores, one of dP = dO V^T, the sums.  While four warpgroups
-// (32 columns of a row a thread) make dS = P (dP - D) of a tile, the tensor cores compute
-// the next scores, and dP as soon as the last one has been read.
+// TMEM holds scores, dP = dO V^T and two sums, and is full: P takes the scores' place and
+// dS = P (dP - D) that of dP, and while one of them is made, the tensor cores use up the
+// other and compute what comes next in its place.
+//   D = dO . o has the rounding of o in it, in 16 bits, which for rows with few keys that
+// count is larger than that of everything else (2 tokens of 2 heads of 64, bf16: dQ 0.7 %
+// off, dK 1.2 %).  Its exact value is D + e, e = sum P (dP - D), which this kernel has
+// when it is done; so it adds up P K beside dS K, and dQ = dS K - e P K.  The keys'
+// gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
-constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
+constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 6;
 constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 32;
 
 template <typename T>
@@ -149,8 +129,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t bars = v_at + kValueSlots * kTileBytes;
     const uint32_t k_full = bars, k_empty = k_full + 8 * kKeySlots;
     const uint32_t v_full = k_empty + 8 * kKeySlots, v_empty = v_full + 8 * kValueSlots;
-    const uint32_t in_full = v_empty + 8 * kValueSlots, s_full = in_full + 8, dp_full = s_full + 16;
-    const uint32_t dp_read = dp_full + 8, ds_full = dp_read + 8, dq_full = ds_full + 8;
+    const uint32_t in_full = v_empty + 8 * kValueSlots, s_full = in_full + 8, dp_full = s_full + 8;
+    const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, dq_full = ds_full + 8;
     const uint32_t slot = dq_full + 8;
     unsigned char *tail = aligned + (slot - base);
     volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
@@ -159,7 +139,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDqBars; ++i) {
-            const bool sums = bars + 8 * i == dp_read || bars + 8 * i == ds_full;
+            const bool sums = bars + 8 * i == p_full || bars + 8 * i == ds_full;
             bar_init(bars + 8 * i, sums ? 4 * kSumGroups : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -178,7 +158,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     grid_dep_wait();
     grid_dep_trigger();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
-    const uint32_t dp_tm = tmem + 2 * kTile, dq_tm = tmem + 3 * kTile;
+    const uint32_t dp_tm = tmem + kTile, pk_tm = tmem + 2 * kTile, dq_tm = tmem + 3 * kTile;
 
     const int head = blockIdx.x % p.heads_q;
     AttnUnit u;
@@ -227,8 +207,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const uint32_t at = k_at + i % kKeySlots * kTileBytes;
                 const int seen = u.len - (n - 1 - i) * kTile;
                 if (seen < kTile) zero_rows(at, seen, boxes, lane);
-                mma_rows<T>(tmem + i % 2 * kTile, q_at, at, steps, mine);
-                commit(s_full + 8 * (i % 2), mine);
+                mma_rows<T>(tmem, q_at, at, steps, mine);
+                commit(s_full, mine);
                 return true;
             };
             const auto grads = [&](int i) {  // dP
@@ -242,40 +222,42 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (any) {
                 ok = wait_warp(in_full, 0, gave_up);
                 tmem_after();
-                ok = ok && scores(0) && grads(0) && (n == 1 || scores(1));
+                ok = ok && scores(0) && grads(0);
             }
             for (int i = 0; i < n && ok; ++i) {
-                if (i + 1 < n) {
-                    ok = wait_warp(dp_read, i & 1, gave_up);
-                    tmem_after();
-                    ok = ok && grads(i + 1);
-                    if (!ok) break;
-                }
-                ok = wait_warp(ds_full, i & 1, gave_up);
+                const uint32_t at = k_at + i % kKeySlots * kTileBytes;
+                ok = wait_warp(p_full, i & 1, gave_up);
                 if (!ok) break;
                 tmem_after();
-                mma_columns<T, kCols>(dq_tm, tmem + i % 2 * kTile,
-                                      k_at + i % kKeySlots * kTileBytes, steps, i > 0, mine);
+                mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
+                if (i + 1 < n) ok = scores(i + 1);
+                ok = ok && wait_warp(ds_full, i & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
                 commit(k_empty + 8 * (i % kKeySlots), mine);
                 if (i == n - 1) commit(dq_full, mine);
-                if (i + 2 < n) ok = scores(i + 2);
+                else ok = grads(i + 1);
             }
         }
         __syncwarp();
     } else {
         take_registers<kBackRegs>();
-        const int side = group, row = u.tile * kTile + warp % 4 * 32 + lane;
+        const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
         const bool live = any && row < u.len;
         float2 st = make_float2(0.f, 0.f);
         const Shift<T> shift(p);
         if (live) st = p.stats[head * p.tokens + u.start + row];
+        F2 rest = both(0.f);  // e, of this part of the columns
         for (int i = 0; i < n; ++i) {
-            const uint32_t s_tm = tmem + i % 2 * kTile + kCols * side + lanes;
-            ok = ok && wait_warp(s_full + 8 * (i % 2), i / 2 & 1, gave_up);
+            ok = ok && wait_warp(s_full, i & 1, gave_up);
             if (!ok) break;
             tmem_after();
-            uint32_t s[kCols], d[kCols];
+            uint32_t s[kCols], d[kCols], w[kCols / 2];
+            // the last key of this part that the row sees; a row that sees one has dS = 0
+            const int seen = row - (n - 1) * kTile - kCols * side;
             tmem_load32(s_tm, s);
             tmem_wait_loads();
 #pragma unroll
@@ -284,25 +266,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                                   both(p.scale2), both(-st.x));
                 s[c] = __float_as_uint(exp2_fast(x.x));
                 s[c + 1] = __float_as_uint(exp2_fast(x.y));
-            }
-            ok = wait_warp(dp_full, i & 1, gave_up);
-            if (!ok) break;
-            tmem_after();
-            tmem_load32(dp_tm + kCols * side + lanes, d);
-            tmem_wait_loads();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(dp_read);
-            uint32_t w[kCols / 2];
-            // the last key of this part that the row sees; a row that sees one has P = 1 and
-            // dS = 0, and D, of the rounded o, would leave a rounding
-            const int seen = i ? kCols : row ? row - (n - 1) * kTile - kCols * side : -1;
-#pragma unroll
-            for (int c = 0; c < kCols; c += 2) {
-                const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
-                                  both(shift.grads), both(-st.y * shift.grads));
-                const F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
-                s[c] = __float_as_uint(v.x), s[c + 1] = __float_as_uint(v.y);
             }
             if (i == 0) {
 #pragma unroll
@@ -316,19 +279,71 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
+            if (lane == 0) bar_arrive(p_full);
+            ok = wait_warp(dp_full, i & 1, gave_up);
+            if (!ok) break;
+            tmem_after();
+            tmem_load32(d_tm, d);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2) {
+                const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
+                                  both(shift.grads), both(-st.y * shift.grads));
+                const F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
+                d[c] = __float_as_uint(v.x), d[c + 1] = __float_as_uint(v.y);
+            }
+            if (i == 0) {
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (c > seen || row == 0) d[c] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2) {
+                rest = add2(rest, {__uint_as_float(d[c]), __uint_as_float(d[c + 1])});
+                w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
+            }
+            tmem_store16(d_tm, w);
+            tmem_wait_stores();
+            tmem_before();
+            __syncwarp();
             if (lane == 0) bar_arrive(ds_full);
         }
         if (any) {
             if (ok) ok = wait_warp(dq_full, 0, gave_up);
             tmem_after();
-            T *out = static_cast<T *>(p.dq) + (u.start + (int64_t)row) * p.d_token[0] +
-                     head * p.d_head[0];
-            const bool good =
-                write_sums<T>(dq_tm + lanes, side,
-                              ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu), out, live,
-                              p.d_vectors[0], p.dim, p.dim_out);
+            // every tile of keys and values has been used: their places hold e's parts and
+            // the results
+            float *parts = reinterpret_cast<float *>(aligned + (v_at - base));
+            parts[side * kTile + mine] = rest.x + rest.y;
+            sums_barrier();
+            const float e = (parts[mine] + parts[kTile + mine] + parts[2 * kTile + mine] +
+                             parts[3 * kTile + mine]) * shift.undo;
+            if (live && side == 0) p.stats[head * p.tokens + u.start + row].y = st.y + e;
+            const float a = ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu);
+            const float b = -e * p.scale * Shift<T>::kUndoProbs;
+            bool good = true;
+            for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
+                uint32_t v[16], k[16];
+                tmem_load16(dq_tm + lanes + c, v);
+                tmem_load16(pk_tm + lanes + c, k);
+                tmem_wait_loads();
+                Vec8 x[2];
+#pragma unroll
+                for (int h = 0; h < 16; ++h) {
+                    const float y = __uint_as_float(v[h]) * a + __uint_as_float(k[h]) * b;
+                    x[h / 8].v[h % 8] = y;
+                    good = good && finite(y);
+                }
+                put_columns<T>(k_at, mine, c, x);
+            }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
             if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            sums_barrier();
+            const int64_t token = u.start + (int64_t)u.tile * kTile;
+            write_tile(k_at, min(kTile, u.len - u.tile * kTile),
+                       static_cast<T *>(p.dq) + token * p.d_token[0] + head * p.d_head[0],
+                       p.d_token[0], p.d_vectors[0], p.dim, p.dim_out, (int)threadIdx.x,
+                       128 * kSumGroups);
             sums_barrier();
             uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
             while (rows) {
@@ -366,11 +381,9 @@ constexpr int kDkvBars = 6 * kQuerySlots + 6;
 constexpr int kDkvSmem = 1024 + (2 + 2 * kQuerySlots) * kTileBytes + kQuerySlots * kStatBytes +
                          8 * kDkvBars + 32;
 
-__device__ __forceinline__ float4 load_stats(uint32_t at) {
-    float4 l;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(l.x), "=f"(l.y), "=f"(l.z), "=f"(l.w)
-                 : "r"(at));
+__device__ __forceinline__ F2 load_stats(uint32_t at) {
+    F2 l;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l.x), "=f"(l.y) : "r"(at));
     return l;
 }
 
@@ -565,71 +578,69 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
         const bool live = any && row < u.len;
+        // A thread's 32 values are of four keys and eight queries (tmem_load_block), so that it
+        // reads lse and D of eight queries and not of 32: shared memory is what bounds
+        // this kernel (2786 cycles a tile of 128 x 128 with 32 of them)
+        const int key = warp % 4 * 32 + lane / 4, query = kCols * side + lane % 4 * 2;
         for (int i = 0; i < n; ++i) {
             const int slot_i = i % kQuerySlots;
-            const uint32_t st = st_at + slot_i * kStatBytes + 4 * kCols * side;
-            // queries of this part before the first that sees the key
-            const int unseen = i % each ? 0 : mine - kCols * side;
-            // (dS of the row that sees one key is 0, as above)
-            const int no_grad = row ? unseen : i % each ? 0 : 1 - kCols * side;
+            const uint32_t st = st_at + slot_i * kStatBytes + 4 * query;
             ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, gave_up) &&
                  wait_warp(s_full, i & 1, gave_up);
             if (!ok) break;
             tmem_after();
             uint32_t s[kCols], d[kCols], w[kCols / 2];
-            tmem_load32(s_tm, s);
+            tmem_load_block(s_tm, s);
+            F2 l[kCols / 8];
+#pragma unroll
+            for (int b = 0; b < kCols / 8; ++b) l[b] = load_stats(st + 32 * b);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < kCols; c += 4) {
-                const float4 l = load_stats(st + 4 * c);
+            for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
-                                  both(p.scale2), {l.x, l.y});
-                const F2 y = fma2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])},
-                                  both(p.scale2), {l.z, l.w});
+                                  both(p.scale2), l[c / 4 % (kCols / 8)]);
                 s[c] = __float_as_uint(exp2_fast(x.x));
                 s[c + 1] = __float_as_uint(exp2_fast(x.y));
-                s[c + 2] = __float_as_uint(exp2_fast(y.x));
-                s[c + 3] = __float_as_uint(exp2_fast(y.y));
             }
-            if (i % each == 0) {
+            const bool diagonal = i % each == 0;
+            if (diagonal) {
 #pragma unroll
                 for (int c = 0; c < kCols; ++c)
-                    if (c < unseen) s[c] = 0;
+                    if (query + c % 16 / 4 * 8 + c % 2 < key + c / 16 * 16 + c % 4 / 2 * 8) s[c] = 0;
             }
 #pragma unroll
             for (int c = 0; c < kCols; c += 2)
                 w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-            tmem_store16(s_tm, w);
+            tmem_store_block(s_tm, w);
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
             if (lane == 0) bar_arrive(p_full);
+#pragma unroll
+            for (int b = 0; b < kCols / 8; ++b) l[b] = load_stats(st + 512 + 32 * b);
             ok = wait_warp(dp_full, i & 1, gave_up);
             if (!ok) break;
             tmem_after();
-            tmem_load32(d_tm, d);
+            tmem_load_block(d_tm, d);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < kCols; c += 4) {
-                const float4 l = load_stats(st + 512 + 4 * c);
+            for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
-                                  both(shift.grads), {l.x, l.y});
-                const F2 y = fma2({__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])},
-                                  both(shift.grads), {l.z, l.w});
+                                  both(shift.grads), l[c / 4 % (kCols / 8)]);
                 const F2 a = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, x);
-                const F2 b = mul2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])}, y);
                 d[c] = __float_as_uint(a.x), d[c + 1] = __float_as_uint(a.y);
-                d[c + 2] = __float_as_uint(b.x), d[c + 3] = __float_as_uint(b.y);
             }
-            if (i % each == 0) {
+            if (diagonal) {  // (dS of the query that sees one key is 0, as above)
 #pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                    if (c < no_grad) d[c] = 0;
+                for (int c = 0; c < kCols; ++c) {
+                    const int a = query + c % 16 / 4 * 8 + c % 2, b = key + c / 16 * 16 + c % 4 / 2 * 8;
+                    if (a < b || a + u.tile == 0) d[c] = 0;
+                }
             }
 #pragma unroll
             for (int c = 0; c < kCols; c += 2)
                 w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
-            tmem_store16(d_tm, w);
+            tmem_store_block(d_tm, w);
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
@@ -641,16 +652,36 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         if (any) {
             if (ok) ok = wait_warp(out_full, 0, gave_up);
             tmem_after();
-            const int64_t token = u.start + (int64_t)row;
+            // every tile of queries has been used: their places hold the results
             const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
-            bool good = write_sums<T>(dk_tm + lanes, side, ok ? p.scale * shift.undo : lost,
-                                      static_cast<T *>(p.dk) + token * p.d_token[1] + g * p.d_head[1],
-                                      live, p.d_vectors[1], p.dim, p.dim_out);
-            good &= write_sums<T>(dv_tm + lanes, side, ok ? Shift<T>::kUndoProbs : lost,
-                                  static_cast<T *>(p.dv) + token * p.d_token[2] + g * p.d_head[2],
-                                  live, p.d_vectors[2], p.dim, p.dim_out);
+            const float factor[2] = {ok ? p.scale * shift.undo : lost,
+                                     ok ? Shift<T>::kUndoProbs : lost};
+            bool good = true;
+            for (int t = 0; t < 2; ++t)
+                for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
+                    uint32_t v[16];
+                    tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
+                    tmem_wait_loads();
+                    Vec8 x[2];
+#pragma unroll
+                    for (int h = 0; h < 16; ++h) {
+                        x[h / 8].v[h % 8] = __uint_as_float(v[h]) * factor[t];
+                        good = good && finite(__uint_as_float(v[h]));
+                    }
+                    put_columns<T>(q_at + t * kTileBytes, mine, c, x);
+                }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
             if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            sums_barrier();
+            const int64_t token = u.start + (int64_t)u.tile * kTile;
+            const int count = min(kTile, u.len - u.tile * kTile);
+            write_tile(q_at, count, static_cast<T *>(p.dk) + token * p.d_token[1] + g * p.d_head[1],
+                       p.d_token[1], p.d_vectors[1], p.dim, p.dim_out, (int)threadIdx.x,
+                       128 * kSumGroups);
+            write_tile(q_at + kTileBytes, count,
+                       static_cast<T *>(p.dv) + token * p.d_token[2] + g * p.d_head[2],
+                       p.d_token[2], p.d_vectors[2], p.dim, p.dim_out, (int)threadIdx.x,
+                       128 * kSumGroups);
             sums_barrier();
             uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
             while (rows) {
