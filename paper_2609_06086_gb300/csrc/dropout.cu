@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutPara
     }
 #pragma unroll
     for (int i = 0; i < kDropUnroll; ++i) {
-        if (left[i] <= 0) continue;
+        if (ALIGNED && left[i] <= 0) continue;
         Vec8 v = to_float(x[i]);
         if (p.res) {
             // residual + x * factor with one rounding, as norm.cu has it
@@ -57,8 +57,15 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutPara
         } else if (p.drop.threshold) {
             drop8(p.drop, offset, p.row0 + row[i], j[i], v);
         }
-        store8<ALIGNED>(static_cast<Y *>(p.y) + row[i] * p.ldy + 8 * j[i], from_float<Y>(v),
-                        left[i]);
+        Y *to = static_cast<Y *>(p.y) + row[i] * p.ldy + 8 * j[i];
+        if constexpr (ALIGNED) {
+            store8<true>(to, from_float<Y>(v), left[i]);
+        } else {
+            // (a row's last vector has its end stored by its own lane: the next is of another)
+            const int lane = threadIdx.x % 32;
+            store8_shifted(to, from_float<Y>(v), left[i], lane > 0 && j[i] > 0 && left[i] > 0,
+                           lane < 31 && j[i] + 1 < p.per_row.d && left[i] > 0);
+        }
     }
 }
 

@@ -263,6 +263,67 @@ __device__ __forceinline__ void store8(T *p, const Raw8<T> &r, int n) {
     }
 }
 
+// 8 elements at p, which need not be 16-byte aligned, as aligned words: a lane takes the
+// last elements of the lane before it and leaves its own last ones to the lane behind it.
+// Called by all lanes of a warp; `left` elements exist from p on (any number), of which 8
+// at most are this lane's.  has_prev, has_next: the lane before or behind holds the 8
+// elements before or behind these, and calls with them.  What has no such lane is
+// stored element by element.
+template <typename T>
+__device__ __forceinline__ void store8_shifted(T *p, const Raw8<T> &r, int left, bool has_prev,
+                                               bool has_next) {
+    constexpr int kPer = 16 / sizeof(T), kWords = 2 * sizeof(T);  // 32-bit words of 8 elements
+    // (at least one lane is off the alignment in the cases that this is for)
+    const int m = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % kPer);
+    uint32_t w[2 * kWords];
+    w[kWords] = r.a.x, w[kWords + 1] = r.a.y, w[kWords + 2] = r.a.z, w[kWords + 3] = r.a.w;
+    if constexpr (sizeof(T) == 4)
+        w[12] = r.b.x, w[13] = r.b.y, w[14] = r.b.z, w[15] = r.b.w;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = __shfl_up_sync(0xffffffffu, w[kWords + i], 1);
+    if (m == 0) {
+        store8<true>(p, r, left);
+        return;
+    }
+    if (left + m > 0 && has_prev) {
+        // the words from 8 - m elements of the lane before on: down by as many
+        const int down = 8 - m, q = sizeof(T) == 2 ? down / 2 : down;
+        uint32_t v[2 * kWords];
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) v[i] = w[i];
+        if (sizeof(T) == 4 && (q & 4)) {
+#pragma unroll
+            for (int i = 0; i + 4 < 2 * kWords; ++i) v[i] = v[i + 4];
+        }
+        if (q & 2) {
+#pragma unroll
+            for (int i = 0; i + 2 < 2 * kWords; ++i) v[i] = v[i + 2];
+        }
+        if (q & 1) {
+#pragma unroll
+            for (int i = 0; i + 1 < 2 * kWords; ++i) v[i] = v[i + 1];
+        }
+        if (sizeof(T) == 2 && (down & 1)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 16);
+        }
+        Raw8<T> o;
+        o.a = make_uint4(v[0], v[1], v[2], v[3]);
+        if constexpr (sizeof(T) == 4) o.b = make_uint4(v[4], v[5], v[6], v[7]);
+        store8<true>(p - m, o, left + m);
+    }
+    if (!has_prev || !has_next) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e >= left || (e < 8 - m ? has_prev : has_next)) continue;
+            if constexpr (sizeof(T) == 4)
+                reinterpret_cast<uint32_t *>(p)[e] = w[kWords + e];
+            else
+                reinterpret_cast<uint16_t *>(p)[e] = (uint16_t)(w[kWords + e / 2] >> (16 * (e % 2)));
+        }
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ Vec8 to_float(const Raw8<T> &r) {
     Vec8 x;

@@ -5,30 +5,61 @@
 namespace pos {
 
 // A team takes a row at a time and holds it in registers, so that every matrix goes
-// through HBM once.  h is rounded to its type before it is squared, kept or
-// normalised: what the backward pass reads is what the forward pass used.
-template <typename T, typename H, class TEAM, bool ALIGNED>
+// through HBM once; the next rows are on their way meanwhile (RING; without it rows are
+// read in place, from any alignment).  h is rounded to its type before it is squared,
+// kept or normalised: what the backward pass reads is what the forward pass used.
+template <typename T, typename H, class TEAM, bool RING>
 __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormParams p) {
     grid_dep_wait();
     grid_dep_trigger();
+    extern __shared__ uint4 cells[];
     __shared__ float shared[2][32];
-    constexpr int V = TEAM::V;
+    constexpr int V = TEAM::V, kX = sizeof(T) / 2, kH = sizeof(H) / 2;
     const int rank = TEAM::rank(), step = TEAM::threads();
     const uint64_t offset = drop_offset(p.drop);
+    const int64_t rows_step = (int64_t)gridDim.x * TEAM::teams();
+    const Ring ring(cells);
+    const auto fetch = [&](int64_t r, int slot) {
+        if (r < p.rows)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int j = rank + i * step, left = p.cols - 8 * j, cell = (slot * V + i) * (kX + kH);
+                ring.copy(cell, static_cast<const T *>(p.x) + r * p.ldx + (left > 0 ? 8 * j : 0), left);
+                if (p.res)
+                    ring.copy(cell + kX,
+                              static_cast<const H *>(p.res) + r * p.ldr + (left > 0 ? 8 * j : 0), left);
+            }
+        Ring::row_done();
+    };
     Vec8 w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] = load_w(p, rank + i * step);
-    int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index(); r < p.rows;
-         r += (int64_t)gridDim.x * TEAM::teams(), turn ^= 1) {
-        const T *x = static_cast<const T *>(p.x) + r * p.ldx;
-        const H *res = static_cast<const H *>(p.res) + r * p.ldr;
+    int turn = 0, slot = 0;
+    const int64_t first = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index();
+    if constexpr (RING)
+        for (int k = 0; k + 1 < p.depth; ++k) fetch(first + k * rows_step, k);
+    for (int64_t r = first; r < p.rows; r += rows_step, turn ^= 1) {
         Raw8<T> xr[V];
         Raw8<H> hr[V];
+        if constexpr (RING) {
+            int to = slot + p.depth - 1;
+            if (to >= p.depth) to -= p.depth;
+            fetch(r + (p.depth - 1) * rows_step, to);
+            Ring::wait(p.depth - 1);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            xr[i] = load_vec<ALIGNED>(x, rank + i * step, p.cols);
-            if (p.res) hr[i] = load_vec<ALIGNED>(res, rank + i * step, p.cols);
+            for (int i = 0; i < V; ++i) {
+                const int cell = (slot * V + i) * (kX + kH);
+                xr[i] = ring.take<T>(cell);
+                if (p.res) hr[i] = ring.take<H>(cell + kX);
+            }
+            if (++slot == p.depth) slot = 0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                xr[i] = load_vec(static_cast<const T *>(p.x) + r * p.ldx, rank + i * step, p.cols);
+                if (p.res)
+                    hr[i] = load_vec(static_cast<const H *>(p.res) + r * p.ldr, rank + i * step, p.cols);
+            }
         }
         float squares = 0.f;
 #pragma unroll
@@ -41,8 +72,7 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
                 drop8(p.drop, offset, (uint32_t)r, (uint32_t)j, v);
             }
             hr[i] = from_float<H>(v);
-            if (p.h && 8 * j < p.cols)
-                store8<ALIGNED>(static_cast<H *>(p.h) + r * p.ldh + 8 * j, hr[i], p.cols - 8 * j);
+            if (p.h) store_vec(p.out_aligned, static_cast<H *>(p.h) + r * p.ldh, j, hr[i], p.cols);
             if (p.codes_h)
                 keep8(p.format, hr[i], p.codes_h + r * p.pitch, p.scales_h + r * p.spitch, j,
                       8 * j < p.pitch);
@@ -62,8 +92,7 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
             for (int e = 0; e < 8; ++e)  // (past the last column 0, also under a norm that is NaN)
                 v.v[e] = 8 * j + e < p.cols ? v.v[e] * rstd * w[i].v[e] : 0.f;
             const Raw8<T> y = from_float<T>(v);
-            if (p.y && 8 * j < p.cols)
-                store8<ALIGNED>(static_cast<T *>(p.y) + r * p.ldy + 8 * j, y, p.cols - 8 * j);
+            if (p.y) store_vec(p.out_aligned, static_cast<T *>(p.y) + r * p.ldy, j, y, p.cols);
             if (p.codes_y)
                 keep8(p.format, y, p.codes_y + r * p.pitch, p.scales_y + r * p.spitch, j,
                       8 * j < p.pitch);
@@ -108,17 +137,29 @@ pos_status check_matrix(const char *what, const void *d, int32_t dtype, int64_t 
     return POS_OK;
 }
 
+template <typename T, typename H, class TEAM, bool RING>
+static pos_status launch_forward(NormParams p, const NormShape &shape, cudaStream_t s) {
+    auto kern = norm_forward_kernel<T, H, TEAM, RING>;
+    int smem = 0;
+    if constexpr (RING) {
+        const int row = TEAM::V * (int)(sizeof(T) + sizeof(H)) / 2;
+        p.depth = ring_depth(row, shape.threads);
+        smem = 16 * p.depth * row * shape.threads;
+        POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), smem));
+    }
+    int per_sm = 0;
+    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), shape.threads, smem, &per_sm));
+    const int64_t blocks = (p.rows + shape.rows - 1) / shape.rows;
+    POS_CUDA(launch_dependent(kern, (int)std::min<int64_t>(blocks, (int64_t)sm_count() * per_sm),
+                              shape.threads, smem, s, p));
+    return POS_OK;
+}
+
 template <typename T, typename H, class TEAM>
 static pos_status launch_forward(const NormParams &p, const NormShape &shape, bool aligned,
                                  cudaStream_t s) {
-    auto kern = aligned ? norm_forward_kernel<T, H, TEAM, true>
-                        : norm_forward_kernel<T, H, TEAM, false>;
-    int per_sm = 0;
-    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), shape.threads, 0, &per_sm));
-    const int64_t blocks = (p.rows + shape.rows - 1) / shape.rows;
-    POS_CUDA(launch_dependent(kern, (int)std::min<int64_t>(blocks, (int64_t)sm_count() * per_sm),
-                              shape.threads, 0, s, p));
-    return POS_OK;
+    return aligned ? launch_forward<T, H, TEAM, true>(p, shape, s)
+                   : launch_forward<T, H, TEAM, false>(p, shape, s);
 }
 
 template <typename T, typename H>
@@ -129,7 +170,8 @@ static pos_status forward_of(const NormParams &p, bool aligned, cudaStream_t s) 
         case 1: return launch_forward<T, H, Team<true, 4, 256>>(p, shape, aligned, s);
         case 2: return launch_forward<T, H, Team<false, 2, 512>>(p, shape, aligned, s);
         case 3: return launch_forward<T, H, Team<false, 4, 512>>(p, shape, aligned, s);
-        default: return launch_forward<T, H, Team<false, 4, 1024>>(p, shape, aligned, s);
+        // (a row of 1024 threads would fill an SM's shared memory)
+        default: return launch_forward<T, H, Team<false, 4, 1024>, false>(p, shape, s);
     }
 }
 
@@ -147,8 +189,9 @@ extern "C" pos_status poseidon_norm_forward(const pos_norm *norm, const void *d_
         const int64_t rows = norm->rows, cols = norm->cols;
         POS_TRY(check_matrix("x", d_x, norm->dtype, rows, cols, ldx, false, &aligned));
         POS_TRY(check_matrix("the residual", d_res, norm->dtype_h, rows, cols, ldr, false, &aligned));
-        POS_TRY(check_matrix("h", d_h, norm->dtype_h, rows, cols, ldh, true, &aligned));
-        POS_TRY(check_matrix("y", d_y, norm->dtype, rows, cols, ldy, true, &aligned));
+        p.out_aligned = true;
+        POS_TRY(check_matrix("h", d_h, norm->dtype_h, rows, cols, ldh, true, &p.out_aligned));
+        POS_TRY(check_matrix("y", d_y, norm->dtype, rows, cols, ldy, true, &p.out_aligned));
         if (!aligned16(d_ckpt_h) || !aligned16(d_ckpt_y))
             return fail(POS_EINVAL, "norm: checkpoint not 16-byte aligned");
         if (reinterpret_cast<uintptr_t>(d_rstd) % 4)

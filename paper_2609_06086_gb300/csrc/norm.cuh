@@ -23,6 +23,8 @@ struct NormParams {
     int32_t cols, format;
     float eps, inv_cols;
     bool w_vectors;                    // w can be read 16 bytes at a time
+    bool out_aligned;                  // outputs can be written 16 bytes at a time
+    int32_t depth;                     // rows on their way to shared memory
     DropParams drop;
 };
 
@@ -52,11 +54,88 @@ struct Team {
     }
 };
 
-template <bool ALIGNED, typename T>
+template <typename T>
 __device__ __forceinline__ Raw8<T> load_vec(const T *row, int j, int cols) {
-    const int left = cols - 8 * j;
-    if constexpr (ALIGNED) return load8<true>(row + 8 * j, left);
-    else return load8_shifted(row + 8 * j, 8 * j, left);
+    return load8_shifted(row + 8 * j, 8 * j, cols - 8 * j);
+}
+
+// Rows on their way to shared memory, `depth` - 1 of them ahead: a thread copies and
+// reads its own vectors, so the block need not meet.  Without them a row's loads, its
+// sum over the block and its stores take turns, and registers leave room for one block of
+// 512 threads an SM.  A cell is 16 bytes; a vector takes some cells, a slot of the ring
+// one row.
+struct Ring {
+    uint32_t base;   // this thread's first cell
+    int step;        // bytes from cell to cell
+    __device__ __forceinline__ explicit Ring(void *smem)
+        : base((uint32_t)__cvta_generic_to_shared(smem) + 16 * threadIdx.x), step(16 * blockDim.x) {}
+    // 8 elements, of which `left` exist (the others read as zeros)
+    template <typename T>
+    __device__ __forceinline__ void copy(int cell, const T *from, int left) const {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            constexpr int kPer = 16 / sizeof(T);
+            const int n = max(0, min(kPer, left - kPer * k));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                             base + (cell + k) * step),
+                         "l"(n ? from + kPer * k : from), "r"((int)(n * sizeof(T)))
+                         : "memory");
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ Raw8<T> take(int cell) const {
+        Raw8<T> r;
+        r.a = word(cell);
+        if constexpr (sizeof(T) == 4) r.b = word(cell + 1);
+        return r;
+    }
+    // 8 codes and the word of scales that has theirs
+    __device__ __forceinline__ void copy_codes(int cell, const uint8_t *codes, const uint8_t *scales,
+                                               bool there) const {
+        const uint32_t at = base + cell * step;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(at), "l"(codes),
+                     "r"(there ? 8 : 0)
+                     : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + 8), "l"(scales),
+                     "r"(there ? 4 : 0)
+                     : "memory");
+    }
+    __device__ __forceinline__ uint4 word(int cell) const {
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(base + cell * step));
+        return v;
+    }
+    static __device__ __forceinline__ void row_done() {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // All rows but the last `ahead` have arrived.
+    static __device__ __forceinline__ void wait(int ahead) {
+        if (ahead >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+};
+constexpr int kNormDepth = 3;
+// Depth of the ring whose rows take `cells` cells of `threads` threads: as deep as two
+// blocks an SM allow, or one where the rows are long.
+inline int ring_depth(int cells, int threads) {
+    const int slot = 16 * cells * threads;
+    for (int most : {110 << 10, 220 << 10})
+        if (kNormDepth * slot <= most) return kNormDepth;
+    return 2 * slot <= (220 << 10) ? 2 : 1;
+}
+
+// All lanes of a warp take part.
+template <typename T>
+__device__ __forceinline__ void store_vec(bool aligned, T *row, int j, const Raw8<T> &r, int cols) {
+    const int left = cols - 8 * j, lane = threadIdx.x % 32;
+    if (aligned) {
+        if (left > 0) store8<true>(row + 8 * j, r, left);
+    } else {
+        store8_shifted(row + 8 * j, r, left, lane > 0, lane < 31);
+    }
 }
 
 __device__ __forceinline__ Vec8 load_w(const NormParams &p, int j) {

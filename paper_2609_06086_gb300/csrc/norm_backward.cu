@@ -3,50 +3,106 @@
 
 namespace pos {
 
-// 8 values of h from its 8-bit checkpoint.
-__device__ __forceinline__ Vec8 kept8(const NormParams &p, int64_t r, int j) {
-    if (8 * j >= p.pitch) return Vec8{};
-    const uint2 c = *reinterpret_cast<const uint2 *>(p.codes_h + r * p.pitch + 8 * j);
-    const float scale = scale_value(p.scales_h[r * p.spitch + j / 4]);
-    return p.format == POS_CKPT_INT8 ? decode8<POS_CKPT_INT8>(c, scale)
-                                     : decode8<POS_CKPT_E4M3>(c, scale);
+// 8 values of h from its codes and a scale byte.
+__device__ __forceinline__ Vec8 kept8(const NormParams &p, uint2 codes, int byte) {
+    const float scale = scale_value(byte);
+    return p.format == POS_CKPT_INT8 ? decode8<POS_CKPT_INT8>(codes, scale)
+                                     : decode8<POS_CKPT_E4M3>(codes, scale);
 }
 
 // A team takes a row at a time, as the forward pass does.  dw is summed over a
 // thread's rows in registers, over a block's teams in shared memory, and written as
 // one partial sum per block, which norm_dw_kernel adds up in order: no atomics.
-template <typename T, typename H, class TEAM, bool ALIGNED>
+template <typename T, typename H, class TEAM, bool RING>
 __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormParams p) {
     grid_dep_wait();
     grid_dep_trigger();
+    extern __shared__ uint4 cells[];
     __shared__ float shared[2][32];
-    constexpr int V = TEAM::V;
+    constexpr int V = TEAM::V, kX = sizeof(T) / 2, kH = sizeof(H) / 2;
     const int rank = TEAM::rank(), step = TEAM::threads();
     const uint64_t offset = drop_offset(p.drop);
-    Vec8 dw[V];
+    const int64_t rows_step = (int64_t)gridDim.x * TEAM::teams();
+    const Ring ring(cells);
+    // cells of a vector: dy, h (or its codes), dh_in
+    const int in_h = kX + (p.h_in ? kH : 1), per = in_h + (p.dh_in ? kH : 0);
+    const auto fetch = [&](int64_t r, int slot) {
+        if (r < p.rows)
 #pragma unroll
-    for (int i = 0; i < V; ++i) dw[i] = Vec8{};
-    int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index(); r < p.rows;
-         r += (int64_t)gridDim.x * TEAM::teams(), turn ^= 1) {
-        const T *dy = static_cast<const T *>(p.dy) + r * p.ldy;
-        const H *h = static_cast<const H *>(p.h_in) + r * p.ldh;
-        const H *dh_in = static_cast<const H *>(p.dh_in) + r * p.lddh_in;
+            for (int i = 0; i < V; ++i) {
+                const int j = rank + i * step, left = p.cols - 8 * j, cell = (slot * V + i) * per;
+                const int c = left > 0 ? 8 * j : 0;
+                ring.copy(cell, static_cast<const T *>(p.dy) + r * p.ldy + c, left);
+                if (p.h_in)
+                    ring.copy(cell + kX, static_cast<const H *>(p.h_in) + r * p.ldh + c, left);
+                else
+                    ring.copy_codes(cell + kX, p.codes_h + r * p.pitch + c,
+                                    p.scales_h + r * p.spitch + c / 128 * 4, left > 0);
+                if (p.dh_in)
+                    ring.copy(cell + in_h, static_cast<const H *>(p.dh_in) + r * p.lddh_in + c, left);
+            }
+        Ring::row_done();
+    };
+    constexpr bool kHoldW = V <= 2;  // (registers)
+    Vec8 dw[V], w_held[kHoldW ? V : 1];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        dw[i] = Vec8{};
+        if constexpr (kHoldW) w_held[i] = load_w(p, rank + i * step);
+    }
+    int turn = 0, slot = 0;
+    const int64_t first = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index();
+    if constexpr (RING)
+        for (int k = 0; k + 1 < p.depth; ++k) fetch(first + k * rows_step, k);
+    float next = first < p.rows ? p.rstd[first] : 0.f;
+    for (int64_t r = first; r < p.rows; r += rows_step, turn ^= 1) {
         Raw8<T> g[V];
         Raw8<H> add[V];
         Vec8 n[V];
+        const float rstd = next;
+        if (r + rows_step < p.rows) next = p.rstd[r + rows_step];
+        if constexpr (RING) {
+            int to = slot + p.depth - 1;
+            if (to >= p.depth) to -= p.depth;
+            fetch(r + (p.depth - 1) * rows_step, to);
+            Ring::wait(p.depth - 1);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int j = rank + i * step;
-            g[i] = load_vec<ALIGNED>(dy, j, p.cols);
-            n[i] = p.h_in ? to_float(load_vec<ALIGNED>(h, j, p.cols)) : kept8(p, r, j);
-            if (p.dh_in) add[i] = load_vec<ALIGNED>(dh_in, j, p.cols);
+            for (int i = 0; i < V; ++i) {
+                const int cell = (slot * V + i) * per;
+                g[i] = ring.take<T>(cell);
+                if (p.h_in) {
+                    n[i] = to_float(ring.take<H>(cell + kX));
+                } else {
+                    const uint4 c = ring.word(cell + kX);
+                    n[i] = kept8(p, make_uint2(c.x, c.y),
+                                 (int)(c.z >> ((rank + i * step) / 4 % 4 * 8) & 255));
+                }
+                if (p.dh_in) add[i] = ring.take<H>(cell + in_h);
+            }
+            if (++slot == p.depth) slot = 0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int j = rank + i * step;
+                g[i] = load_vec(static_cast<const T *>(p.dy) + r * p.ldy, j, p.cols);
+                if (p.h_in)
+                    n[i] = to_float(load_vec(static_cast<const H *>(p.h_in) + r * p.ldh, j, p.cols));
+                else if (8 * j < p.pitch)
+                    n[i] = kept8(p, *reinterpret_cast<const uint2 *>(p.codes_h + r * p.pitch + 8 * j),
+                                 p.scales_h[r * p.spitch + j / 4]);
+                else
+                    n[i] = Vec8{};
+                if (p.dh_in)
+                    add[i] = load_vec(static_cast<const H *>(p.dh_in) + r * p.lddh_in, j, p.cols);
+            }
         }
-        const float rstd = p.rstd[r];
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const Vec8 w = load_w(p, rank + i * step), v = to_float(g[i]);
+            const Vec8 v = to_float(g[i]);
+            Vec8 w;
+            if constexpr (kHoldW) w = w_held[i];
+            else w = load_w(p, rank + i * step);
             const int left = p.cols - 8 * (rank + i * step);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -61,20 +117,19 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int j = rank + i * step;
-            if (8 * j >= p.cols) continue;
-            const Vec8 w = load_w(p, j), v = to_float(g[i]);
-            Vec8 d;
+            const Vec8 v = to_float(g[i]);
+            Vec8 w, d;
+            if constexpr (kHoldW) w = w_held[i];
+            else w = load_w(p, j);
             if (p.dh_in) d = to_float(add[i]);
             else d = Vec8{};
 #pragma unroll
             for (int e = 0; e < 8; ++e) d.v[e] += rstd * (v.v[e] * w.v[e] - n[i].v[e] * mean);
             if (p.dh)
-                store8<ALIGNED>(static_cast<H *>(p.dh) + r * p.lddh + 8 * j, from_float<H>(d),
-                                p.cols - 8 * j);
+                store_vec(p.out_aligned, static_cast<H *>(p.dh) + r * p.lddh, j, from_float<H>(d), p.cols);
             if (!p.dx) continue;
             if (p.drop.threshold) drop8(p.drop, offset, (uint32_t)r, (uint32_t)j, d);
-            store8<ALIGNED>(static_cast<T *>(p.dx) + r * p.lddx + 8 * j, from_float<T>(d),
-                            p.cols - 8 * j);
+            store_vec(p.out_aligned, static_cast<T *>(p.dx) + r * p.lddx, j, from_float<T>(d), p.cols);
         }
     }
     if (!p.part) return;
@@ -105,9 +160,9 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
     }
 }
 
-// dw = dw_in + the blocks' partial sums: a block takes 32 columns, 16 warps a strided
+// dw = dw_in + the blocks' partial sums: a block takes 32 columns, 32 warps a strided
 // share of the partial sums each.
-constexpr int kNormDwWarps = 16;
+constexpr int kNormDwWarps = 32;
 __global__ void __launch_bounds__(32 * kNormDwWarps)
     norm_dw_kernel(const float *part, int n_part, int cols, const float *dw_in, float *dw) {
     grid_dep_wait();
@@ -116,7 +171,7 @@ __global__ void __launch_bounds__(32 * kNormDwWarps)
     const int lane = threadIdx.x % 32, c = blockIdx.x * 32 + lane;
     float v = 0.f;
     if (c < cols)
-#pragma unroll 4
+#pragma unroll 8
         for (int b = threadIdx.x / 32; b < n_part; b += kNormDwWarps) v += part[b * (int64_t)cols + c];
     sum[threadIdx.x / 32][lane] = v;
     __syncthreads();
@@ -130,13 +185,20 @@ __global__ void __launch_bounds__(32 * kNormDwWarps)
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-template <typename T, typename H, class TEAM>
-static pos_status launch_backward(NormParams &p, const NormShape &shape, bool aligned,
-                                  const float *dw_in, float *dw, cudaStream_t s) {
-    auto kern = aligned ? norm_backward_kernel<T, H, TEAM, true>
-                        : norm_backward_kernel<T, H, TEAM, false>;
+template <typename T, typename H, class TEAM, bool RING>
+static pos_status launch_backward(NormParams &p, const NormShape &shape, const float *dw_in,
+                                  float *dw, cudaStream_t s) {
+    auto kern = norm_backward_kernel<T, H, TEAM, RING>;
+    int smem = 0;
+    if constexpr (RING) {
+        constexpr int kX = sizeof(T) / 2, kH = sizeof(H) / 2;
+        const int row = TEAM::V * (kX + (p.h_in ? kH : 1) + (p.dh_in ? kH : 0));
+        p.depth = ring_depth(row, shape.threads);
+        smem = 16 * p.depth * row * shape.threads;
+        POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), smem));
+    }
     int per_sm = 0;
-    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), shape.threads, 0, &per_sm));
+    POS_TRY(blocks_per_sm(reinterpret_cast<const void *>(kern), shape.threads, smem, &per_sm));
     const int64_t blocks = (p.rows + shape.rows - 1) / shape.rows;
     const int grid = (int)std::min<int64_t>(blocks, (int64_t)sm_count() * std::min(per_sm, 16));
     void *scratch = nullptr;
@@ -147,13 +209,20 @@ static pos_status launch_backward(NormParams &p, const NormShape &shape, bool al
         p.part = static_cast<float *>(scratch);
     }
     cudaError_t e =
-        grid > 0 ? launch_dependent(kern, grid, shape.threads, 0, s, p) : cudaSuccess;
+        grid > 0 ? launch_dependent(kern, grid, shape.threads, smem, s, p) : cudaSuccess;
     if (dw && e == cudaSuccess)
         e = launch_dependent(norm_dw_kernel, (p.cols + 31) / 32, 32 * kNormDwWarps, 0, s,
                              (const float *)p.part, grid, (int)p.cols, dw_in, dw);
     const cudaError_t e2 = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
     if (e == cudaSuccess) e = e2;
     return e == cudaSuccess ? POS_OK : cuda_fail(e, "norm backward");
+}
+
+template <typename T, typename H, class TEAM>
+static pos_status launch_backward(NormParams &p, const NormShape &shape, bool aligned,
+                                  const float *dw_in, float *dw, cudaStream_t s) {
+    return aligned ? launch_backward<T, H, TEAM, true>(p, shape, dw_in, dw, s)
+                   : launch_backward<T, H, TEAM, false>(p, shape, dw_in, dw, s);
 }
 
 template <typename T, typename H>
@@ -165,7 +234,7 @@ static pos_status backward_of(NormParams &p, bool aligned, const float *dw_in, f
         case 1: return launch_backward<T, H, Team<true, 4, 256>>(p, shape, aligned, dw_in, dw, s);
         case 2: return launch_backward<T, H, Team<false, 2, 512>>(p, shape, aligned, dw_in, dw, s);
         case 3: return launch_backward<T, H, Team<false, 4, 512>>(p, shape, aligned, dw_in, dw, s);
-        default: return launch_backward<T, H, Team<false, 4, 1024>>(p, shape, aligned, dw_in, dw, s);
+        default: return launch_backward<T, H, Team<false, 4, 1024>, false>(p, shape, dw_in, dw, s);
     }
 }
 
@@ -187,8 +256,9 @@ extern "C" pos_status poseidon_norm_backward(const pos_norm *norm, const void *d
         POS_TRY(check_matrix("h", d_h, over, rows, cols, ldh, false, &aligned));
         POS_TRY(check_matrix("dy", d_dy, norm->dtype, rows, cols, lddy, false, &aligned));
         POS_TRY(check_matrix("dh_in", d_dh_in, over, rows, cols, lddh_in, false, &aligned));
-        POS_TRY(check_matrix("dh", d_dh, over, rows, cols, lddh, true, &aligned));
-        POS_TRY(check_matrix("dx", d_dx, norm->dtype, rows, cols, lddx, true, &aligned));
+        p.out_aligned = true;
+        POS_TRY(check_matrix("dh", d_dh, over, rows, cols, lddh, true, &p.out_aligned));
+        POS_TRY(check_matrix("dx", d_dx, norm->dtype, rows, cols, lddx, true, &p.out_aligned));
         if (!aligned16(d_ckpt_h)) return fail(POS_EINVAL, "norm: checkpoint not 16-byte aligned");
         if (reinterpret_cast<uintptr_t>(d_rstd) % 4)
             return fail(POS_EINVAL, "norm: misaligned rstd");
