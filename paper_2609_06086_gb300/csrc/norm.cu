@@ -23,11 +23,11 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
         if (r < p.rows)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int j = rank + i * step, left = p.cols - 8 * j, cell = (slot * V + i) * (kX + kH);
-                ring.copy(cell, static_cast<const T *>(p.x) + r * p.ldx + (left > 0 ? 8 * j : 0), left);
+                const int cell = (slot * V + i) * (kX + kH);
+                ring.copy(cell, static_cast<const T *>(p.x) + r * p.ldx, rank + i * step, p.cols);
                 if (p.res)
-                    ring.copy(cell + kX,
-                              static_cast<const H *>(p.res) + r * p.ldr + (left > 0 ? 8 * j : 0), left);
+                    ring.copy(cell + kX, static_cast<const H *>(p.res) + r * p.ldr, rank + i * step,
+                              p.cols);
             }
         Ring::row_done();
     };
@@ -37,14 +37,11 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
     int turn = 0, slot = 0;
     const int64_t first = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index();
     if constexpr (RING)
-        for (int k = 0; k + 1 < p.depth; ++k) fetch(first + k * rows_step, k);
+        for (int k = 0; k < p.depth; ++k) fetch(first + k * rows_step, k);
     for (int64_t r = first; r < p.rows; r += rows_step, turn ^= 1) {
         Raw8<T> xr[V];
         Raw8<H> hr[V];
         if constexpr (RING) {
-            int to = slot + p.depth - 1;
-            if (to >= p.depth) to -= p.depth;
-            fetch(r + (p.depth - 1) * rows_step, to);
             Ring::wait(p.depth - 1);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -52,7 +49,6 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
                 xr[i] = ring.take<T>(cell);
                 if (p.res) hr[i] = ring.take<H>(cell + kX);
             }
-            if (++slot == p.depth) slot = 0;
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -61,7 +57,7 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
                     hr[i] = load_vec(static_cast<const H *>(p.res) + r * p.ldr, rank + i * step, p.cols);
             }
         }
-        float squares = 0.f;
+        F2 squares = both(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int j = rank + i * step;
@@ -72,30 +68,54 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormPara
                 drop8(p.drop, offset, (uint32_t)r, (uint32_t)j, v);
             }
             hr[i] = from_float<H>(v);
-            if (p.h) store_vec(p.out_aligned, static_cast<H *>(p.h) + r * p.ldh, j, hr[i], p.cols);
+            H *h = static_cast<H *>(p.h) + r * p.ldh;
+            if constexpr (RING && kH == 2) {
+                if (p.h && p.out_aligned)
+                    ring.store((slot * V + i) * (kX + kH) + kX, hr[i], h, j, p.cols);
+                else if (p.h) store_vec(false, h, j, hr[i], p.cols);
+            } else if (p.h) {
+                store_vec(p.out_aligned, h, j, hr[i], p.cols);
+            }
             if (p.codes_h)
                 keep8(p.format, hr[i], p.codes_h + r * p.pitch, p.scales_h + r * p.spitch, j,
                       8 * j < p.pitch);
             v = to_float(hr[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) squares += v.v[e] * v.v[e];
+            for (int e = 0; e < 8; e += 2) squares = fma2(pair(v, e), pair(v, e), squares);
         }
-        squares = TEAM::sum(squares, shared, turn);
-        const float rstd = rsqrtf(squares * p.inv_cols + p.eps);
+        const int done = slot;
+        if constexpr (RING) {
+            if constexpr (kX == 1) {  // (else y goes through x's cells first)
+                __syncwarp();
+                fetch(r + p.depth * rows_step, slot);
+            }
+            if (++slot == p.depth) slot = 0;
+        }
+        const float rstd = rsqrtf(TEAM::sum(squares.x + squares.y, shared, turn) * p.inv_cols + p.eps);
         if (p.rstd && rank == 0) p.rstd[r] = rstd;
-        if (!p.y && !p.codes_y) continue;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            if (!p.y && !p.codes_y) break;
             const int j = rank + i * step;
             Vec8 v = to_float(hr[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)  // (past the last column 0, also under a norm that is NaN)
-                v.v[e] = 8 * j + e < p.cols ? v.v[e] * rstd * w[i].v[e] : 0.f;
+            for (int e = 0; e < 8; e += 2)  // (past the last column 0, or NaN with the whole group)
+                set_pair(v, e, mul2(mul2(pair(v, e), both(rstd)), pair(w[i], e)));
             const Raw8<T> y = from_float<T>(v);
-            if (p.y) store_vec(p.out_aligned, static_cast<T *>(p.y) + r * p.ldy, j, y, p.cols);
+            T *to = static_cast<T *>(p.y) + r * p.ldy;
+            if constexpr (RING && kX == 2) {
+                if (p.y && p.out_aligned) ring.store((done * V + i) * (kX + kH), y, to, j, p.cols);
+                else if (p.y) store_vec(false, to, j, y, p.cols);
+            } else if (p.y) {
+                store_vec(p.out_aligned, to, j, y, p.cols);
+            }
             if (p.codes_y)
                 keep8(p.format, y, p.codes_y + r * p.pitch, p.scales_y + r * p.spitch, j,
                       8 * j < p.pitch);
+        }
+        if constexpr (RING && kX == 2) {
+            __syncwarp();
+            fetch(r + p.depth * rows_step, done);
         }
     }
 }
@@ -164,11 +184,10 @@ static pos_status launch_forward(const NormParams &p, const NormShape &shape, bo
 
 template <typename T, typename H>
 static pos_status forward_of(const NormParams &p, bool aligned, cudaStream_t s) {
-    const NormShape shape = norm_shape(p.cols);
+    const NormShape shape = norm_shape(p.cols, false);
     switch (shape.team) {
         case 0: return launch_forward<T, H, Team<true, 1, 256>>(p, shape, aligned, s);
-        case 1: return launch_forward<T, H, Team<true, 4, 256>>(p, shape, aligned, s);
-        case 2: return launch_forward<T, H, Team<false, 2, 512>>(p, shape, aligned, s);
+        case 1: return launch_forward<T, H, Team<false, 1, 1024>>(p, shape, aligned, s);
         case 3: return launch_forward<T, H, Team<false, 4, 512>>(p, shape, aligned, s);
         // (a row of 1024 threads would fill an SM's shared memory)
         default: return launch_forward<T, H, Team<false, 4, 1024>, false>(p, shape, s);

@@ -59,62 +59,103 @@ __device__ __forceinline__ Raw8<T> load_vec(const T *row, int j, int cols) {
     return load8_shifted(row + 8 * j, 8 * j, cols - 8 * j);
 }
 
-// Rows on their way to shared memory, `depth` - 1 of them ahead: a thread copies and
-// reads its own vectors, so the block need not meet.  Without them a row's loads, its
-// sum over the block and its stores take turns, and registers leave room for one block of
-// 512 threads an SM.  A cell is 16 bytes; a vector takes some cells, a slot of the ring
-// one row.
+// Rows on their way to shared memory, ahead of the one that is worked on.  Without them
+// a row's loads, its sum over the block and its stores take turns, and registers leave
+// room for few blocks an SM.  A slot of the ring is a row, a vector takes 16-byte cells of
+// it: one for 16-bit elements and for codes, two for f32.  A warp copies and reads its own
+// vectors, so the block need not meet.  A lane's 8 values in f32 are 32 bytes, but a copy
+// or store of 16 bytes of each lane's would use half of every sector at a time: the two
+// cells of a warp are the 1024 bytes as they lie in memory, which its lanes copy, and
+// write from, 512 bytes at a time.
 struct Ring {
-    uint32_t base;   // this thread's first cell
+    uint32_t smem;
     int step;        // bytes from cell to cell
-    __device__ __forceinline__ explicit Ring(void *smem)
-        : base((uint32_t)__cvta_generic_to_shared(smem) + 16 * threadIdx.x), step(16 * blockDim.x) {}
-    // 8 elements, of which `left` exist (the others read as zeros)
+    int lane, warp;
+    __device__ __forceinline__ explicit Ring(void *at)
+        : smem((uint32_t)__cvta_generic_to_shared(at)), step(16 * blockDim.x),
+          lane(threadIdx.x % 32), warp(threadIdx.x / 32) {}
+    __device__ __forceinline__ uint32_t own(int cell) const {
+        return smem + cell * step + 16 * threadIdx.x;
+    }
+    // 16 bytes of two cells in memory's order; exchanged so that reading every second
+    // one meets no bank twice
+    __device__ __forceinline__ uint32_t word(int cell, int w) const {
+        return smem + cell * step + 1024 * warp + 16 * (w ^ (w >> 3 & 1));
+    }
+    // The warp's vectors of a row, 8 `rank` its lane's first column.
     template <typename T>
-    __device__ __forceinline__ void copy(int cell, const T *from, int left) const {
+    __device__ __forceinline__ void copy(int cell, const T *row, int rank, int cols) const {
+        constexpr int kPer = 16 / sizeof(T);
 #pragma unroll
         for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-            constexpr int kPer = 16 / sizeof(T);
-            const int n = max(0, min(kPer, left - kPer * k));
+            const int w = lane + 32 * k;
+            const int c = sizeof(T) == 4 ? 8 * (rank - lane) + kPer * w : 8 * rank;
+            const int n = max(0, min(kPer, cols - c));
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                             base + (cell + k) * step),
-                         "l"(n ? from + kPer * k : from), "r"((int)(n * sizeof(T)))
+                             sizeof(T) == 4 ? word(cell, w) : own(cell)),
+                         "l"(row + (n ? c : 0)), "r"((int)(n * sizeof(T)))
                          : "memory");
         }
     }
     template <typename T>
     __device__ __forceinline__ Raw8<T> take(int cell) const {
         Raw8<T> r;
-        r.a = word(cell);
-        if constexpr (sizeof(T) == 4) r.b = word(cell + 1);
+        if constexpr (sizeof(T) == 4) r.a = read(word(cell, 2 * lane)), r.b = read(word(cell, 2 * lane + 1));
+        else r.a = read(own(cell));
         return r;
     }
     // 8 codes and the word of scales that has theirs
     __device__ __forceinline__ void copy_codes(int cell, const uint8_t *codes, const uint8_t *scales,
                                                bool there) const {
-        const uint32_t at = base + cell * step;
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(at), "l"(codes),
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(own(cell)), "l"(codes),
                      "r"(there ? 8 : 0)
                      : "memory");
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + 8), "l"(scales),
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(own(cell) + 8), "l"(scales),
                      "r"(there ? 4 : 0)
                      : "memory");
     }
-    __device__ __forceinline__ uint4 word(int cell) const {
+    // f32: the warp's vectors through two cells to an aligned row
+    __device__ __forceinline__ void store(int cell, const Raw8<float> &r, float *row, int rank,
+                                          int cols) const {
+        write(word(cell, 2 * lane), r.a);
+        write(word(cell, 2 * lane + 1), r.b);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int w = lane + 32 * k, c = 8 * (rank - lane) + 4 * w;
+            const uint4 v = read(word(cell, w));
+            if (c + 4 <= cols) {
+                *reinterpret_cast<uint4 *>(row + c) = v;
+            } else {
+                const uint32_t e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c + i < cols) row[c + i] = __uint_as_float(e[i]);
+            }
+        }
+    }
+    static __device__ __forceinline__ uint4 read(uint32_t at) {
         uint4 v;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(base + cell * step));
+                     : "r"(at)
+                     : "memory");
         return v;
+    }
+    static __device__ __forceinline__ void write(uint32_t at, const uint4 &v) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y),
+                     "r"(v.z), "r"(v.w)
+                     : "memory");
     }
     static __device__ __forceinline__ void row_done() {
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // All rows but the last `ahead` have arrived.
+    // All rows but the last `ahead` have arrived, for the whole warp.
     static __device__ __forceinline__ void wait(int ahead) {
         if (ahead >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
 };
 constexpr int kNormDepth = 3;
@@ -137,6 +178,9 @@ __device__ __forceinline__ void store_vec(bool aligned, T *row, int j, const Raw
         store8_shifted(row + 8 * j, r, left, lane > 0, lane < 31);
     }
 }
+
+__device__ __forceinline__ F2 pair(const Vec8 &x, int i) { return {x.v[i], x.v[i + 1]}; }
+__device__ __forceinline__ void set_pair(Vec8 &x, int i, F2 v) { x.v[i] = v.x, x.v[i + 1] = v.y; }
 
 __device__ __forceinline__ Vec8 load_w(const NormParams &p, int j) {
     Vec8 w;
@@ -166,25 +210,36 @@ __device__ __forceinline__ void keep8(int format, const Raw8<T> &raw, uint8_t *c
     const int byte = i8 ? scale_byte<POS_CKPT_INT8>(bits) : scale_byte<POS_CKPT_E4M3>(bits);
     if (!live) return;
     const Vec8 x = to_float(raw);
-    *reinterpret_cast<uint2 *>(codes + 8 * j) =
-        i8 ? encode8<POS_CKPT_INT8>(x, byte) : encode8<POS_CKPT_E4M3>(x, byte);
+    uint2 c;
+    if (byte >= Fmt<POS_CKPT_E4M3>::kScaleHi)  // (the lower of the two formats' largest)
+        c = i8 ? encode8<POS_CKPT_INT8>(x, byte) : encode8<POS_CKPT_E4M3>(x, byte);
+    else if (i8)
+        c = make_uint2(encode4_inside<POS_CKPT_INT8>(x.v[0], x.v[1], x.v[2], x.v[3], byte),
+                       encode4_inside<POS_CKPT_INT8>(x.v[4], x.v[5], x.v[6], x.v[7], byte));
+    else
+        c = make_uint2(encode4_inside<POS_CKPT_E4M3>(x.v[0], x.v[1], x.v[2], x.v[3], byte),
+                       encode4_inside<POS_CKPT_E4M3>(x.v[4], x.v[5], x.v[6], x.v[7], byte));
+    *reinterpret_cast<uint2 *>(codes + 8 * j) = c;
     if (j % 4 == 0) scales[j / 4] = (uint8_t)byte;
 }
 
-// Threads of a block for a call, and which Team: rows of up to 1024 columns by a warp
-// each, up to 32 elements a thread else.
+// Threads of a block for a call, and which Team.  Up to 8192 columns a vector a thread:
+// 64 registers, so that 32 warps an SM hide one another's sums and codes; the backward pass
+// from 2056 on two, which need half as many warps to meet (16384 x 8192, stream in f32, from
+// 8 bits: 288 us, with one 340; forward of 16384 x 4096 bf16 with both checkpoints and dropout:
+// one 128 us, with two 138).
 struct NormShape {
-    int team;     // 0..4: Team<true, 1, 256>, <true, 4, 256>, <false, 2, 512>, <false, 4, 512>,
+    int team;     // 0..4: Team<true, 1, 256>, <false, 1, 1024>, <false, 2, 512>, <false, 4, 512>,
                   // <false, 4, 1024>
     int threads, rows;  // of a block
 };
-inline NormShape norm_shape(int cols) {
+inline NormShape norm_shape(int cols, bool backward) {
     // (vectors of the padded codes: 32 columns each four)
     const int nv = (cols + kGroup - 1) / kGroup * 4;
     if (nv <= 32) return {0, 256, 8};
-    if (nv <= 128) return {1, 256, 8};
-    const int v = nv <= 1024 ? 2 : 4, threads = ((nv + v - 1) / v + 31) / 32 * 32;
-    return {v == 2 ? 2 : threads <= 512 ? 3 : 4, threads, 1};
+    const int v = nv > 1024 ? 4 : backward && nv > 256 ? 2 : 1;
+    const int threads = ((nv + v - 1) / v + 31) / 32 * 32;
+    return {v < 4 ? v : threads <= 512 ? 3 : 4, threads, 1};
 }
 
 pos_status check_norm(const pos_norm *n, NormParams *p);

@@ -24,22 +24,23 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
     const uint64_t offset = drop_offset(p.drop);
     const int64_t rows_step = (int64_t)gridDim.x * TEAM::teams();
     const Ring ring(cells);
-    // cells of a vector: dy, h (or its codes), dh_in
-    const int in_h = kX + (p.h_in ? kH : 1), per = in_h + (p.dh_in ? kH : 0);
+    // cells of a vector: dy, h (or its codes), dh_in or dh
+    const int in_h = kX + (p.h_in ? kH : 1), per = in_h + kH;
     const auto fetch = [&](int64_t r, int slot) {
         if (r < p.rows)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int j = rank + i * step, left = p.cols - 8 * j, cell = (slot * V + i) * per;
-                const int c = left > 0 ? 8 * j : 0;
-                ring.copy(cell, static_cast<const T *>(p.dy) + r * p.ldy + c, left);
-                if (p.h_in)
-                    ring.copy(cell + kX, static_cast<const H *>(p.h_in) + r * p.ldh + c, left);
-                else
+                const int j = rank + i * step, cell = (slot * V + i) * per;
+                ring.copy(cell, static_cast<const T *>(p.dy) + r * p.ldy, j, p.cols);
+                if (p.h_in) {
+                    ring.copy(cell + kX, static_cast<const H *>(p.h_in) + r * p.ldh, j, p.cols);
+                } else {
+                    const int c = 8 * j < p.cols ? 8 * j : 0;
                     ring.copy_codes(cell + kX, p.codes_h + r * p.pitch + c,
-                                    p.scales_h + r * p.spitch + c / 128 * 4, left > 0);
+                                    p.scales_h + r * p.spitch + c / 128 * 4, 8 * j < p.cols);
+                }
                 if (p.dh_in)
-                    ring.copy(cell + in_h, static_cast<const H *>(p.dh_in) + r * p.lddh_in + c, left);
+                    ring.copy(cell + in_h, static_cast<const H *>(p.dh_in) + r * p.lddh_in, j, p.cols);
             }
         Ring::row_done();
     };
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
     int turn = 0, slot = 0;
     const int64_t first = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index();
     if constexpr (RING)
-        for (int k = 0; k + 1 < p.depth; ++k) fetch(first + k * rows_step, k);
+        for (int k = 0; k < p.depth; ++k) fetch(first + k * rows_step, k);
     float next = first < p.rows ? p.rstd[first] : 0.f;
     for (int64_t r = first; r < p.rows; r += rows_step, turn ^= 1) {
         Raw8<T> g[V];
@@ -62,9 +63,6 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
         const float rstd = next;
         if (r + rows_step < p.rows) next = p.rstd[r + rows_step];
         if constexpr (RING) {
-            int to = slot + p.depth - 1;
-            if (to >= p.depth) to -= p.depth;
-            fetch(r + (p.depth - 1) * rows_step, to);
             Ring::wait(p.depth - 1);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -73,13 +71,12 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
                 if (p.h_in) {
                     n[i] = to_float(ring.take<H>(cell + kX));
                 } else {
-                    const uint4 c = ring.word(cell + kX);
+                    const uint4 c = Ring::read(ring.own(cell + kX));
                     n[i] = kept8(p, make_uint2(c.x, c.y),
                                  (int)(c.z >> ((rank + i * step) / 4 % 4 * 8) & 255));
                 }
                 if (p.dh_in) add[i] = ring.take<H>(cell + in_h);
             }
-            if (++slot == p.depth) slot = 0;
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -96,26 +93,25 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
                     add[i] = load_vec(static_cast<const H *>(p.dh_in) + r * p.lddh_in, j, p.cols);
             }
         }
-        float dot = 0.f;
+        F2 dot = both(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const Vec8 v = to_float(g[i]);
             Vec8 w;
             if constexpr (kHoldW) w = w_held[i];
             else w = load_w(p, rank + i * step);
-            const int left = p.cols - 8 * (rank + i * step);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // (past the last column 0, also in a group that is NaN)
-                n[i].v[e] = e < left ? n[i].v[e] * rstd : 0.f;
-                dw[i].v[e] += v.v[e] * n[i].v[e];
-                dot += v.v[e] * w.v[e] * n[i].v[e];
+            for (int e = 0; e < 8; e += 2) {
+                const F2 x = mul2(pair(n[i], e), both(rstd));
+                set_pair(n[i], e, x);
+                set_pair(dw[i], e, fma2(pair(v, e), x, pair(dw[i], e)));
+                dot = fma2(mul2(pair(v, e), pair(w, e)), x, dot);
             }
         }
-        const float mean = TEAM::sum(dot, shared, turn) * p.inv_cols;
-        if (!p.dh && !p.dx) continue;
+        const float mean = TEAM::sum(dot.x + dot.y, shared, turn) * p.inv_cols;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            if (!p.dh && !p.dx) break;
             const int j = rank + i * step;
             const Vec8 v = to_float(g[i]);
             Vec8 w, d;
@@ -124,12 +120,32 @@ __global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormPar
             if (p.dh_in) d = to_float(add[i]);
             else d = Vec8{};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d.v[e] += rstd * (v.v[e] * w.v[e] - n[i].v[e] * mean);
-            if (p.dh)
-                store_vec(p.out_aligned, static_cast<H *>(p.dh) + r * p.lddh, j, from_float<H>(d), p.cols);
+            for (int e = 0; e < 8; e += 2) {
+                const F2 a = fma2(pair(n[i], e), both(-mean), mul2(pair(v, e), pair(w, e)));
+                set_pair(d, e, fma2(a, both(rstd), pair(d, e)));
+            }
+            H *dh = static_cast<H *>(p.dh) + r * p.lddh;
+            if constexpr (RING && kH == 2) {
+                if (p.dh && p.out_aligned)
+                    ring.store((slot * V + i) * per + in_h, from_float<H>(d), dh, j, p.cols);
+                else if (p.dh) store_vec(false, dh, j, from_float<H>(d), p.cols);
+            } else if (p.dh) {
+                store_vec(p.out_aligned, dh, j, from_float<H>(d), p.cols);
+            }
             if (!p.dx) continue;
             if (p.drop.threshold) drop8(p.drop, offset, (uint32_t)r, (uint32_t)j, d);
-            store_vec(p.out_aligned, static_cast<T *>(p.dx) + r * p.lddx, j, from_float<T>(d), p.cols);
+            T *dx = static_cast<T *>(p.dx) + r * p.lddx;
+            if constexpr (RING && kX == 2) {
+                if (p.out_aligned) ring.store((slot * V + i) * per, from_float<T>(d), dx, j, p.cols);
+                else store_vec(false, dx, j, from_float<T>(d), p.cols);
+            } else {
+                store_vec(p.out_aligned, dx, j, from_float<T>(d), p.cols);
+            }
+        }
+        if constexpr (RING) {
+            __syncwarp();
+            fetch(r + p.depth * rows_step, slot);
+            if (++slot == p.depth) slot = 0;
         }
     }
     if (!p.part) return;
@@ -192,7 +208,7 @@ static pos_status launch_backward(NormParams &p, const NormShape &shape, const f
     int smem = 0;
     if constexpr (RING) {
         constexpr int kX = sizeof(T) / 2, kH = sizeof(H) / 2;
-        const int row = TEAM::V * (kX + (p.h_in ? kH : 1) + (p.dh_in ? kH : 0));
+        const int row = TEAM::V * (kX + (p.h_in ? kH : 1) + kH);
         p.depth = ring_depth(row, shape.threads);
         smem = 16 * p.depth * row * shape.threads;
         POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), smem));
@@ -228,10 +244,10 @@ static pos_status launch_backward(NormParams &p, const NormShape &shape, bool al
 template <typename T, typename H>
 static pos_status backward_of(NormParams &p, bool aligned, const float *dw_in, float *dw,
                               cudaStream_t s) {
-    const NormShape shape = norm_shape(p.cols);
+    const NormShape shape = norm_shape(p.cols, true);
     switch (shape.team) {
         case 0: return launch_backward<T, H, Team<true, 1, 256>>(p, shape, aligned, dw_in, dw, s);
-        case 1: return launch_backward<T, H, Team<true, 4, 256>>(p, shape, aligned, dw_in, dw, s);
+        case 1: return launch_backward<T, H, Team<false, 1, 1024>>(p, shape, aligned, dw_in, dw, s);
         case 2: return launch_backward<T, H, Team<false, 2, 512>>(p, shape, aligned, dw_in, dw, s);
         case 3: return launch_backward<T, H, Team<false, 4, 512>>(p, shape, aligned, dw_in, dw, s);
         default: return launch_backward<T, H, Team<false, 4, 1024>, false>(p, shape, dw_in, dw, s);
