@@ -291,9 +291,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             ph ^= 1;
             tmem_after();
             uint32_t s[kTile];
-#pragma unroll
-            for (int c = 0; c < kTile; c += 32) tmem_load32(s_tm + c, s + c);
-            tmem_wait_loads();
+            tmem_load128(s_tm, s);
             if (j == n - 1) {
                 const int seen = row - j * kTile;  // the last key that the row sees
 #pragma unroll
@@ -325,7 +323,6 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     for (int c = 0; c < dim16; c += 16) {
                         uint32_t o[16];
                         tmem_load16(o_tm + c, o);
-                        tmem_wait_loads();
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
                             o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
@@ -366,7 +363,6 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             for (int c = 0; c < dim16; c += 16) {
                 uint32_t o[16];
                 tmem_load16(o_tm + c, o);
-                tmem_wait_loads();
                 Vec8 x[2];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {

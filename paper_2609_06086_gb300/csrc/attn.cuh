@@ -29,6 +29,8 @@ struct AttnParams {
     float *lse;                 // [heads_q][tokens] or NULL
     float2 *stats;              // backward: [heads_q][tokens]: lse in powers of two, D
     uint32_t *largest;          // backward in f16: bits of dO's largest magnitude
+    float *part;                // backward: sums of parts of the keys' gradients
+    int32_t parts;
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
     const int32_t *n_tiles;
     int64_t tokens;
@@ -86,9 +88,9 @@ __device__ __forceinline__ uint32_t one_lane() {
 // them 32 bytes on), and rows that are the inner index themselves (16 of them 2048
 // bytes on, the next 64 columns a block on).  High words are alike.
 constexpr uint32_t kDescHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
-__device__ __forceinline__ uint32_t by_rows(uint32_t addr) { return addr >> 4 | 1u << 16; }
-__device__ __forceinline__ uint32_t by_columns(uint32_t addr) {
-    return addr >> 4 | (uint32_t)(kBox >> 4) << 16;
+__device__ __forceinline__ uint32_t by_rows(uint32_t addr) { return (addr >> 4 & 0x3fffu) | 1u << 16; }
+__device__ __forceinline__ uint32_t by_columns(uint32_t addr) {  // (in a cluster an address has
+    return (addr >> 4 & 0x3fffu) | (uint32_t)(kBox >> 4) << 16;  // the block's rank above)
 }
 // f32 sums of 16-bit products, 128 rows, n columns.
 template <typename T>
@@ -153,33 +155,77 @@ __device__ __forceinline__ void tmem_before() {
 __device__ __forceinline__ void tmem_after() {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
-__device__ __forceinline__ void tmem_wait_loads() {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
 __device__ __forceinline__ void tmem_wait_stores() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
-// 16 or 32 columns of the warp's lanes; the loads are there after tmem_wait_loads().
+// 16 or 32 columns of the warp's lanes.  A load and its wait are one instruction to the
+// compiler: between the two it may not use, or copy, the registers.
 __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t *r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
-        "%11, %12, %13, %14, %15}, [%16];"
+        "%11, %12, %13, %14, %15}, [%16];\ntcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15])
-        : "r"(addr));
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t *r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
         "%11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
-        "%28, %29, %30, %31}, [%32];"
+        "%28, %29, %30, %31}, [%32];\ntcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-          "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+// A thread's whole row of scores.
+__device__ __forceinline__ void tmem_load128(uint32_t addr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
+        "%12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31"
+        "}, [%128];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, "
+        "%44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, "
+        "%56, %57, %58, %59, %60, %61, %62, %63"
+        "}, [%129];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, "
+        "%76, %77, %78, %79, %80, %81, %82, %83, %84, %85, %86, %87, "
+        "%88, %89, %90, %91, %92, %93, %94, %95"
+        "}, [%130];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%96, %97, %98, %99, %100, %101, %102, %103, %104, %105, %106, %107, "
+        "%108, %109, %110, %111, %112, %113, %114, %115, %116, %117, %118, %119, "
+        "%120, %121, %122, %123, %124, %125, %126, %127"
+        "}, [%131];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]),
+          "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]),
+          "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]),
+          "=r"(r[80]), "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]),
+          "=r"(r[88]), "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]),
+          "=r"(r[96]), "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]),
+          "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]),
+          "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]),
+          "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+        : "r"(addr), "r"(addr + 32), "r"(addr + 64), "r"(addr + 96)
+        : "memory");
 }
 __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t *r) {
     asm volatile(
@@ -194,15 +240,20 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t *r) {
 // 16 h + 4 b + 2 r + e is that of row 16 h + 8 r + lane / 4, column 8 b + lane % 4 * 2 + e;
 // and 16 columns of pairs of 16-bit values in the same places.
 __device__ __forceinline__ void tmem_load_block(uint32_t addr, uint32_t *r) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h, r += 16)
-        asm volatile(
-            "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
-            "%11, %12, %13, %14, %15}, [%16];"
-            : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-              "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
-              "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-            : "r"(addr + ((uint32_t)(16 * h) << 16)));
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, "
+        "%11, %12, %13, %14, %15}, [%32];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, "
+        "%25, %26, %27, %28, %29, %30, %31}, [%33];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(addr), "r"(addr + (16u << 16))
+        : "memory");
 }
 __device__ __forceinline__ void tmem_store_block(uint32_t addr, const uint32_t *r) {
 #pragma unroll
@@ -323,10 +374,11 @@ __device__ __forceinline__ void add_row(RowPart &sum, float w, const T *row, int
 }
 template <typename T>
 __device__ __forceinline__ void write_row(void *out, int64_t at, const RowPart &sum, float factor,
-                                          int dim, int lane) {
+                                          int dim, int lane, int side = -1) {
+    // (side: which of four in turn of 16 columns, or all)
 #pragma unroll
     for (int i = 0; i < kAttnMaxDim / 32; ++i)
-        if (lane + 32 * i < dim) static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
+        if (lane + 32 * i < dim && (side < 0 || (lane + 32 * i) / 16 % 4 == side)) static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
 }
 
 // ---------------------------------------------------------------------------
@@ -342,6 +394,7 @@ pos_status attn_input(const pos_attn *a, const pos_heads &t, int64_t heads, char
                       cudaStream_t s, AttnTensor *out);
 pos_status attn_map(CUtensorMap *map, const pos_attn *a, const AttnTensor &t, int64_t heads,
                     int32_t dim);
+int64_t attn_most_tiles(const pos_attn *a, int rows);
 int64_t attn_list_bytes(const pos_attn *a, int rows);
 pos_status attn_list(const pos_attn *a, int rows, char **at, cudaStream_t s, AttnParams *p);
 pos_status attn_grid(const pos_attn *a, int rows, int64_t heads, int *grid);

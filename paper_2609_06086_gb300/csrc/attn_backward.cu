@@ -1,4 +1,6 @@
 // poseidon_attn_backward (formulas: poseidon.h).
+#include <cmath>
+
 #include "attn.cuh"
 
 namespace pos {
@@ -259,7 +261,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             // the last key of this part that the row sees; a row that sees one has dS = 0
             const int seen = row - (n - 1) * kTile - kCols * side;
             tmem_load32(s_tm, s);
-            tmem_wait_loads();
 #pragma unroll
             for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
@@ -284,7 +285,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (!ok) break;
             tmem_after();
             tmem_load32(d_tm, d);
-            tmem_wait_loads();
 #pragma unroll
             for (int c = 0; c < kCols; c += 2) {
                 const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
@@ -326,7 +326,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 uint32_t v[16], k[16];
                 tmem_load16(dq_tm + lanes + c, v);
                 tmem_load16(pk_tm + lanes + c, k);
-                tmem_wait_loads();
                 Vec8 x[2];
 #pragma unroll
                 for (int h = 0; h < 16; ++h) {
@@ -375,6 +374,10 @@ __global__ void __launch_bounds__(kBackThreads, 1)
 // scores, dP, and both sums, and is full: P takes the scores' place and dS that of dP,
 // and while one of them is made, the tensor cores use up the other and compute what
 // comes next in its place.
+//   Up to eight blocks share 128 keys where the most steps of one block would outlast the
+// others: each takes a run of the steps and puts its sums in memory, and attn_join_kernel
+// adds them up in order.  (As a cluster that adds them up through its blocks' shared
+// memory, 8 microseconds more for a pair.)
 constexpr int kQuerySlots = 2;
 constexpr int kStatBytes = kTile * 8;
 constexpr int kDkvBars = 6 * kQuerySlots + 6;
@@ -387,9 +390,10 @@ __device__ __forceinline__ F2 load_stats(uint32_t at) {
     return l;
 }
 
+// side >= 0: only the columns that a block of attn_join_kernel takes are written.
 template <typename T>
 __device__ __forceinline__ void dkv_row(const AttnParams &p, const AttnUnit &u, int row, int g,
-                                        int lane) {
+                                        int lane, int side = -1) {
     const T *k = row_at<T>(p.k, u.start + row, g), *v = row_at<T>(p.v, u.start + row, g);
     RowPart dk = {}, dv = {};
     for (int head = g * p.group; head < (g + 1) * p.group; ++head)
@@ -410,9 +414,29 @@ __device__ __forceinline__ void dkv_row(const AttnParams &p, const AttnUnit &u, 
             }
         }
     write_row<T>(p.dk, (u.start + row) * p.d_token[1] + g * p.d_head[1], dk, p.scale, p.dim_out,
-                 lane);
-    write_row<T>(p.dv, (u.start + row) * p.d_token[2] + g * p.d_head[2], dv, 1.f, p.dim_out, lane);
+                 lane, side);
+    write_row<T>(p.dv, (u.start + row) * p.d_token[2] + g * p.d_head[2], dv, 1.f, p.dim_out, lane,
+                 side);
 }
+
+// Where the sums of a part of a block's steps go: [tensor][16 columns][4 columns][128 keys][4].
+__device__ __forceinline__ float4 *part_at(const AttnParams &p, int part, int t, int c, int key) {
+    const int dim16 = (p.dim + 15) / 16 * 16;
+    return reinterpret_cast<float4 *>(p.part) +
+           (((int64_t)part * 2 + t) * dim16 + c) * (kTile / 4) + key;
+}
+// The key tile's number, steps of all heads and those of one part of them.
+struct KeySteps {
+    int each, first, n;  // steps of a head; the part's first, and how many it has
+    __device__ __forceinline__ KeySteps(const AttnParams &p, AttnUnit &u, int part) {
+        // the list is in the order of a query tile's keys; of a key tile's queries it is this
+        const int tiles = (u.len + kTile - 1) / kTile;
+        u.tile = tiles - 1 - u.tile;
+        each = tiles - u.tile;
+        first = (int)((int64_t)each * p.group * part / p.parts);
+        n = (int)((int64_t)each * p.group * (part + 1) / p.parts) - first;
+    }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(kBackThreads, 1)
@@ -463,21 +487,20 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
     const uint32_t dp_tm = tmem + kTile, dv_tm = tmem + 2 * kTile, dk_tm = tmem + 3 * kTile;
 
-    const int g = blockIdx.x % p.heads_k;
+    const int unit = blockIdx.x / p.parts, part = blockIdx.x % p.parts, g = unit % p.heads_k;
     AttnUnit u;
-    const bool any = unit_at<kTile>(p, blockIdx.x / p.heads_k, u);
-    // the list is in the order of a query tile's keys; of a key tile's queries it is this
-    const int tiles = any ? (u.len + kTile - 1) / kTile : 0;
-    if (any) u.tile = tiles - 1 - u.tile;
-    const int each = any ? tiles - u.tile : 0;  // tiles of queries of a head
-    const int n = each * p.group;
+    int each = 0, step0 = 0, n = 0;  // this block's steps: from step0 on, n of them
+    if (unit_at<kTile>(p, unit / p.heads_k, u)) {
+        const KeySteps steps(p, u, part);
+        each = steps.each, step0 = steps.first, n = steps.n;
+    }
     const int boxes = p.dim > 64 ? 2 : 1;
     bool ok = true;
 
     if (group == kSumGroups) {
         give_registers<kBackIssueRegs>();
         if (warp == kLoadWarp) {
-            if (lane == 0 && any) {
+            if (lane == 0 && n > 0) {
                 bar_expect(in_full, 2 * boxes * kBox);
                 for (int b = 0; b < boxes; ++b) {
                     const int token = u.start + u.tile * kTile;
@@ -487,8 +510,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 int s = 0;
                 uint32_t ph = 1;
                 for (int i = 0; i < n && ok; ++i) {
-                    const int head = g * p.group + i / each;
-                    const int token = u.start + (u.tile + i % each) * kTile;
+                    const int head = g * p.group + (step0 + i) / each;
+                    const int token = u.start + (u.tile + (step0 + i) % each) * kTile;
                     for (int w = 0; w < 2 && ok; ++w) {
                         const uint32_t full = (w ? g_full : q_full) + 8 * s;
                         ok = bar_wait((w ? g_empty : q_empty) + 8 * s, ph, gave_up);
@@ -507,7 +530,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             const auto arrived = [&](uint32_t full, uint32_t at, int i) {
                 const int s = i % kQuerySlots;
                 if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, gave_up)) return false;
-                const int seen = u.len - (u.tile + i % each) * kTile;
+                const int seen = u.len - (u.tile + (step0 + i) % each) * kTile;
                 if (seen < kTile) zero_rows(at + s * kTileBytes, seen, boxes, lane);
                 return true;
             };
@@ -523,7 +546,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 commit(dp_full, mine);
                 return true;
             };
-            if (any) {
+            if (n > 0) {
                 ok = wait_warp(in_full, 0, gave_up);
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
@@ -549,8 +572,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             // probabilities are 2^(0 - inf) = 0
             const Shift<T> shift(p);
             for (int i = 0; i < n && ok; ++i) {
-                const int s = i % kQuerySlots, head = g * p.group + i / each;
-                const int row = (u.tile + i % each) * kTile;
+                const int s = i % kQuerySlots, head = g * p.group + (step0 + i) / each;
+                const int row = (u.tile + (step0 + i) % each) * kTile;
                 const float2 *from = p.stats + head * p.tokens + u.start + row;
                 float2 st[4];
 #pragma unroll
@@ -577,7 +600,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
-        const bool live = any && row < u.len;
+        const bool live = n > 0 && row < u.len;
         // A thread's 32 values are of four keys and eight queries (tmem_load_block), so that it
         // reads lse and D of eight queries and not of 32: shared memory is what bounds
         // this kernel (2786 cycles a tile of 128 x 128 with 32 of them)
@@ -594,7 +617,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             F2 l[kCols / 8];
 #pragma unroll
             for (int b = 0; b < kCols / 8; ++b) l[b] = load_stats(st + 32 * b);
-            tmem_wait_loads();
 #pragma unroll
             for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
@@ -602,7 +624,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 s[c] = __float_as_uint(exp2_fast(x.x));
                 s[c + 1] = __float_as_uint(exp2_fast(x.y));
             }
-            const bool diagonal = i % each == 0;
+            const bool diagonal = (step0 + i) % each == 0;
             if (diagonal) {
 #pragma unroll
                 for (int c = 0; c < kCols; ++c)
@@ -622,7 +644,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (!ok) break;
             tmem_after();
             tmem_load_block(d_tm, d);
-            tmem_wait_loads();
 #pragma unroll
             for (int c = 0; c < kCols; c += 2) {
                 const F2 x = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
@@ -649,11 +670,25 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 bar_arrive(st_empty + 8 * slot_i);
             }
         }
-        if (any) {
+        if (n > 0) {
             if (ok) ok = wait_warp(out_full, 0, gave_up);
             tmem_after();
+        }
+        const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
+        if (n > 0 && p.parts > 1) {
+            for (int t = 0; t < 2; ++t)
+                for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
+                    uint32_t v[16];
+                    tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
+                    if (!ok) v[0] = 0x7fffffffu;
+#pragma unroll
+                    for (int h = 0; h < 16; h += 4)
+                        *part_at(p, blockIdx.x, t, c + h, mine) =
+                            make_float4(__uint_as_float(v[h]), __uint_as_float(v[h + 1]),
+                                        __uint_as_float(v[h + 2]), __uint_as_float(v[h + 3]));
+                }
+        } else if (n > 0) {
             // every tile of queries has been used: their places hold the results
-            const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
             const float factor[2] = {ok ? p.scale * shift.undo : lost,
                                      ok ? Shift<T>::kUndoProbs : lost};
             bool good = true;
@@ -661,7 +696,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                     uint32_t v[16];
                     tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
-                    tmem_wait_loads();
                     Vec8 x[2];
 #pragma unroll
                     for (int h = 0; h < 16; ++h) {
@@ -704,9 +738,97 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     }
 }
 
+// The parts' sums, in order, as results.  A block takes every fourth 16 columns of a key
+// tile's gradients, a thread a key.
+template <typename T>
+__global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    const int unit = blockIdx.x / kSumGroups, side = blockIdx.x % kSumGroups, g = unit % p.heads_k;
+    AttnUnit u;
+    if (!unit_at<kTile>(p, unit / p.heads_k, u)) return;
+    const int given = u.tile;
+    const Shift<T> shift(p);
+    const int lane = threadIdx.x % 32;
+    uint32_t used = 0;  // parts that have steps
+    for (int r = 0; r < p.parts; ++r) {
+        u.tile = given;
+        if (KeySteps(p, u, r).n > 0) used |= 1u << r;
+    }
+    const int row = u.tile * kTile + threadIdx.x;
+    const bool live = row < u.len;
+    const int64_t token = u.start + (int64_t)row;
+    bool good = true;
+    for (int t = 0; t < 2; ++t) {
+        const float factor = t ? Shift<T>::kUndoProbs : p.scale * shift.undo;
+        T *out = static_cast<T *>(t ? p.dv : p.dk) + token * p.d_token[1 + t] + g * p.d_head[1 + t];
+        for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
+            Vec8 x[2] = {};
+            for (int r = 0; r < p.parts; ++r) {
+                if (!(used >> r & 1)) continue;
+#pragma unroll
+                for (int h = 0; h < 16; h += 4) {
+                    const float4 v = *part_at(p, unit * p.parts + r, t, c + h, threadIdx.x);
+                    float *y = &x[h / 8].v[h % 8];
+                    y[0] += v.x, y[1] += v.y, y[2] += v.z, y[3] += v.w;
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 16; ++h) {
+                good = good && finite(x[h / 8].v[h % 8]);
+                x[h / 8].v[h % 8] *= factor;
+            }
+            if (!live) continue;
+#pragma unroll
+            for (int h = 0; h < 16; h += 8) {
+                if (p.d_vectors[1 + t])
+                    store8<true>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+            }
+        }
+    }
+    uint32_t again = __ballot_sync(0xffffffffu, live && !good);
+    __syncwarp();
+    while (again) {
+        const int i = __ffs(again) - 1;
+        again &= again - 1;
+        dkv_row<T>(p, u, row - lane + i, g, lane, side);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+// Blocks that share 128 keys: as many as end soonest.  The steps of the longest block, or an
+// even share of all (1.4 us each); a block's start and end (5 us); joining, which writes
+// and reads 128 KB of sums for each block.  The lengths are on the device: sequences of
+// the same length, the longest three times as long.  1024 tokens of 16 + 2 heads of 128, both
+// passes: 76 us (one block each 138); 8192 of 8 + 1 471 (967); 4096 of 32 + 8 stay at
+// one block each, 479 us (two 501).
+static int parts_of(const pos_attn *a) {
+    const double count = a->starts ? std::max(1, a->sequences) : 1, sms = sm_count();
+    const double len = std::max(1., (double)a->tokens / count / kTile);
+    const double group = (double)a->heads_q / a->heads_k;
+    const double most =
+        std::min(std::ceil((double)a->tokens / kTile), std::ceil(count > 1 ? 3 * len : len)) * group;
+    const double all = count * len * (len + 1) / 2 * group * a->heads_k / sms;
+    const double units = count * std::ceil(len) * a->heads_k;
+    int best = 1;
+    double least = 1e300;
+    for (int c = 1; c <= 8; c *= 2) {
+        const double t = 1.4 * std::max(std::ceil(most / c), all) +
+                         5. * std::max(1., units * c / sms) + (c > 1 ? 4. + 0.055 * units * c : 0.);
+        if (t < least) least = t, best = c;
+    }
+    // (their sums take 128 KB each)
+    while (best > 1 && attn_most_tiles(a, kTile) * a->heads_k * best > 16 * (int64_t)sms) best /= 2;
+    return best;
+}
+static int64_t part_bytes(const pos_attn *a, int parts) {
+    return parts == 1 ? 0 : attn_most_tiles(a, kTile) * a->heads_k * parts *
+                                ((a->dim + 15) / 16 * 16) * kTile * 8;
+}
+
 template <typename T>
 static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaStream_t s) {
     CUtensorMap q, k, v, g;
@@ -725,7 +847,9 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     POS_CUDA(launch_dependent(dq, grid_q, kBackThreads, kDqSmem, s, q, k, v, g, p));
     auto dkv = attn_dkv_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dkv), kDkvSmem));
-    POS_CUDA(launch_dependent(dkv, grid_k, kBackThreads, kDkvSmem, s, q, k, v, g, p));
+    POS_CUDA(launch_dependent(dkv, grid_k * p.parts, kBackThreads, kDkvSmem, s, q, k, v, g, p));
+    if (p.parts > 1)
+        POS_CUDA(launch_dependent(attn_join_kernel<T>, grid_k * kSumGroups, kTile, 0, s, p));
     return POS_OK;
 }
 
@@ -734,10 +858,13 @@ static int64_t stats_bytes(const pos_attn *a) {
 }
 
 static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_heads &d_o,
-                           AttnParams p, char *at, cudaStream_t s) {
+                           AttnParams p, int parts, char *at, cudaStream_t s) {
     p.largest = reinterpret_cast<uint32_t *>(at);
     p.stats = reinterpret_cast<float2 *>(at + 16);
     at += stats_bytes(a);
+    p.parts = parts;
+    p.part = reinterpret_cast<float *>(at);
+    at += part_bytes(a, parts);
     const pos_heads t[4] = {x[0], x[1], x[2], d_o};
     const int64_t heads[4] = {a->heads_q, a->heads_k, a->heads_k, a->heads_q};
     AttnTensor *to[4] = {&p.q, &p.k, &p.v, &p.g};
@@ -779,14 +906,15 @@ extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_hea
             p.d_vectors[i] = aligned16(dx[i].data) && dx[i].token_stride % 8 == 0 &&
                              dx[i].head_stride % 8 == 0;
         }
-        int64_t bytes = stats_bytes(attn) + attn_list_bytes(attn, kTile);
+        const int parts = parts_of(attn);
+        int64_t bytes = stats_bytes(attn) + part_bytes(attn, parts) + attn_list_bytes(attn, kTile);
         for (int i = 0; i < 4; ++i)
             if (!attn_direct(attn, i < 3 ? x[i] : *d_o, heads[i]))
                 bytes += attn_copy_bytes(attn, heads[i]);
         const auto s = static_cast<cudaStream_t>(stream);
         void *scratch = nullptr;
         POS_TRY(attn_scratch(bytes, s, &scratch));
-        const pos_status st = backward(attn, x, *d_o, p, static_cast<char *>(scratch), s);
+        const pos_status st = backward(attn, x, *d_o, p, parts, static_cast<char *>(scratch), s);
         const cudaError_t e = cudaFreeAsync(scratch, s);
         if (st != POS_OK) return st;
         return e == cudaSuccess ? POS_OK : cuda_fail(e, "attention scratch");
