@@ -18,58 +18,63 @@ constexpr int kLoadWarp = 4 * kSumGroups, kIssueWarp = kLoadWarp + 1, kStatsWarp
 
 // f16 holds probabilities of long rows and small gradients badly (below 2^-14 with
 // fewer bits, below 2^-25 not at all).  There P is multiplied by 2^12 and dS by 2^k, k the
-// same for a whole call: the largest magnitude of dO becomes 2^8 to 2^9.  A dS that is
-// too large all the same gives an infinity and its rows are done again in 32 bits.
+// same for a product's sums: the largest magnitude of dO (of the block's queries for
+// theirs, of all for the keys') becomes 2^8 to 2^9.  A dS that is too large all the
+// same gives an infinity and its rows are done again in 32 bits.
 template <typename T>
 struct Shift {
     static constexpr float kProbs = std::is_same<T, __half>::value ? 12.f : 0.f;
     float grads, undo;  // of dP - D, so that P (dP - D) has its factor; 2^-k
-    __device__ __forceinline__ explicit Shift(const AttnParams &p) : grads(1.f), undo(1.f) {
-        if constexpr (std::is_same<T, __half>::value) {
-            const uint32_t big = *p.largest;  // bits of an f32
+    __device__ __forceinline__ explicit Shift(uint32_t big) : grads(1.f), undo(1.f) {
+        if constexpr (std::is_same<T, __half>::value) {  // big: bits of an f32
             const int k = big ? 8 - ((int)(big >> 23) - 127) : 0;
             grads = __uint_as_float((uint32_t)(127 + k - 12) << 23);
             undo = __uint_as_float((uint32_t)(127 - k) << 23);
         }
     }
+    static __device__ __forceinline__ Shift of_all(const AttnParams &p) {
+        return Shift(std::is_same<T, __half>::value ? *p.largest : 0u);
+    }
     static constexpr float kUndoProbs = std::is_same<T, __half>::value ? 1.f / 4096.f : 1.f;
 };
 
-// Of the queries of a tile: lse in powers of two (less the probabilities' factor), and
-// D = dO . O; f16: the largest finite magnitude of dO.  16 lanes a row.
+// Of the queries of a tile, by the 16 warps of sums: lse in powers of two (less the
+// probabilities' factor) and do . o, 16 lanes a row; f16: bits of the largest finite
+// magnitude of dO, in *largest.
 template <typename T>
-__global__ void __launch_bounds__(256) attn_stats_kernel(const AttnParams p) {
-    grid_dep_wait();
-    grid_dep_trigger();
-    AttnUnit u;
-    if (!unit_at<kTile>(p, blockIdx.x / p.heads_q, u)) return;
-    const int l = threadIdx.x % 16, head = blockIdx.x % p.heads_q;
+__device__ __forceinline__ void row_stats(const AttnParams &p, const AttnUnit &u, int head,
+                                          float2 *stats, uint32_t *largest) {
+    const int l = threadIdx.x % 16;
     uint32_t big = 0;
-#pragma unroll 4
-    for (int r = threadIdx.x / 16; r < kTile; r += 16) {
-        const int row = u.tile * kTile + r;
-        const int64_t token = u.start + (int64_t)row;
-        float d = 0.f;
-        if (row < u.len && 8 * l < p.dim) {
-            // (o may lie anywhere; past its last element dO's copy holds zeros)
-            const Vec8 a = to_float(load8_shifted(row_at<T>(p.o, token, head) + 8 * l, 8 * l,
-                                                  p.dim_out - 8 * l));
-            const Vec8 b = load_row8(row_at<T>(p.g, token, head) + 8 * l);
+    Vec8 a[4], b[4];
+    float lse[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                d += a.v[e] * b.v[e];
-                if (finite(b.v[e])) big = max(big, __float_as_uint(fabsf(b.v[e])));
-            }
+    for (int k = 0; k < 4; ++k) {
+        const int r = threadIdx.x / 16 + 32 * k, row = u.tile * kTile + r;
+        const int64_t token = u.start + (int64_t)row;
+        const bool there = row < u.len && 8 * l < p.dim;
+        // (o may lie anywhere; past its last element dO's copy holds zeros)
+        a[k] = to_float(load8_shifted(row_at<T>(p.o, token, head) + 8 * l, 8 * l,
+                                      there ? p.dim_out - 8 * l : 0));
+        b[k] = there ? load_row8(row_at<T>(p.g, token, head) + 8 * l) : Vec8{};
+        lse[k] = row < u.len ? p.lse[head * p.tokens + token] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            d += a[k].v[e] * b[k].v[e];
+            if (finite(b[k].v[e])) big = max(big, __float_as_uint(fabsf(b[k].v[e])));
         }
 #pragma unroll
         for (int o = 8; o; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
-        if (l == 0 && row < u.len)
-            p.stats[head * p.tokens + token] =
-                make_float2(p.lse[head * p.tokens + token] * kLog2e - Shift<T>::kProbs, d);
+        if (l == 0)
+            stats[threadIdx.x / 16 + 32 * k] = make_float2(lse[k] * kLog2e - Shift<T>::kProbs, d);
     }
     if constexpr (std::is_same<T, __half>::value) {
         big = __reduce_max_sync(0xffffffffu, big);
-        if (threadIdx.x % 32 == 0 && big) atomicMax(p.largest, big);
+        if (threadIdx.x % 32 == 0 && big) atomicMax(largest, big);
     }
 }
 
@@ -84,14 +89,17 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // TMEM holds scores, dP = dO V^T and two sums, and is full: P takes the scores' place and
 // dS = P (dP - D) that of dP, and while one of them is made, the tensor cores use up the
 // other and compute what comes next in its place.
-//   D = dO . o has the rounding of o in it, in 16 bits, which for rows with few keys that
+//   Before that its warps compute D = dO . o while the first tiles are on their way
+// (a kernel of its own took 16 of 480 us for 4096 tokens of 32 heads of 128).
+//   D has the rounding of o in it, in 16 bits, which for rows with few keys that
 // count is larger than that of everything else (2 tokens of 2 heads of 64, bf16: dQ 0.7 %
 // off, dK 1.2 %).  Its exact value is D + e, e = sum P (dP - D), which this kernel has
 // when it is done; so it adds up P K beside dS K, and dQ = dS K - e P K.  The keys'
 // gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
 constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 6;
-constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 32;
+constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 32 +
+                        kTile * 8;
 
 template <typename T>
 __device__ __forceinline__ void dq_row(const AttnParams &p, const AttnUnit &u, int row, int head,
@@ -137,6 +145,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     unsigned char *tail = aligned + (slot - base);
     volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
     uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);  // rows to do again
+    uint32_t *largest = reinterpret_cast<uint32_t *>(tail + 24);
+    float2 *stats = reinterpret_cast<float2 *>(tail + 32);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -146,6 +156,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gave_up = 0;
+        *largest = 0;
         for (int i = 0; i < 4; ++i) bad[i] = 0;
     }
     if (warp == kIssueWarp) {
@@ -249,9 +260,14 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
         const bool live = any && row < u.len;
-        float2 st = make_float2(0.f, 0.f);
-        const Shift<T> shift(p);
-        if (live) st = p.stats[head * p.tokens + u.start + row];
+        if (any) {
+            row_stats<T>(p, u, head, stats, largest);
+            sums_barrier();
+        }
+        const float2 st = stats[mine];  // (whatever a block without work finds there)
+        const Shift<T> shift(*largest);
+        if (std::is_same<T, __half>::value && threadIdx.x == 0 && *largest)
+            atomicMax(p.largest, *largest);
         F2 rest = both(0.f);  // e, of this part of the columns
         for (int i = 0; i < n; ++i) {
             ok = ok && wait_warp(s_full, i & 1, gave_up);
@@ -318,7 +334,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             sums_barrier();
             const float e = (parts[mine] + parts[kTile + mine] + parts[2 * kTile + mine] +
                              parts[3 * kTile + mine]) * shift.undo;
-            if (live && side == 0) p.stats[head * p.tokens + u.start + row].y = st.y + e;
+            if (live && side == 0)
+                p.stats[head * p.tokens + u.start + row] = make_float2(st.x, st.y + e);
             const float a = ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu);
             const float b = -e * p.scale * Shift<T>::kUndoProbs;
             bool good = true;
@@ -570,7 +587,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         } else if (warp == kStatsWarp) {
             // lse and D of the queries; none for rows past the sequence: their
             // probabilities are 2^(0 - inf) = 0
-            const Shift<T> shift(p);
+            const Shift<T> shift = Shift<T>::of_all(p);
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kQuerySlots, head = g * p.group + (step0 + i) / each;
                 const int row = (u.tile + (step0 + i) % each) * kTile;
@@ -596,7 +613,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         __syncwarp();
     } else {
         take_registers<kBackRegs>();
-        const Shift<T> shift(p);
+        const Shift<T> shift = Shift<T>::of_all(p);
         const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
@@ -748,7 +765,7 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
     AttnUnit u;
     if (!unit_at<kTile>(p, unit / p.heads_k, u)) return;
     const int given = u.tile;
-    const Shift<T> shift(p);
+    const Shift<T> shift = Shift<T>::of_all(p);
     const int lane = threadIdx.x % 32;
     uint32_t used = 0;  // parts that have steps
     for (int r = 0; r < p.parts; ++r) {
@@ -841,7 +858,6 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     POS_TRY(attn_grid(a, kTile, a->heads_k, &grid_k));
     if (grid_q == 0) return POS_OK;
     if (std::is_same<T, __half>::value) POS_CUDA(cudaMemsetAsync(p.largest, 0, 4, s));
-    POS_CUDA(launch_dependent(attn_stats_kernel<T>, grid_q, 256, 0, s, p));
     auto dq = attn_dq_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dq), kDqSmem));
     POS_CUDA(launch_dependent(dq, grid_q, kBackThreads, kDqSmem, s, q, k, v, g, p));
