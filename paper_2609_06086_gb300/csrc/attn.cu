@@ -105,11 +105,12 @@ __global__ void __launch_bounds__(256) attn_copy_kernel(const T *x, int64_t toke
 // stay in TMEM.  One thread issues the products of both tiles in turn, so the
 // tensor cores work on one tile while the other's exponentials are computed.  Keys
 // go from the diagonal down, so the first tile is the one with a mask and no row's
-// largest score is ever of nothing.
+// largest score is ever of nothing.  A block takes one such unit after another, so that a
+// unit's first loads and scores come while the one before it ends.
 constexpr int kSlots = 5;                    // tiles of keys and values on their way
 constexpr int kForwardRows = 2 * kTile;
 constexpr int kForwardThreads = 3 * 128;     // two warpgroups of rows, one of loads and products
-constexpr int kForwardBars = 2 * kSlots + 8;
+constexpr int kForwardBars = 2 * kSlots + 10;
 constexpr int kForwardSmem = 1024 + (2 + kSlots) * kTileBytes + 8 * kForwardBars + 16;
 // 2 * 208 + 88 = 504 = 3 * 168, what the block is launched with
 constexpr int kRowRegs = 208, kIssueRegs = 88;
@@ -152,6 +153,32 @@ __device__ __forceinline__ void forward_row(const AttnParams &p, const AttnUnit 
         p.lse[head * p.tokens + u.start + row] = (top + log2f(total)) * kLn2;
 }
 
+// A block's units: in rounds, every second one in the opposite order, since they are
+// sorted by their length.
+struct ForwardUnit {
+    AttnUnit u;
+    int head, r0, n0, n1, first;  // first token; tiles of keys that its two tiles see, the last
+    __device__ __forceinline__ bool next(const AttnParams &p, int &round) {
+        const int64_t total =
+            (int64_t)(p.tiles ? *p.n_tiles : ((int)p.tokens + kForwardRows - 1) / kForwardRows) *
+            p.heads_q;
+        for (;; ++round) {
+            const int64_t start = (int64_t)round * gridDim.x;
+            if (start >= total) return false;
+            const int64_t at = start + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            if (at >= total) continue;
+            head = (int)(at % p.heads_q);
+            unit_at<kForwardRows>(p, (int)(at / p.heads_q), u);
+            r0 = u.tile * kForwardRows;
+            n0 = 2 * u.tile + 1;
+            n1 = r0 + kTile < u.len ? n0 + 1 : 0;
+            first = max(n0, n1) - 1;
+            ++round;
+            return true;
+        }
+    }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(kForwardThreads, 1)
     attn_forward_kernel(const __grid_constant__ CUtensorMap q_map,
@@ -164,8 +191,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
     const uint32_t bars = kv_at + kSlots * kTileBytes;
     const uint32_t kv_full = bars, kv_empty = kv_full + 8 * kSlots;
     const uint32_t q_full = kv_empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 16,
-                   o_full = p_full + 16;
-    const uint32_t slot = o_full + 16;
+                   o_full = p_full + 16, q_empty = o_full + 16;
+    const uint32_t slot = q_empty + 16;
     unsigned char *tail = aligned + (slot - base);
     volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
@@ -194,172 +221,186 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
     grid_dep_trigger();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
 
-    const int head = blockIdx.x % p.heads_q;
-    AttnUnit u;
-    const bool any = unit_at<kForwardRows>(p, blockIdx.x / p.heads_q, u);
-    // tiles of keys that the two tiles of queries see
-    const int r0 = any ? u.tile * kForwardRows : 0;
-    const int n0 = any ? 2 * u.tile + 1 : 0, n1 = any && r0 + kTile < u.len ? n0 + 1 : 0;
-    const int first = max(n0, n1) - 1;
     const int boxes = p.dim > 64 ? 2 : 1;
+    ForwardUnit w;
+    int round = 0;
     bool ok = true;
 
     if (group == 2) {
         give_registers<kIssueRegs>();
         if (warp == 8) {
-            if (lane == 0 && any) {
-                for (int t = 0; t < (n1 ? 2 : 1); ++t) {
+            int s = 0;
+            uint32_t ph = 1, q_ph[2] = {1, 1};  // an empty slot's first wait passes
+            while (lane == 0 && ok && w.next(p, round)) {
+                const auto load = [&](bool v, int j) {
+                    if (!bar_wait(kv_empty + 8 * s, ph, gave_up)) return false;
+                    bar_expect(kv_full + 8 * s, boxes * kBox);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_rows(kv_at + s * kTileBytes + b * kBox, v ? &v_map : &k_map, 64 * b,
+                                 w.head / p.group, w.u.start + j * kTile, kv_full + 8 * s);
+                    if (++s == kSlots) s = 0, ph ^= 1;
+                    return true;
+                };
+                ok = load(false, w.first);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!ok || (t && !w.n1)) break;
+                    ok = bar_wait(q_empty + 8 * t, q_ph[t], gave_up);
+                    if (!ok) break;
+                    q_ph[t] ^= 1;
                     bar_expect(q_full + 8 * t, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
-                        tma_rows(q_at + t * kTileBytes + b * kBox, &q_map, 64 * b, head,
-                                 u.start + r0 + t * kTile, q_full + 8 * t);
+                        tma_rows(q_at + t * kTileBytes + b * kBox, &q_map, 64 * b, w.head,
+                                 w.u.start + w.r0 + t * kTile, q_full + 8 * t);
                 }
-                int s = 0;
-                uint32_t ph = 1;  // an empty slot's first wait passes
-                for (int j = first; j >= 0 && ok; --j)
-                    for (int v = 0; v < 2 && ok; ++v) {
-                        ok = bar_wait(kv_empty + 8 * s, ph, gave_up);
-                        if (!ok) break;
-                        bar_expect(kv_full + 8 * s, boxes * kBox);
-                        for (int b = 0; b < boxes; ++b)
-                            tma_rows(kv_at + s * kTileBytes + b * kBox, v ? &v_map : &k_map, 64 * b,
-                                     head / p.group, u.start + j * kTile, kv_full + 8 * s);
-                        if (++s == kSlots) s = 0, ph ^= 1;
-                    }
+                for (int j = w.first; j >= 0 && ok; --j)
+                    ok = load(true, j) && (j == 0 || load(false, j - 1));
             }
         } else if (warp == 9) {
             const uint32_t mine = one_lane();
             const int steps = (p.dim + 15) / 16;
-            // the i-th tile of keys or values to arrive: keys 2 i, values 2 i + 1
-            const auto arrived = [&](int i) {
-                return wait_warp(kv_full + 8 * (i % kSlots), i / kSlots & 1, gave_up);
-            };
-            const auto scores = [&](int t, int i) {  // i: steps of keys from the first on
-                mma_rows<T>(tmem + t * kTile, q_at + t * kTileBytes,
-                            kv_at + 2 * i % kSlots * kTileBytes, steps, mine);
-                commit(s_full + 8 * t, mine);
-            };
-            if (any) {
-                ok = wait_warp(q_full, 0, gave_up) && (!n1 || wait_warp(q_full + 8, 0, gave_up)) &&
-                     arrived(0);
-                tmem_after();
-                if (ok) {
-                    if (first < n0) scores(0, 0);
-                    if (first < n1) scores(1, 0);
-                    commit(kv_empty, mine);
-                }
-            }
-            uint32_t ph[2] = {0, 0};
-            for (int j = first, i = 0; j >= 0 && ok; --j, ++i) {
-                const uint32_t v_at = kv_at + (2 * i + 1) % kSlots * kTileBytes;
-                ok = arrived(2 * i + 1);
-                if (!ok) break;
-                const int seen = u.len - j * kTile;
-                if (seen < kTile) zero_rows(v_at, seen, boxes, lane);
-                if (j > 0) ok = arrived(2 * i + 2);
+            uint32_t ph[2] = {0, 0}, q_ph[2] = {0, 0};
+            int base = 0;  // tiles of keys and values of the units before
+            while (ok && w.next(p, round)) {
+                // the i-th tile to arrive: keys 2 i, values 2 i + 1
+                const auto arrived = [&](int i) {
+                    return wait_warp(kv_full + 8 * ((base + i) % kSlots), (base + i) / kSlots & 1,
+                                     gave_up);
+                };
+                const auto place = [&](int i) { return kv_at + (base + i) % kSlots * kTileBytes; };
+                const auto scores = [&](int t, int i) {  // i: steps of keys from the first on
+                    mma_rows<T>(tmem + t * kTile, q_at + t * kTileBytes, place(2 * i), steps, mine);
+                    commit(s_full + 8 * t, mine);
+                    if (i == w.first) commit(q_empty + 8 * t, mine);  // the last ones
+                };
+                ok = arrived(0);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int n = t ? n1 : n0;
-                    if (j < n && ok) {
-                        ok = wait_warp(p_full + 8 * t, ph[t], gave_up);
-                        if (!ok) break;
-                        ph[t] ^= 1;
-                        tmem_after();
-                        mma_columns<T>(tmem + 2 * kTile + t * kTile, tmem + t * kTile, v_at, steps,
-                                       j < n - 1, mine);
-                        if (j == 0) commit(o_full + 8 * t, mine);
+                for (int t = 0; t < 2; ++t)
+                    if (ok && (t == 0 || w.n1)) {
+                        ok = wait_warp(q_full + 8 * t, q_ph[t], gave_up);
+                        q_ph[t] ^= 1;
                     }
-                    if (j > 0 && j - 1 < n && ok) scores(t, i + 1);
+                if (!ok) break;
+                tmem_after();
+                if (w.first < w.n0) scores(0, 0);
+                if (w.first < w.n1) scores(1, 0);
+                commit(kv_empty + 8 * (base % kSlots), mine);
+                for (int j = w.first, i = 0; j >= 0 && ok; --j, ++i) {
+                    ok = arrived(2 * i + 1);
+                    if (!ok) break;
+                    const int seen = w.u.len - j * kTile;
+                    if (seen < kTile) zero_rows(place(2 * i + 1), seen, boxes, lane);
+                    if (j > 0) ok = arrived(2 * i + 2);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int n = t ? w.n1 : w.n0;
+                        if (j < n && ok) {
+                            ok = wait_warp(p_full + 8 * t, ph[t], gave_up);
+                            if (!ok) break;
+                            ph[t] ^= 1;
+                            tmem_after();
+                            // (the sums of the unit before have been read: its rows' warps
+                            // have gone on to these probabilities)
+                            mma_columns<T>(tmem + 2 * kTile + t * kTile, tmem + t * kTile,
+                                           place(2 * i + 1), steps, j < n - 1, mine);
+                            if (j == 0) commit(o_full + 8 * t, mine);
+                        }
+                        if (j > 0 && j - 1 < n && ok) scores(t, i + 1);
+                    }
+                    commit(kv_empty + 8 * ((base + 2 * i + 1) % kSlots), mine);
+                    if (j > 0) commit(kv_empty + 8 * ((base + 2 * i + 2) % kSlots), mine);
                 }
-                commit(kv_empty + 8 * ((2 * i + 1) % kSlots), mine);
-                if (j > 0) commit(kv_empty + 8 * ((2 * i + 2) % kSlots), mine);
+                base += 2 * (w.first + 1);
             }
         }
         __syncwarp();
     } else {
         take_registers<kRowRegs>();
-        const int t = group, n = t ? n1 : n0;
-        const int row = r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
+        const int t = group;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + t * kTile + lanes, o_tm = tmem + 2 * kTile + t * kTile + lanes;
         const int dim16 = (p.dim + 15) / 16 * 16;
-        float top = 0.f, total = 0.f;
-        uint32_t ph = 0;
-        for (int j = n - 1; j >= 0 && ok; --j) {
-            ok = wait_warp(s_full + 8 * t, ph, gave_up);
-            if (!ok) break;
-            ph ^= 1;
-            tmem_after();
-            uint32_t s[kTile];
-            tmem_load128(s_tm, s);
-            if (j == n - 1) {
-                const int seen = row - j * kTile;  // the last key that the row sees
+        uint32_t ph = 0, o_ph = 0;
+        while (ok && w.next(p, round)) {
+            const int n = t ? w.n1 : w.n0;
+            if (n == 0) continue;
+            const int row = w.r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
+            float top = 0.f, total = 0.f;
+            for (int j = n - 1; j >= 0 && ok; --j) {
+                ok = wait_warp(s_full + 8 * t, ph, gave_up);
+                if (!ok) break;
+                ph ^= 1;
+                tmem_after();
+                uint32_t s[kTile];
+                tmem_load128(s_tm, s);
+                if (j == n - 1) {
+                    const int seen = row - j * kTile;  // the last key that the row sees
 #pragma unroll
-                for (int c = 0; c < kTile; ++c)
-                    if (c > seen) s[c] = 0xff800000u;
-            }
-            float part[4];  // (four chains: one of 128 steps is longer than the exponentials)
+                    for (int c = 0; c < kTile; ++c)
+                        if (c > seen) s[c] = 0xff800000u;
+                }
+                float part[4];  // (four chains: one of 128 steps is longer than the exponentials)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) part[c] = max3(s[c], s[c + 4], s[c + 8]);
+                for (int c = 0; c < 4; ++c) part[c] = max3(s[c], s[c + 4], s[c + 8]);
 #pragma unroll
-            for (int c = 12; c + 8 <= kTile; c += 8)
+                for (int c = 12; c + 8 <= kTile; c += 8)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    part[e] = max3(__float_as_uint(part[e]), s[c + e], s[c + e + 4]);
+                    for (int e = 0; e < 4; ++e)
+                        part[e] = max3(__float_as_uint(part[e]), s[c + e], s[c + e + 4]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[e] = fmaxf(part[e], __uint_as_float(s[kTile - 4 + e]));
-            const float m =
-                fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * p.scale2;
-            if (j == n - 1) {
-                top = m;
-            } else {
-                const bool more = m > top + kSlack;
-                if (__any_sync(0xffffffffu, more)) {
-                    // the scores of this step were issued after the last product into O
-                    // and are there, so that one is done
-                    const float shrink = more ? exp2_fast(top - m) : 1.f;
-                    if (more) top = m;
-                    total *= shrink;
-                    for (int c = 0; c < dim16; c += 16) {
-                        uint32_t o[16];
-                        tmem_load16(o_tm + c, o);
+                for (int e = 0; e < 4; ++e) part[e] = fmaxf(part[e], __uint_as_float(s[kTile - 4 + e]));
+                const float m =
+                    fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * p.scale2;
+                if (j == n - 1) {
+                    top = m;
+                } else {
+                    const bool more = m > top + kSlack;
+                    if (__any_sync(0xffffffffu, more)) {
+                        // the scores of this step were issued after the last product into O
+                        // and are there, so that one is done
+                        const float shrink = more ? exp2_fast(top - m) : 1.f;
+                        if (more) top = m;
+                        total *= shrink;
+                        for (int c = 0; c < dim16; c += 16) {
+                            uint32_t o[16];
+                            tmem_load16(o_tm + c, o);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                        tmem_store16(o_tm + c, o);
+                            for (int e = 0; e < 16; ++e)
+                                o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                            tmem_store16(o_tm + c, o);
+                        }
                     }
                 }
-            }
-            F2 sum[4] = {};
+                F2 sum[4] = {};
 #pragma unroll
-            for (int c = 0; c < kTile; c += 32) {
-                uint32_t w[16];
+                for (int c = 0; c < kTile; c += 32) {
+                    uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const F2 x = fma2({__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])},
-                                      both(p.scale2), both(-top));
-                    const F2 y = {exp2_fast(x.x), exp2_fast(x.y)};
-                    sum[e % 4] = add2(sum[e % 4], y);
-                    w[e] = pack2<T>(y.x, y.y);
+                    for (int e = 0; e < 16; ++e) {
+                        const F2 x = fma2({__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])},
+                                          both(p.scale2), both(-top));
+                        const F2 y = {exp2_fast(x.x), exp2_fast(x.y)};
+                        sum[e % 4] = add2(sum[e % 4], y);
+                        w[e] = pack2<T>(y.x, y.y);
+                    }
+                    tmem_store16(s_tm + c / 2, w);
                 }
-                tmem_store16(s_tm + c / 2, w);
+                const F2 a = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                total += a.x + a.y;
+                tmem_wait_stores();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full + 8 * t);
             }
-            const F2 a = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
-            total += a.x + a.y;
-            tmem_wait_stores();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * t);
-        }
-        if (n > 0) {
-            if (ok) ok = wait_warp(o_full + 8 * t, 0, gave_up);
+            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, gave_up);
+            o_ph ^= 1;
             tmem_after();
-            const bool live = row < u.len;
+            const bool live = row < w.u.len;
             bool good = finite(top) && finite(total);
             float factor = 1.f / total;
             if (!ok) factor = __uint_as_float(0x7fffffffu);  // a wait that gave up: no result
-            // the queries' tile has been used: its place holds the results
-            const uint32_t out_at = q_at + t * kTileBytes;
+            T *out = static_cast<T *>(p.out) + (w.u.start + (int64_t)row) * p.out_token +
+                     w.head * p.out_head;
             for (int c = 0; c < dim16; c += 16) {
                 uint32_t o[16];
                 tmem_load16(o_tm + c, o);
@@ -369,24 +410,23 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
                     good = good && finite(__uint_as_float(o[e]));
                 }
-                put_columns<T>(out_at, threadIdx.x % kTile, c, x);
+                if (!live) continue;
+#pragma unroll
+                for (int e = 0; e < 16; e += 8) {
+                    if (p.out_vectors)
+                        store8<true>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
+                    else store8<false>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
+                }
             }
-            asm volatile("barrier.sync %0, 128;" ::"r"(t + 1) : "memory");
-            const int row0 = r0 + t * kTile;
-            write_tile(out_at, min(kTile, u.len - row0),
-                       static_cast<T *>(p.out) + (u.start + (int64_t)row0) * p.out_token +
-                           head * p.out_head,
-                       p.out_token, p.out_vectors, p.dim, p.dim_out, (int)threadIdx.x % kTile,
-                       kTile);
             if (p.lse && live)
-                p.lse[head * p.tokens + u.start + row] =
+                p.lse[w.head * p.tokens + w.u.start + row] =
                     ok ? (top + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);
             uint32_t again = __ballot_sync(0xffffffffu, ok && live && !good);
-            asm volatile("barrier.sync %0, 128;" ::"r"(t + 1) : "memory");
+            __syncwarp();
             while (again) {
                 const int i = __ffs(again) - 1;
                 again &= again - 1;
-                forward_row<T>(p, u, row - lane + i, head, lane);
+                forward_row<T>(p, w.u, row - lane + i, w.head, lane);
             }
         }
     }
@@ -537,7 +577,8 @@ static pos_status launch_forward(const pos_attn *a, const AttnParams &p, int gri
     POS_TRY(attn_map(&v, a, p.v, p.heads_k, p.dim));
     auto kern = attn_forward_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(kern), kForwardSmem));
-    POS_CUDA(launch_dependent(kern, grid, kForwardThreads, kForwardSmem, s, q, k, v, p));
+    POS_CUDA(launch_dependent(kern, std::min(grid, std::max(1, sm_count())), kForwardThreads,
+                              kForwardSmem, s, q, k, v, p));
     return POS_OK;
 }
 
