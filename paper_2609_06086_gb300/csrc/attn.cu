@@ -18,13 +18,14 @@ struct AttnListParams {
     int32_t *n_tiles;
     int64_t tokens;
     int32_t sequences, rows, shift;  // bin = tile >> shift
+    int32_t bins;                    // that a tile can be in, a multiple of 32
 };
 __global__ void __launch_bounds__(kListThreads) attn_tiles_kernel(const AttnListParams p) {
     grid_dep_wait();
     grid_dep_trigger();
     __shared__ int bins[kBins], most[kListThreads / 32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int i = threadIdx.x; i < kBins; i += kListThreads) bins[i] = 0;
+    for (int i = threadIdx.x; i < p.bins; i += kListThreads) bins[i] = 0;
     __syncthreads();
     // each warp a run of sequences; the largest start before the run
     const int each = (p.sequences + kListThreads / 32 - 1) / (kListThreads / 32);
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(kListThreads) attn_tiles_kernel(const AttnList
         // bins become places: the tiles of higher bins come first
         if (warp == 0) {
             int sum = 0;
-            for (int b0 = kBins - 32; b0 >= 0; b0 -= 32) {
+            for (int b0 = p.bins - 32; b0 >= 0; b0 -= 32) {
                 const int b = b0 + 31 - lane, v = bins[b];
                 int up = v;
                 for (int o = 1; o < 32; o *= 2) {
@@ -153,29 +154,15 @@ __device__ __forceinline__ void forward_row(const AttnParams &p, const AttnUnit 
         p.lse[head * p.tokens + u.start + row] = (top + log2f(total)) * kLn2;
 }
 
-// A block's units: in rounds, every second one in the opposite order, since they are
-// sorted by their length.
-struct ForwardUnit {
-    AttnUnit u;
-    int head, r0, n0, n1, first;  // first token; tiles of keys that its two tiles see, the last
+struct ForwardUnit : BlockUnit<kForwardRows> {
+    int r0, n0, n1, first;  // first token; tiles of keys that its two tiles see, the last
     __device__ __forceinline__ bool next(const AttnParams &p, int &round) {
-        const int64_t total =
-            (int64_t)(p.tiles ? *p.n_tiles : ((int)p.tokens + kForwardRows - 1) / kForwardRows) *
-            p.heads_q;
-        for (;; ++round) {
-            const int64_t start = (int64_t)round * gridDim.x;
-            if (start >= total) return false;
-            const int64_t at = start + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-            if (at >= total) continue;
-            head = (int)(at % p.heads_q);
-            unit_at<kForwardRows>(p, (int)(at / p.heads_q), u);
-            r0 = u.tile * kForwardRows;
-            n0 = 2 * u.tile + 1;
-            n1 = r0 + kTile < u.len ? n0 + 1 : 0;
-            first = max(n0, n1) - 1;
-            ++round;
-            return true;
-        }
+        if (!BlockUnit::next(p, round)) return false;
+        r0 = u.tile * kForwardRows;
+        n0 = 2 * u.tile + 1;
+        n1 = r0 + kTile < u.len ? n0 + 1 : 0;
+        first = max(n0, n1) - 1;
+        return true;
     }
 };
 
@@ -556,6 +543,7 @@ pos_status attn_list(const pos_attn *a, int rows, char **at, cudaStream_t s, Att
     l.n_tiles = reinterpret_cast<int32_t *>(*at);
     l.tiles = reinterpret_cast<int4 *>(*at + 16);
     while ((a->tokens / rows >> l.shift) >= kBins) ++l.shift;
+    l.bins = (int32_t)std::min<int64_t>(kBins, ((a->tokens / rows >> l.shift) + 32) / 32 * 32);
     *at += attn_list_bytes(a, rows);
     p->tiles = l.tiles, p->n_tiles = l.n_tiles;
     POS_CUDA(launch_dependent(attn_tiles_kernel, 1, kListThreads, 0, s, l));

@@ -58,6 +58,28 @@ __device__ __forceinline__ bool unit_at(const AttnParams &p, int i, AttnUnit &u)
     return true;
 }
 
+// A block's units, tiles of ROWS queries of a head, one after another: in rounds, every
+// second one in the opposite order, since they are sorted by their length.
+template <int ROWS>
+struct BlockUnit {
+    AttnUnit u;
+    int head;
+    __device__ __forceinline__ bool next(const AttnParams &p, int &round) {
+        const int64_t total =
+            (int64_t)(p.tiles ? *p.n_tiles : ((int)p.tokens + ROWS - 1) / ROWS) * p.heads_q;
+        for (;; ++round) {
+            const int64_t start = (int64_t)round * gridDim.x;
+            if (start >= total) return false;
+            const int64_t at = start + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            if (at >= total) continue;
+            head = (int)(at % p.heads_q);
+            unit_at<ROWS>(p, (int)(at / p.heads_q), u);
+            ++round;
+            return true;
+        }
+    }
+};
+
 // ---------------------------------------------------------------------------
 // PTX
 // ---------------------------------------------------------------------------

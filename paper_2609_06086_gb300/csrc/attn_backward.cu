@@ -89,7 +89,8 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // TMEM holds scores, dP = dO V^T and two sums, and is full: P takes the scores' place and
 // dS = P (dP - D) that of dP, and while one of them is made, the tensor cores use up the
 // other and compute what comes next in its place.
-//   Before that its warps compute D = dO . o while the first tiles are on their way
+//   A block takes one such unit after another, so that the next one's first loads, scores
+// and dP come while the last one ends.  Before a unit its warps compute D = dO . o while the first tiles are on their way
 // (a kernel of its own took 16 of 480 us for 4096 tokens of 32 heads of 128).
 //   D has the rounding of o in it, in 16 bits, which for rows with few keys that
 // count is larger than that of everything else (2 tokens of 2 heads of 64, bf16: dQ 0.7 %
@@ -97,9 +98,9 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // when it is done; so it adds up P K beside dS K, and dQ = dS K - e P K.  The keys'
 // gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
-constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 6;
-constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 32 +
-                        kTile * 8;
+constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
+constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 48 +
+                        8 + kTile * 8;
 
 template <typename T>
 __device__ __forceinline__ void dq_row(const AttnParams &p, const AttnUnit &u, int row, int head,
@@ -141,12 +142,14 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t v_full = k_empty + 8 * kKeySlots, v_empty = v_full + 8 * kValueSlots;
     const uint32_t in_full = v_empty + 8 * kValueSlots, s_full = in_full + 8, dp_full = s_full + 8;
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, dq_full = ds_full + 8;
-    const uint32_t slot = dq_full + 8;
+    const uint32_t in_empty = dq_full + 8;
+    const uint32_t slot = in_empty + 8;
     unsigned char *tail = aligned + (slot - base);
     volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
     uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);  // rows to do again
-    uint32_t *largest = reinterpret_cast<uint32_t *>(tail + 24);
-    float2 *stats = reinterpret_cast<float2 *>(tail + 32);
+    uint32_t *largest = reinterpret_cast<uint32_t *>(tail + 24);  // units in turn
+    volatile int *stop = reinterpret_cast<volatile int *>(tail + 32);
+    float2 *stats = reinterpret_cast<float2 *>(tail + 48);  // and e's parts
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -156,7 +159,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gave_up = 0;
-        *largest = 0;
+        largest[0] = largest[1] = 0;
+        *stop = 0;
         for (int i = 0; i < 4; ++i) bad[i] = 0;
     }
     if (warp == kIssueWarp) {
@@ -173,33 +177,26 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
     const uint32_t dp_tm = tmem + kTile, pk_tm = tmem + 2 * kTile, dq_tm = tmem + 3 * kTile;
 
-    const int head = blockIdx.x % p.heads_q;
-    AttnUnit u;
-    const bool any = unit_at<kTile>(p, blockIdx.x / p.heads_q, u);
-    const int n = any ? u.tile + 1 : 0;  // tiles of keys
     const int boxes = p.dim > 64 ? 2 : 1;
+    BlockUnit<kTile> w;
+    int round = 0;
     bool ok = true;
 
     if (group == kSumGroups) {
         give_registers<kBackIssueRegs>();
         if (warp == kLoadWarp) {
-            if (lane == 0 && any) {
-                bar_expect(in_full, 2 * boxes * kBox);
-                for (int b = 0; b < boxes; ++b) {
-                    const int token = u.start + u.tile * kTile;
-                    tma_rows(q_at + b * kBox, &q_map, 64 * b, head, token, in_full);
-                    tma_rows(g_at + b * kBox, &g_map, 64 * b, head, token, in_full);
-                }
-                int sk = 0, sv = 0;
-                uint32_t phk = 1, phv = 1;
+            int sk = 0, sv = 0;
+            uint32_t phk = 1, phv = 1, ph = 1;
+            while (lane == 0 && ok && w.next(p, round)) {
+                const int n = w.u.tile + 1;  // tiles of keys
                 const auto load = [&](uint32_t full, uint32_t empty, uint32_t at,
                                       const CUtensorMap *map, int &s, uint32_t &ph, int slots,
                                       int j) {
                     if (!bar_wait(empty + 8 * s, ph, gave_up)) return false;
                     bar_expect(full + 8 * s, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
-                        tma_rows(at + s * kTileBytes + b * kBox, map, 64 * b, head / p.group,
-                                 u.start + j * kTile, full + 8 * s);
+                        tma_rows(at + s * kTileBytes + b * kBox, map, 64 * b, w.head / p.group,
+                                 w.u.start + j * kTile, full + 8 * s);
                     if (++s == slots) s = 0, ph ^= 1;
                     return true;
                 };
@@ -207,6 +204,17 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 for (int i = 0; i <= n && ok; ++i) {
                     if (i < n)
                         ok = load(k_full, k_empty, k_at, &k_map, sk, phk, kKeySlots, n - 1 - i);
+                    if (i == 0 && ok) {
+                        ok = bar_wait(in_empty, ph, gave_up);
+                        if (!ok) break;
+                        ph ^= 1;
+                        bar_expect(in_full, 2 * boxes * kBox);
+                        for (int b = 0; b < boxes; ++b) {
+                            const int token = w.u.start + w.u.tile * kTile;
+                            tma_rows(q_at + b * kBox, &q_map, 64 * b, w.head, token, in_full);
+                            tma_rows(g_at + b * kBox, &g_map, 64 * b, w.head, token, in_full);
+                        }
+                    }
                     if (i > 0 && ok)
                         ok = load(v_full, v_empty, v_at, &v_map, sv, phv, kValueSlots, n - i);
                 }
@@ -214,130 +222,146 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         } else if (warp == kIssueWarp) {
             const uint32_t mine = one_lane();
             const int steps = (p.dim + 15) / 16;
-            const auto scores = [&](int i) {
-                if (!wait_warp(k_full + 8 * (i % kKeySlots), i / kKeySlots & 1, gave_up))
-                    return false;
-                const uint32_t at = k_at + i % kKeySlots * kTileBytes;
-                const int seen = u.len - (n - 1 - i) * kTile;
-                if (seen < kTile) zero_rows(at, seen, boxes, lane);
-                mma_rows<T>(tmem, q_at, at, steps, mine);
-                commit(s_full, mine);
-                return true;
-            };
-            const auto grads = [&](int i) {  // dP
-                if (!wait_warp(v_full + 8 * (i % kValueSlots), i / kValueSlots & 1, gave_up))
-                    return false;
-                mma_rows<T>(dp_tm, g_at, v_at + i % kValueSlots * kTileBytes, steps, mine);
-                commit(dp_full, mine);
-                commit(v_empty + 8 * (i % kValueSlots), mine);
-                return true;
-            };
-            if (any) {
-                ok = wait_warp(in_full, 0, gave_up);
+            uint32_t ph = 0;
+            int it = 0;  // steps so far
+            while (ok && w.next(p, round)) {
+                const int n = w.u.tile + 1, base = it;
+                const auto scores = [&](int i) {
+                    const int at_i = base + i, slot_i = at_i % kKeySlots;
+                    if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, gave_up)) return false;
+                    const uint32_t at = k_at + slot_i * kTileBytes;
+                    const int seen = w.u.len - (n - 1 - i) * kTile;
+                    if (seen < kTile) zero_rows(at, seen, boxes, lane);
+                    mma_rows<T>(tmem, q_at, at, steps, mine);
+                    commit(s_full, mine);
+                    return true;
+                };
+                const auto grads = [&](int i) {  // dP
+                    const int at_i = base + i, slot_i = at_i % kValueSlots;
+                    if (!wait_warp(v_full + 8 * slot_i, at_i / kValueSlots & 1, gave_up))
+                        return false;
+                    mma_rows<T>(dp_tm, g_at, v_at + slot_i * kTileBytes, steps, mine);
+                    commit(dp_full, mine);
+                    commit(v_empty + 8 * slot_i, mine);
+                    if (i == n - 1) commit(in_empty, mine);  // the last ones
+                    return true;
+                };
+                ok = wait_warp(in_full, ph, gave_up);
+                ph ^= 1;
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
-            }
-            for (int i = 0; i < n && ok; ++i) {
-                const uint32_t at = k_at + i % kKeySlots * kTileBytes;
-                ok = wait_warp(p_full, i & 1, gave_up);
-                if (!ok) break;
-                tmem_after();
-                mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
-                if (i + 1 < n) ok = scores(i + 1);
-                ok = ok && wait_warp(ds_full, i & 1, gave_up);
-                if (!ok) break;
-                tmem_after();
-                mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
-                commit(k_empty + 8 * (i % kKeySlots), mine);
-                if (i == n - 1) commit(dq_full, mine);
-                else ok = grads(i + 1);
+                for (int i = 0; i < n && ok; ++i, ++it) {
+                    const uint32_t at = k_at + it % kKeySlots * kTileBytes;
+                    ok = wait_warp(p_full, it & 1, gave_up);
+                    if (!ok) break;
+                    tmem_after();
+                    // (the unit before has been read: its warps have gone on to this one)
+                    mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
+                    if (i + 1 < n) ok = scores(i + 1);
+                    ok = ok && wait_warp(ds_full, it & 1, gave_up);
+                    if (!ok) break;
+                    tmem_after();
+                    mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
+                    commit(k_empty + 8 * (it % kKeySlots), mine);
+                    if (i == n - 1) commit(dq_full, mine);
+                    else ok = grads(i + 1);
+                }
             }
         }
         __syncwarp();
     } else {
         take_registers<kBackRegs>();
-        const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
+        const int side = group, mine = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
-        const bool live = any && row < u.len;
-        if (any) {
-            row_stats<T>(p, u, head, stats, largest);
+        int it = 0, units = 0;
+        // The warps meet at barriers, so they end together: not where a wait of one gave up,
+        // but after the unit in which a thread saw it for all.
+        for (; !*stop && w.next(p, round); ++units) {
+            const AttnUnit &u = w.u;
+            const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
+            const bool live = row < u.len;
+            row_stats<T>(p, u, head, stats, largest + units % 2);
             sums_barrier();
-        }
-        const float2 st = stats[mine];  // (whatever a block without work finds there)
-        const Shift<T> shift(*largest);
-        if (std::is_same<T, __half>::value && threadIdx.x == 0 && *largest)
-            atomicMax(p.largest, *largest);
-        F2 rest = both(0.f);  // e, of this part of the columns
-        for (int i = 0; i < n; ++i) {
-            ok = ok && wait_warp(s_full, i & 1, gave_up);
-            if (!ok) break;
+            const float2 st = stats[mine];
+            const uint32_t big = largest[units % 2];
+            const Shift<T> shift(big);
+            if (std::is_same<T, __half>::value && threadIdx.x == 0) {
+                if (big) atomicMax(p.largest, big);
+                largest[(units + 1) % 2] = 0;
+            }
+            F2 rest = both(0.f);  // e, of this part of the columns
+            for (int i = 0; i < n; ++i, ++it) {
+                ok = ok && wait_warp(s_full, it & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                uint32_t s[kCols], d[kCols], w[kCols / 2];
+                // the last key of this part that the row sees; a row that sees one has dS = 0
+                const int seen = row - (n - 1) * kTile - kCols * side;
+                tmem_load32(s_tm, s);
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
+                                      both(p.scale2), both(-st.x));
+                    s[c] = __float_as_uint(exp2_fast(x.x));
+                    s[c + 1] = __float_as_uint(exp2_fast(x.y));
+                }
+                if (i == 0) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+                        if (c > seen) s[c] = 0;
+                }
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2)
+                    w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                tmem_store16(s_tm, w);
+                tmem_wait_stores();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full);
+                ok = wait_warp(dp_full, it & 1, gave_up);
+                if (!ok) break;
+                tmem_after();
+                tmem_load32(d_tm, d);
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
+                                      both(shift.grads), both(-st.y * shift.grads));
+                    const F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
+                    d[c] = __float_as_uint(v.x), d[c + 1] = __float_as_uint(v.y);
+                }
+                if (i == 0) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+                        if (c > seen || row == 0) d[c] = 0;
+                }
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    rest = add2(rest, {__uint_as_float(d[c]), __uint_as_float(d[c + 1])});
+                    w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
+                }
+                tmem_store16(d_tm, w);
+                tmem_wait_stores();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(ds_full);
+            }
+            if (ok) ok = wait_warp(dq_full, units & 1, gave_up);
             tmem_after();
-            uint32_t s[kCols], d[kCols], w[kCols / 2];
-            // the last key of this part that the row sees; a row that sees one has dS = 0
-            const int seen = row - (n - 1) * kTile - kCols * side;
-            tmem_load32(s_tm, s);
-#pragma unroll
-            for (int c = 0; c < kCols; c += 2) {
-                const F2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])},
-                                  both(p.scale2), both(-st.x));
-                s[c] = __float_as_uint(exp2_fast(x.x));
-                s[c + 1] = __float_as_uint(exp2_fast(x.y));
-            }
-            if (i == 0) {
-#pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                    if (c > seen) s[c] = 0;
-            }
-#pragma unroll
-            for (int c = 0; c < kCols; c += 2)
-                w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-            tmem_store16(s_tm, w);
-            tmem_wait_stores();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(p_full);
-            ok = wait_warp(dp_full, i & 1, gave_up);
-            if (!ok) break;
-            tmem_after();
-            tmem_load32(d_tm, d);
-#pragma unroll
-            for (int c = 0; c < kCols; c += 2) {
-                const F2 e = fma2({__uint_as_float(d[c]), __uint_as_float(d[c + 1])},
-                                  both(shift.grads), both(-st.y * shift.grads));
-                const F2 v = mul2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, e);
-                d[c] = __float_as_uint(v.x), d[c + 1] = __float_as_uint(v.y);
-            }
-            if (i == 0) {
-#pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                    if (c > seen || row == 0) d[c] = 0;
-            }
-#pragma unroll
-            for (int c = 0; c < kCols; c += 2) {
-                rest = add2(rest, {__uint_as_float(d[c]), __uint_as_float(d[c + 1])});
-                w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
-            }
-            tmem_store16(d_tm, w);
-            tmem_wait_stores();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(ds_full);
-        }
-        if (any) {
-            if (ok) ok = wait_warp(dq_full, 0, gave_up);
-            tmem_after();
-            // every tile of keys and values has been used: their places hold e's parts and
-            // the results
-            float *parts = reinterpret_cast<float *>(aligned + (v_at - base));
-            parts[side * kTile + mine] = rest.x + rest.y;
+            // e's parts through the place of the stats, which every warp has read
+            float *parts = reinterpret_cast<float *>(stats);
+            float e = rest.x + rest.y;
+            if (side >= 2) parts[(side - 2) * kTile + mine] = e;
             sums_barrier();
-            const float e = (parts[mine] + parts[kTile + mine] + parts[2 * kTile + mine] +
-                             parts[3 * kTile + mine]) * shift.undo;
+            if (side < 2) parts[side * kTile + mine] += e;
+            sums_barrier();
+            e = (parts[mine] + parts[kTile + mine]) * shift.undo;
             if (live && side == 0)
                 p.stats[head * p.tokens + u.start + row] = make_float2(st.x, st.y + e);
             const float a = ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu);
             const float b = -e * p.scale * Shift<T>::kUndoProbs;
+            T *out = static_cast<T *>(p.dq) + (u.start + (int64_t)row) * p.d_token[0] +
+                     head * p.d_head[0];
             bool good = true;
             for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                 uint32_t v[16], k[16];
@@ -350,22 +374,27 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     x[h / 8].v[h % 8] = y;
                     good = good && finite(y);
                 }
-                put_columns<T>(k_at, mine, c, x);
+                if (!live) continue;
+#pragma unroll
+                for (int h = 0; h < 16; h += 8) {
+                    if (p.d_vectors[0])
+                        store8<true>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                    else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                }
             }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
             if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            if (threadIdx.x == 0) *stop = *gave_up;
             sums_barrier();
-            const int64_t token = u.start + (int64_t)u.tile * kTile;
-            write_tile(k_at, min(kTile, u.len - u.tile * kTile),
-                       static_cast<T *>(p.dq) + token * p.d_token[0] + head * p.d_head[0],
-                       p.d_token[0], p.d_vectors[0], p.dim, p.dim_out, (int)threadIdx.x,
-                       128 * kSumGroups);
-            sums_barrier();
-            uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
-            while (rows) {
-                const int i = __ffs(rows) - 1;
-                rows &= rows - 1;
-                dq_row<T>(p, u, row - lane + i, head, lane);
+            if (side == 0) {
+                uint32_t rows = ok && !*gave_up ? bad[warp] : 0;
+                __syncwarp();
+                if (lane == 0) bad[warp] = 0;
+                while (rows) {
+                    const int i = __ffs(rows) - 1;
+                    rows &= rows - 1;
+                    dq_row<T>(p, u, row - lane + i, head, lane);
+                }
             }
         }
     }
@@ -860,7 +889,8 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     if (std::is_same<T, __half>::value) POS_CUDA(cudaMemsetAsync(p.largest, 0, 4, s));
     auto dq = attn_dq_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dq), kDqSmem));
-    POS_CUDA(launch_dependent(dq, grid_q, kBackThreads, kDqSmem, s, q, k, v, g, p));
+    POS_CUDA(launch_dependent(dq, std::min(grid_q, std::max(1, sm_count())), kBackThreads, kDqSmem, s,
+                              q, k, v, g, p));
     auto dkv = attn_dkv_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dkv), kDkvSmem));
     POS_CUDA(launch_dependent(dkv, grid_k * p.parts, kBackThreads, kDkvSmem, s, q, k, v, g, p));
