@@ -2,7 +2,8 @@
 memory feasibility, the stage-level prune and the exact search, in CUDA
 kernels behind the C ABI of include/poseidon.h (libposeidon.so); and the
 operators of a layer that keeps its activations in 8 bits between a
-micro-batch's forward and backward pass.
+micro-batch's forward and backward pass: checkpoints and weight gradients, norms,
+dropout and attention.
 
 The Python side is the ctypes binding in ``binding``; it loads the in-tree
 library and never computes anything itself.

@@ -9,7 +9,7 @@ namespace pos {
 // read in place, from any alignment).  h is rounded to its type before it is squared,
 // kept or normalised: what the backward pass reads is what the forward pass used.
 template <typename T, typename H, class TEAM, bool RING>
-__global__ void __launch_bounds__(TEAM::M, 1) norm_forward_kernel(const NormParams p) {
+__global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_forward_kernel(const NormParams p) {
     grid_dep_wait();
     grid_dep_trigger();
     extern __shared__ uint4 cells[];
@@ -189,6 +189,7 @@ static pos_status forward_of(const NormParams &p, bool aligned, cudaStream_t s) 
         case 0: return launch_forward<T, H, Team<true, 1, 256>>(p, shape, aligned, s);
         case 1: return launch_forward<T, H, Team<false, 1, 1024>>(p, shape, aligned, s);
         case 3: return launch_forward<T, H, Team<false, 4, 512>>(p, shape, aligned, s);
+        case 5: return launch_forward<T, H, Team<false, 1, 640, 2>>(p, shape, aligned, s);
         // (a row of 1024 threads would fill an SM's shared memory)
         default: return launch_forward<T, H, Team<false, 4, 1024>, false>(p, shape, s);
     }

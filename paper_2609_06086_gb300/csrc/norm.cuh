@@ -29,11 +29,12 @@ struct NormParams {
 };
 
 // A row's threads: one warp with V vectors of 8 elements a thread (rows of 8 W of
-// them share a block), or a whole block.  M: the most threads of a block.
-template <bool WARP, int V_, int M_>
+// them share a block), or a whole block.  M: the most threads of a block, of which an SM
+// holds BLOCKS at least.
+template <bool WARP, int V_, int M_, int BLOCKS = 1>
 struct Team {
     static constexpr bool kWarp = WARP;
-    static constexpr int V = V_, M = M_;
+    static constexpr int V = V_, M = M_, kBlocks = BLOCKS;
     static __device__ __forceinline__ int threads() { return WARP ? 32 : blockDim.x; }
     static __device__ __forceinline__ int rank() { return WARP ? threadIdx.x % 32 : threadIdx.x; }
     static __device__ __forceinline__ int teams() { return WARP ? blockDim.x / 32 : 1; }
@@ -229,8 +230,8 @@ __device__ __forceinline__ void keep8(int format, const Raw8<T> &raw, uint8_t *c
 // 8 bits: 288 us, with one 340; forward of 16384 x 4096 bf16 with both checkpoints and dropout:
 // one 128 us, with two 138).
 struct NormShape {
-    int team;     // 0..4: Team<true, 1, 256>, <false, 1, 1024>, <false, 2, 512>, <false, 4, 512>,
-                  // <false, 4, 1024>
+    int team;     // 0..5: Team<true, 1, 256>, <false, 1, 1024>, <false, 2, 512>, <false, 4, 512>,
+                  // <false, 4, 1024>, and <false, 1, 640, 2> or <false, 2, 320, 2>
     int threads, rows;  // of a block
 };
 inline NormShape norm_shape(int cols, bool backward) {
@@ -239,6 +240,8 @@ inline NormShape norm_shape(int cols, bool backward) {
     if (nv <= 32) return {0, 256, 8};
     const int v = nv > 1024 ? 4 : backward && nv > 256 ? 2 : 1;
     const int threads = ((nv + v - 1) / v + 31) / 32 * 32;
+    // rows of 4097 to 5120 columns: two blocks an SM with a few registers less
+    if (nv > 512 && nv <= 640) return {5, threads, 1};
     return {v < 4 ? v : threads <= 512 ? 3 : 4, threads, 1};
 }
 

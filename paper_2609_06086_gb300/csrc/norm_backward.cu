@@ -14,7 +14,7 @@ __device__ __forceinline__ Vec8 kept8(const NormParams &p, uint2 codes, int byte
 // thread's rows in registers, over a block's teams in shared memory, and written as
 // one partial sum per block, which norm_dw_kernel adds up in order: no atomics.
 template <typename T, typename H, class TEAM, bool RING>
-__global__ void __launch_bounds__(TEAM::M, 1) norm_backward_kernel(const NormParams p) {
+__global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_backward_kernel(const NormParams p) {
     grid_dep_wait();
     grid_dep_trigger();
     extern __shared__ uint4 cells[];
@@ -250,6 +250,7 @@ static pos_status backward_of(NormParams &p, bool aligned, const float *dw_in, f
         case 1: return launch_backward<T, H, Team<false, 1, 1024>>(p, shape, aligned, dw_in, dw, s);
         case 2: return launch_backward<T, H, Team<false, 2, 512>>(p, shape, aligned, dw_in, dw, s);
         case 3: return launch_backward<T, H, Team<false, 4, 512>>(p, shape, aligned, dw_in, dw, s);
+        case 5: return launch_backward<T, H, Team<false, 2, 320, 2>>(p, shape, aligned, dw_in, dw, s);
         default: return launch_backward<T, H, Team<false, 4, 1024>, false>(p, shape, dw_in, dw, s);
     }
 }

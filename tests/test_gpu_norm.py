@@ -152,6 +152,7 @@ class Call:
 SIZES = [(1, 1, 0, 0), (3, 8, 0, 0), (9, 31, 0, 0), (20, 100, 5, 1), (11, 256, 0, 0),
          (10, 264, 0, 0), (7, 1024, 8, 0), (5, 1025, 0, 0), (40, 1100, 3, 2), (3, 8192, 0, 0),
          (3, 8197, 0, 0), (2, 16384, 0, 0), (2, 16390, 0, 0), (2, 32768, 0, 0), (700, 48, 0, 0),
+         (3, 4097, 0, 0), (5, 5001, 7, 0), (4, 5001, 0, 0), (3, 5120, 0, 0), (3, 2100, 4, 3),
          (333, 1290, 0, 0)]
 
 
