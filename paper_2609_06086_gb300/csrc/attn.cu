@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kListThreads) attn_tiles_kernel(const AttnList
                 const int len = __shfl_sync(0xffffffffu, b, i) - at;
                 for (int t = lane; t < (len + p.rows - 1) / p.rows; t += 32) {
                     const int to = atomicAdd(&bins[t >> p.shift], 1);
-                    if (pass) p.tiles[to] = make_int4(at, len, t, 0);
+                    if (pass) p.tiles[to] = make_int4(at, len, t, p.sequences > tokens ? at : s + i);
                 }
             }
             last = __shfl_sync(0xffffffffu, a, 31);
@@ -112,7 +112,7 @@ constexpr int kSlots = 5;                    // tiles of keys and values on thei
 constexpr int kForwardRows = 2 * kTile;
 constexpr int kForwardThreads = 3 * 128;     // two warpgroups of rows, one of loads and products
 constexpr int kForwardBars = 2 * kSlots + 10;
-constexpr int kForwardSmem = 1024 + (2 + kSlots) * kTileBytes + 8 * kForwardBars + 16;
+constexpr int kForwardSmem = 1024 + (2 + kSlots) * kTileBytes + 8 * kForwardBars + kSharedBytes;
 // 2 * 208 + 88 = 504 = 3 * 168, what the block is launched with
 constexpr int kRowRegs = 208, kIssueRegs = 88;
 // A row's reference, which its exponentials are relative to, follows its largest
@@ -180,8 +180,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
     const uint32_t q_full = kv_empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 16,
                    o_full = p_full + 16, q_empty = o_full + 16;
     const uint32_t slot = q_empty + 16;
-    unsigned char *tail = aligned + (slot - base);
-    volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
+    AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -190,7 +189,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             bar_init(bars + 8 * i, rows ? 4 : 1);  // p_full: a tile's four warps
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        *gave_up = 0;
+        init_shared(sh);
         asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
@@ -206,7 +205,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
     tmem_after();
     grid_dep_wait();
     grid_dep_trigger();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sh->tmem);
 
     const int boxes = p.dim > 64 ? 2 : 1;
     ForwardUnit w;
@@ -220,7 +219,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             uint32_t ph = 1, q_ph[2] = {1, 1};  // an empty slot's first wait passes
             while (lane == 0 && ok && w.next(p, round)) {
                 const auto load = [&](bool v, int j) {
-                    if (!bar_wait(kv_empty + 8 * s, ph, gave_up)) return false;
+                    if (!attn_wait(kv_empty + 8 * s, ph, sh)) return false;
                     bar_expect(kv_full + 8 * s, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
                         tma_rows(kv_at + s * kTileBytes + b * kBox, v ? &v_map : &k_map, 64 * b,
@@ -232,7 +231,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     if (!ok || (t && !w.n1)) break;
-                    ok = bar_wait(q_empty + 8 * t, q_ph[t], gave_up);
+                    ok = attn_wait(q_empty + 8 * t, q_ph[t], sh);
                     if (!ok) break;
                     q_ph[t] ^= 1;
                     bar_expect(q_full + 8 * t, boxes * kBox);
@@ -252,7 +251,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 // the i-th tile to arrive: keys 2 i, values 2 i + 1
                 const auto arrived = [&](int i) {
                     return wait_warp(kv_full + 8 * ((base + i) % kSlots), (base + i) / kSlots & 1,
-                                     gave_up);
+                                     sh);
                 };
                 const auto place = [&](int i) { return kv_at + (base + i) % kSlots * kTileBytes; };
                 const auto scores = [&](int t, int i) {  // i: steps of keys from the first on
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (ok && (t == 0 || w.n1)) {
-                        ok = wait_warp(q_full + 8 * t, q_ph[t], gave_up);
+                        ok = wait_warp(q_full + 8 * t, q_ph[t], sh);
                         q_ph[t] ^= 1;
                     }
                 if (!ok) break;
@@ -282,7 +281,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     for (int t = 0; t < 2; ++t) {
                         const int n = t ? w.n1 : w.n0;
                         if (j < n && ok) {
-                            ok = wait_warp(p_full + 8 * t, ph[t], gave_up);
+                            ok = wait_warp(p_full + 8 * t, ph[t], sh);
                             if (!ok) break;
                             ph[t] ^= 1;
                             tmem_after();
@@ -314,7 +313,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             const int row = w.r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
             float top = 0.f, total = 0.f;
             for (int j = n - 1; j >= 0 && ok; --j) {
-                ok = wait_warp(s_full + 8 * t, ph, gave_up);
+                ok = wait_warp(s_full + 8 * t, ph, sh);
                 if (!ok) break;
                 ph ^= 1;
                 tmem_after();
@@ -379,7 +378,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full + 8 * t);
             }
-            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, gave_up);
+            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, sh);
             o_ph ^= 1;
             tmem_after();
             const bool live = row < w.u.len;
@@ -408,24 +407,12 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             if (p.lse && live)
                 p.lse[w.head * p.tokens + w.u.start + row] =
                     ok ? (top + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);
-            uint32_t again = __ballot_sync(0xffffffffu, ok && live && !good);
-            __syncwarp();
-            while (again) {
-                const int i = __ffs(again) - 1;
-                again &= again - 1;
+            do_again(__ballot_sync(0xffffffffu, ok && live && !good), sh, [&](int i) {
                 forward_row<T>(p, w.u, row - lane + i, w.head, lane);
-            }
+            });
         }
     }
-    // Where a wait gave up, copies and products may still be on their way: they end by
-    // themselves within microseconds.
-    __syncthreads();
-    if (*gave_up) {
-        const uint64_t t0 = now_ns();
-        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
-    tmem_before();
-    __syncthreads();
+    end_block(sh);
     if (warp == 9) {
         tmem_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));

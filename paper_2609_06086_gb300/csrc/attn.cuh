@@ -28,7 +28,8 @@ struct AttnParams {
     int64_t d_token[3], d_head[3];
     float *lse;                 // [heads_q][tokens] or NULL
     float2 *stats;              // backward: [heads_q][tokens]: lse in powers of two, D
-    uint32_t *largest;          // backward in f16: bits of dO's largest magnitude
+    uint32_t *largest;          // backward in f16: bits of dO's largest magnitudes, of each
+                                // [sequence][key head]
     float *part;                // backward: sums of parts of the keys' gradients
     int32_t parts;
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
@@ -41,20 +42,20 @@ struct AttnParams {
 };
 
 // A tile of queries or keys: the first token of its sequence, the sequence's
-// length, and which tile of it.
+// length, which tile of it, and a number of the sequence's own.
 struct AttnUnit {
-    int start, len, tile;
+    int start, len, tile, sequence;
 };
 template <int ROWS>
 __device__ __forceinline__ bool unit_at(const AttnParams &p, int i, AttnUnit &u) {
     if (!p.tiles) {  // longest first, as the list is
-        u.start = 0, u.len = (int)p.tokens;
+        u.start = 0, u.len = (int)p.tokens, u.sequence = 0;
         u.tile = (u.len + ROWS - 1) / ROWS - 1 - i;
         return u.tile >= 0;
     }
     if (i >= *p.n_tiles) return false;
     const int4 t = p.tiles[i];
-    u.start = t.x, u.len = t.y, u.tile = t.z;
+    u.start = t.x, u.len = t.y, u.tile = t.z, u.sequence = t.w;
     return true;
 }
 
@@ -83,10 +84,62 @@ struct BlockUnit {
 // ---------------------------------------------------------------------------
 // PTX
 // ---------------------------------------------------------------------------
+// What a block's warps share besides tiles and barriers.
+struct AttnShared {
+    uint32_t tmem;
+    volatile int gave_up, again, stop;  // a wait did; warps that do rows again; a block's units end
+    uint32_t bad[4];                    // rows to do again
+    uint32_t largest[2];                // of dO, units in turn
+};
+constexpr int kSharedBytes = 48;
+static_assert(sizeof(AttnShared) <= kSharedBytes, "room for it");
+__device__ __forceinline__ void init_shared(AttnShared *sh) {
+    sh->gave_up = sh->again = sh->stop = 0;
+    for (int i = 0; i < 4; ++i) sh->bad[i] = 0;
+    sh->largest[0] = sh->largest[1] = 0;
+}
+// Waits for a phase, two seconds at most (WaitLimit), not counting time in which the
+// block does rows again: a long row takes a warp milliseconds.
+__device__ __forceinline__ bool attn_wait_long(uint32_t bar, uint32_t parity, AttnShared *sh) {
+    WaitLimit limit(now_ns());
+    for (;;) {
+        if (bar_try(bar, parity)) return true;
+        if (sh->gave_up) return false;
+        if (sh->again) limit = WaitLimit(now_ns());
+        if (limit.reached(now_ns())) {
+            sh->gave_up = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, AttnShared *sh) {
+    if (bar_try(bar, parity)) return true;
+    return attn_wait_long(bar, parity, sh);
+}
 // A wait of a whole warp: all lanes go on or none does.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up) {
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, AttnShared *sh) {
     if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-    return __all_sync(0xffffffffu, bar_wait(bar, parity, gave_up));
+    return __all_sync(0xffffffffu, attn_wait(bar, parity, sh));
+}
+// By a warp, the rows of a mask again (row(i) does the i-th).
+template <typename F>
+__device__ __forceinline__ void do_again(uint32_t rows, AttnShared *sh, F row) {
+    if (!rows) return;
+    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), 1);
+    for (; rows; rows &= rows - 1) row(__ffs(rows) - 1);
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), -1);
+}
+// The block's end.  Where a wait gave up, copies and products may still be on their way:
+// they end by themselves within microseconds.
+__device__ __forceinline__ void end_block(AttnShared *sh) {
+    __syncthreads();
+    if (sh->gave_up) {
+        const uint64_t t0 = now_ns();
+        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
 }
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *map, int x, int head,
                                          int token, uint32_t bar) {
@@ -400,7 +453,8 @@ __device__ __forceinline__ void write_row(void *out, int64_t at, const RowPart &
     // (side: which of four in turn of 16 columns, or all)
 #pragma unroll
     for (int i = 0; i < kAttnMaxDim / 32; ++i)
-        if (lane + 32 * i < dim && (side < 0 || (lane + 32 * i) / 16 % 4 == side)) static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
+        if (lane + 32 * i < dim && (side < 0 || (lane + 32 * i) / 16 % 4 == side))
+            static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
 }
 
 // ---------------------------------------------------------------------------

@@ -19,8 +19,8 @@ constexpr int kLoadWarp = 4 * kSumGroups, kIssueWarp = kLoadWarp + 1, kStatsWarp
 // f16 holds probabilities of long rows and small gradients badly (below 2^-14 with
 // fewer bits, below 2^-25 not at all).  There P is multiplied by 2^12 and dS by 2^k, k the
 // same for a product's sums: the largest magnitude of dO (of the block's queries for
-// theirs, of all for the keys') becomes 2^8 to 2^9.  A dS that is too large all the
-// same gives an infinity and its rows are done again in 32 bits.
+// theirs, of the sequence's under the key head for the keys') becomes 2^8 to 2^9.  A dS
+// that is too large all the same gives an infinity and its rows are done again in 32 bits.
 template <typename T>
 struct Shift {
     static constexpr float kProbs = std::is_same<T, __half>::value ? 12.f : 0.f;
@@ -32,8 +32,10 @@ struct Shift {
             undo = __uint_as_float((uint32_t)(127 - k) << 23);
         }
     }
-    static __device__ __forceinline__ Shift of_all(const AttnParams &p) {
-        return Shift(std::is_same<T, __half>::value ? *p.largest : 0u);
+    static __device__ __forceinline__ Shift of_keys(const AttnParams &p, const AttnUnit &u, int g) {
+        return Shift(std::is_same<T, __half>::value
+                         ? p.largest[(int64_t)u.sequence * p.heads_k + g]
+                         : 0u);
     }
     static constexpr float kUndoProbs = std::is_same<T, __half>::value ? 1.f / 4096.f : 1.f;
 };
@@ -90,8 +92,9 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // dS = P (dP - D) that of dP, and while one of them is made, the tensor cores use up the
 // other and compute what comes next in its place.
 //   A block takes one such unit after another, so that the next one's first loads, scores
-// and dP come while the last one ends.  Before a unit its warps compute D = dO . o while the first tiles are on their way
-// (a kernel of its own took 16 of 480 us for 4096 tokens of 32 heads of 128).
+// and dP come while the last one ends.  Before a unit its warps
+// compute D = dO . o while the first tiles are on their way (a kernel of its own took 16
+// of 480 us for 4096 tokens of 32 heads of 128).
 //   D has the rounding of o in it, in 16 bits, which for rows with few keys that
 // count is larger than that of everything else (2 tokens of 2 heads of 64, bf16: dQ 0.7 %
 // off, dK 1.2 %).  Its exact value is D + e, e = sum P (dP - D), which this kernel has
@@ -99,8 +102,8 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
 constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
-constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars + 48 +
-                        8 + kTile * 8;
+constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars +
+                        kSharedBytes + kTile * 8;
 
 template <typename T>
 __device__ __forceinline__ void dq_row(const AttnParams &p, const AttnUnit &u, int row, int head,
@@ -144,12 +147,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, dq_full = ds_full + 8;
     const uint32_t in_empty = dq_full + 8;
     const uint32_t slot = in_empty + 8;
-    unsigned char *tail = aligned + (slot - base);
-    volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
-    uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);  // rows to do again
-    uint32_t *largest = reinterpret_cast<uint32_t *>(tail + 24);  // units in turn
-    volatile int *stop = reinterpret_cast<volatile int *>(tail + 32);
-    float2 *stats = reinterpret_cast<float2 *>(tail + 48);  // and e's parts
+    AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
+    // rows' statistics, and the parts of e
+    float2 *stats = reinterpret_cast<float2 *>(aligned + (slot - base) + kSharedBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -158,10 +158,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             bar_init(bars + 8 * i, sums ? 4 * kSumGroups : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        *gave_up = 0;
-        largest[0] = largest[1] = 0;
-        *stop = 0;
-        for (int i = 0; i < 4; ++i) bad[i] = 0;
+        init_shared(sh);
     }
     if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
@@ -174,7 +171,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     tmem_after();
     grid_dep_wait();
     grid_dep_trigger();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sh->tmem);
     const uint32_t dp_tm = tmem + kTile, pk_tm = tmem + 2 * kTile, dq_tm = tmem + 3 * kTile;
 
     const int boxes = p.dim > 64 ? 2 : 1;
@@ -192,7 +189,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const auto load = [&](uint32_t full, uint32_t empty, uint32_t at,
                                       const CUtensorMap *map, int &s, uint32_t &ph, int slots,
                                       int j) {
-                    if (!bar_wait(empty + 8 * s, ph, gave_up)) return false;
+                    if (!attn_wait(empty + 8 * s, ph, sh)) return false;
                     bar_expect(full + 8 * s, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
                         tma_rows(at + s * kTileBytes + b * kBox, map, 64 * b, w.head / p.group,
@@ -205,7 +202,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (i < n)
                         ok = load(k_full, k_empty, k_at, &k_map, sk, phk, kKeySlots, n - 1 - i);
                     if (i == 0 && ok) {
-                        ok = bar_wait(in_empty, ph, gave_up);
+                        ok = attn_wait(in_empty, ph, sh);
                         if (!ok) break;
                         ph ^= 1;
                         bar_expect(in_full, 2 * boxes * kBox);
@@ -228,7 +225,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const int n = w.u.tile + 1, base = it;
                 const auto scores = [&](int i) {
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
-                    if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, gave_up)) return false;
+                    if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, sh)) return false;
                     const uint32_t at = k_at + slot_i * kTileBytes;
                     const int seen = w.u.len - (n - 1 - i) * kTile;
                     if (seen < kTile) zero_rows(at, seen, boxes, lane);
@@ -238,7 +235,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 };
                 const auto grads = [&](int i) {  // dP
                     const int at_i = base + i, slot_i = at_i % kValueSlots;
-                    if (!wait_warp(v_full + 8 * slot_i, at_i / kValueSlots & 1, gave_up))
+                    if (!wait_warp(v_full + 8 * slot_i, at_i / kValueSlots & 1, sh))
                         return false;
                     mma_rows<T>(dp_tm, g_at, v_at + slot_i * kTileBytes, steps, mine);
                     commit(dp_full, mine);
@@ -246,19 +243,19 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (i == n - 1) commit(in_empty, mine);  // the last ones
                     return true;
                 };
-                ok = wait_warp(in_full, ph, gave_up);
+                ok = wait_warp(in_full, ph, sh);
                 ph ^= 1;
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
                 for (int i = 0; i < n && ok; ++i, ++it) {
                     const uint32_t at = k_at + it % kKeySlots * kTileBytes;
-                    ok = wait_warp(p_full, it & 1, gave_up);
+                    ok = wait_warp(p_full, it & 1, sh);
                     if (!ok) break;
                     tmem_after();
                     // (the unit before has been read: its warps have gone on to this one)
                     mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
                     if (i + 1 < n) ok = scores(i + 1);
-                    ok = ok && wait_warp(ds_full, it & 1, gave_up);
+                    ok = ok && wait_warp(ds_full, it & 1, sh);
                     if (!ok) break;
                     tmem_after();
                     mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
@@ -277,22 +274,23 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         int it = 0, units = 0;
         // The warps meet at barriers, so they end together: not where a wait of one gave up,
         // but after the unit in which a thread saw it for all.
-        for (; !*stop && w.next(p, round); ++units) {
+        for (; !sh->stop && w.next(p, round); ++units) {
             const AttnUnit &u = w.u;
             const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
             const bool live = row < u.len;
-            row_stats<T>(p, u, head, stats, largest + units % 2);
+            row_stats<T>(p, u, head, stats, sh->largest + units % 2);
             sums_barrier();
             const float2 st = stats[mine];
-            const uint32_t big = largest[units % 2];
+            const uint32_t big = sh->largest[units % 2];
             const Shift<T> shift(big);
             if (std::is_same<T, __half>::value && threadIdx.x == 0) {
-                if (big) atomicMax(p.largest, big);
-                largest[(units + 1) % 2] = 0;
+                if (big)
+                    atomicMax(p.largest + (int64_t)u.sequence * p.heads_k + head / p.group, big);
+                sh->largest[(units + 1) % 2] = 0;
             }
             F2 rest = both(0.f);  // e, of this part of the columns
             for (int i = 0; i < n; ++i, ++it) {
-                ok = ok && wait_warp(s_full, it & 1, gave_up);
+                ok = ok && wait_warp(s_full, it & 1, sh);
                 if (!ok) break;
                 tmem_after();
                 uint32_t s[kCols], d[kCols], w[kCols / 2];
@@ -319,7 +317,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 tmem_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full);
-                ok = wait_warp(dp_full, it & 1, gave_up);
+                ok = wait_warp(dp_full, it & 1, sh);
                 if (!ok) break;
                 tmem_after();
                 tmem_load32(d_tm, d);
@@ -346,7 +344,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(ds_full);
             }
-            if (ok) ok = wait_warp(dq_full, units & 1, gave_up);
+            if (ok) ok = wait_warp(dq_full, units & 1, sh);
             tmem_after();
             // e's parts through the place of the stats, which every warp has read
             float *parts = reinterpret_cast<float *>(stats);
@@ -383,28 +381,20 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 }
             }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
-            if (lane == 0 && again) atomicOr(bad + warp % 4, again);
-            if (threadIdx.x == 0) *stop = *gave_up;
+            if (lane == 0 && again) atomicOr(sh->bad + warp % 4, again);
+            if (threadIdx.x == 0) sh->stop = sh->gave_up;
             sums_barrier();
             if (side == 0) {
-                uint32_t rows = ok && !*gave_up ? bad[warp] : 0;
+                const uint32_t rows = ok && !sh->gave_up ? sh->bad[warp] : 0;
                 __syncwarp();
-                if (lane == 0) bad[warp] = 0;
-                while (rows) {
-                    const int i = __ffs(rows) - 1;
-                    rows &= rows - 1;
+                if (lane == 0) sh->bad[warp] = 0;
+                do_again(__shfl_sync(0xffffffffu, rows, 0), sh, [&](int i) {
                     dq_row<T>(p, u, row - lane + i, head, lane);
-                }
+                });
             }
         }
     }
-    __syncthreads();
-    if (*gave_up) {  // copies and products may still be on their way
-        const uint64_t t0 = now_ns();
-        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
-    tmem_before();
-    __syncthreads();
+    end_block(sh);
     if (warp == kIssueWarp) {
         tmem_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
@@ -428,7 +418,7 @@ constexpr int kQuerySlots = 2;
 constexpr int kStatBytes = kTile * 8;
 constexpr int kDkvBars = 6 * kQuerySlots + 6;
 constexpr int kDkvSmem = 1024 + (2 + 2 * kQuerySlots) * kTileBytes + kQuerySlots * kStatBytes +
-                         8 * kDkvBars + 32;
+                         8 * kDkvBars + kSharedBytes;
 
 __device__ __forceinline__ F2 load_stats(uint32_t at) {
     F2 l;
@@ -503,9 +493,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t in_full = st_empty + 8 * kQuerySlots, s_full = in_full + 8, dp_full = s_full + 8;
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, out_full = ds_full + 8;
     const uint32_t slot = out_full + 8;
-    unsigned char *tail = aligned + (slot - base);
-    volatile int *gave_up = reinterpret_cast<volatile int *>(tail + 4);
-    uint32_t *bad = reinterpret_cast<uint32_t *>(tail + 8);
+    AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -516,8 +504,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                             : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        *gave_up = 0;
-        for (int i = 0; i < 4; ++i) bad[i] = 0;
+        init_shared(sh);
     }
     if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
@@ -530,7 +517,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     tmem_after();
     grid_dep_wait();
     grid_dep_trigger();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tail);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&sh->tmem);
     const uint32_t dp_tm = tmem + kTile, dv_tm = tmem + 2 * kTile, dk_tm = tmem + 3 * kTile;
 
     const int unit = blockIdx.x / p.parts, part = blockIdx.x % p.parts, g = unit % p.heads_k;
@@ -560,7 +547,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     const int token = u.start + (u.tile + (step0 + i) % each) * kTile;
                     for (int w = 0; w < 2 && ok; ++w) {
                         const uint32_t full = (w ? g_full : q_full) + 8 * s;
-                        ok = bar_wait((w ? g_empty : q_empty) + 8 * s, ph, gave_up);
+                        ok = attn_wait((w ? g_empty : q_empty) + 8 * s, ph, sh);
                         if (!ok) break;
                         bar_expect(full, boxes * kBox);
                         for (int b = 0; b < boxes; ++b)
@@ -575,7 +562,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             const int steps = (p.dim + 15) / 16;
             const auto arrived = [&](uint32_t full, uint32_t at, int i) {
                 const int s = i % kQuerySlots;
-                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, gave_up)) return false;
+                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, sh)) return false;
                 const int seen = u.len - (u.tile + (step0 + i) % each) * kTile;
                 if (seen < kTile) zero_rows(at + s * kTileBytes, seen, boxes, lane);
                 return true;
@@ -593,19 +580,19 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 return true;
             };
             if (n > 0) {
-                ok = wait_warp(in_full, 0, gave_up);
+                ok = wait_warp(in_full, 0, sh);
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
             }
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kQuerySlots;
-                ok = wait_warp(p_full, i & 1, gave_up);
+                ok = wait_warp(p_full, i & 1, sh);
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dv_tm, tmem, g_at + s * kTileBytes, steps, i > 0, mine);
                 commit(g_empty + 8 * s, mine);
                 if (i + 1 < n) ok = scores(i + 1);
-                ok = ok && wait_warp(ds_full, i & 1, gave_up);
+                ok = ok && wait_warp(ds_full, i & 1, sh);
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dk_tm, dp_tm, q_at + s * kTileBytes, steps, i > 0, mine);
@@ -616,7 +603,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         } else if (warp == kStatsWarp) {
             // lse and D of the queries; none for rows past the sequence: their
             // probabilities are 2^(0 - inf) = 0
-            const Shift<T> shift = Shift<T>::of_all(p);
+            const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0u);
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kQuerySlots, head = g * p.group + (step0 + i) / each;
                 const int row = (u.tile + (step0 + i) % each) * kTile;
@@ -627,7 +614,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     st[h] = row + lane + 32 * h < u.len
                                 ? from[lane + 32 * h]
                                 : make_float2(__uint_as_float(0x7f800000u), 0.f);
-                ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, gave_up);
+                ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, sh);
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h)  // -lse in the first half, -D in the second
@@ -642,7 +629,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         __syncwarp();
     } else {
         take_registers<kBackRegs>();
-        const Shift<T> shift = Shift<T>::of_all(p);
+        const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0u);
         const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
@@ -654,8 +641,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         for (int i = 0; i < n; ++i) {
             const int slot_i = i % kQuerySlots;
             const uint32_t st = st_at + slot_i * kStatBytes + 4 * query;
-            ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, gave_up) &&
-                 wait_warp(s_full, i & 1, gave_up);
+            ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, sh) &&
+                 wait_warp(s_full, i & 1, sh);
             if (!ok) break;
             tmem_after();
             uint32_t s[kCols], d[kCols], w[kCols / 2];
@@ -686,7 +673,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (lane == 0) bar_arrive(p_full);
 #pragma unroll
             for (int b = 0; b < kCols / 8; ++b) l[b] = load_stats(st + 512 + 32 * b);
-            ok = wait_warp(dp_full, i & 1, gave_up);
+            ok = wait_warp(dp_full, i & 1, sh);
             if (!ok) break;
             tmem_after();
             tmem_load_block(d_tm, d);
@@ -717,7 +704,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
         }
         if (n > 0) {
-            if (ok) ok = wait_warp(out_full, 0, gave_up);
+            if (ok) ok = wait_warp(out_full, 0, sh);
             tmem_after();
         }
         const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
@@ -751,7 +738,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     put_columns<T>(q_at + t * kTileBytes, mine, c, x);
                 }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
-            if (lane == 0 && again) atomicOr(bad + warp % 4, again);
+            if (lane == 0 && again) atomicOr(sh->bad + warp % 4, again);
             sums_barrier();
             const int64_t token = u.start + (int64_t)u.tile * kTile;
             const int count = min(kTile, u.len - u.tile * kTile);
@@ -763,21 +750,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                        p.d_token[2], p.d_vectors[2], p.dim, p.dim_out, (int)threadIdx.x,
                        128 * kSumGroups);
             sums_barrier();
-            uint32_t rows = ok && side == 0 && !*gave_up ? bad[warp] : 0;
-            while (rows) {
-                const int i = __ffs(rows) - 1;
-                rows &= rows - 1;
+            const uint32_t rows = ok && side == 0 && !sh->gave_up ? sh->bad[warp] : 0;
+            do_again(__shfl_sync(0xffffffffu, rows, 0), sh, [&](int i) {
                 dkv_row<T>(p, u, row - lane + i, g, lane);
-            }
+            });
         }
     }
-    __syncthreads();
-    if (*gave_up) {  // copies and products may still be on their way
-        const uint64_t t0 = now_ns();
-        while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
-    }
-    tmem_before();
-    __syncthreads();
+    end_block(sh);
     if (warp == kIssueWarp) {
         tmem_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
@@ -794,7 +773,7 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
     AttnUnit u;
     if (!unit_at<kTile>(p, unit / p.heads_k, u)) return;
     const int given = u.tile;
-    const Shift<T> shift = Shift<T>::of_all(p);
+    const Shift<T> shift = Shift<T>::of_keys(p, u, g);
     const int lane = threadIdx.x % 32;
     uint32_t used = 0;  // parts that have steps
     for (int r = 0; r < p.parts; ++r) {
@@ -867,12 +846,22 @@ static int parts_of(const pos_attn *a) {
         if (t < least) least = t, best = c;
     }
     // (their sums take 128 KB each)
-    while (best > 1 && attn_most_tiles(a, kTile) * a->heads_k * best > 16 * (int64_t)sms) best /= 2;
+    while (best > 1 && attn_most_tiles(a, kTile) * a->heads_k * best > 8 * (int64_t)sms) best /= 2;
     return best;
 }
 static int64_t part_bytes(const pos_attn *a, int parts) {
     return parts == 1 ? 0 : attn_most_tiles(a, kTile) * a->heads_k * parts *
                                 ((a->dim + 15) / 16 * 16) * kTile * 8;
+}
+
+static int64_t stats_bytes(const pos_attn *a) {
+    return (a->tokens * a->heads_q * 8 + 15) / 16 * 16;
+}
+// f16: sequences are numbered in order, or by their first tokens if fewer of these are
+// possible than sequences.
+static int64_t largest_bytes(const pos_attn *a) {
+    const int64_t n = a->starts ? std::min<int64_t>(a->sequences, a->tokens) : 1;
+    return a->dtype == POS_F16 ? (n * a->heads_k * 4 + 15) / 16 * 16 : 0;
 }
 
 template <typename T>
@@ -886,7 +875,8 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     POS_TRY(attn_grid(a, kTile, a->heads_q, &grid_q));
     POS_TRY(attn_grid(a, kTile, a->heads_k, &grid_k));
     if (grid_q == 0) return POS_OK;
-    if (std::is_same<T, __half>::value) POS_CUDA(cudaMemsetAsync(p.largest, 0, 4, s));
+    if (std::is_same<T, __half>::value)
+        POS_CUDA(cudaMemsetAsync(p.largest, 0, largest_bytes(a), s));
     auto dq = attn_dq_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dq), kDqSmem));
     POS_CUDA(launch_dependent(dq, std::min(grid_q, std::max(1, sm_count())), kBackThreads, kDqSmem, s,
@@ -899,14 +889,11 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     return POS_OK;
 }
 
-static int64_t stats_bytes(const pos_attn *a) {
-    return 16 + (a->tokens * a->heads_q * 8 + 15) / 16 * 16;
-}
-
 static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_heads &d_o,
                            AttnParams p, int parts, char *at, cudaStream_t s) {
     p.largest = reinterpret_cast<uint32_t *>(at);
-    p.stats = reinterpret_cast<float2 *>(at + 16);
+    at += largest_bytes(a);
+    p.stats = reinterpret_cast<float2 *>(at);
     at += stats_bytes(a);
     p.parts = parts;
     p.part = reinterpret_cast<float *>(at);
@@ -953,7 +940,8 @@ extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_hea
                              dx[i].head_stride % 8 == 0;
         }
         const int parts = parts_of(attn);
-        int64_t bytes = stats_bytes(attn) + part_bytes(attn, parts) + attn_list_bytes(attn, kTile);
+        int64_t bytes = largest_bytes(attn) + stats_bytes(attn) + part_bytes(attn, parts) +
+                        attn_list_bytes(attn, kTile);
         for (int i = 0; i < 4; ++i)
             if (!attn_direct(attn, i < 3 ? x[i] : *d_o, heads[i]))
                 bytes += attn_copy_bytes(attn, heads[i]);

@@ -147,11 +147,14 @@ class Call:
         tol = [zeros(self.hq), zeros(self.hk), zeros(self.hk)]
         f16 = self.dtype == "f16"
         g = self.g.double()
-        # f16: half the smallest step of P times 2^12 and of dS under its factor
+        # f16: half the smallest step of P times 2^12 and of dS under its factor, by which the
+        # largest dO of the sequence and key head is 2^8 at least
         step_p = tiny / 4096 if f16 else 0.0
-        step_ds = tiny * float(g[self.live].abs().max()) / 256 if f16 and self.live.any() else 0.0
         for a, b, h, j, Q, K, V, s, off in self.sequences():
             n, G, O = b - a, g[a:b, h], self.o[a:b, h].double()
+            group = self.hq // self.hk
+            large = float(g[a:b, j * group:(j + 1) * group].abs().max())
+            step_ds = tiny * large / 256 if f16 else 0.0
             lse = self.lse[h, a:b, None].double()
             seen = s > -math.inf
             p = torch.exp(s - lse)
@@ -238,6 +241,61 @@ def test_distributions(P, dtype, spread, grad):
     """Flat and sharp probabilities, whose largest score moves by far more than 2^8 from
     tile to tile, and small and large gradients."""
     Call(P, [600], 2, 1, 128, dtype, spread=spread, grad=grad).check()
+
+
+def test_gradients_of_sequences_far_apart_in_size(P):
+    """Of the second sequence, and of the first's second key head, dO is 1e-7 of the first
+    one's in f16: their own dS keep their bits.  Alone or beside the others, the same
+    results."""
+    c = Call(P, [200, 150, 40], 4, 2, 64, "f16", grad=3000.0, starts=True)
+    c.g[200:350] *= 1e-7
+    c.g[:200, 2:] *= 1e-7
+    c.check()
+    alone = Call(P, [200, 150, 40], 4, 2, 64, "f16")
+    for a, b in zip((*alone.x, alone.g), (*c.x, c.g)):
+        a.copy_(b)
+    alone.g[:200] = 0
+    alone.g[350:] = 0
+    alone.forward()
+    alone.backward()
+    for a, b in zip(alone.dx, c.dx):
+        assert torch.equal(a[200:350], b[200:350])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_other_sequences_are_not_read(P, dtype, what):
+    """Sequences of values that are not finite on both sides of one, within its tiles: its
+    rows are as the formulas have them, and the others' are written and not finite."""
+    c = Call(P, [150, 200, 90], 4, 2, 64, dtype)
+    around = torch.ones(440, dtype=torch.bool, device="cuda")
+    around[150:350] = False
+    for t in (*c.x, c.g):
+        t[around] = float(what)
+    c.forward()
+    c.backward()
+    for t in (c.o, *c.dx):
+        assert not torch.isfinite(t[around].double()).any()
+    c.without_what_is_not_finite()
+    c.check_forward(~around)
+    c.check_backward((~around,) * 3)
+
+
+def test_heads_outermost(P):
+    """Tensors [heads][tokens][dim], inputs and results."""
+    c = Call(P, [130, 60], 4, 2, 80, "bf16", "apart", behind=2)
+    outer = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    c.x, c.g, c.o, c.dx = [outer(t) for t in c.x], outer(c.g), outer(c.o), [outer(t) for t in c.dx]
+    c.check()
+
+
+def test_more_sequences_than_tokens(P):
+    """Most of them empty."""
+    for dtype in ("bf16", "f16"):
+        lengths = [0] * 700
+        for i in (3, 4, 299, 699):
+            lengths[i] = 70 + i % 7
+        Call(P, lengths, 2, 1, 64, dtype, behind=1).check()
 
 
 def test_a_scale_of_its_own(P):
