@@ -603,7 +603,8 @@ typedef struct pos_norm {
  * Forward pass.  d_res may be NULL (h = dropout(x)).  Each output may be NULL: h, y,
  * the checkpoints (16-byte aligned) of h, which the backward pass can read in h's
  * place, and of y, which poseidon_ckpt_wgrad reads (both as poseidon_ckpt_pack makes
- * them of the tensor written), rstd [rows] (r).  h may be d_res and y may be x
+ * them of the tensor written), rstd [rows] (r).  y is h r w rounded once to 32 bits,
+ * but for the sum of the squares, and then to its type.  h may be d_res and y may be x
  * itself (the same pointers and strides); other overlaps are not allowed.
  * Errors: POS_EINVAL (NULL, sizes, strides, dtypes, format, eps, p, alignment),
  * POS_ECUDA.

@@ -4,10 +4,26 @@
 
 namespace pos {
 
+// r = 1 / sqrt(s / cols + eps) as rsqrtf's result and a step of Newton's method from it.
+__device__ __forceinline__ Double32 rstd_of(const NormParams &p, Double32 s) {
+    const float m = __fmul_rn(s.hi, p.inv_cols), v = m + p.eps, c = v - m;
+    const float rest = ((m - (v - c)) + (p.eps - c)) + fmaf(s.hi, p.inv_cols, -m) +
+                       fmaf(s.hi, p.inv_cols_lo, s.lo * p.inv_cols);  // v's own
+    const float r = rsqrtf(v), t = __fmul_rn(v, r);
+    const float e = fmaf(-fmaf(rest, r, fmaf(v, r, -t)), r, fmaf(-t, r, 1.f));  // 1 - v r^2
+    return {r, fabsf(e) < 0.001f ? 0.5f * r * e : 0.f};  // (r of 0 and infinity as it is)
+}
+
 // A team takes a row at a time and holds it in registers, so that every matrix goes
 // through HBM once; the next rows are on their way meanwhile (RING; without it rows are
 // read in place, from any alignment).  h is rounded to its type before it is squared,
 // kept or normalised: what the backward pass reads is what the forward pass used.
+//   The sum over a row's threads, r and h r w carry their roundings along in a second f32,
+// so that y is rounded once, as if it had been computed in more bits.  Without that one in
+// 130,000 bf16 values (15,000 in f16) is on the other side of a rounding border, and with
+// them 8-bit codes that have a border there too.  It costs 12 of 123 us for 16384 x 4096
+// bf16 with both checkpoints, where instructions bound; 16384 x 8192 with an f32 stream takes
+// 283 us with the integer sums, 297 without.
 template <typename T, typename H, class TEAM, bool RING>
 __global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_forward_kernel(const NormParams p) {
     grid_dep_wait();
@@ -34,6 +50,11 @@ __global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_forward_kernel(co
     Vec8 w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) w[i] = load_w(p, rank + i * step);
+    bool plain = false;  // weights that are not finite: an infinity is not to become a NaN
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) plain = plain || !isfinite(w[i].v[e]);
     int turn = 0, slot = 0;
     const int64_t first = (int64_t)blockIdx.x * TEAM::teams() + TEAM::index();
     if constexpr (RING)
@@ -91,16 +112,32 @@ __global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_forward_kernel(co
             }
             if (++slot == p.depth) slot = 0;
         }
-        const float rstd = rsqrtf(TEAM::sum(squares.x + squares.y, shared, turn) * p.inv_cols + p.eps);
-        if (p.rstd && rank == 0) p.rstd[r] = rstd;
+        const Double32 rstd =
+            rstd_of(p, TEAM::sum_positive(squares.x + squares.y, shared, turn));
+        if (p.rstd && rank == 0) p.rstd[r] = rstd.hi + rstd.lo;
+        // h of 16 bits has at most 11, so with 13 of r their product is exact
+        const float r_hi = kH == 2 ? rstd.hi : __uint_as_float(__float_as_uint(rstd.hi) & ~0x7ffu);
+        const float r_lo = kH == 2 ? rstd.lo : (rstd.hi - r_hi) + rstd.lo;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (!p.y && !p.codes_y) break;
             const int j = rank + i * step;
             Vec8 v = to_float(hr[i]);
+            // (past the last column 0, or NaN with the whole group)
+            if (plain) {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2)  // (past the last column 0, or NaN with the whole group)
-                set_pair(v, e, mul2(mul2(pair(v, e), both(rstd)), pair(w[i], e)));
+                for (int e = 0; e < 8; e += 2)
+                    set_pair(v, e, mul2(mul2(pair(v, e), both(rstd.hi + rstd.lo)), pair(w[i], e)));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const F2 x = pair(v, e), n = mul2(x, both(r_hi));
+                    F2 rest = mul2(x, both(r_lo));
+                    if constexpr (kH == 2)
+                        rest = fma2(x, both(r_lo), fma2(x, both(r_hi), {-n.x, -n.y}));
+                    set_pair(v, e, fma2(n, pair(w[i], e), mul2(rest, pair(w[i], e))));
+                }
+            }
             const Raw8<T> y = from_float<T>(v);
             T *to = static_cast<T *>(p.y) + r * p.ldy;
             if constexpr (RING && kX == 2) {
@@ -139,6 +176,7 @@ pos_status check_norm(const pos_norm *n, NormParams *p) {
     p->pitch = s.pitch, p->spitch = s.spitch;
     p->rows = n->rows, p->cols = n->cols, p->format = n->format;
     p->eps = n->eps, p->inv_cols = 1.f / n->cols;
+    p->inv_cols_lo = (float)(1. / n->cols - p->inv_cols);
     p->w = n->w, p->w_vectors = aligned16(n->w);
     return POS_OK;
 }

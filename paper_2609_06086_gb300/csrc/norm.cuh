@@ -21,12 +21,41 @@ struct NormParams {
     int64_t ldx, ldr, ldh, ldy, lddh_in, lddh, lddx;
     int64_t rows, pitch, spitch;
     int32_t cols, format;
-    float eps, inv_cols;
+    float eps, inv_cols, inv_cols_lo;  // 1 / cols as the sum of two
     bool w_vectors;                    // w can be read 16 bytes at a time
     bool out_aligned;                  // outputs can be written 16 bytes at a time
     int32_t depth;                     // rows on their way to shared memory
     DropParams drop;
 };
+
+// A number as the sum of two f32, of which the second is small.
+struct Double32 {
+    float hi, lo;
+};
+// Sums over a warp, in each of its lanes: as whole numbers of 2^-26 (2^-25 with signs)
+// of the largest one's power of two, so that the warp's integer sums do in two steps
+// what takes five exchanges of floats, and nothing is rounded after that.
+__device__ __forceinline__ Double32 warp_sum_positive(float v) {
+    const uint32_t big = __reduce_max_sync(0xffffffffu, __float_as_uint(v));
+    if (big >= 0x7f800000u) return {__uint_as_float(big), 0.f};  // an infinity or a NaN
+    const uint32_t e = max(big >> 23, 27u);
+    const uint32_t total = __reduce_add_sync(
+        0xffffffffu, __float2uint_rn(v * __uint_as_float((280u - e) << 23)));
+    const float undo = __uint_as_float((e - 26u) << 23);
+    return {(float)(total & ~255u) * undo, (float)(total & 255u) * undo};
+}
+__device__ __forceinline__ float warp_sum(float v) {
+    const uint32_t big = __reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu);
+    if (big >= 0x7f800000u) {
+#pragma unroll
+        for (int o = 16; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return v;
+    }
+    const uint32_t e = max(big >> 23, 27u);
+    const int total = __reduce_add_sync(0xffffffffu,
+                                        __float2int_rn(v * __uint_as_float((279u - e) << 23)));
+    return (float)total * __uint_as_float((e - 25u) << 23);
+}
 
 // A row's threads: one warp with V vectors of 8 elements a thread (rows of 8 W of
 // them share a block), or a whole block.  M: the most threads of a block, of which an SM
@@ -42,16 +71,21 @@ struct Team {
     // The sum over the row's threads, in each of them; `turn` alternates between
     // calls, so that one barrier a call is enough.
     static __device__ __forceinline__ float sum(float v, float (*shared)[32], int turn) {
-#pragma unroll
-        for (int o = 16; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+        v = warp_sum(v);
         if constexpr (WARP) return v;
+        return warp_sum(of_warps(v, shared, turn));
+    }
+    // The same of numbers that are not negative, as exact as the threads' own sums.
+    static __device__ __forceinline__ Double32 sum_positive(float v, float (*shared)[32], int turn) {
+        const Double32 mine = warp_sum_positive(v);
+        if constexpr (WARP) return mine;
+        return warp_sum_positive(of_warps(mine.hi + mine.lo, shared, turn));
+    }
+    static __device__ __forceinline__ float of_warps(float v, float (*shared)[32], int turn) {
         const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
         if (lane == 0) shared[turn][threadIdx.x / 32] = v;
         __syncthreads();
-        v = lane < warps ? shared[turn][lane] : 0.f;
-#pragma unroll
-        for (int o = 16; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-        return v;
+        return lane < warps ? shared[turn][lane] : 0.f;
     }
 };
 
@@ -227,8 +261,8 @@ __device__ __forceinline__ void keep8(int format, const Raw8<T> &raw, uint8_t *c
 // Threads of a block for a call, and which Team.  Up to 8192 columns a vector a thread:
 // 64 registers, so that 32 warps an SM hide one another's sums and codes; the backward pass
 // from 2056 on two, which need half as many warps to meet (16384 x 8192, stream in f32, from
-// 8 bits: 288 us, with one 340; forward of 16384 x 4096 bf16 with both checkpoints and dropout:
-// one 128 us, with two 138).
+// 8 bits: 280 us, with one 340; forward of the same with both checkpoints: one 283 us, with
+// two 291).
 struct NormShape {
     int team;     // 0..5: Team<true, 1, 256>, <false, 1, 1024>, <false, 2, 512>, <false, 4, 512>,
                   // <false, 4, 1024>, and <false, 1, 640, 2> or <false, 2, 320, 2>

@@ -245,6 +245,40 @@ def test_nan_stays_in_its_row(P):
     assert (scales[4] == 255).all() and (codes[:, cols:] == 0).all()
 
 
+@pytest.mark.parametrize("rows,cols", [(20, 100), (40, 1100), (9, 4096), (5, 5001), (3, 8192),
+                                       (2, 20001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_y_is_rounded_once(P, rows, cols, dtype):
+    """Of whole numbers, whose squares' sums are exact in 32 bits, y is the formula's value
+    rounded to f32 (or to the neighbour next to a border, by 2^-20 of a step) and then to its
+    type: r and the products come with their roundings, so 2^-45 of a value is all else."""
+    values = np.random.default_rng(cols).integers(-8, 9, (rows, cols)).astype(float)
+    c = Call(P, rows, cols, dtype, dtype, "int8", add=False, x=values)
+    c.forward()
+    want = values / np.sqrt((values * values).mean(1, keepdims=True) + np.float32(EPS)) * f64(c.w)
+    if dtype == "f32":
+        assert (np.abs(f64(c.y) - want) <= F32 * (1 + 2.0 ** -20) * np.abs(want)).all()
+    else:
+        assert torch.equal(c.y, torch.from_numpy(want).float().to(U.DTYPES[dtype]).cuda())
+
+
+def test_weights_that_are_not_finite(P):
+    """They reach their own columns as the formula has it: infinities stay infinities."""
+    for dtype in ("bf16", "f32"):
+        clean, c = (Call(P, 6, 300, dtype, dtype, "int8") for _ in range(2))
+        c.w[7], c.w[150] = np.inf, np.nan
+        clean.forward()
+        c.forward()
+        sign = f64(clean.h)[:, 7]
+        assert (f64(c.y)[:, 7] == np.where(sign > 0, np.inf, -np.inf)).all()
+        assert c.y[:, 150].isnan().all()
+        rest = np.ones(300, bool)
+        rest[[7, 150]] = False
+        # beside them in a thread's columns, y has two more roundings of 32 bits
+        a, b = f64(c.y)[:, rest], f64(clean.y)[:, rest]
+        assert (np.abs(a - b) <= (2 * U.ROUND[dtype] + 4 * F32) * np.abs(b)).all()
+
+
 def test_gradients_against_differences(P):
     """dx, dh and dw in f32 against central differences of the formula in 64 bits, whose own
     error is of the order of step^2."""
