@@ -206,7 +206,7 @@ __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, int
     }
 }
 // d (+)= A B, A [128][128] in TMEM, `part` columns of it one after another and then as many
-// unused, B the rows of a tile, 16 `steps` columns of it.
+// unused or with the rests of those (pack2_rest), B the rows of a tile, 16 `steps` columns of it.
 template <typename T, int PART = kTile>
 __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b, int steps, bool add,
                                             uint32_t mine) {
@@ -369,6 +369,14 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+// What pack2 cut off, in 16 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2_rest(uint32_t packed, float lo, float hi) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        return pack2<T>(lo - __uint_as_float(packed << 16), hi - __uint_as_float(packed & 0xffff0000u));
+    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&packed));
+    return pack2<T>(lo - v.x, hi - v.y);
 }
 // Results on their way out: a thread's 16 columns from c on of a row, into a tile of
 // shared memory (256 bytes a row, pieces of 16 bytes exchanged so that neither side's

@@ -80,6 +80,12 @@ __device__ __forceinline__ void row_stats(const AttnParams &p, const AttnUnit &u
     }
 }
 
+// Sequences of one tile: their P and dS go into the products as two 16-bit values each, so
+// that only the results are rounded.  (Rounded once, they add as much to the error as the
+// results' own rounding does, 1.4 times that in all; in a few short rows it was up to 2.1.
+// 8192 tokens of 32 + 8 heads of 128 in 80 sequences: both passes 436 us, with one value 417.)
+__device__ __forceinline__ bool one_tile(const AttnUnit &u) { return u.len <= kTile; }
+
 __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
     asm volatile("barrier.sync 1, %0;" ::"n"(128 * kSumGroups) : "memory");
 }
@@ -223,6 +229,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             int it = 0;  // steps so far
             while (ok && w.next(p, round)) {
                 const int n = w.u.tile + 1, base = it;
+                const bool fine = one_tile(w.u);
                 const auto scores = [&](int i) {
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
                     if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, sh)) return false;
@@ -254,11 +261,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     tmem_after();
                     // (the unit before has been read: its warps have gone on to this one)
                     mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
+                    if (fine) mma_columns<T, kCols>(pk_tm, tmem + kCols / 2, at, steps, true, mine);
                     if (i + 1 < n) ok = scores(i + 1);
                     ok = ok && wait_warp(ds_full, it & 1, sh);
                     if (!ok) break;
                     tmem_after();
                     mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
+                    if (fine) mma_columns<T, kCols>(dq_tm, dp_tm + kCols / 2, at, steps, true, mine);
                     commit(k_empty + 8 * (it % kKeySlots), mine);
                     if (i == n - 1) commit(dq_full, mine);
                     else ok = grads(i + 1);
@@ -277,7 +286,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         for (; !sh->stop && w.next(p, round); ++units) {
             const AttnUnit &u = w.u;
             const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
-            const bool live = row < u.len;
+            const bool live = row < u.len, fine = one_tile(u);
             row_stats<T>(p, u, head, stats, sh->largest + units % 2);
             sums_barrier();
             const float2 st = stats[mine];
@@ -313,6 +322,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 for (int c = 0; c < kCols; c += 2)
                     w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
                 tmem_store16(s_tm, w);
+                if (fine) {
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 2)
+                        w[c / 2] = pack2_rest<T>(w[c / 2], __uint_as_float(s[c]),
+                                                 __uint_as_float(s[c + 1]));
+                    tmem_store16(s_tm + kCols / 2, w);
+                }
                 tmem_wait_stores();
                 tmem_before();
                 __syncwarp();
@@ -339,6 +355,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
                 }
                 tmem_store16(d_tm, w);
+                if (fine) {
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 2)
+                        w[c / 2] = pack2_rest<T>(w[c / 2], __uint_as_float(d[c]),
+                                                 __uint_as_float(d[c + 1]));
+                    tmem_store16(d_tm + kCols / 2, w);
+                }
                 tmem_wait_stores();
                 tmem_before();
                 __syncwarp();
@@ -528,6 +551,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         each = steps.each, step0 = steps.first, n = steps.n;
     }
     const int boxes = p.dim > 64 ? 2 : 1;
+    const bool fine = n > 0 && one_tile(u);
     bool ok = true;
 
     if (group == kSumGroups) {
@@ -590,12 +614,18 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dv_tm, tmem, g_at + s * kTileBytes, steps, i > 0, mine);
+                if (fine)
+                    mma_columns<T, kCols>(dv_tm, tmem + kCols / 2, g_at + s * kTileBytes, steps, true,
+                                          mine);
                 commit(g_empty + 8 * s, mine);
                 if (i + 1 < n) ok = scores(i + 1);
                 ok = ok && wait_warp(ds_full, i & 1, sh);
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dk_tm, dp_tm, q_at + s * kTileBytes, steps, i > 0, mine);
+                if (fine)
+                    mma_columns<T, kCols>(dk_tm, dp_tm + kCols / 2, q_at + s * kTileBytes, steps, true,
+                                          mine);
                 commit(q_empty + 8 * s, mine);
                 if (i == n - 1) commit(out_full, mine);
                 if (i + 1 < n) ok = grads(i + 1);
@@ -667,6 +697,12 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             for (int c = 0; c < kCols; c += 2)
                 w[c / 2] = pack2<T>(__uint_as_float(s[c]), __uint_as_float(s[c + 1]));
             tmem_store_block(s_tm, w);
+            if (fine) {
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2)
+                    w[c / 2] = pack2_rest<T>(w[c / 2], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                tmem_store_block(s_tm + kCols / 2, w);
+            }
             tmem_wait_stores();
             tmem_before();
             __syncwarp();
@@ -695,6 +731,12 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             for (int c = 0; c < kCols; c += 2)
                 w[c / 2] = pack2<T>(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
             tmem_store_block(d_tm, w);
+            if (fine) {
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2)
+                    w[c / 2] = pack2_rest<T>(w[c / 2], __uint_as_float(d[c]), __uint_as_float(d[c + 1]));
+                tmem_store_block(d_tm + kCols / 2, w);
+            }
             tmem_wait_stores();
             tmem_before();
             __syncwarp();

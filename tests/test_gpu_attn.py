@@ -174,10 +174,12 @@ class Call:
             e = D - guess
             e[0] = 0
             rest = p * 1.01 * (dp_off + D_off) + (step_ds + FLUSH * (1 + (dp - D).abs())) * seen
-            ds_off = (u + 1.01 * off + 4 * F32) * ds.abs() + rest
-            p_off = (u + 1.01 * off) * p + (step_p + FLUSH) * seen
+            # one rounding; of one tile, what a second value of 16 bits leaves
+            inner = u if n > 128 else u * u
+            ds_off = (inner + 1.01 * off + 4 * F32) * ds.abs() + rest
+            p_off = (inner + 1.01 * off) * p + (step_p + FLUSH) * seen
             # dq = (p (dp - guess)) k - e p k
-            q_off = (u + 1.01 * off + 4 * F32) * first.abs() + rest + e.abs() * p_off + \
+            q_off = (inner + 1.01 * off + 4 * F32) * first.abs() + rest + e.abs() * p_off + \
                 (n + 2) * CUT * (first.abs() + e.abs() * p)
             out[0][a:b, h] = self.scale * ds @ K
             tol[0][a:b, h] = self.scale * q_off @ K.abs()
