@@ -121,10 +121,12 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, AttnSha
     if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
     return __all_sync(0xffffffffu, attn_wait(bar, parity, sh));
 }
-// By a warp, the rows of a mask again (row(i) does the i-th).
+// By a warp, the rows of a mask again (row(i) does the i-th).  What its lanes stored of
+// them before comes first: votes and shuffles alone order no memory.
 template <typename F>
 __device__ __forceinline__ void do_again(uint32_t rows, AttnShared *sh, F row) {
     if (!rows) return;
+    __syncwarp();
     if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), 1);
     for (; rows; rows &= rows - 1) row(__ffs(rows) - 1);
     __syncwarp();
