@@ -1,5 +1,7 @@
 // poseidon_attn_forward, and what both passes of attention share on the host
 // (formulas: poseidon.h).
+#include <cstdlib>
+
 #include "attn.cuh"
 
 namespace pos {
@@ -181,6 +183,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                    o_full = p_full + 16, q_empty = o_full + 16;
     const uint32_t slot = q_empty + 16;
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
+    const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -219,7 +222,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             uint32_t ph = 1, q_ph[2] = {1, 1};  // an empty slot's first wait passes
             while (lane == 0 && ok && w.next(p, round)) {
                 const auto load = [&](bool v, int j) {
-                    if (!attn_wait(kv_empty + 8 * s, ph, sh)) return false;
+                    if (!attn_wait(kv_empty + 8 * s, ph, waits)) return false;
                     bar_expect(kv_full + 8 * s, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
                         tma_rows(kv_at + s * kTileBytes + b * kBox, v ? &v_map : &k_map, 64 * b,
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     if (!ok || (t && !w.n1)) break;
-                    ok = attn_wait(q_empty + 8 * t, q_ph[t], sh);
+                    ok = attn_wait(q_empty + 8 * t, q_ph[t], waits);
                     if (!ok) break;
                     q_ph[t] ^= 1;
                     bar_expect(q_full + 8 * t, boxes * kBox);
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 // the i-th tile to arrive: keys 2 i, values 2 i + 1
                 const auto arrived = [&](int i) {
                     return wait_warp(kv_full + 8 * ((base + i) % kSlots), (base + i) / kSlots & 1,
-                                     sh);
+                                     waits);
                 };
                 const auto place = [&](int i) { return kv_at + (base + i) % kSlots * kTileBytes; };
                 const auto scores = [&](int t, int i) {  // i: steps of keys from the first on
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (ok && (t == 0 || w.n1)) {
-                        ok = wait_warp(q_full + 8 * t, q_ph[t], sh);
+                        ok = wait_warp(q_full + 8 * t, q_ph[t], waits);
                         q_ph[t] ^= 1;
                     }
                 if (!ok) break;
@@ -281,7 +284,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     for (int t = 0; t < 2; ++t) {
                         const int n = t ? w.n1 : w.n0;
                         if (j < n && ok) {
-                            ok = wait_warp(p_full + 8 * t, ph[t], sh);
+                            ok = wait_warp(p_full + 8 * t, ph[t], waits);
                             if (!ok) break;
                             ph[t] ^= 1;
                             tmem_after();
@@ -307,13 +310,13 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
         const uint32_t s_tm = tmem + t * kTile + lanes, o_tm = tmem + 2 * kTile + t * kTile + lanes;
         const int dim16 = (p.dim + 15) / 16 * 16;
         uint32_t ph = 0, o_ph = 0;
-        while (ok && w.next(p, round)) {
+        while (w.next(p, round)) {
             const int n = t ? w.n1 : w.n0;
             if (n == 0) continue;
             const int row = w.r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
             float top = 0.f, total = 0.f;
             for (int j = n - 1; j >= 0 && ok; --j) {
-                ok = wait_warp(s_full + 8 * t, ph, sh);
+                ok = wait_warp(s_full + 8 * t, ph, waits);
                 if (!ok) break;
                 ph ^= 1;
                 tmem_after();
@@ -378,7 +381,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full + 8 * t);
             }
-            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, sh);
+            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, waits);
             o_ph ^= 1;
             tmem_after();
             const bool live = row < w.u.len;
@@ -422,6 +425,16 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+// How long a wait lasts: two seconds, or POSEIDON_ATTN_WAIT_NS as the process has it when
+// it makes its first call.
+static uint64_t wait_limit_ns() {
+    static const uint64_t ns = [] {
+        const char *v = std::getenv("POSEIDON_ATTN_WAIT_NS");
+        return v && *v ? std::strtoull(v, nullptr, 10) : kWaitNs;
+    }();
+    return ns;
+}
+
 pos_status check_attn(const pos_attn *a, AttnParams *p) {
     if (!a) return fail(POS_EINVAL, "attention: NULL pointer");
     if (a->tokens < 0 || a->tokens >= (1ll << 31) - 2 * kForwardRows)
@@ -443,6 +456,7 @@ pos_status check_attn(const pos_attn *a, AttnParams *p) {
     p->group = a->heads_k ? a->heads_q / a->heads_k : 1;
     p->dim = (a->dim + 7) / 8 * 8, p->dim_out = a->dim;
     p->scale = a->scale, p->scale2 = a->scale * kLog2e;
+    p->wait_ns = wait_limit_ns(), p->try_ns = (uint32_t)std::min<uint64_t>(kTryNs, p->wait_ns);
     return POS_OK;
 }
 

@@ -39,6 +39,8 @@ struct AttnParams {
     int32_t dim_out;            // elements of a row that are written
     bool out_vectors, d_vectors[3];  // rows that can be written 16 bytes at a time
     float scale, scale2;        // scale2 = scale * log2(e)
+    uint64_t wait_ns;           // how long a wait lasts, and a try of it
+    uint32_t try_ns;
 };
 
 // A tile of queries or keys: the first token of its sequence, the sequence's
@@ -87,39 +89,48 @@ struct BlockUnit {
 // What a block's warps share besides tiles and barriers.
 struct AttnShared {
     uint32_t tmem;
-    volatile int gave_up, again, stop;  // a wait did; warps that do rows again; a block's units end
+    volatile int gave_up, again;        // a wait did; warps that do rows again
     uint32_t bad[4];                    // rows to do again
     uint32_t largest[2];                // of dO, units in turn
 };
 constexpr int kSharedBytes = 48;
 static_assert(sizeof(AttnShared) <= kSharedBytes, "room for it");
 __device__ __forceinline__ void init_shared(AttnShared *sh) {
-    sh->gave_up = sh->again = sh->stop = 0;
+    sh->gave_up = sh->again = 0;
     for (int i = 0; i < 4; ++i) sh->bad[i] = 0;
     sh->largest[0] = sh->largest[1] = 0;
 }
 // Waits for a phase, two seconds at most (WaitLimit), not counting time in which the
-// block does rows again: a long row takes a warp milliseconds.
-__device__ __forceinline__ bool attn_wait_long(uint32_t bar, uint32_t parity, AttnShared *sh) {
+// block does rows again: a long row takes a warp milliseconds.  Where one ran out, the warps
+// that write results go on through the rest of the block's units without waiting, and make
+// theirs NaN: what was in memory is not to pass for a result.
+struct Waits {
+    AttnShared *sh;
+    uint64_t ns;
+    uint32_t try_ns;
+    __device__ __forceinline__ Waits(AttnShared *sh, const AttnParams &p)
+        : sh(sh), ns(p.wait_ns), try_ns(p.try_ns) {}
+};
+__device__ __forceinline__ bool attn_wait_long(uint32_t bar, uint32_t parity, const Waits &w) {
     WaitLimit limit(now_ns());
     for (;;) {
-        if (bar_try(bar, parity)) return true;
-        if (sh->gave_up) return false;
-        if (sh->again) limit = WaitLimit(now_ns());
-        if (limit.reached(now_ns())) {
-            sh->gave_up = 1;
+        if (bar_try(bar, parity, w.try_ns)) return true;
+        if (w.sh->gave_up) return false;
+        if (w.sh->again) limit = WaitLimit(now_ns());
+        if (w.ns == 0 || limit.reached(now_ns(), w.ns)) {
+            w.sh->gave_up = 1;
             return false;
         }
     }
 }
-__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, AttnShared *sh) {
-    if (bar_try(bar, parity)) return true;
-    return attn_wait_long(bar, parity, sh);
+__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, const Waits &w) {
+    if (bar_try(bar, parity, w.try_ns)) return true;
+    return attn_wait_long(bar, parity, w);
 }
 // A wait of a whole warp: all lanes go on or none does.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, AttnShared *sh) {
-    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-    return __all_sync(0xffffffffu, attn_wait(bar, parity, sh));
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Waits &w) {
+    if (__all_sync(0xffffffffu, bar_try(bar, parity, w.try_ns))) return true;
+    return __all_sync(0xffffffffu, attn_wait(bar, parity, w));
 }
 // By a warp, the rows of a mask again (row(i) does the i-th).  What its lanes stored of
 // them before comes first: votes and shuffles alone order no memory.

@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
     // rows' statistics, and the parts of e
     float2 *stats = reinterpret_cast<float2 *>(aligned + (slot - base) + kSharedBytes);
+    const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const auto load = [&](uint32_t full, uint32_t empty, uint32_t at,
                                       const CUtensorMap *map, int &s, uint32_t &ph, int slots,
                                       int j) {
-                    if (!attn_wait(empty + 8 * s, ph, sh)) return false;
+                    if (!attn_wait(empty + 8 * s, ph, waits)) return false;
                     bar_expect(full + 8 * s, boxes * kBox);
                     for (int b = 0; b < boxes; ++b)
                         tma_rows(at + s * kTileBytes + b * kBox, map, 64 * b, w.head / p.group,
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (i < n)
                         ok = load(k_full, k_empty, k_at, &k_map, sk, phk, kKeySlots, n - 1 - i);
                     if (i == 0 && ok) {
-                        ok = attn_wait(in_empty, ph, sh);
+                        ok = attn_wait(in_empty, ph, waits);
                         if (!ok) break;
                         ph ^= 1;
                         bar_expect(in_full, 2 * boxes * kBox);
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const bool fine = one_tile(w.u);
                 const auto scores = [&](int i) {
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
-                    if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, sh)) return false;
+                    if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, waits)) return false;
                     const uint32_t at = k_at + slot_i * kTileBytes;
                     const int seen = w.u.len - (n - 1 - i) * kTile;
                     if (seen < kTile) zero_rows(at, seen, boxes, lane);
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 };
                 const auto grads = [&](int i) {  // dP
                     const int at_i = base + i, slot_i = at_i % kValueSlots;
-                    if (!wait_warp(v_full + 8 * slot_i, at_i / kValueSlots & 1, sh))
+                    if (!wait_warp(v_full + 8 * slot_i, at_i / kValueSlots & 1, waits))
                         return false;
                     mma_rows<T>(dp_tm, g_at, v_at + slot_i * kTileBytes, steps, mine);
                     commit(dp_full, mine);
@@ -250,20 +251,20 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (i == n - 1) commit(in_empty, mine);  // the last ones
                     return true;
                 };
-                ok = wait_warp(in_full, ph, sh);
+                ok = wait_warp(in_full, ph, waits);
                 ph ^= 1;
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
                 for (int i = 0; i < n && ok; ++i, ++it) {
                     const uint32_t at = k_at + it % kKeySlots * kTileBytes;
-                    ok = wait_warp(p_full, it & 1, sh);
+                    ok = wait_warp(p_full, it & 1, waits);
                     if (!ok) break;
                     tmem_after();
                     // (the unit before has been read: its warps have gone on to this one)
                     mma_columns<T, kCols>(pk_tm, tmem, at, steps, i > 0, mine);
                     if (fine) mma_columns<T, kCols>(pk_tm, tmem + kCols / 2, at, steps, true, mine);
                     if (i + 1 < n) ok = scores(i + 1);
-                    ok = ok && wait_warp(ds_full, it & 1, sh);
+                    ok = ok && wait_warp(ds_full, it & 1, waits);
                     if (!ok) break;
                     tmem_after();
                     mma_columns<T, kCols>(dq_tm, dp_tm, at, steps, i > 0, mine);
@@ -281,9 +282,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
         int it = 0, units = 0;
-        // The warps meet at barriers, so they end together: not where a wait of one gave up,
-        // but after the unit in which a thread saw it for all.
-        for (; !sh->stop && w.next(p, round); ++units) {
+        // The warps meet at barriers, so they end together, whether a wait of one gave up or not.
+        for (; w.next(p, round); ++units) {
             const AttnUnit &u = w.u;
             const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
             const bool live = row < u.len, fine = one_tile(u);
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
             F2 rest = both(0.f);  // e, of this part of the columns
             for (int i = 0; i < n; ++i, ++it) {
-                ok = ok && wait_warp(s_full, it & 1, sh);
+                ok = ok && wait_warp(s_full, it & 1, waits);
                 if (!ok) break;
                 tmem_after();
                 uint32_t s[kCols], d[kCols], w[kCols / 2];
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 tmem_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full);
-                ok = wait_warp(dp_full, it & 1, sh);
+                ok = wait_warp(dp_full, it & 1, waits);
                 if (!ok) break;
                 tmem_after();
                 tmem_load32(d_tm, d);
@@ -367,11 +367,11 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(ds_full);
             }
-            if (ok) ok = wait_warp(dq_full, units & 1, sh);
+            if (ok) ok = wait_warp(dq_full, units & 1, waits);
             tmem_after();
             // e's parts through the place of the stats, which every warp has read
             float *parts = reinterpret_cast<float *>(stats);
-            float e = rest.x + rest.y;
+            float e = ok ? rest.x + rest.y : __uint_as_float(0x7fffffffu);  // (no result)
             if (side >= 2) parts[(side - 2) * kTile + mine] = e;
             sums_barrier();
             if (side < 2) parts[side * kTile + mine] += e;
@@ -405,7 +405,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
             const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
             if (lane == 0 && again) atomicOr(sh->bad + warp % 4, again);
-            if (threadIdx.x == 0) sh->stop = sh->gave_up;
             sums_barrier();
             if (side == 0) {
                 const uint32_t rows = ok && !sh->gave_up ? sh->bad[warp] : 0;
@@ -517,6 +516,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, out_full = ds_full + 8;
     const uint32_t slot = out_full + 8;
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
+    const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     const int token = u.start + (u.tile + (step0 + i) % each) * kTile;
                     for (int w = 0; w < 2 && ok; ++w) {
                         const uint32_t full = (w ? g_full : q_full) + 8 * s;
-                        ok = attn_wait((w ? g_empty : q_empty) + 8 * s, ph, sh);
+                        ok = attn_wait((w ? g_empty : q_empty) + 8 * s, ph, waits);
                         if (!ok) break;
                         bar_expect(full, boxes * kBox);
                         for (int b = 0; b < boxes; ++b)
@@ -586,7 +586,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             const int steps = (p.dim + 15) / 16;
             const auto arrived = [&](uint32_t full, uint32_t at, int i) {
                 const int s = i % kQuerySlots;
-                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, sh)) return false;
+                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, waits)) return false;
                 const int seen = u.len - (u.tile + (step0 + i) % each) * kTile;
                 if (seen < kTile) zero_rows(at + s * kTileBytes, seen, boxes, lane);
                 return true;
@@ -604,13 +604,13 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 return true;
             };
             if (n > 0) {
-                ok = wait_warp(in_full, 0, sh);
+                ok = wait_warp(in_full, 0, waits);
                 tmem_after();
                 ok = ok && scores(0) && grads(0);
             }
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kQuerySlots;
-                ok = wait_warp(p_full, i & 1, sh);
+                ok = wait_warp(p_full, i & 1, waits);
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dv_tm, tmem, g_at + s * kTileBytes, steps, i > 0, mine);
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                                           mine);
                 commit(g_empty + 8 * s, mine);
                 if (i + 1 < n) ok = scores(i + 1);
-                ok = ok && wait_warp(ds_full, i & 1, sh);
+                ok = ok && wait_warp(ds_full, i & 1, waits);
                 if (!ok) break;
                 tmem_after();
                 mma_columns<T, kCols>(dk_tm, dp_tm, q_at + s * kTileBytes, steps, i > 0, mine);
@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     st[h] = row + lane + 32 * h < u.len
                                 ? from[lane + 32 * h]
                                 : make_float2(__uint_as_float(0x7f800000u), 0.f);
-                ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, sh);
+                ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, waits);
                 if (!ok) break;
 #pragma unroll
                 for (int h = 0; h < 4; ++h)  // -lse in the first half, -D in the second
@@ -671,8 +671,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         for (int i = 0; i < n; ++i) {
             const int slot_i = i % kQuerySlots;
             const uint32_t st = st_at + slot_i * kStatBytes + 4 * query;
-            ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, sh) &&
-                 wait_warp(s_full, i & 1, sh);
+            ok = ok && wait_warp(st_full + 8 * slot_i, i / kQuerySlots & 1, waits) &&
+                 wait_warp(s_full, i & 1, waits);
             if (!ok) break;
             tmem_after();
             uint32_t s[kCols], d[kCols], w[kCols / 2];
@@ -709,7 +709,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             if (lane == 0) bar_arrive(p_full);
 #pragma unroll
             for (int b = 0; b < kCols / 8; ++b) l[b] = load_stats(st + 512 + 32 * b);
-            ok = wait_warp(dp_full, i & 1, sh);
+            ok = wait_warp(dp_full, i & 1, waits);
             if (!ok) break;
             tmem_after();
             tmem_load_block(d_tm, d);
@@ -746,7 +746,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
         }
         if (n > 0) {
-            if (ok) ok = wait_warp(out_full, 0, sh);
+            if (ok) ok = wait_warp(out_full, 0, waits);
             tmem_after();
         }
         const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
@@ -755,7 +755,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                     uint32_t v[16];
                     tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
-                    if (!ok) v[0] = 0x7fffffffu;
+#pragma unroll
+                    for (int h = 0; h < 16; ++h) v[h] = ok ? v[h] : 0x7fffffffu;
 #pragma unroll
                     for (int h = 0; h < 16; h += 4)
                         *part_at(p, blockIdx.x, t, c + h, mine) =

@@ -23,14 +23,15 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                  : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+constexpr uint32_t kTryNs = 1000000;  // a try sleeps for up to 1 ms
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity, uint32_t sleep = kTryNs) {
     uint32_t ok;
     asm volatile(
         "{\n.reg .pred p;\n"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
         "selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(1000000)  // sleeps for up to 1 ms
+        : "r"(bar), "r"(parity), "r"(sleep)
         : "memory");
     return ok;
 }

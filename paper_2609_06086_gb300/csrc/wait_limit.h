@@ -20,11 +20,11 @@ struct WaitLimit {
     uint64_t last, spent;
     explicit POS_HD WaitLimit(uint64_t now) : last(now), spent(0) {}
     // Called after a try that failed: whether the wait is over.
-    POS_HD bool reached(uint64_t now) {
+    POS_HD bool reached(uint64_t now, uint64_t most = kWaitNs) {
         const uint64_t gap = now - last;
         last = now;
         spent += gap < kWaitGapNs ? gap : kWaitGapNs;
-        return spent > kWaitNs;
+        return spent > most;
     }
 };
 
