@@ -109,52 +109,25 @@ __global__ void __launch_bounds__(256) attn_copy_kernel(const T *x, int64_t toke
 // tensor cores work on one tile while the other's exponentials are computed.  Keys
 // go from the diagonal down, so the first tile is the one with a mask and no row's
 // largest score is ever of nothing.  A block takes one such unit after another, so that a
-// unit's first loads and scores come while the one before it ends.
+// unit's first loads and scores come while the one before it ends.  Two warps look over the
+// values of the tiles on the diagonal, half a tile each, while the first exponentials are computed.
 constexpr int kSlots = 5;                    // tiles of keys and values on their way
 constexpr int kForwardRows = 2 * kTile;
 constexpr int kForwardThreads = 3 * 128;     // two warpgroups of rows, one of loads and products
-constexpr int kForwardBars = 2 * kSlots + 10;
-constexpr int kForwardSmem = 1024 + (2 + kSlots) * kTileBytes + 8 * kForwardBars + kSharedBytes;
+constexpr int kForwardBars = 2 * kSlots + 13;
+// and the first row of each column whose value is not finite, of two units, tiles, halves
+constexpr int kForwardSmem =
+    1024 + (2 + kSlots) * kTileBytes + 8 * kForwardBars + kSharedBytes + 8 * kAttnMaxDim;
 // 2 * 208 + 88 = 504 = 3 * 168, what the block is launched with
 constexpr int kRowRegs = 208, kIssueRegs = 88;
 // A row's reference, which its exponentials are relative to, follows its largest
 // score only when that is 2^8 times more: sums of up to 2^8 times their size have
 // the same precision, and O in TMEM is rescaled that much more rarely.
 constexpr float kSlack = 8.f;
-
+// In bf16 they are 2^-8 of that besides, 1 at most, so that sums of values near the type's
+// largest do not pass f32's.
 template <typename T>
-__device__ __forceinline__ void forward_row(const AttnParams &p, const AttnUnit &u, int row,
-                                            int head, int lane) {
-    const int g = head / p.group;
-    const T *q = row_at<T>(p.q, u.start + row, head);
-    float top = -__uint_as_float(0x7f800000u), total = 0.f;
-    RowPart sum = {};
-    for (int j0 = 0; j0 <= row; j0 += 32) {
-        const int j = j0 + lane, n = min(32, row + 1 - j0);
-        float s = -__uint_as_float(0x7f800000u);
-        if (j <= row) s = dot_rows(q, row_at<T>(p.k, u.start + j, g), p.dim) * p.scale2;
-        float m = s;
-        for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        m = fmaxf(m, top);
-        if (__any_sync(0xffffffffu, !(s == s))) m = __uint_as_float(0x7fffffffu);  // (passed over)
-        const float shrink = m == top ? 1.f : exp2f(top - m);
-        top = m;
-        // (scores of minus infinity alone, so far: nothing yet)
-        const float e = j <= row && m != -__uint_as_float(0x7f800000u) ? exp2f(s - m) : 0.f;
-        total *= shrink;
-#pragma unroll
-        for (int i = 0; i < kAttnMaxDim / 32; ++i) sum.v[i] *= shrink;
-        for (int t = 0; t < n; ++t) {
-            const float w = __shfl_sync(0xffffffffu, e, t);
-            total += w;
-            add_row(sum, w, row_at<T>(p.v, u.start + j0 + t, g), p.dim, lane);
-        }
-    }
-    write_row<T>(p.out, (u.start + row) * p.out_token + head * p.out_head, sum, 1.f / total,
-                 p.dim_out, lane);
-    if (p.lse && lane == 0)
-        p.lse[head * p.tokens + u.start + row] = (top + log2f(total)) * kLn2;
-}
+constexpr float kLift = std::is_same<T, __nv_bfloat16>::value ? -kSlack : 0.f;
 
 struct ForwardUnit : BlockUnit<kForwardRows> {
     int r0, n0, n1, first;  // first token; tiles of keys that its two tiles see, the last
@@ -180,16 +153,19 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
     const uint32_t bars = kv_at + kSlots * kTileBytes;
     const uint32_t kv_full = bars, kv_empty = kv_full + 8 * kSlots;
     const uint32_t q_full = kv_empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 16,
-                   o_full = p_full + 16, q_empty = o_full + 16;
-    const uint32_t slot = q_empty + 16;
+                   o_full = p_full + 16, q_empty = o_full + 16, v_in = q_empty + 16,
+                   v_out = v_in + 8;
+    const uint32_t slot = v_out + 16;
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
+    // the first row of each column's value that is not finite, of a tile's units in turn
+    uint8_t *first_bad = aligned + (slot - base) + kSharedBytes;
     const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kForwardBars; ++i) {
-            const bool rows = bars + 8 * i >= p_full && bars + 8 * i < o_full;
-            bar_init(bars + 8 * i, rows ? 4 : 1);  // p_full: a tile's four warps
+            const uint32_t b = bars + 8 * i;  // p_full: a tile's four warps
+            bar_init(b, b >= p_full && b < o_full ? 4 : b >= v_out ? 2 : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         init_shared(sh);
@@ -263,6 +239,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                     if (i == w.first) commit(q_empty + 8 * t, mine);  // the last ones
                 };
                 ok = arrived(0);
+                bar_arrive_one(v_in, mine);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (ok && (t == 0 || w.n1)) {
@@ -277,8 +254,6 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 for (int j = w.first, i = 0; j >= 0 && ok; --j, ++i) {
                     ok = arrived(2 * i + 1);
                     if (!ok) break;
-                    const int seen = w.u.len - j * kTile;
-                    if (seen < kTile) zero_rows(place(2 * i + 1), seen, boxes, lane);
                     if (j > 0) ok = arrived(2 * i + 2);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -301,6 +276,55 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 }
                 base += 2 * (w.first + 1);
             }
+        } else {
+            const int half = warp - 10;
+            uint32_t ph = 0;
+            int base = 0, units[2] = {0, 0};
+            while (ok && w.next(p, round)) {
+                const auto at_tile = [&](int t) {
+                    return first_bad + ((2 * (units[t] & 1) + t) * 2 + half) * kAttnMaxDim;
+                };
+                // t's values are the i-th tile to arrive
+                const auto look = [&](int t, int i) {
+                    ok = ok && wait_warp(kv_full + 8 * ((base + i) % kSlots), (base + i) / kSlots & 1,
+                                         waits);
+                    if (!ok) return false;
+                    const uint32_t at = kv_at + (base + i) % kSlots * kTileBytes;
+                    const int seen = min(kTile, w.u.len - ((t ? w.n1 : w.n0) - 1) * kTile);
+                    const int from = half * (kTile / 2), end = min(seen, from + kTile / 2);
+                    const bool bad = tile_bad<T>(at, from, end, boxes, lane);
+                    if (bad) {
+                        uint8_t *first = at_tile(t);
+                        for (int c = lane; c < kAttnMaxDim; c += 32) first[c] = kTile;
+                        tile_clean<T>(at, from, end, boxes, lane,
+                                      [&](int c, int row, int) { first[c] = (uint8_t)row; });
+                    }
+                    zero_rows(at, max(from, seen), from + kTile / 2, boxes, lane);
+                    tile_done();
+                    return bad;
+                };
+                // (from its first tile on, the phases of the places are this unit's)
+                ok = wait_warp(v_in, ph, waits);
+                ph ^= 1;
+                const bool second = w.n1 > 0 && look(1, 1);
+                const bool first = look(0, w.n1 > 0 ? 3 : 1);
+                if (!ok) break;
+                const auto tell = [&](int t, bool bad) {
+                    if (lane == 0) sh->bad[units[t] & 1][t][half] = bad;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(v_out + 8 * t);
+                };
+                if (w.n1) {  // the second tile's rows see all of the first one's
+                    uint8_t *to = at_tile(1), *from = at_tile(0);
+                    for (int c = lane; first && c < kAttnMaxDim; c += 32)
+                        to[c] = from[c] < kTile ? 0 : second ? to[c] : kTile;
+                    tell(1, first || second);
+                    ++units[1];
+                }
+                tell(0, first);
+                ++units[0];
+                base += 2 * (w.first + 1);
+            }
         }
         __syncwarp();
     } else {
@@ -309,12 +333,14 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + t * kTile + lanes, o_tm = tmem + 2 * kTile + t * kTile + lanes;
         const int dim16 = (p.dim + 15) / 16 * 16;
-        uint32_t ph = 0, o_ph = 0;
+        uint32_t ph = 0;
+        int unit = 0;
         while (w.next(p, round)) {
             const int n = t ? w.n1 : w.n0;
             if (n == 0) continue;
             const int row = w.r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
             float top = 0.f, total = 0.f;
+            int bad = 0;  // halves of the tile's values that hold some that are not finite
             for (int j = n - 1; j >= 0 && ok; --j) {
                 ok = wait_warp(s_full + 8 * t, ph, waits);
                 if (!ok) break;
@@ -367,7 +393,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const F2 x = fma2({__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])},
-                                          both(p.scale2), both(-top));
+                                          both(p.scale2), both(kLift<T> - top));
                         const F2 y = {exp2_fast(x.x), exp2_fast(x.y)};
                         sum[e % 4] = add2(sum[e % 4], y);
                         w[e] = pack2<T>(y.x, y.y);
@@ -378,14 +404,17 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 total += a.x + a.y;
                 tmem_wait_stores();
                 tmem_before();
+                // (the values that these are multiplied by are looked over)
+                if (j == n - 1) {
+                    ok = wait_warp(v_out + 8 * t, unit & 1, waits);
+                    bad = sh->bad[unit & 1][t][0] + 2 * sh->bad[unit & 1][t][1];
+                }
                 __syncwarp();
-                if (lane == 0) bar_arrive(p_full + 8 * t);
+                if (ok && lane == 0) bar_arrive(p_full + 8 * t);
             }
-            if (ok) ok = wait_warp(o_full + 8 * t, o_ph, waits);
-            o_ph ^= 1;
+            if (ok) ok = wait_warp(o_full + 8 * t, unit & 1, waits);
             tmem_after();
             const bool live = row < w.u.len;
-            bool good = finite(top) && finite(total);
             float factor = 1.f / total;
             if (!ok) factor = __uint_as_float(0x7fffffffu);  // a wait that gave up: no result
             T *out = static_cast<T *>(p.out) + (w.u.start + (int64_t)row) * p.out_token +
@@ -393,12 +422,18 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             for (int c = 0; c < dim16; c += 16) {
                 uint32_t o[16];
                 tmem_load16(o_tm + c, o);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    if (bad >> half & 1) {
+                        const uint8_t *first =
+                            first_bad + ((2 * (unit & 1) + t) * 2 + half) * kAttnMaxDim + c;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if ((int)(threadIdx.x % kTile) >= first[e]) o[e] = 0x7fffffffu;
+                    }
                 Vec8 x[2];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
-                    good = good && finite(__uint_as_float(o[e]));
-                }
+                for (int e = 0; e < 16; ++e) x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
                 if (!live) continue;
 #pragma unroll
                 for (int e = 0; e < 16; e += 8) {
@@ -409,10 +444,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             }
             if (p.lse && live)
                 p.lse[w.head * p.tokens + w.u.start + row] =
-                    ok ? (top + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);
-            do_again(__ballot_sync(0xffffffffu, ok && live && !good), sh, [&](int i) {
-                forward_row<T>(p, w.u, row - lane + i, w.head, lane);
-            });
+                    ok ? (top - kLift<T> + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);
+            ++unit;
         }
     }
     end_block(sh);

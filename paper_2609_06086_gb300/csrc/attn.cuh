@@ -28,8 +28,10 @@ struct AttnParams {
     int64_t d_token[3], d_head[3];
     float *lse;                 // [heads_q][tokens] or NULL
     float2 *stats;              // backward: [heads_q][tokens]: lse in powers of two, D
-    uint32_t *largest;          // backward in f16: bits of dO's largest magnitudes, of each
+    uint32_t *largest;          // backward in f16: bits of the largest |dO|^2 of a row, of each
                                 // [sequence][key head]
+    float *values;              // the largest |v|^2 of a tile, [heads_k][its first token],
+    float *most;                // and of a sequence, as `largest` is
     float *part;                // backward: sums of parts of the keys' gradients
     int32_t parts;
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
@@ -89,20 +91,19 @@ struct BlockUnit {
 // What a block's warps share besides tiles and barriers.
 struct AttnShared {
     uint32_t tmem;
-    volatile int gave_up, again;        // a wait did; warps that do rows again
-    uint32_t bad[4];                    // rows to do again
+    volatile int gave_up;               // a wait did
     uint32_t largest[2];                // of dO, units in turn
+    volatile int bad[2][2][2];          // of units in turn: see the kernels
 };
 constexpr int kSharedBytes = 48;
 static_assert(sizeof(AttnShared) <= kSharedBytes, "room for it");
 __device__ __forceinline__ void init_shared(AttnShared *sh) {
-    sh->gave_up = sh->again = 0;
-    for (int i = 0; i < 4; ++i) sh->bad[i] = 0;
+    sh->gave_up = 0;
+    for (int i = 0; i < 8; ++i) sh->bad[i / 4][i / 2 % 2][i % 2] = 0;
     sh->largest[0] = sh->largest[1] = 0;
 }
-// Waits for a phase, two seconds at most (WaitLimit), not counting time in which the
-// block does rows again: a long row takes a warp milliseconds.  Where one ran out, the warps
-// that write results go on through the rest of the block's units without waiting, and make
+// Waits for a phase, two seconds at most (WaitLimit).  Where one ran out, the warps that
+// write results go on through the rest of the block's units without waiting, and make
 // theirs NaN: what was in memory is not to pass for a result.
 struct Waits {
     AttnShared *sh;
@@ -116,7 +117,6 @@ __device__ __forceinline__ bool attn_wait_long(uint32_t bar, uint32_t parity, co
     for (;;) {
         if (bar_try(bar, parity, w.try_ns)) return true;
         if (w.sh->gave_up) return false;
-        if (w.sh->again) limit = WaitLimit(now_ns());
         if (w.ns == 0 || limit.reached(now_ns(), w.ns)) {
             w.sh->gave_up = 1;
             return false;
@@ -131,17 +131,6 @@ __device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, const W
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Waits &w) {
     if (__all_sync(0xffffffffu, bar_try(bar, parity, w.try_ns))) return true;
     return __all_sync(0xffffffffu, attn_wait(bar, parity, w));
-}
-// By a warp, the rows of a mask again (row(i) does the i-th).  What its lanes stored of
-// them before comes first: votes and shuffles alone order no memory.
-template <typename F>
-__device__ __forceinline__ void do_again(uint32_t rows, AttnShared *sh, F row) {
-    if (!rows) return;
-    __syncwarp();
-    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), 1);
-    for (; rows; rows &= rows - 1) row(__ffs(rows) - 1);
-    __syncwarp();
-    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), -1);
 }
 // The block's end.  Where a wait gave up, copies and products may still be on their way:
 // they end by themselves within microseconds.
@@ -228,6 +217,14 @@ __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b, 
     for (int k = 0; k < kTile / 16; ++k)
         mma_ts(d, a + (16 * k / PART * PART + 16 * k % PART / 2), db + k * (2048 >> 4), idesc,
                add || k > 0, mine);
+}
+// By one thread of a warp that remains together.
+__device__ __forceinline__ void bar_arrive_one(uint32_t bar, uint32_t mine) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.u32 q, %1, 0;\n"
+        "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(bar),
+        "r"(mine)
+        : "memory");
 }
 // Arrives on a barrier once the products issued so far are done.
 __device__ __forceinline__ void commit(uint32_t bar, uint32_t mine) {
@@ -421,25 +418,84 @@ __device__ __forceinline__ void write_tile(uint32_t tile, int rows, T *out, int6
         else store8<false>(out + row * token + 8 * c, r, dim_out - 8 * c);
     }
 }
-// Rows from `first` on of a tile become zeros: what belongs to another sequence, or
-// to none and may hold anything, would make a NaN of a probability of 0.
-__device__ __forceinline__ void zero_rows(uint32_t tile, int first, int boxes, int lane) {
-    for (int i = first * 8 + lane; i < kTile * 8; i += 32)
+// What a tile holds that is not finite.  A product multiplies what is masked by 0 and would
+// let a later token's infinities and NaNs into the rows before it in the tile on the
+// diagonal (rows of other tiles see all of them), and what lies behind the sequence into
+// all.  So a warp that has nothing else to do looks that tile over before its product, makes
+// zeros of what is not finite, and tells the warps of sums which rows see it; those write
+// NaNs there.  It adds up products with 0, four instructions for eight elements; where that
+// is not 0, it looks column by column.
+//   Both passes of 4096 tokens of 32 + 8 heads of 128: forward 105 -> 109 us, back 377 ->
+// 382; with an infinity in one dO back the same, in all values of all inputs 0.6 ms.  (Rows whose
+// products were not finite computed again by the formulas, one at a time by a warp: 229 ms
+// for the infinity in one dO, and with the square of the length.)
+__device__ __forceinline__ uint32_t tile_at(int row, int c) {  // 16 bytes of columns 8 c ..
+    return c / 8 * kBox + row * 128 + ((c % 8 ^ (row & 7)) << 4);
+}
+// sum += 0 x of two elements.
+template <typename T>
+__device__ __forceinline__ void add_zeros(uint32_t &sum, uint32_t x) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+    else
+        asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+}
+// By a warp: rows `first` to `end` - 1 hold something that is not finite.
+template <typename T>
+__device__ __forceinline__ bool tile_bad(uint32_t tile, int first, int end, int boxes, int lane) {
+    uint32_t sum[4] = {0, 0, 0, 0};
+    for (int b = 0; b < boxes; ++b)
+        for (int i0 = first * 8; i0 < end * 8; i0 += 8 * 32) {
+            uint4 r[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = min(i0 + 32 * k + lane, end * 8 - 1);
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(r[k].x), "=r"(r[k].y), "=r"(r[k].z), "=r"(r[k].w)
+                             : "r"(tile + b * kBox + 16 * i));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                add_zeros<T>(sum[0], r[k].x), add_zeros<T>(sum[1], r[k].y);
+                add_zeros<T>(sum[2], r[k].z), add_zeros<T>(sum[3], r[k].w);
+            }
+        }
+    // (a NaN has other bits set than a zero's sign)
+    return __any_sync(0xffffffffu, ((sum[0] | sum[1] | sum[2] | sum[3]) & 0x7fff7fffu) != 0);
+}
+// By a warp: zeros in their place, and f(column, first, last) by one lane of each column that
+// had any.
+template <typename T, typename F>
+__device__ __forceinline__ void tile_clean(uint32_t tile, int from, int end, int boxes, int lane,
+                                           F f) {
+    for (int c = lane; c < 64 * boxes; c += 32) {
+        int first = kTile, last = -1;
+        for (int row = from; row < end; ++row) {
+            const uint32_t at = tile + tile_at(row, c / 8) + 2 * (c % 8);
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+            if (f32_bits<T>(v & 0x7fffu) < 0x7f800000u) continue;
+            first = min(first, row), last = row;
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)0) : "memory");
+        }
+        if (last >= 0) f(c, first, last);
+    }
+}
+// Rows become zeros: of another sequence or none.
+__device__ __forceinline__ void zero_rows(uint32_t tile, int first, int end, int boxes, int lane) {
+    for (int i = first * 8 + lane; i < end * 8; i += 32)
         for (int b = 0; b < boxes; ++b)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + b * kBox + 16 * i),
                          "r"(0)
                          : "memory");
-    // before the tensor cores' reads
+}
+// By the warp, before it tells others: its stores before the tensor cores' reads.
+__device__ __forceinline__ void tile_done() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
 }
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < __uint_as_float(0x7f800000u); }
 
-// ---------------------------------------------------------------------------
-// One row by the formulas alone, by a warp: where a tensor-core product gave an
-// infinity or a NaN.  Those multiply what is masked by 0 and so let a later token's
-// infinities into an earlier one's row; here only what a row sees is read.
-// ---------------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ const T *row_at(const AttnTensor &t, int64_t token, int head) {
     return static_cast<const T *>(t.p) + token * t.token + head * t.head;
@@ -448,36 +504,6 @@ template <typename T>
 __device__ __forceinline__ Vec8 load_row8(const T *at) {
     return to_float(load8<true>(at, 8));
 }
-template <typename T>
-__device__ __forceinline__ float dot_rows(const T *a, const T *b, int dim) {
-    float s = 0.f;
-    for (int d = 0; d < dim; d += 8) {
-        const Vec8 x = load_row8(a + d), y = load_row8(b + d);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += x.v[e] * y.v[e];
-    }
-    return s;
-}
-// A lane's part of a row: elements lane + 32 i.
-struct RowPart {
-    float v[kAttnMaxDim / 32];
-};
-template <typename T>
-__device__ __forceinline__ void add_row(RowPart &sum, float w, const T *row, int dim, int lane) {
-#pragma unroll
-    for (int i = 0; i < kAttnMaxDim / 32; ++i)
-        if (lane + 32 * i < dim) sum.v[i] += w * static_cast<float>(row[lane + 32 * i]);
-}
-template <typename T>
-__device__ __forceinline__ void write_row(void *out, int64_t at, const RowPart &sum, float factor,
-                                          int dim, int lane, int side = -1) {
-    // (side: which of four in turn of 16 columns, or all)
-#pragma unroll
-    for (int i = 0; i < kAttnMaxDim / 32; ++i)
-        if (lane + 32 * i < dim && (side < 0 || (lane + 32 * i) / 16 % 4 == side))
-            static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
-}
-
 // ---------------------------------------------------------------------------
 // Host side (attn.cu)
 // ---------------------------------------------------------------------------

@@ -7,8 +7,8 @@ namespace pos {
 
 // Two kernels, so that every sum has one place and one order: the queries' gradients
 // by blocks that go over the keys, the keys' and values' by blocks that go over the
-// queries.  Scores and their gradients are computed in both: seven products instead of
-// the five of a single pass, which would add up the queries' gradients across blocks.
+// queries.  Scores and dP are computed in both, and P K for D (below): eight products instead
+// of the five of a single pass, which would add up the queries' gradients across blocks.
 constexpr int kSumGroups = 4;            // warpgroups of sums, a quarter of the columns each
 constexpr int kCols = kTile / kSumGroups;  // columns of a tile that a thread takes
 constexpr int kBackThreads = 128 * (kSumGroups + 1);  // and one of loads and products
@@ -18,31 +18,72 @@ constexpr int kLoadWarp = 4 * kSumGroups, kIssueWarp = kLoadWarp + 1, kStatsWarp
 
 // f16 holds probabilities of long rows and small gradients badly (below 2^-14 with
 // fewer bits, below 2^-25 not at all).  There P is multiplied by 2^12 and dS by 2^k, k the
-// same for a product's sums: the largest magnitude of dO (of the block's queries for
-// theirs, of the sequence's under the key head for the keys') becomes 2^8 to 2^9.  A dS
-// that is too large all the same gives an infinity and its rows are done again in 32 bits.
+// same for a product's sums and as large as the rows' norms allow: dP and D are at most
+// |dO| |v|, so |dS| <= 2 |dO| |v|, of which the largest (dO of the block's queries and v that
+// they see for theirs, all of the sequence's under the key head for the keys') becomes 2^14
+// to 2^15 for any values, and the smallest step of dS 2^-38 of it.
 template <typename T>
 struct Shift {
-    static constexpr float kProbs = std::is_same<T, __half>::value ? 12.f : 0.f;
+    static constexpr bool kOn = std::is_same<T, __half>::value;
+    static constexpr float kProbs = kOn ? 12.f : 0.f;
+    static constexpr float kUndoProbs = kOn ? 1.f / 4096.f : 1.f;
     float grads, undo;  // of dP - D, so that P (dP - D) has its factor; 2^-k
-    __device__ __forceinline__ explicit Shift(uint32_t big) : grads(1.f), undo(1.f) {
-        if constexpr (std::is_same<T, __half>::value) {  // big: bits of an f32
-            const int k = big ? 8 - ((int)(big >> 23) - 127) : 0;
+    // the largest |dO|^2 and |v|^2
+    __device__ __forceinline__ Shift(float d_o, float v) : grads(1.f), undo(1.f) {
+        if constexpr (kOn) {
+            // e + 127, e the exponent of the product: e + 2 k is 26 or 27
+            const uint32_t b = __float_as_uint(d_o * v) >> 23;
+            const int k = b ? 77 - (int)((b + 1) / 2) : 0;
             grads = __uint_as_float((uint32_t)(127 + k - 12) << 23);
             undo = __uint_as_float((uint32_t)(127 - k) << 23);
         }
     }
     static __device__ __forceinline__ Shift of_keys(const AttnParams &p, const AttnUnit &u, int g) {
-        return Shift(std::is_same<T, __half>::value
-                         ? p.largest[(int64_t)u.sequence * p.heads_k + g]
-                         : 0u);
+        if constexpr (!kOn) return Shift(0.f, 0.f);
+        const int64_t at = (int64_t)u.sequence * p.heads_k + g;
+        return Shift(__uint_as_float(p.largest[at]), p.most[at]);
     }
-    static constexpr float kUndoProbs = std::is_same<T, __half>::value ? 1.f / 4096.f : 1.f;
 };
 
+// f16: the largest |v|^2 of every tile and key head, rows that are not finite apart, and the
+// zeros that the queries' kernel starts from.
+template <typename T>
+__global__ void __launch_bounds__(kTile) attn_values_kernel(const AttnParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    __shared__ uint32_t warps[kTile / 32];
+    const int64_t units =
+        (int64_t)(p.tiles ? *p.n_tiles : ((int)p.tokens + kTile - 1) / kTile) * p.heads_k;
+    for (int64_t i = blockIdx.x; i < units; i += gridDim.x) {
+        AttnUnit u;
+        unit_at<kTile>(p, (int)(i / p.heads_k), u);
+        const int g = (int)(i % p.heads_k), row = u.tile * kTile + (int)threadIdx.x;
+        float sum = 0.f;
+        if (row < u.len) {
+            const T *v = row_at<T>(p.v, u.start + (int64_t)row, g);
+#pragma unroll 4
+            for (int d = 0; d < p.dim; d += 8) {
+                const Vec8 x = load_row8(v + d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += x.v[e] * x.v[e];
+            }
+        }
+        const uint32_t most =
+            __reduce_max_sync(0xffffffffu, finite(sum) ? __float_as_uint(sum) : 0u);
+        if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            p.values[g * p.tokens + u.start + (int64_t)u.tile * kTile] =
+                __uint_as_float(max(max(warps[0], warps[1]), max(warps[2], warps[3])));
+            if (u.tile == 0) p.largest[(int64_t)u.sequence * p.heads_k + g] = 0;
+        }
+        __syncthreads();
+    }
+}
+
 // Of the queries of a tile, by the 16 warps of sums: lse in powers of two (less the
-// probabilities' factor) and do . o, 16 lanes a row; f16: bits of the largest finite
-// magnitude of dO, in *largest.
+// probabilities' factor) and do . o, 16 lanes a row; f16: bits of the largest |dO|^2 of the
+// rows that are finite, in *largest.
 template <typename T>
 __device__ __forceinline__ void row_stats(const AttnParams &p, const AttnUnit &u, int head,
                                           float2 *stats, uint32_t *largest) {
@@ -63,18 +104,22 @@ __device__ __forceinline__ void row_stats(const AttnParams &p, const AttnUnit &u
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float d = 0.f;
+        float d = 0.f, size = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             d += a[k].v[e] * b[k].v[e];
-            if (finite(b[k].v[e])) big = max(big, __float_as_uint(fabsf(b[k].v[e])));
+            if (Shift<T>::kOn) size += b[k].v[e] * b[k].v[e];
         }
 #pragma unroll
-        for (int o = 8; o; o /= 2) d += __shfl_xor_sync(0xffffffffu, d, o);
+        for (int o = 8; o; o /= 2) {
+            d += __shfl_xor_sync(0xffffffffu, d, o);
+            if (Shift<T>::kOn) size += __shfl_xor_sync(0xffffffffu, size, o);
+        }
+        if (Shift<T>::kOn && finite(size)) big = max(big, __float_as_uint(size));
         if (l == 0)
             stats[threadIdx.x / 16 + 32 * k] = make_float2(lse[k] * kLog2e - Shift<T>::kProbs, d);
     }
-    if constexpr (std::is_same<T, __half>::value) {
+    if constexpr (Shift<T>::kOn) {
         big = __reduce_max_sync(0xffffffffu, big);
         if (threadIdx.x % 32 == 0 && big) atomicMax(largest, big);
     }
@@ -107,33 +152,9 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // when it is done; so it adds up P K beside dS K, and dQ = dS K - e P K.  The keys'
 // gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
-constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 7;
+constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 10;
 constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars +
                         kSharedBytes + kTile * 8;
-
-template <typename T>
-__device__ __forceinline__ void dq_row(const AttnParams &p, const AttnUnit &u, int row, int head,
-                                       int lane) {
-    const int g = head / p.group;
-    const T *q = row_at<T>(p.q, u.start + row, head), *dy = row_at<T>(p.g, u.start + row, head);
-    const float2 st = p.stats[head * p.tokens + u.start + row];
-    RowPart sum = {};
-    for (int j0 = 0; j0 <= row; j0 += 32) {
-        const int j = j0 + lane, n = min(32, row + 1 - j0);
-        float ds = 0.f;
-        if (j <= row) {
-            const float s = dot_rows(q, row_at<T>(p.k, u.start + j, g), p.dim) * p.scale2;
-            if (row)
-                ds = exp2f(s - (st.x + Shift<T>::kProbs)) *
-                     (dot_rows(dy, row_at<T>(p.v, u.start + j, g), p.dim) - st.y);
-        }
-        for (int t = 0; t < n; ++t)
-            add_row(sum, __shfl_sync(0xffffffffu, ds, t), row_at<T>(p.k, u.start + j0 + t, g),
-                    p.dim, lane);
-    }
-    write_row<T>(p.dq, (u.start + row) * p.d_token[0] + head * p.d_head[0], sum, p.scale,
-                 p.dim_out, lane);
-}
 
 template <typename T>
 __global__ void __launch_bounds__(kBackThreads, 1)
@@ -151,8 +172,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t v_full = k_empty + 8 * kKeySlots, v_empty = v_full + 8 * kValueSlots;
     const uint32_t in_full = v_empty + 8 * kValueSlots, s_full = in_full + 8, dp_full = s_full + 8;
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, dq_full = ds_full + 8;
-    const uint32_t in_empty = dq_full + 8;
-    const uint32_t slot = in_empty + 8;
+    const uint32_t in_empty = dq_full + 8, bad_full = in_empty + 8, k_in = bad_full + 16;
+    const uint32_t slot = k_in + 8;
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
     // rows' statistics, and the parts of e
     float2 *stats = reinterpret_cast<float2 *>(aligned + (slot - base) + kSharedBytes);
@@ -161,8 +182,10 @@ __global__ void __launch_bounds__(kBackThreads, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDqBars; ++i) {
-            const bool sums = bars + 8 * i == p_full || bars + 8 * i == ds_full;
-            bar_init(bars + 8 * i, sums ? 4 * kSumGroups : 1);
+            const uint32_t b = bars + 8 * i;
+            bar_init(b, b == p_full || b == ds_full          ? 4 * kSumGroups
+                        : b == bad_full || b == bad_full + 8 ? 2
+                                                             : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         init_shared(sh);
@@ -227,7 +250,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             const uint32_t mine = one_lane();
             const int steps = (p.dim + 15) / 16;
             uint32_t ph = 0;
-            int it = 0;  // steps so far
+            int it = 0, units = 0;  // steps and units so far
             while (ok && w.next(p, round)) {
                 const int n = w.u.tile + 1, base = it;
                 const bool fine = one_tile(w.u);
@@ -235,8 +258,10 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
                     if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, waits)) return false;
                     const uint32_t at = k_at + slot_i * kTileBytes;
-                    const int seen = w.u.len - (n - 1 - i) * kTile;
-                    if (seen < kTile) zero_rows(at, seen, boxes, lane);
+                    if (i == 0) {  // on the diagonal
+                        bar_arrive_one(k_in, mine);
+                        if (!wait_warp(bad_full + 8 * (units & 1), units >> 1 & 1, waits)) return false;
+                    }
                     mma_rows<T>(tmem, q_at, at, steps, mine);
                     commit(s_full, mine);
                     return true;
@@ -273,6 +298,29 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     if (i == n - 1) commit(dq_full, mine);
                     else ok = grads(i + 1);
                 }
+                ++units;
+            }
+        } else {
+            // two warps look over half of the diagonal's keys each
+            const int half = warp - kIssueWarp - 1;
+            int it = 0, units = 0;
+            while (ok && w.next(p, round)) {
+                ok = wait_warp(k_in, units & 1, waits);
+                if (!ok) break;
+                const uint32_t at = k_at + it % kKeySlots * kTileBytes;
+                const int seen = min(kTile, w.u.len - w.u.tile * kTile);
+                const int from = half * (kTile / 2), end = min(seen, from + kTile / 2);
+                int first = kTile;
+                if (tile_bad<T>(at, from, end, boxes, lane)) {
+                    tile_clean<T>(at, from, end, boxes, lane,
+                                  [&](int, int row, int) { first = min(first, row); });
+                    first = __reduce_min_sync(0xffffffffu, first);
+                }
+                zero_rows(at, max(from, seen), from + kTile / 2, boxes, lane);
+                if (lane == 0) sh->bad[units & 1][0][half] = first;
+                tile_done();
+                if (lane == 0) bar_arrive(bad_full + 8 * (units & 1));
+                it += w.u.tile + 1, ++units;
             }
         }
         __syncwarp();
@@ -287,14 +335,25 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             const AttnUnit &u = w.u;
             const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
             const bool live = row < u.len, fine = one_tile(u);
+            // the largest |v|^2 that the queries see (the first load while others are)
+            const float *v_at =
+                Shift<T>::kOn ? p.values + head / p.group * p.tokens + u.start : nullptr;
+            float values = Shift<T>::kOn && lane < n ? v_at[(int64_t)lane * kTile] : 0.f;
             row_stats<T>(p, u, head, stats, sh->largest + units % 2);
             sums_barrier();
             const float2 st = stats[mine];
             const uint32_t big = sh->largest[units % 2];
-            const Shift<T> shift(big);
-            if (std::is_same<T, __half>::value && threadIdx.x == 0) {
-                if (big)
-                    atomicMax(p.largest + (int64_t)u.sequence * p.heads_k + head / p.group, big);
+            if constexpr (Shift<T>::kOn) {
+                for (int i = lane + 32; i < n; i += 32)
+                    values = fmaxf(values, v_at[(int64_t)i * kTile]);
+                values = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(values)));
+            }
+            const Shift<T> shift(__uint_as_float(big), values);
+            if (Shift<T>::kOn && threadIdx.x == 0) {
+                const int64_t at = (int64_t)u.sequence * p.heads_k + head / p.group;
+                if (big) atomicMax(p.largest + at, big);
+                // (by every head of the group, the same)
+                if (n * kTile >= u.len) p.most[at] = values;
                 sh->largest[(units + 1) % 2] = 0;
             }
             F2 rest = both(0.f);  // e, of this part of the columns
@@ -367,11 +426,15 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 __syncwarp();
                 if (lane == 0) bar_arrive(ds_full);
             }
-            if (ok) ok = wait_warp(dq_full, units & 1, waits);
+            if (ok)
+                ok = wait_warp(dq_full, units & 1, waits) &&
+                     wait_warp(bad_full + 8 * (units & 1), units >> 1 & 1, waits);
             tmem_after();
+            // rows that see a key that is not finite
+            const bool lost = !ok || mine >= min(sh->bad[units & 1][0][0], sh->bad[units & 1][0][1]);
             // e's parts through the place of the stats, which every warp has read
             float *parts = reinterpret_cast<float *>(stats);
-            float e = ok ? rest.x + rest.y : __uint_as_float(0x7fffffffu);  // (no result)
+            float e = lost ? __uint_as_float(0x7fffffffu) : rest.x + rest.y;  // (no result)
             if (side >= 2) parts[(side - 2) * kTile + mine] = e;
             sums_barrier();
             if (side < 2) parts[side * kTile + mine] += e;
@@ -379,22 +442,18 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             e = (parts[mine] + parts[kTile + mine]) * shift.undo;
             if (live && side == 0)
                 p.stats[head * p.tokens + u.start + row] = make_float2(st.x, st.y + e);
-            const float a = ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu);
+            const float a = lost ? __uint_as_float(0x7fffffffu) : p.scale * shift.undo;
             const float b = -e * p.scale * Shift<T>::kUndoProbs;
             T *out = static_cast<T *>(p.dq) + (u.start + (int64_t)row) * p.d_token[0] +
                      head * p.d_head[0];
-            bool good = true;
             for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                 uint32_t v[16], k[16];
                 tmem_load16(dq_tm + lanes + c, v);
                 tmem_load16(pk_tm + lanes + c, k);
                 Vec8 x[2];
 #pragma unroll
-                for (int h = 0; h < 16; ++h) {
-                    const float y = __uint_as_float(v[h]) * a + __uint_as_float(k[h]) * b;
-                    x[h / 8].v[h % 8] = y;
-                    good = good && finite(y);
-                }
+                for (int h = 0; h < 16; ++h)
+                    x[h / 8].v[h % 8] = __uint_as_float(v[h]) * a + __uint_as_float(k[h]) * b;
                 if (!live) continue;
 #pragma unroll
                 for (int h = 0; h < 16; h += 8) {
@@ -403,17 +462,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
                 }
             }
-            const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
-            if (lane == 0 && again) atomicOr(sh->bad + warp % 4, again);
             sums_barrier();
-            if (side == 0) {
-                const uint32_t rows = ok && !sh->gave_up ? sh->bad[warp] : 0;
-                __syncwarp();
-                if (lane == 0) sh->bad[warp] = 0;
-                do_again(__shfl_sync(0xffffffffu, rows, 0), sh, [&](int i) {
-                    dq_row<T>(p, u, row - lane + i, head, lane);
-                });
-            }
         }
     }
     end_block(sh);
@@ -438,43 +487,14 @@ __global__ void __launch_bounds__(kBackThreads, 1)
 // memory, 8 microseconds more for a pair.)
 constexpr int kQuerySlots = 2;
 constexpr int kStatBytes = kTile * 8;
-constexpr int kDkvBars = 6 * kQuerySlots + 6;
+constexpr int kDkvBars = 8 * kQuerySlots + 6;
 constexpr int kDkvSmem = 1024 + (2 + 2 * kQuerySlots) * kTileBytes + kQuerySlots * kStatBytes +
-                         8 * kDkvBars + kSharedBytes;
+                         8 * kDkvBars + kSharedBytes + kAttnMaxDim;
 
 __device__ __forceinline__ F2 load_stats(uint32_t at) {
     F2 l;
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(l.x), "=f"(l.y) : "r"(at));
     return l;
-}
-
-// side >= 0: only the columns that a block of attn_join_kernel takes are written.
-template <typename T>
-__device__ __forceinline__ void dkv_row(const AttnParams &p, const AttnUnit &u, int row, int g,
-                                        int lane, int side = -1) {
-    const T *k = row_at<T>(p.k, u.start + row, g), *v = row_at<T>(p.v, u.start + row, g);
-    RowPart dk = {}, dv = {};
-    for (int head = g * p.group; head < (g + 1) * p.group; ++head)
-        for (int i0 = row; i0 < u.len; i0 += 32) {
-            const int i = i0 + lane, n = min(32, u.len - i0);
-            float e = 0.f, ds = 0.f;
-            if (i < u.len) {
-                const float2 st = p.stats[head * p.tokens + u.start + i];
-                e = exp2f(dot_rows(row_at<T>(p.q, u.start + i, head), k, p.dim) * p.scale2 -
-                          (st.x + Shift<T>::kProbs));
-                if (i) ds = e * (dot_rows(row_at<T>(p.g, u.start + i, head), v, p.dim) - st.y);
-            }
-            for (int t = 0; t < n; ++t) {
-                add_row(dv, __shfl_sync(0xffffffffu, e, t), row_at<T>(p.g, u.start + i0 + t, head),
-                        p.dim, lane);
-                add_row(dk, __shfl_sync(0xffffffffu, ds, t), row_at<T>(p.q, u.start + i0 + t, head),
-                        p.dim, lane);
-            }
-        }
-    write_row<T>(p.dk, (u.start + row) * p.d_token[1] + g * p.d_head[1], dk, p.scale, p.dim_out,
-                 lane, side);
-    write_row<T>(p.dv, (u.start + row) * p.d_token[2] + g * p.d_head[2], dv, 1.f, p.dim_out, lane,
-                 side);
 }
 
 // Where the sums of a part of a block's steps go: [tensor][16 columns][4 columns][128 keys][4].
@@ -514,8 +534,11 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const uint32_t st_full = g_empty + 8 * kQuerySlots, st_empty = st_full + 8 * kQuerySlots;
     const uint32_t in_full = st_empty + 8 * kQuerySlots, s_full = in_full + 8, dp_full = s_full + 8;
     const uint32_t p_full = dp_full + 8, ds_full = p_full + 8, out_full = ds_full + 8;
-    const uint32_t slot = out_full + 8;
+    const uint32_t q_clean = out_full + 8, g_clean = q_clean + 8 * kQuerySlots;
+    const uint32_t slot = g_clean + 8 * kQuerySlots;
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
+    // behind the last query of the diagonal's whose dO is not finite, of each column
+    uint8_t *last_bad = aligned + (slot - base) + kSharedBytes;
     const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
@@ -528,6 +551,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         init_shared(sh);
+        for (int i = 0; i < kAttnMaxDim; ++i) last_bad[i] = 0;
     }
     if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot),
@@ -553,6 +577,25 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const int boxes = p.dim > 64 ? 2 : 1;
     const bool fine = n > 0 && one_tile(u);
     bool ok = true;
+    // The i-th step's tile of queries (0) or dO (1): on the diagonal it is looked over; what
+    // is behind the sequence becomes zeros.
+    const auto look = [&](int i, int t) {
+        const int s = i % kQuerySlots, tile = (step0 + i) % each;
+        if (!wait_warp((t ? g_full : q_full) + 8 * s, i / kQuerySlots & 1, waits)) return false;
+        const uint32_t at = (t ? g_at : q_at) + s * kTileBytes;
+        const int seen = min(kTile, u.len - (u.tile + tile) * kTile);
+        if (tile == 0 && tile_bad<T>(at, 0, seen, boxes, lane)) {
+            if (lane == 0 && t) sh->bad[0][0][0] = 1;
+            // (P and dS of a query that is not finite are not, by its lse or D)
+            tile_clean<T>(at, 0, seen, boxes, lane, [&](int c, int, int last) {
+                if (t) last_bad[c] = max(last_bad[c], (uint8_t)(last + 1));
+            });
+        }
+        zero_rows(at, seen, kTile, boxes, lane);
+        tile_done();
+        if (lane == 0) bar_arrive((t ? g_clean : q_clean) + 8 * s);
+        return true;
+    };
 
     if (group == kSumGroups) {
         give_registers<kBackIssueRegs>();
@@ -584,21 +627,17 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         } else if (warp == kIssueWarp) {
             const uint32_t mine = one_lane();
             const int steps = (p.dim + 15) / 16;
-            const auto arrived = [&](uint32_t full, uint32_t at, int i) {
-                const int s = i % kQuerySlots;
-                if (!wait_warp(full + 8 * s, i / kQuerySlots & 1, waits)) return false;
-                const int seen = u.len - (u.tile + (step0 + i) % each) * kTile;
-                if (seen < kTile) zero_rows(at + s * kTileBytes, seen, boxes, lane);
-                return true;
+            const auto arrived = [&](uint32_t clean, int i) {
+                return wait_warp(clean + 8 * (i % kQuerySlots), i / kQuerySlots & 1, waits);
             };
             const auto scores = [&](int i) {
-                if (!arrived(q_full, q_at, i)) return false;
+                if (!arrived(q_clean, i)) return false;
                 mma_rows<T>(tmem, k_at, q_at + i % kQuerySlots * kTileBytes, steps, mine);
                 commit(s_full, mine);
                 return true;
             };
             const auto grads = [&](int i) {  // dP
-                if (!arrived(g_full, g_at, i)) return false;
+                if (!arrived(g_clean, i)) return false;
                 mma_rows<T>(dp_tm, v_at, g_at + i % kQuerySlots * kTileBytes, steps, mine);
                 commit(dp_full, mine);
                 return true;
@@ -633,17 +672,21 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         } else if (warp == kStatsWarp) {
             // lse and D of the queries; none for rows past the sequence: their
             // probabilities are 2^(0 - inf) = 0
-            const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0u);
-            for (int i = 0; i < n && ok; ++i) {
-                const int s = i % kQuerySlots, head = g * p.group + (step0 + i) / each;
+            const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0.f, 0.f);
+            float2 st[4];
+            const auto fetch = [&](int i) {
+                const int head = g * p.group + (step0 + i) / each;
                 const int row = (u.tile + (step0 + i) % each) * kTile;
                 const float2 *from = p.stats + head * p.tokens + u.start + row;
-                float2 st[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
                     st[h] = row + lane + 32 * h < u.len
                                 ? from[lane + 32 * h]
                                 : make_float2(__uint_as_float(0x7f800000u), 0.f);
+            };
+            if (n > 0) fetch(0);
+            for (int i = 0; i < n && ok; ++i) {
+                const int s = i % kQuerySlots;
                 ok = wait_warp(st_empty + 8 * s, (i / kQuerySlots & 1) ^ 1, waits);
                 if (!ok) break;
 #pragma unroll
@@ -654,16 +697,19 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                                  : "memory");
                 __syncwarp();
                 if (lane == 0) bar_arrive(st_full + 8 * s);
+                if (i + 1 < n) fetch(i + 1);
+                ok = look(i, 1);
             }
+        } else {
+            for (int i = 0; i < n && ok; ++i) ok = look(i, 0);
         }
         __syncwarp();
     } else {
         take_registers<kBackRegs>();
-        const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0u);
-        const int side = group, mine = warp % 4 * 32 + lane, row = u.tile * kTile + mine;
+        const Shift<T> shift = n > 0 ? Shift<T>::of_keys(p, u, g) : Shift<T>(0.f, 0.f);
+        const int side = group, mine = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_tm = tmem + kCols * side + lanes, d_tm = dp_tm + kCols * side + lanes;
-        const bool live = n > 0 && row < u.len;
         // A thread's 32 values are of four keys and eight queries (tmem_load_block), so that it
         // reads lse and D of eight queries and not of 32: shared memory is what bounds
         // this kernel (2786 cycles a tile of 128 x 128 with 32 of them)
@@ -746,15 +792,26 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
         }
         if (n > 0) {
-            if (ok) ok = wait_warp(out_full, 0, waits);
+            if (ok)
+                ok = wait_warp(out_full, 0, waits) &&
+                     wait_warp(g_clean + 8 * ((n - 1) % kQuerySlots), (n - 1) / kQuerySlots & 1, waits);
             tmem_after();
         }
+        const bool bad = sh->bad[0][0][0] != 0;
+        // keys that see a dO that is not finite: a column of dv
+        const auto mark = [&](int t, int c, uint32_t *v) {
+            if (t && bad)
+#pragma unroll
+                for (int h = 0; h < 16; ++h)
+                    if (mine < last_bad[c + h]) v[h] = 0x7fffffffu;
+        };
         const float lost = __uint_as_float(0x7fffffffu);  // a wait that gave up: no sums
         if (n > 0 && p.parts > 1) {
             for (int t = 0; t < 2; ++t)
                 for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                     uint32_t v[16];
                     tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
+                    mark(t, c, v);
 #pragma unroll
                     for (int h = 0; h < 16; ++h) v[h] = ok ? v[h] : 0x7fffffffu;
 #pragma unroll
@@ -767,21 +824,17 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             // every tile of queries has been used: their places hold the results
             const float factor[2] = {ok ? p.scale * shift.undo : lost,
                                      ok ? Shift<T>::kUndoProbs : lost};
-            bool good = true;
             for (int t = 0; t < 2; ++t)
                 for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
                     uint32_t v[16];
                     tmem_load16((t ? dv_tm : dk_tm) + lanes + c, v);
+                    mark(t, c, v);
                     Vec8 x[2];
 #pragma unroll
-                    for (int h = 0; h < 16; ++h) {
+                    for (int h = 0; h < 16; ++h)
                         x[h / 8].v[h % 8] = __uint_as_float(v[h]) * factor[t];
-                        good = good && finite(__uint_as_float(v[h]));
-                    }
                     put_columns<T>(q_at + t * kTileBytes, mine, c, x);
                 }
-            const uint32_t again = __ballot_sync(0xffffffffu, live && !good);
-            if (lane == 0 && again) atomicOr(sh->bad + warp % 4, again);
             sums_barrier();
             const int64_t token = u.start + (int64_t)u.tile * kTile;
             const int count = min(kTile, u.len - u.tile * kTile);
@@ -792,11 +845,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                        static_cast<T *>(p.dv) + token * p.d_token[2] + g * p.d_head[2],
                        p.d_token[2], p.d_vectors[2], p.dim, p.dim_out, (int)threadIdx.x,
                        128 * kSumGroups);
-            sums_barrier();
-            const uint32_t rows = ok && side == 0 && !sh->gave_up ? sh->bad[warp] : 0;
-            do_again(__shfl_sync(0xffffffffu, rows, 0), sh, [&](int i) {
-                dkv_row<T>(p, u, row - lane + i, g, lane);
-            });
         }
     }
     end_block(sh);
@@ -817,7 +865,6 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
     if (!unit_at<kTile>(p, unit / p.heads_k, u)) return;
     const int given = u.tile;
     const Shift<T> shift = Shift<T>::of_keys(p, u, g);
-    const int lane = threadIdx.x % 32;
     uint32_t used = 0;  // parts that have steps
     for (int r = 0; r < p.parts; ++r) {
         u.tile = given;
@@ -826,12 +873,12 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
     const int row = u.tile * kTile + threadIdx.x;
     const bool live = row < u.len;
     const int64_t token = u.start + (int64_t)row;
-    bool good = true;
     for (int t = 0; t < 2; ++t) {
         const float factor = t ? Shift<T>::kUndoProbs : p.scale * shift.undo;
         T *out = static_cast<T *>(t ? p.dv : p.dk) + token * p.d_token[1 + t] + g * p.d_head[1 + t];
         for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
             Vec8 x[2] = {};
+#pragma unroll 4
             for (int r = 0; r < p.parts; ++r) {
                 if (!(used >> r & 1)) continue;
 #pragma unroll
@@ -842,10 +889,7 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
                 }
             }
 #pragma unroll
-            for (int h = 0; h < 16; ++h) {
-                good = good && finite(x[h / 8].v[h % 8]);
-                x[h / 8].v[h % 8] *= factor;
-            }
+            for (int h = 0; h < 16; ++h) x[h / 8].v[h % 8] *= factor;
             if (!live) continue;
 #pragma unroll
             for (int h = 0; h < 16; h += 8) {
@@ -854,13 +898,6 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
                 else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
             }
         }
-    }
-    uint32_t again = __ballot_sync(0xffffffffu, live && !good);
-    __syncwarp();
-    while (again) {
-        const int i = __ffs(again) - 1;
-        again &= again - 1;
-        dkv_row<T>(p, u, row - lane + i, g, lane, side);
     }
 }
 
@@ -906,6 +943,9 @@ static int64_t largest_bytes(const pos_attn *a) {
     const int64_t n = a->starts ? std::min<int64_t>(a->sequences, a->tokens) : 1;
     return a->dtype == POS_F16 ? (n * a->heads_k * 4 + 15) / 16 * 16 : 0;
 }
+static int64_t values_bytes(const pos_attn *a) {
+    return a->dtype == POS_F16 ? (a->tokens * a->heads_k * 4 + 15) / 16 * 16 + largest_bytes(a) : 0;
+}
 
 template <typename T>
 static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaStream_t s) {
@@ -918,8 +958,9 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     POS_TRY(attn_grid(a, kTile, a->heads_q, &grid_q));
     POS_TRY(attn_grid(a, kTile, a->heads_k, &grid_k));
     if (grid_q == 0) return POS_OK;
-    if (std::is_same<T, __half>::value)
-        POS_CUDA(cudaMemsetAsync(p.largest, 0, largest_bytes(a), s));
+    if constexpr (Shift<T>::kOn)
+        POS_CUDA(launch_dependent(attn_values_kernel<T>, std::min(grid_k, 16 * std::max(1, sm_count())),
+                                  kTile, 0, s, p));
     auto dq = attn_dq_kernel<T>;
     POS_TRY(ensure_smem(reinterpret_cast<const void *>(dq), kDqSmem));
     POS_CUDA(launch_dependent(dq, std::min(grid_q, std::max(1, sm_count())), kBackThreads, kDqSmem, s,
@@ -936,6 +977,9 @@ static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_head
                            AttnParams p, int parts, char *at, cudaStream_t s) {
     p.largest = reinterpret_cast<uint32_t *>(at);
     at += largest_bytes(a);
+    p.most = reinterpret_cast<float *>(at);
+    p.values = reinterpret_cast<float *>(at + largest_bytes(a));
+    at += values_bytes(a);
     p.stats = reinterpret_cast<float2 *>(at);
     at += stats_bytes(a);
     p.parts = parts;
@@ -983,7 +1027,7 @@ extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_hea
                              dx[i].head_stride % 8 == 0;
         }
         const int parts = parts_of(attn);
-        int64_t bytes = largest_bytes(attn) + stats_bytes(attn) + part_bytes(attn, parts) +
+        int64_t bytes = largest_bytes(attn) + values_bytes(attn) + stats_bytes(attn) + part_bytes(attn, parts) +
                         attn_list_bytes(attn, kTile);
         for (int i = 0; i < 4; ++i)
             if (!attn_direct(attn, i < 3 ? x[i] : *d_o, heads[i]))
