@@ -124,10 +124,12 @@ constexpr int kRowRegs = 208, kIssueRegs = 88;
 // score only when that is 2^8 times more: sums of up to 2^8 times their size have
 // the same precision, and O in TMEM is rescaled that much more rarely.
 constexpr float kSlack = 8.f;
-// In bf16 they are 2^-8 of that besides, 1 at most, so that sums of values near the type's
-// largest do not pass f32's.
+// Besides, in bf16 they are 2^-8 of that, 1 at most, so that sums of values near the type's
+// largest do not pass f32's; in f16 2^7 of it, 2^15 at most, so that many small ones keep
+// their bits: below 2^-14 f16 has fewer, below 2^-25 none, and 32768 keys of 2^-25 are 2^-10 of
+// the weight, half an o's step and more.
 template <typename T>
-constexpr float kLift = std::is_same<T, __nv_bfloat16>::value ? -kSlack : 0.f;
+constexpr float kLift = std::is_same<T, __nv_bfloat16>::value ? -kSlack : 15.f - kSlack;
 
 struct ForwardUnit : BlockUnit<kForwardRows> {
     int r0, n0, n1, first;  // first token; tiles of keys that its two tiles see, the last

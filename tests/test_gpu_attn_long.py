@@ -1,0 +1,45 @@
+"""Attention of long rows: what thousands of small probabilities add up to."""
+import math
+
+import pytest
+
+import layer_util as U
+from test_gpu_attn import F32, Call
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2609_06086_gb300 as P
+    return P
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("bits", [8.3, 17.4, 24.6, 25.4, 27.0])
+@pytest.mark.parametrize("n", [3000, 30000])
+def test_one_large_score_and_many_small_ones(P, dtype, bits, n):
+    """One key, near the end, has 2^bits times the weight of every other and a value of 0, the
+    others' values are 1: a row behind it is the share of the others.  Their probabilities are
+    rounded to dtype (all the same way) as they are relative to the row's reference, in f16
+    with 2^7 of it, so that half of the smallest step is 2^-32 of the large one."""
+    t = n - 50
+    c = Call(P, [n], 2, 1, 64, dtype, starts=False, scale=1.0)
+    q, k, v = c.x
+    q.zero_(), k.zero_(), v.fill_(1.0)
+    q[:, :, 3] = 1
+    k[t, :, 3] = bits * math.log(2)
+    v[t] = 0
+    c.forward()
+    u = U.ROUND[dtype]
+    weight = math.exp(-float(k[t, 0, 3]))
+    others = torch.arange(n, device="cuda", dtype=torch.float64)  # seen beside t, for rows from t on
+    total = torch.where(others < t, others + 1, 1 + others * weight)
+    share = torch.where(others < t, 1.0, others * weight / total)
+    lse = torch.log(total) + torch.where(others < t, 0.0, float(k[t, 0, 3]))
+    step = 2.0 ** -32 if dtype == "f16" else 0.0
+    # P and o rounded; a sum of n that the tensor cores cut (2^-23 an addition of 16)
+    tol = (2 * u + (n / 16 + 70) * 2 * F32) * 1.01 * share + step * others + U.TINY[dtype]
+    assert ((c.o.double() - share[:, None, None]).abs() <= tol[:, None, None]).all()
+    assert ((c.lse.double() - lse).abs() <= (n + 70) * 2 * F32 + 4 * F32 * lse.abs()).all()
