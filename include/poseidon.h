@@ -681,7 +681,7 @@ pos_status poseidon_attn_forward(const pos_attn *attn, const pos_heads *x, const
  * the keys' and values' summed over the query heads of their group.  x, dx: host arrays of
  * three, o and d_o: one; dx must not overlap what is read.  Sums are in 32 bits, in an
  * order that the sizes and the GPU fix; p and ds are rounded to dtype for their products
- * (in sequences of at most 128 tokens each is two values of dtype).
+ * (of a sequence's first 128 queries each is two values of dtype).
  * Scratch from the library's pool: 8 bytes a token and query head, in f16 4 a token and 8 a
  * sequence and key head, what the forward pass takes (16 bytes a tile of 128; a copy of d_o too where
  * it needs one) and, where there are few tiles of keys, 1 KB for each element of dim and

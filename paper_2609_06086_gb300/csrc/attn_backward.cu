@@ -125,11 +125,12 @@ __device__ __forceinline__ void row_stats(const AttnParams &p, const AttnUnit &u
     }
 }
 
-// Sequences of one tile: their P and dS go into the products as two 16-bit values each, so
-// that only the results are rounded.  (Rounded once, they add as much to the error as the
-// results' own rounding does, 1.4 times that in all; in a few short rows it was up to 2.1.
-// 8192 tokens of 32 + 8 heads of 128 in 80 sequences: both passes 436 us, with one value 417.)
-__device__ __forceinline__ bool one_tile(const AttnUnit &u) { return u.len <= kTile; }
+// The first tile's queries, whose rows are short, with its keys: their P and dS go into the
+// products as two 16-bit values each, so that only the results are rounded.  (Rounded once, they
+// add as much to the error as the results' own rounding does, 1.4 times that in all; in a
+// few short rows it was up to 2.1.  8192 tokens of 32 + 8 heads of 128 in 80 sequences: both
+// passes 436 us, with one value 417.)
+__device__ __forceinline__ bool short_rows(const AttnUnit &u) { return u.tile == 0; }
 
 __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
     asm volatile("barrier.sync 1, %0;" ::"n"(128 * kSumGroups) : "memory");
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             int it = 0, units = 0;  // steps and units so far
             while (ok && w.next(p, round)) {
                 const int n = w.u.tile + 1, base = it;
-                const bool fine = one_tile(w.u);
+                const bool fine = short_rows(w.u);
                 const auto scores = [&](int i) {
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
                     if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, waits)) return false;
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         for (; w.next(p, round); ++units) {
             const AttnUnit &u = w.u;
             const int n = u.tile + 1, head = w.head, row = u.tile * kTile + mine;
-            const bool live = row < u.len, fine = one_tile(u);
+            const bool live = row < u.len, fine = short_rows(u);
             // the largest |v|^2 that the queries see (the first load while others are)
             const float *v_at =
                 Shift<T>::kOn ? p.values + head / p.group * p.tokens + u.start : nullptr;
@@ -575,7 +576,6 @@ __global__ void __launch_bounds__(kBackThreads, 1)
         each = steps.each, step0 = steps.first, n = steps.n;
     }
     const int boxes = p.dim > 64 ? 2 : 1;
-    const bool fine = n > 0 && one_tile(u);
     bool ok = true;
     // The i-th step's tile of queries (0) or dO (1): on the diagonal it is looked over; what
     // is behind the sequence becomes zeros.
@@ -649,6 +649,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             }
             for (int i = 0; i < n && ok; ++i) {
                 const int s = i % kQuerySlots;
+                const bool fine = (step0 + i) % each == 0 && short_rows(u);
                 ok = wait_warp(p_full, i & 1, waits);
                 if (!ok) break;
                 tmem_after();
@@ -733,7 +734,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 s[c] = __float_as_uint(exp2_fast(x.x));
                 s[c + 1] = __float_as_uint(exp2_fast(x.y));
             }
-            const bool diagonal = (step0 + i) % each == 0;
+            const bool diagonal = (step0 + i) % each == 0, fine = diagonal && short_rows(u);
             if (diagonal) {
 #pragma unroll
                 for (int c = 0; c < kCols; ++c)
