@@ -49,8 +49,10 @@ __global__ void __launch_bounds__(kListThreads) attn_tiles_kernel(const AttnList
                 a = max(a, __shfl_up_sync(0xffffffffu, a, o));
             a = max(a, last);
             const int b = max(a, min(tokens, p.starts[mine + 1]));
-            const int n = min(32, s1 - s);
-            for (int i = 0; i < n; ++i) {
+            // (many may be empty)
+            uint32_t there = __ballot_sync(0xffffffffu, lane < s1 - s && b > a);
+            for (; there; there &= there - 1) {
+                const int i = __ffs(there) - 1;
                 const int at = __shfl_sync(0xffffffffu, a, i);
                 const int len = __shfl_sync(0xffffffffu, b, i) - at;
                 for (int t = lane; t < (len + p.rows - 1) / p.rows; t += 32) {
@@ -567,7 +569,9 @@ pos_status attn_map(CUtensorMap *map, const pos_attn *a, const AttnTensor &t, in
 }
 
 int64_t attn_most_tiles(const pos_attn *a, int rows) {
-    return a->starts ? a->tokens / rows + a->sequences : (a->tokens + rows - 1) / rows;
+    // (a sequence that has a tile has a token)
+    return a->starts ? a->tokens / rows + std::min<int64_t>(a->sequences, a->tokens)
+                     : (a->tokens + rows - 1) / rows;
 }
 int64_t attn_list_bytes(const pos_attn *a, int rows) {
     return a->starts ? 16 * (attn_most_tiles(a, rows) + 1) : 0;
@@ -585,12 +589,9 @@ pos_status attn_list(const pos_attn *a, int rows, char **at, cudaStream_t s, Att
     POS_CUDA(launch_dependent(attn_tiles_kernel, 1, kListThreads, 0, s, l));
     return POS_OK;
 }
-// Blocks of a kernel that takes a head of a tile each.
-pos_status attn_grid(const pos_attn *a, int rows, int64_t heads, int *grid) {
-    const int64_t n = attn_most_tiles(a, rows) * heads;
-    if (n > 0x7fffffffll) return fail(POS_EINVAL, "attention: too many tiles");
-    *grid = (int)n;
-    return POS_OK;
+// Units of a head of a tile each, kMostUnits at most.
+int attn_grid(const pos_attn *a, int rows, int64_t heads) {
+    return (int)std::min<int64_t>(attn_most_tiles(a, rows) * heads, kMostUnits);
 }
 
 template <typename T>
@@ -612,8 +613,7 @@ static pos_status forward(const pos_attn *a, const pos_heads *x, AttnParams p, c
     AttnTensor *to[3] = {&p.q, &p.k, &p.v};
     for (int i = 0; i < 3; ++i) POS_TRY(attn_input(a, x[i], heads[i], &at, s, to[i]));
     POS_TRY(attn_list(a, kForwardRows, &at, s, &p));
-    int grid = 0;
-    POS_TRY(attn_grid(a, kForwardRows, a->heads_q, &grid));
+    const int grid = attn_grid(a, kForwardRows, a->heads_q);
     if (grid == 0) return POS_OK;
     return a->dtype == POS_BF16 ? launch_forward<__nv_bfloat16>(a, p, grid, s)
                                 : launch_forward<__half>(a, p, grid, s);

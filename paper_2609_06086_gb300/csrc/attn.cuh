@@ -33,7 +33,7 @@ struct AttnParams {
     float *values;              // the largest |v|^2 of a tile, [heads_k][its first token],
     float *most;                // and of a sequence, as `largest` is
     float *part;                // backward: sums of parts of the keys' gradients
-    int32_t parts;
+    int32_t parts, first_blocks;  // blocks of the keys' kernel that start at once
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
     const int32_t *n_tiles;
     int64_t tokens;
@@ -520,6 +520,7 @@ pos_status attn_map(CUtensorMap *map, const pos_attn *a, const AttnTensor &t, in
 int64_t attn_most_tiles(const pos_attn *a, int rows);
 int64_t attn_list_bytes(const pos_attn *a, int rows);
 pos_status attn_list(const pos_attn *a, int rows, char **at, cudaStream_t s, AttnParams *p);
-pos_status attn_grid(const pos_attn *a, int rows, int64_t heads, int *grid);
+constexpr int kMostUnits = 1 << 30;
+int attn_grid(const pos_attn *a, int rows, int64_t heads);
 
 }  // namespace pos

@@ -543,6 +543,11 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
+    // A block that starts when others have ended, and has no tile, ends at once.
+    if (p.tiles && blockIdx.x >= p.first_blocks) {
+        grid_dep_wait();
+        if (blockIdx.x / p.parts / p.heads_k >= *p.n_tiles) return;
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < kDkvBars; ++i) {
             const uint32_t b = bars + 8 * i;
@@ -955,10 +960,9 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     POS_TRY(attn_map(&k, a, p.k, p.heads_k, p.dim));
     POS_TRY(attn_map(&v, a, p.v, p.heads_k, p.dim));
     POS_TRY(attn_map(&g, a, p.g, p.heads_q, p.dim));
-    int grid_q = 0, grid_k = 0;
-    POS_TRY(attn_grid(a, kTile, a->heads_q, &grid_q));
-    POS_TRY(attn_grid(a, kTile, a->heads_k, &grid_k));
+    const int grid_q = attn_grid(a, kTile, a->heads_q), grid_k = attn_grid(a, kTile, a->heads_k);
     if (grid_q == 0) return POS_OK;
+    if (grid_k == kMostUnits) return fail(POS_EINVAL, "attention: too many tiles of keys");
     if constexpr (Shift<T>::kOn)
         POS_CUDA(launch_dependent(attn_values_kernel<T>, std::min(grid_k, 16 * std::max(1, sm_count())),
                                   kTile, 0, s, p));
@@ -983,7 +987,7 @@ static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_head
     at += values_bytes(a);
     p.stats = reinterpret_cast<float2 *>(at);
     at += stats_bytes(a);
-    p.parts = parts;
+    p.parts = parts, p.first_blocks = sm_count();
     p.part = reinterpret_cast<float *>(at);
     at += part_bytes(a, parts);
     const pos_heads t[4] = {x[0], x[1], x[2], d_o};
