@@ -663,7 +663,9 @@ typedef struct pos_attn {
  * on output.
  * Scratch from the library's pool (stream-ordered): 16 bytes a tile of 256 tokens and
  * sequence where starts is not NULL; a copy of each of x that is off the 16-byte
- * alignment (base, strides and dim) or has a stride of 0.  Waits inside the kernels are
+ * alignment (base, strides and dim) or has a stride of 0.  Of a call's scratch the library
+ * keeps up to 320 MB for later ones; more than that is given back when the stream, an
+ * event or the device is next waited for.  Waits inside the kernels are
  * bounded as poseidon_ckpt_wgrad's are (POSEIDON_ATTN_WAIT_NS in the environment of the
  * process's first call, in nanoseconds, is another limit); where one ran out, every row
  * whose result is lost by that is NaN.

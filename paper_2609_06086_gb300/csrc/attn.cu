@@ -515,7 +515,7 @@ pos_status attn_scratch(int64_t bytes, cudaStream_t s, void **out) {
     *out = nullptr;
     if (bytes == 0) return POS_OK;
     cudaMemPool_t pool;
-    POS_TRY(scratch_pool(&pool));
+    POS_TRY(scratch_pool(&pool, bytes));
     POS_CUDA(cudaMallocFromPoolAsync(out, (size_t)bytes, pool, s));
     return POS_OK;
 }

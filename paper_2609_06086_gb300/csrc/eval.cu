@@ -439,29 +439,37 @@ pos_status launch_decode(const EvalParams &p, cudaStream_t stream) {
 // keeps its memory between calls (release threshold: unlimited), so what is
 // taken from it is bounded: 39 bytes per candidate of a chunk of 2^24, an
 // argmin's partial results, host batches up to kHostPoolBytes, and the layer
-// operators' scratch (at most 320 MB a call, see poseidon.h).
+// operators' scratch of up to kKeptScratch a call.  What they
+// need beyond (attention's copies of tensors off the alignment and its statistics
+// grow with the tensors) comes from a second pool, which gives all of it back
+// when the stream, an event or the device is next waited for.
 constexpr size_t kHostPoolBytes = 64ull << 20;
+constexpr int64_t kKeptScratch = 320ll << 20;
 static std::mutex g_pool_mutex;
-static cudaMemPool_t g_pool[64];
+static cudaMemPool_t g_pool[2][64];
 
-pos_status scratch_pool(cudaMemPool_t *out) {
+static pos_status pool_of(bool kept, cudaMemPool_t *out) {
     int dev = 0;
     POS_CUDA(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return fail(POS_EINVAL, "device index above 63");
     std::lock_guard<std::mutex> lock(g_pool_mutex);
-    if (!g_pool[dev]) {
+    if (!g_pool[kept][dev]) {
         cudaMemPoolProps props = {};
         props.allocType = cudaMemAllocationTypePinned;
         props.location.type = cudaMemLocationTypeDevice;
         props.location.id = dev;
         cudaMemPool_t pool;
         POS_CUDA(cudaMemPoolCreate(&pool, &props));
-        uint64_t keep = ~0ull;
+        uint64_t keep = kept ? ~0ull : 0ull;
         POS_CUDA(cudaMemPoolSetAttribute(pool, cudaMemPoolAttrReleaseThreshold, &keep));
-        g_pool[dev] = pool;
+        g_pool[kept][dev] = pool;
     }
-    *out = g_pool[dev];
+    *out = g_pool[kept][dev];
     return POS_OK;
+}
+pos_status scratch_pool(cudaMemPool_t *out) { return pool_of(true, out); }
+pos_status scratch_pool(cudaMemPool_t *out, int64_t bytes) {
+    return pool_of(bytes <= kKeptScratch, out);
 }
 
 // Side streams per device.  Every makespan kernel depends only on the decode

@@ -1,5 +1,5 @@
-// Shared by the layer operators (ckpt.cu, qk.cu, wgrad.cu): element types,
-// 8-element vectors, and the arithmetic of an 8-bit checkpoint (poseidon.h).
+// Shared by the layer operators (ckpt.cu, qk.cu, wgrad.cu, norm*.cu, dropout.cu, attn*.cu):
+// element types, 8-element vectors, and the arithmetic of an 8-bit checkpoint (poseidon.h).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -11,8 +11,10 @@
 
 namespace pos {
 
-// The library's scratch pool of the current device (eval.cu).
+// The library's scratch pool of the current device (eval.cu), and the one for a call's `bytes`:
+// that one, which keeps its memory, or for many one that gives it back.
 pos_status scratch_pool(cudaMemPool_t *out);
+pos_status scratch_pool(cudaMemPool_t *out, int64_t bytes);
 
 constexpr int kGroup = 32;             // columns that share a scale
 constexpr int kScaleLo = 17;           // scale byte of e = -110

@@ -220,7 +220,7 @@ static pos_status launch_backward(NormParams &p, const NormShape &shape, const f
     void *scratch = nullptr;
     if (dw && grid > 0) {
         cudaMemPool_t pool;
-        POS_TRY(scratch_pool(&pool));
+        POS_TRY(scratch_pool(&pool, (int64_t)grid * p.cols * 4));
         POS_CUDA(cudaMallocFromPoolAsync(&scratch, (size_t)grid * p.cols * 4, pool, s));
         p.part = static_cast<float *>(scratch);
     }
