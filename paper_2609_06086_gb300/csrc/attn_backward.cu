@@ -907,6 +907,25 @@ __global__ void __launch_bounds__(kTile) attn_join_kernel(const AttnParams p) {
     }
 }
 
+// The gradients of keys and values that no query head reads: zeros.
+template <typename T>
+__global__ void __launch_bounds__(kTile) attn_zero_kernel(const AttnParams p) {
+    grid_dep_wait();
+    grid_dep_trigger();
+    const int64_t units =
+        (int64_t)(p.tiles ? *p.n_tiles : ((int)p.tokens + kTile - 1) / kTile) * p.heads_k;
+    for (int64_t i = blockIdx.x; i < units; i += gridDim.x) {
+        AttnUnit u;
+        unit_at<kTile>(p, (int)(i / p.heads_k), u);
+        const int g = (int)(i % p.heads_k), rows = min(kTile, u.len - u.tile * kTile);
+        const int64_t token = u.start + (int64_t)u.tile * kTile;
+        for (int t = 0; t < 2; ++t)
+            for (int e = threadIdx.x; e < rows * p.dim_out; e += kTile)
+                static_cast<T *>(t ? p.dv : p.dk)[(token + e / p.dim_out) * p.d_token[1 + t] +
+                                                  g * p.d_head[1 + t] + e % p.dim_out] = T(0.f);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
@@ -978,6 +997,15 @@ static pos_status launch_backward(const pos_attn *a, const AttnParams &p, cudaSt
     return POS_OK;
 }
 
+static pos_status no_queries(const pos_attn *a, AttnParams p, char *at, cudaStream_t s) {
+    POS_TRY(attn_list(a, kTile, &at, s, &p));
+    const int grid = std::min(attn_grid(a, kTile, a->heads_k), 16 * std::max(1, sm_count()));
+    if (grid == 0) return POS_OK;
+    const auto kern = a->dtype == POS_BF16 ? attn_zero_kernel<__nv_bfloat16> : attn_zero_kernel<__half>;
+    POS_CUDA(launch_dependent(kern, grid, kTile, 0, s, p));
+    return POS_OK;
+}
+
 static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_heads &d_o,
                            AttnParams p, int parts, char *at, cudaStream_t s) {
     p.largest = reinterpret_cast<uint32_t *>(at);
@@ -1021,8 +1049,8 @@ extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_hea
         POS_TRY(check_attn_tensor(attn, *d_o, attn->heads_q, "o's gradient", false));
         if (reinterpret_cast<uintptr_t>(d_lse) % 4)
             return fail(POS_EINVAL, "attention: misaligned lse");
-        if (attn->tokens == 0 || attn->heads_q == 0) return POS_OK;
-        if (!d_lse) return fail(POS_EINVAL, "attention: NULL lse");
+        if (attn->tokens == 0 || attn->heads_k == 0) return POS_OK;
+        if (!d_lse && attn->heads_q > 0) return fail(POS_EINVAL, "attention: NULL lse");
         p.o = {o->data, o->token_stride, o->head_stride};
         p.lse = const_cast<float *>(d_lse);
         void **out[3] = {&p.dq, &p.dk, &p.dv};
@@ -1031,14 +1059,21 @@ extern "C" pos_status poseidon_attn_backward(const pos_attn *attn, const pos_hea
             p.d_vectors[i] = aligned16(dx[i].data) && dx[i].token_stride % 8 == 0 &&
                              dx[i].head_stride % 8 == 0;
         }
+        const auto s = static_cast<cudaStream_t>(stream);
+        void *scratch = nullptr;
+        if (attn->heads_q == 0) {
+            POS_TRY(attn_scratch(attn_list_bytes(attn, kTile), s, &scratch));
+            const pos_status st = no_queries(attn, p, static_cast<char *>(scratch), s);
+            const cudaError_t e = scratch ? cudaFreeAsync(scratch, s) : cudaSuccess;
+            if (st != POS_OK) return st;
+            return e == cudaSuccess ? POS_OK : cuda_fail(e, "attention scratch");
+        }
         const int parts = parts_of(attn);
         int64_t bytes = largest_bytes(attn) + values_bytes(attn) + stats_bytes(attn) + part_bytes(attn, parts) +
                         attn_list_bytes(attn, kTile);
         for (int i = 0; i < 4; ++i)
             if (!attn_direct(attn, i < 3 ? x[i] : *d_o, heads[i]))
                 bytes += attn_copy_bytes(attn, heads[i]);
-        const auto s = static_cast<cudaStream_t>(stream);
-        void *scratch = nullptr;
         POS_TRY(attn_scratch(bytes, s, &scratch));
         const pos_status st = backward(attn, x, *d_o, p, parts, static_cast<char *>(scratch), s);
         const cudaError_t e = cudaFreeAsync(scratch, s);

@@ -79,3 +79,17 @@ def test_more_sequences_and_heads_than_blocks(P):
         x.backward()
     for x, y in zip((c.o, c.lse, *c.dx), (want.o, want.lse, *want.dx)):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("lengths,starts", [([300], False), ([130, 0, 1, 257], True), ([], True)])
+def test_no_query_heads(P, dtype, lengths, starts):
+    """Keys and values that no query head reads have gradients of 0: sums over nothing.  What
+    belongs to no sequence is left as it was."""
+    c = Call(P, lengths, 2, 2, 40, dtype, "odd", behind=5 if starts else 0, starts=starts)
+    c.a.heads_q = 0
+    c.forward()
+    c.backward()
+    assert (c.o == 77).all() and (c.lse == 77).all() and (c.dx[0] == 77).all()
+    for t in c.dx[1:]:
+        assert (t[c.live] == 0).all() and (t[~c.live] == 77).all()
