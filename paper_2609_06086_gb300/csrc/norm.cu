@@ -123,8 +123,9 @@ __global__ void __launch_bounds__(TEAM::M, TEAM::kBlocks) norm_forward_kernel(co
             if (!p.y && !p.codes_y) break;
             const int j = rank + i * step;
             Vec8 v = to_float(hr[i]);
-            // (past the last column 0, or NaN with the whole group)
-            if (plain) {
+            // (past the last column 0, or NaN with the whole group; r is infinite where eps
+            // is 0 and the squares' sum as well)
+            if (plain || !isfinite(rstd.hi)) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2)
                     set_pair(v, e, mul2(mul2(pair(v, e), both(rstd.hi + rstd.lo)), pair(w[i], e)));
