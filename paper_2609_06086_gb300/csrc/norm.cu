@@ -223,7 +223,7 @@ static pos_status launch_forward(const NormParams &p, const NormShape &shape, bo
 
 template <typename T, typename H>
 static pos_status forward_of(const NormParams &p, bool aligned, cudaStream_t s) {
-    const NormShape shape = norm_shape(p.cols, false);
+    const NormShape shape = norm_shape(p.cols, aligned, sizeof(H) == 4, p.drop.threshold > 0, false);
     switch (shape.team) {
         case 0: return launch_forward<T, H, Team<true, 1, 256>>(p, shape, aligned, s);
         case 1: return launch_forward<T, H, Team<false, 1, 1024>>(p, shape, aligned, s);

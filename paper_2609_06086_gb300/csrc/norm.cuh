@@ -268,14 +268,19 @@ struct NormShape {
                   // <false, 4, 1024>, and <false, 1, 640, 2> or <false, 2, 320, 2>
     int threads, rows;  // of a block
 };
-inline NormShape norm_shape(int cols, bool backward) {
+inline NormShape norm_shape(int cols, bool aligned, bool wide, bool drop, bool backward) {
     // (vectors of the padded codes: 32 columns each four)
     const int nv = (cols + kGroup - 1) / kGroup * 4;
     if (nv <= 32) return {0, 256, 8};
     const int v = nv > 1024 ? 4 : backward && nv > 256 ? 2 : 1;
     const int threads = ((nv + v - 1) / v + 31) / 32 * 32;
-    // rows of 4097 to 5120 columns: two blocks an SM with a few registers less
-    if (nv > 512 && nv <= 640) return {5, threads, 1};
+    // Rows of 4097 to 5120 columns: two blocks an SM with a few registers less.  8192 rows of
+    // 5001, off the alignment: 114 and 178 us with one forward, 195 and 342 back.  8192 of 5120,
+    // whose next rows are on their way in shared memory, bf16: 54 and 59 forward, with dropout
+    // 67 and 72, back with dropout 86 and 91, but without 81 and 77; and with an f32 stream, which
+    // fills shared memory, 88 and 75, back 139 and 106.
+    if (nv > 512 && nv <= 640 && (!aligned || (!wide && (!backward || drop))))
+        return {5, threads, 1};
     return {v < 4 ? v : threads <= 512 ? 3 : 4, threads, 1};
 }
 

@@ -244,7 +244,7 @@ static pos_status launch_backward(NormParams &p, const NormShape &shape, bool al
 template <typename T, typename H>
 static pos_status backward_of(NormParams &p, bool aligned, const float *dw_in, float *dw,
                               cudaStream_t s) {
-    const NormShape shape = norm_shape(p.cols, true);
+    const NormShape shape = norm_shape(p.cols, aligned, sizeof(H) == 4, p.drop.threshold > 0, true);
     switch (shape.team) {
         case 0: return launch_backward<T, H, Team<true, 1, 256>>(p, shape, aligned, dw_in, dw, s);
         case 1: return launch_backward<T, H, Team<false, 1, 1024>>(p, shape, aligned, dw_in, dw, s);

@@ -44,3 +44,17 @@ def test_squares_past_32_bits(P, cols):
     c.forward()
     assert c.rstd[1] == 0 and (c.y[1] == 0).all()
     assert torch.isfinite(c.y).all() and (c.y[[0, 2]] != 0).any()
+
+
+@pytest.mark.parametrize("cols", [4097, 5001, 5120])
+@pytest.mark.parametrize("pad,start", [(0, 0), (8, 0), (3, 1)])
+@pytest.mark.parametrize("dtype,over,p", [("bf16", "bf16", 0.0), ("f16", "f16", 0.2), ("bf16", "f32", 0.0),
+                                          ("bf16", "f32", 0.2), ("f32", "f32", 0.0)])
+def test_widths_with_two_kinds_of_team(P, cols, pad, start, dtype, over, p):
+    """Which one depends on the alignment, the stream, dropout and the pass."""
+    c = Call(P, 333, cols, dtype, over, "int8", p, pad, start)
+    c.forward()
+    c.check_forward()
+    for from_8 in (False, True):
+        c.backward(from_8)
+        c.check_backward(from_8)
