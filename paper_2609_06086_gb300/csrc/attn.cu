@@ -344,7 +344,6 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
             if (n == 0) continue;
             const int row = w.r0 + t * kTile + threadIdx.x % kTile;  // of the sequence
             float top = 0.f, total = 0.f;
-            int bad = 0;  // halves of the tile's values that hold some that are not finite
             for (int j = n - 1; j >= 0 && ok; --j) {
                 ok = wait_warp(s_full + 8 * t, ph, waits);
                 if (!ok) break;
@@ -409,23 +408,21 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 tmem_wait_stores();
                 tmem_before();
                 // (the values that these are multiplied by are looked over)
-                if (j == n - 1) {
-                    ok = wait_warp(v_out + 8 * t, unit & 1, waits);
-                    bad = sh->bad[unit & 1][t][0] + 2 * sh->bad[unit & 1][t][1];
-                }
+                if (j == n - 1) ok = wait_warp(v_out + 8 * t, unit & 1, waits);
                 __syncwarp();
                 if (ok && lane == 0) bar_arrive(p_full + 8 * t);
             }
             if (ok) ok = wait_warp(o_full + 8 * t, unit & 1, waits);
             tmem_after();
             const bool live = row < w.u.len;
+            // halves of the tile's values that hold some that are not finite
+            const int bad = sh->bad[unit & 1][t][0] + 2 * sh->bad[unit & 1][t][1];
             float factor = 1.f / total;
             if (!ok) factor = __uint_as_float(0x7fffffffu);  // a wait that gave up: no result
             T *out = static_cast<T *>(p.out) + (w.u.start + (int64_t)row) * p.out_token +
                      w.head * p.out_head;
-            for (int c = 0; c < dim16; c += 16) {
-                uint32_t o[16];
-                tmem_load16(o_tm + c, o);
+            // rows that see values that are not finite
+            const auto mark = [&](int c, uint32_t *o) {
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
                     if (bad >> half & 1) {
@@ -435,17 +432,26 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                         for (int e = 0; e < 16; ++e)
                             if ((int)(threadIdx.x % kTile) >= first[e]) o[e] = 0x7fffffffu;
                     }
-                Vec8 x[2];
+            };
+            const auto write = [&](bool check) {
+                for (int c = 0; c < dim16; c += 16) {
+                    uint32_t o[16];
+                    tmem_load16(o_tm + c, o);
+                    if (check) mark(c, o);
+                    Vec8 x[2];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
-                if (!live) continue;
+                    for (int e = 0; e < 16; ++e) x[e / 8].v[e % 8] = __uint_as_float(o[e]) * factor;
+                    if (!live) continue;
 #pragma unroll
-                for (int e = 0; e < 16; e += 8) {
-                    if (p.out_vectors)
-                        store8<true>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
-                    else store8<false>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
+                    for (int e = 0; e < 16; e += 8) {
+                        if (p.out_vectors)
+                            store8<true>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
+                        else store8<false>(out + c + e, from_float<T>(x[e / 8]), p.dim_out - c - e);
+                    }
                 }
-            }
+            };
+            if (bad) write(true);  // (a copy of its own)
+            else write(false);
             if (p.lse && live)
                 p.lse[w.head * p.tokens + w.u.start + row] =
                     ok ? (top - kLift<T> + log2f(total)) * kLn2 : __uint_as_float(0x7fffffffu);

@@ -425,7 +425,7 @@ __device__ __forceinline__ void write_tile(uint32_t tile, int rows, T *out, int6
 // zeros of what is not finite, and tells the warps of sums which rows see it; those write
 // NaNs there.  It adds up products with 0, four instructions for eight elements; where that
 // is not 0, it looks column by column.
-//   Both passes of 4096 tokens of 32 + 8 heads of 128: forward 105 -> 109 us, back 377 ->
+//   Both passes of 4096 tokens of 32 + 8 heads of 128: forward 105 -> 108 us, back 377 ->
 // 382; with an infinity in one dO back the same, in all values of all inputs 0.6 ms.  (Rows whose
 // products were not finite computed again by the formulas, one at a time by a warp: 229 ms
 // for the infinity in one dO, and with the square of the length.)
