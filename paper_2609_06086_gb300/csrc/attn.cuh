@@ -349,7 +349,7 @@ __device__ __forceinline__ void tmem_store_block(uint32_t addr, const uint32_t *
             "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
             : "memory");
 }
-// 2^x, both halves of the result within two units of its last place.
+// 2^x within two units of its last place; 0 below 2^-126.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
