@@ -33,7 +33,7 @@ struct AttnParams {
     float *values;              // the largest |v|^2 of a tile, [heads_k][its first token],
     float *most;                // and of a sequence, as `largest` is
     float *part;                // backward: sums of parts of the keys' gradients
-    int32_t parts, first_blocks;  // blocks of the keys' kernel that start at once
+    int32_t parts, first_blocks;  // blocks of the keys' kernel that start at once (no list: all)
     const int4 *tiles;          // of the sequences (attn_tiles_kernel), or NULL: one sequence
     const int32_t *n_tiles;
     int64_t tokens;

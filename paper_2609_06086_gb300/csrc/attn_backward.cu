@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
     // A block that starts when others have ended, and has no tile, ends at once.
-    if (p.tiles && blockIdx.x >= p.first_blocks) {
+    if (blockIdx.x >= p.first_blocks) {
         grid_dep_wait();
         if (blockIdx.x / p.parts / p.heads_k >= *p.n_tiles) return;
     }
@@ -1015,7 +1015,7 @@ static pos_status backward(const pos_attn *a, const pos_heads *x, const pos_head
     at += values_bytes(a);
     p.stats = reinterpret_cast<float2 *>(at);
     at += stats_bytes(a);
-    p.parts = parts, p.first_blocks = sm_count();
+    p.parts = parts, p.first_blocks = a->starts ? std::max(1, sm_count()) : 0x7fffffff;
     p.part = reinterpret_cast<float *>(at);
     at += part_bytes(a, parts);
     const pos_heads t[4] = {x[0], x[1], x[2], d_o};
