@@ -370,7 +370,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
                 const float m =
                     fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * p.scale2;
                 if (j == n - 1) {
-                    top = m;
+                    // (scores of minus infinity alone, so far: nothing yet)
+                    top = fmaxf(m, -__uint_as_float(0x7f7fffffu));
                 } else {
                     const bool more = m > top + kSlack;
                     if (__any_sync(0xffffffffu, more)) {

@@ -154,8 +154,9 @@ __device__ __forceinline__ void sums_barrier() {  // of the warpgroups of sums
 // gradients are then computed with D + e.
 constexpr int kKeySlots = 3, kValueSlots = 2;
 constexpr int kDqBars = 2 * (kKeySlots + kValueSlots) + 10;
+// and the first row of each column whose key is not finite, of two units, halves
 constexpr int kDqSmem = 1024 + (2 + kKeySlots + kValueSlots) * kTileBytes + 8 * kDqBars +
-                        kSharedBytes + kTile * 8;
+                        kSharedBytes + kTile * 8 + 4 * kAttnMaxDim;
 
 template <typename T>
 __global__ void __launch_bounds__(kBackThreads, 1)
@@ -178,6 +179,7 @@ __global__ void __launch_bounds__(kBackThreads, 1)
     AttnShared *sh = reinterpret_cast<AttnShared *>(aligned + (slot - base));
     // rows' statistics, and the parts of e
     float2 *stats = reinterpret_cast<float2 *>(aligned + (slot - base) + kSharedBytes);
+    uint8_t *first_bad = aligned + (slot - base) + kSharedBytes + kTile * 8;
     const Waits waits(sh, p);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, group = warp / 4;
 
@@ -259,12 +261,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                     const int at_i = base + i, slot_i = at_i % kKeySlots;
                     if (!wait_warp(k_full + 8 * slot_i, at_i / kKeySlots & 1, waits)) return false;
                     const uint32_t at = k_at + slot_i * kTileBytes;
-                    if (i == 0) {  // on the diagonal
-                        bar_arrive_one(k_in, mine);
-                        if (!wait_warp(bad_full + 8 * (units & 1), units >> 1 & 1, waits)) return false;
-                    }
                     mma_rows<T>(tmem, q_at, at, steps, mine);
                     commit(s_full, mine);
+                    if (i == 0) commit(k_in, mine);  // on the diagonal: the scores see it as it is
                     return true;
                 };
                 const auto grads = [&](int i) {  // dP
@@ -283,7 +282,8 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 ok = ok && scores(0) && grads(0);
                 for (int i = 0; i < n && ok; ++i, ++it) {
                     const uint32_t at = k_at + it % kKeySlots * kTileBytes;
-                    ok = wait_warp(p_full, it & 1, waits);
+                    ok = wait_warp(p_full, it & 1, waits) &&
+                         (i > 0 || wait_warp(bad_full + 8 * (units & 1), units >> 1 & 1, waits));
                     if (!ok) break;
                     tmem_after();
                     // (the unit before has been read: its warps have gone on to this one)
@@ -311,14 +311,15 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 const uint32_t at = k_at + it % kKeySlots * kTileBytes;
                 const int seen = min(kTile, w.u.len - w.u.tile * kTile);
                 const int from = half * (kTile / 2), end = min(seen, from + kTile / 2);
-                int first = kTile;
-                if (tile_bad<T>(at, from, end, boxes, lane)) {
+                const bool bad = tile_bad<T>(at, from, end, boxes, lane);
+                if (bad) {
+                    uint8_t *first = first_bad + (2 * (units & 1) + half) * kAttnMaxDim;
+                    for (int c = lane; c < kAttnMaxDim; c += 32) first[c] = kTile;
                     tile_clean<T>(at, from, end, boxes, lane,
-                                  [&](int, int row, int) { first = min(first, row); });
-                    first = __reduce_min_sync(0xffffffffu, first);
+                                  [&](int c, int row, int) { first[c] = (uint8_t)row; });
                 }
                 zero_rows(at, max(from, seen), from + kTile / 2, boxes, lane);
-                if (lane == 0) sh->bad[units & 1][0][half] = first;
+                if (lane == 0) sh->bad[units & 1][0][half] = bad;
                 tile_done();
                 if (lane == 0) bar_arrive(bad_full + 8 * (units & 1));
                 it += w.u.tile + 1, ++units;
@@ -431,11 +432,9 @@ __global__ void __launch_bounds__(kBackThreads, 1)
                 ok = wait_warp(dq_full, units & 1, waits) &&
                      wait_warp(bad_full + 8 * (units & 1), units >> 1 & 1, waits);
             tmem_after();
-            // rows that see a key that is not finite
-            const bool lost = !ok || mine >= min(sh->bad[units & 1][0][0], sh->bad[units & 1][0][1]);
             // e's parts through the place of the stats, which every warp has read
             float *parts = reinterpret_cast<float *>(stats);
-            float e = lost ? __uint_as_float(0x7fffffffu) : rest.x + rest.y;  // (no result)
+            float e = ok ? rest.x + rest.y : __uint_as_float(0x7fffffffu);  // (no result)
             if (side >= 2) parts[(side - 2) * kTile + mine] = e;
             sums_barrier();
             if (side < 2) parts[side * kTile + mine] += e;
@@ -443,26 +442,44 @@ __global__ void __launch_bounds__(kBackThreads, 1)
             e = (parts[mine] + parts[kTile + mine]) * shift.undo;
             if (live && side == 0)
                 p.stats[head * p.tokens + u.start + row] = make_float2(st.x, st.y + e);
-            const float a = lost ? __uint_as_float(0x7fffffffu) : p.scale * shift.undo;
+            const float a = ok ? p.scale * shift.undo : __uint_as_float(0x7fffffffu);
             const float b = -e * p.scale * Shift<T>::kUndoProbs;
             T *out = static_cast<T *>(p.dq) + (u.start + (int64_t)row) * p.d_token[0] +
                      head * p.d_head[0];
-            for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
-                uint32_t v[16], k[16];
-                tmem_load16(dq_tm + lanes + c, v);
-                tmem_load16(pk_tm + lanes + c, k);
-                Vec8 x[2];
+            // halves of the tile's keys that hold some that are not finite: rows that see them
+            const int bad = sh->bad[units & 1][0][0] + 2 * sh->bad[units & 1][0][1];
+            const auto mark = [&](int c, uint32_t *v) {
 #pragma unroll
-                for (int h = 0; h < 16; ++h)
-                    x[h / 8].v[h % 8] = __uint_as_float(v[h]) * a + __uint_as_float(k[h]) * b;
-                if (!live) continue;
+                for (int half = 0; half < 2; ++half)
+                    if (bad >> half & 1) {
+                        const uint8_t *first =
+                            first_bad + (2 * (units & 1) + half) * kAttnMaxDim + c;
 #pragma unroll
-                for (int h = 0; h < 16; h += 8) {
-                    if (p.d_vectors[0])
-                        store8<true>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
-                    else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                        for (int h = 0; h < 16; ++h)
+                            if (mine >= first[h]) v[h] = 0x7fffffffu;
+                    }
+            };
+            const auto write = [&](bool check) {
+                for (int c = 16 * side; c < p.dim; c += 16 * kSumGroups) {
+                    uint32_t v[16], k[16];
+                    tmem_load16(dq_tm + lanes + c, v);
+                    tmem_load16(pk_tm + lanes + c, k);
+                    if (check) mark(c, v);
+                    Vec8 x[2];
+#pragma unroll
+                    for (int h = 0; h < 16; ++h)
+                        x[h / 8].v[h % 8] = __uint_as_float(v[h]) * a + __uint_as_float(k[h]) * b;
+                    if (!live) continue;
+#pragma unroll
+                    for (int h = 0; h < 16; h += 8) {
+                        if (p.d_vectors[0])
+                            store8<true>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                        else store8<false>(out + c + h, from_float<T>(x[h / 8]), p.dim_out - c - h);
+                    }
                 }
-            }
+            };
+            if (bad) write(true);  // (a copy of its own)
+            else write(false);
             sums_barrier();
         }
     }
