@@ -91,20 +91,21 @@ struct BlockUnit {
 // What a block's warps share besides tiles and barriers.
 struct AttnShared {
     uint32_t tmem;
-    volatile int gave_up;               // a wait did
+    volatile int gave_up, again;        // a wait did; warps that do rows again
     uint32_t largest[2];                // of dO, units in turn
     volatile int bad[2][2][2];          // of units in turn: see the kernels
 };
-constexpr int kSharedBytes = 48;
+constexpr int kSharedBytes = 56;
 static_assert(sizeof(AttnShared) <= kSharedBytes, "room for it");
 __device__ __forceinline__ void init_shared(AttnShared *sh) {
-    sh->gave_up = 0;
+    sh->gave_up = sh->again = 0;
     for (int i = 0; i < 8; ++i) sh->bad[i / 4][i / 2 % 2][i % 2] = 0;
     sh->largest[0] = sh->largest[1] = 0;
 }
-// Waits for a phase, two seconds at most (WaitLimit).  Where one ran out, the warps that
-// write results go on through the rest of the block's units without waiting, and make
-// theirs NaN: what was in memory is not to pass for a result.
+// Waits for a phase, two seconds at most (WaitLimit), not counting time in which the block
+// does rows again.  Where one ran out, the warps that write results go on through the rest of
+// the block's units without waiting, and make theirs NaN: what was in memory is not to pass for
+// a result.
 struct Waits {
     AttnShared *sh;
     uint64_t ns;
@@ -117,6 +118,7 @@ __device__ __forceinline__ bool attn_wait_long(uint32_t bar, uint32_t parity, co
     for (;;) {
         if (bar_try(bar, parity, w.try_ns)) return true;
         if (w.sh->gave_up) return false;
+        if (w.sh->again) limit = WaitLimit(now_ns());
         if (w.ns == 0 || limit.reached(now_ns(), w.ns)) {
             w.sh->gave_up = 1;
             return false;
@@ -131,6 +133,17 @@ __device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, const W
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, const Waits &w) {
     if (__all_sync(0xffffffffu, bar_try(bar, parity, w.try_ns))) return true;
     return __all_sync(0xffffffffu, attn_wait(bar, parity, w));
+}
+// By a warp, the rows of a mask again (row(i) does the i-th).  What its lanes stored of
+// them before comes first: votes and shuffles alone order no memory.
+template <typename F>
+__device__ __forceinline__ void do_again(uint32_t rows, AttnShared *sh, F row) {
+    if (!rows) return;
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), 1);
+    for (; rows; rows &= rows - 1) row(__ffs(rows) - 1);
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) atomicAdd(const_cast<int *>(&sh->again), -1);
 }
 // The block's end.  Where a wait gave up, copies and products may still be on their way:
 // they end by themselves within microseconds.
@@ -425,8 +438,8 @@ __device__ __forceinline__ void write_tile(uint32_t tile, int rows, T *out, int6
 // zeros of what is not finite, and tells the warps of sums which rows see it; those write
 // NaNs there.  It adds up products with 0, four instructions for eight elements; where that
 // is not 0, it looks column by column.
-//   Both passes of 4096 tokens of 32 + 8 heads of 128: forward 105 -> 108 us, back 377 ->
-// 382; with an infinity in one dO back the same, in all values of all inputs 0.6 ms.  (Rows whose
+//   Both passes of 4096 tokens of 32 + 8 heads of 128: forward 105 -> 109 us, back 377 ->
+// 389; with an infinity in one dO back the same, in all values of all inputs 0.6 ms.  (Rows whose
 // products were not finite computed again by the formulas, one at a time by a warp: 229 ms
 // for the infinity in one dO, and with the square of the length.)
 __device__ __forceinline__ uint32_t tile_at(int row, int c) {  // 16 bytes of columns 8 c ..
@@ -504,6 +517,35 @@ template <typename T>
 __device__ __forceinline__ Vec8 load_row8(const T *at) {
     return to_float(load8<true>(at, 8));
 }
+template <typename T>
+__device__ __forceinline__ float dot_rows(const T *a, const T *b, int dim) {
+    float s = 0.f;
+    for (int d = 0; d < dim; d += 8) {
+        const Vec8 x = load_row8(a + d), y = load_row8(b + d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += x.v[e] * y.v[e];
+    }
+    return s;
+}
+// A lane's part of a row: elements lane + 32 i.
+struct RowPart {
+    float v[kAttnMaxDim / 32];
+};
+template <typename T>
+__device__ __forceinline__ void add_row(RowPart &sum, float w, const T *row, int dim, int lane) {
+#pragma unroll
+    for (int i = 0; i < kAttnMaxDim / 32; ++i)
+        if (lane + 32 * i < dim) sum.v[i] += w * static_cast<float>(row[lane + 32 * i]);
+}
+template <typename T>
+__device__ __forceinline__ void write_row(void *out, int64_t at, const RowPart &sum, float factor,
+                                          int dim, int lane) {
+#pragma unroll
+    for (int i = 0; i < kAttnMaxDim / 32; ++i)
+        if (lane + 32 * i < dim)
+            static_cast<T *>(out)[at + lane + 32 * i] = T(sum.v[i] * factor);
+}
+
 // ---------------------------------------------------------------------------
 // Host side (attn.cu)
 // ---------------------------------------------------------------------------

@@ -70,3 +70,36 @@ def test_short_rows_of_a_longer_sequence(P):
         c.backward()
         want = c.formulas()[0][0][:100]
         assert float((c.dx[0][:100].double() - want).norm() / want.norm()) < 1.5 * 2.0 ** -9
+
+
+@pytest.mark.parametrize("dtype,q,k,scale", [("f16", 3e4, 2.0 ** 16, 0.125), ("f16", 6e4, 2.0 ** 16, 1.0),
+                                             ("bf16", 1e5, 2.0 ** 17, 0.125),
+                                             ("bf16", 1e15, 2.0 ** 50, 0.125),
+                                             ("bf16", 1e18, 2.0 ** 60, 0.7)])
+def test_scores_far_past_the_steps_of_32_bits(P, dtype, q, k, scale):
+    """One element of queries and keys, 300 different keys: a row is the value of the largest
+    key that it sees, the others' weights being less than e^-1000."""
+    n = 300
+    c = Call(P, [n], 2, 1, 64, dtype, "apart", scale=scale)
+    for x in c.x[:2]:
+        x.zero_()
+    gen = torch.Generator().manual_seed(7)
+    steps = torch.randperm(3 * 128, generator=gen)[:n].cuda()
+    sign = torch.where(torch.randperm(n, generator=gen).cuda() % 2 == 0, 1.0, -1.0)
+    values = 2.0 ** (-(steps // 128).double()) * (1 + (steps % 128).double() / 128) / 2 * k * sign
+    c.x[0][:, :, 5] = q
+    c.x[1][:, 0, 5] = values.to(c.dt)
+    key = c.x[1][:, 0, 5].double()
+    assert len(key.unique()) == n
+    c.forward()
+    top, at = key.cummax(0)
+    want = c.x[2][at, 0]
+    # The one weight is 2^d, |d| up to half a step of its score, rounded to 16 bits for the product
+    # (half of eps) and not in the sum (64 + 2 roundings in 32 bits); their ratio's product with the
+    # value is rounded once more (half of eps).
+    eps = torch.finfo(c.dt).eps
+    want = want[:, None].double()
+    bound = (eps + eps * eps / 4 + 100 * 2.0 ** -24) * want.abs()
+    assert ((c.o.double() - want).abs() <= bound).all()
+    lse = top * float(c.x[0][0, 0, 5]) * scale
+    assert ((c.lse.double() - lse).abs() <= 8 * F32 * lse.abs()).all()
