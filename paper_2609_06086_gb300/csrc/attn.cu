@@ -530,7 +530,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1)
 static uint64_t wait_limit_ns() {
     static const uint64_t ns = [] {
         const char *v = std::getenv("POSEIDON_ATTN_WAIT_NS");
-        return v && *v ? std::strtoull(v, nullptr, 10) : kWaitNs;
+        char *end = nullptr;
+        const uint64_t given = v ? std::strtoull(v, &end, 10) : 0;
+        return v && end != v && *end == 0 ? given : kWaitNs;  // (no number: as if not set)
     }();
     return ns;
 }

@@ -74,3 +74,11 @@ def test_what_is_lost_is_nan(tmp_path):
                     lost += int(nan.sum())
             # (a try of no time may sleep long enough for some units all the same)
             assert lost > 0 if limit == 0 else limit < 10 ** 9 or lost == 0
+
+
+def test_a_limit_that_is_no_number(tmp_path):
+    """It counts as none given, not as no time."""
+    import torch
+    right = results(tmp_path, "right")
+    for got, want in zip(results(tmp_path, "got", "2s"), right, strict=True):
+        assert all(torch.equal(a, b) for a, b in zip(got, want, strict=True))
